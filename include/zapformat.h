@@ -246,6 +246,62 @@ int zf_engine_set_profiling(zf_engine *e, int32_t on);
 int zf_apply_mask(zf_engine *e, const void *d_logits, void *d_out, int32_t dtype, int32_t batch,
                   int64_t row_stride_elems, const uint32_t *d_mask, void *hip_stream);
 
+/* ---- the two ends of a step's logits: the product that makes them, the log probabilities that are read from them ----
+ * These calls need no engine.  device is the HIP device ordinal that the tensors and hip_stream belong to.  Everything is
+ * enqueued on hip_stream; nothing is allocated, copied or waited for, so that the calls can be recorded into a HIP graph.
+ * A row count of zero is ZF_OK and does nothing.  Masks are those of zf_compute_mask, [rows][ceil(V/32)]; a null mask
+ * allows everything.  dtype: 0 = fp32, 1 = bf16. */
+
+/* 8-bit floating point with a scale for each block.  q = e4m3 of x / scale (round to nearest, ties to even, the quotient taken in 32 bits), scale =
+ * max(largest |x| of the block / 448, 2^-126).  A block is 128 columns of block_rows = 1 row (activations) or of block_rows = 128
+ * rows (weights).  x: device, [rows][row_stride_elems], cols valid elements per row.  q: device, [rows][P], P = cols rounded
+ * up to a multiple of 128, the columns from cols on zero; scale: device, [ceil(rows / block_rows)][P / 128].  A block with
+ * an infinity has an infinite scale (the infinity becomes NaN, the others 0); a NaN stays one. */
+int zf_quantize_blocks(const void *d_x, int32_t dtype, int64_t rows, int32_t cols, int64_t row_stride_elems, int32_t block_rows,
+                       uint8_t *d_q, float *d_scale, int32_t device, void *hip_stream);
+
+/* logits of a head whose weight is held in 8 bits:
+ *   out[b][v] = sum over blocks k of x_scale[b][k] w_scale[v / 128][k] (sum over the block of x[b][..] w[v][..])   (e4m3, sums in 32 bits)
+ * and -inf where the mask does not allow token v in row b; rows of the weight that no row of the batch allows need not be read
+ * (a grammar in the middle of its punctuation allows a few tokens of a vocabulary).  x: [batch][x_row_stride], w: [V][w_row_stride]
+ * bytes, K of them valid; K and both strides are multiples of 128 and 16, both pointers of 16.  x_scale: [batch][K/128], w_scale:
+ * [ceil(V/128)][K/128].  out: device, [batch][out_row_stride_elems]. */
+int zf_head_logits(const uint8_t *d_x, int64_t x_row_stride, const float *d_x_scale, const uint8_t *d_w, int64_t w_row_stride, const float *d_w_scale,
+                   int32_t batch, int32_t V, int32_t K, const uint32_t *d_mask, void *d_out, int32_t dtype, int64_t out_row_stride_elems,
+                   int32_t device, void *hip_stream);
+
+/* Log probabilities under the mask.  With z = logits / temperature over the allowed tokens of a row:
+ *   logprobs[b][j]  = z[tokens[b][j]] - ln sum e^z      -inf for a token that is not allowed, 0 for a negative id (padding), NaN for an id beyond V;
+ *                     at least the lowest finite number for a finite logit
+ *   entropy[b]      = - sum p ln p
+ *   top_ids, top_logprobs [b][i]: the i-th largest logit's token (equal ones by the lower id) and its log probability; -1 and -inf behind the last one
+ * A row that allows nothing, or whose allowed logits are all -inf, has logprobs -inf, entropy 0 and no alternatives; a NaN among the
+ * allowed logits makes the row's logprobs and entropy NaN (it is no alternative).  What a mask forbids is not looked at. */
+typedef struct {
+    const void *logits;        /* device, [rows][row_stride_elems], V valid elements per row */
+    int32_t dtype;
+    int32_t V;                 /* 1 .. 2^24 */
+    int64_t rows, row_stride_elems;
+    const uint32_t *mask;      /* device, [rows][ceil(V/32)], or null */
+    const void *tokens;        /* device, [rows][n_tokens], null when n_tokens is 0 */
+    int32_t token_bytes;       /* 4 or 8: the ids' type */
+    int32_t n_tokens;          /* 0 .. 1024 */
+    int32_t top;               /* 0 .. 64 alternatives */
+    float temperature;         /* > 0 */
+    float *logprobs;           /* device, [rows][n_tokens] */
+    float *entropy;            /* device, [rows], or null */
+    int32_t *top_ids;          /* device, [rows][top] */
+    float *top_logprobs;       /* device, [rows][top] */
+    float *stats;              /* device, [rows][2], or null: what the gradient is made from (the largest logit, ln of the sum) */
+} zf_logprobs_args;
+int64_t zf_token_logprobs_workspace(const zf_logprobs_args *a); /* bytes of device memory that zf_token_logprobs needs, or a negative error code */
+int zf_token_logprobs(const zf_logprobs_args *a, void *d_workspace, int64_t workspace_bytes, int32_t device, void *hip_stream);
+/* Its gradient: grad[b][v] = sum over what has a gradient of d(that)/d(logits[b][v]), for g_logprobs [rows][n_tokens], g_entropy [rows] and g_top
+ * [rows][top] (each may be null: no gradient), rounded to the logits' type.  a: as it was, with what the call wrote (entropy for g_entropy; stats).  Tokens that are not
+ * allowed have gradient 0, log probabilities of -inf give none.  d_grad: device, [rows][grad_row_stride_elems]; it may be the logits themselves. */
+int zf_token_logprobs_backward(const zf_logprobs_args *a, const float *g_logprobs, const float *g_entropy, const float *g_top,
+                               void *d_grad, int64_t grad_row_stride_elems, int32_t device, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -61,10 +61,16 @@ class MaskReport(ctypes.Structure):
                 ("fallback_ms", ctypes.c_float), ("permute_ms", ctypes.c_float), ("parser_steps", c_i32), ("cache_rows", c_i32)]
 
 
+class LogprobsArgs(ctypes.Structure):
+    _fields_ = [("logits", c_vp), ("dtype", c_i32), ("V", c_i32), ("rows", c_i64), ("row_stride", c_i64), ("mask", c_vp), ("tokens", c_vp), ("token_bytes", c_i32), ("n_tokens", c_i32), ("top", c_i32),
+                ("temperature", ctypes.c_float), ("logprobs", c_vp), ("entropy", c_vp), ("top_ids", c_vp), ("top_logprobs", c_vp), ("stats", c_vp)]
+
+
 EXPORTS = ["zf_strerror", "zf_last_error", "zf_compile", "zf_engine_destroy", "zf_engine_get_info",
            "zf_state_new", "zf_state_clone", "zf_state_reset", "zf_state_destroy", "zf_advance",
            "zf_advance_bytes", "zf_advance_batch", "zf_is_accepting", "zf_state_stats", "zf_state_chart", "zf_position_info",
-           "zf_compute_mask", "zf_compute_mask_noalloc", "zf_compute_mask_async", "zf_compute_mask_apply_async", "zf_mask_wait", "zf_last_mask_report", "zf_engine_clear_state_cache", "zf_engine_set_profiling", "zf_apply_mask"]
+           "zf_compute_mask", "zf_compute_mask_noalloc", "zf_compute_mask_async", "zf_compute_mask_apply_async", "zf_mask_wait", "zf_last_mask_report", "zf_engine_clear_state_cache", "zf_engine_set_profiling", "zf_apply_mask",
+           "zf_quantize_blocks", "zf_head_logits", "zf_token_logprobs_workspace", "zf_token_logprobs", "zf_token_logprobs_backward"]
 # test-only diagnostics (include/zapformat_debug.h)
 DEBUG_EXPORTS = ["zf_debug_host_mask", "zf_debug_host_mask_stats", "zf_debug_host_mask_cached", "zf_debug_host_mask_automaton",
                  "zf_debug_look_polls", "zf_debug_fail_look_ups", "zf_debug_twin_new", "zf_debug_twin_destroy", "zf_debug_twin_advance", "zf_debug_twin_mask"]
@@ -113,6 +119,12 @@ def load_library():
     L.zf_engine_set_profiling.argtypes = [c_vp, c_i32]
     L.zf_engine_clear_state_cache.argtypes = [c_vp]
     L.zf_apply_mask.argtypes = [c_vp, c_vp, c_vp, c_i32, c_i32, c_i64, c_vp, c_vp]
+    L.zf_quantize_blocks.argtypes = [c_vp, c_i32, c_i64, c_i32, c_i64, c_i32, c_vp, c_vp, c_i32, c_vp]
+    L.zf_head_logits.argtypes = [c_vp, c_i64, c_vp, c_vp, c_i64, c_vp, c_i32, c_i32, c_i32, c_vp, c_vp, c_i32, c_i64, c_i32, c_vp]
+    L.zf_token_logprobs_workspace.argtypes = [c_vp]
+    L.zf_token_logprobs_workspace.restype = c_i64
+    L.zf_token_logprobs.argtypes = [c_vp, c_vp, c_i64, c_i32, c_vp]
+    L.zf_token_logprobs_backward.argtypes = [c_vp, c_vp, c_vp, c_vp, c_vp, c_i64, c_i32, c_vp]
     L.zf_debug_host_mask.argtypes = [c_vp, c_vp, c_vp]
     L.zf_debug_host_mask_stats.argtypes = [c_vp, c_vp, c_vp, c_vp]
     L.zf_debug_host_mask_cached.argtypes = [c_vp, c_vp, c_vp, c_vp]
