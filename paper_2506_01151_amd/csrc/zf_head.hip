@@ -154,88 +154,191 @@ template <> struct Operand<uint32_t> {
     }
 };
 
-// A workgroup has the 128 tokens of one scale and up to 16 MT rows of the batch: it lists the tokens that some of its rows allows and
-// its wavefronts take sixteen of them at a time through all columns, straight from memory.  Results gather in LDS, so that the
-// logits go out in whole rows of the range, -inf where nothing was computed.
-template <int MT, bool MASK, typename ElemT>
+// What a lane holds of a 16-byte piece behind the end of its row: nothing.
+__device__ __forceinline__ i32x4 piece_at(const uint8_t *p) { return *reinterpret_cast<const i32x4 *>(p); }
+
+// ---- few rows: the weight streams past them ----
+//
+// A workgroup has TOKENS = 64 GW tokens of one scale and up to 16 MT rows of the batch.  Under a mask it lists the tokens that some of its rows allows.  A
+// wavefront takes 16 GW of them at a time, their weights straight from memory into the operand's registers, two blocks of columns (2 KB each and group) ahead; the rows' activations go through
+// LDS four blocks (CHUNK columns) at a time, with their scales times the weight's.  With no more than 16 GW tokens to do, the four wavefronts
+// share them and take a block of columns of every chunk each (their sums join in a fixed order).  Results gather in LDS, so that the logits
+// go out in whole rows of the range, -inf where nothing was computed.
+static const int CHUNK_BLOCKS = 4, CHUNK = CHUNK_BLOCKS * SCALE_BLOCK;
+
+template <int MT, int GW>
+struct RowsLds {
+    static constexpr int ROWS = MT * 16, TOKENS = 64 * GW, PITCH = TOKENS + 4;
+    static constexpr int X_BYTES = ROWS * CHUNK, S_FLOATS = ROWS * CHUNK_BLOCKS;
+    static constexpr int LOOP = 2 * (X_BYTES + 4 * S_FLOATS), TILE = ROWS * PITCH * 4, JOIN = 3 * ROWS * 16 * GW * 4;   // activations and scales; then the logits, and three wavefronts' sums
+    static constexpr int BYTES = LOOP > TILE + JOIN ? LOOP : TILE + JOIN;
+};
+
+template <int MT, int GW, bool MASK, typename ElemT>
 __global__ __launch_bounds__(256) void head_rows_kernel(HeadArgs a) {
-    constexpr int ROWS = MT * 16, PITCH = SCALE_BLOCK + 4;
-    __shared__ float tile[ROWS][PITCH];
-    __shared__ uint32_t words[ROWS][4], need[4];
-    __shared__ uint8_t list[SCALE_BLOCK];
+    typedef RowsLds<MT, GW> Lds;
+    constexpr int ROWS = Lds::ROWS, TOKENS = Lds::TOKENS, PITCH = Lds::PITCH;
+    __shared__ __align__(16) uint8_t mem[Lds::BYTES];
+    __shared__ uint32_t words[MASK ? ROWS : 1][TOKENS / 32], need[TOKENS / 32];
+    __shared__ uint8_t list[TOKENS];
     const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
-    const int32_t v0 = blockIdx.x * SCALE_BLOCK, m0 = blockIdx.y * ROWS;
-    const int32_t rows = a.M - m0 < ROWS ? a.M - m0 : ROWS, n_v = a.V - v0 < SCALE_BLOCK ? a.V - v0 : SCALE_BLOCK, n_k = a.K / SCALE_BLOCK;
+    const int32_t v0 = blockIdx.x * TOKENS, m0 = blockIdx.y * ROWS;
+    const int32_t rows = a.M - m0 < ROWS ? a.M - m0 : ROWS, n_v = a.V - v0 < TOKENS ? a.V - v0 : TOKENS, n_k = a.K / SCALE_BLOCK;
     int32_t count = n_v;
     if (MASK) {
         const int32_t W = (a.V + 31) / 32;
-        if (tid < 4) need[tid] = 0;
-        for (int i = tid; i < ROWS * PITCH; i += 256) (&tile[0][0])[i] = -INFINITY;
+        if (tid < TOKENS / 32) need[tid] = 0;
         __syncthreads();
-        for (int i = tid; i < rows * 4; i += 256) {
-            const int32_t j = i & 3, left = n_v - 32 * j;                    // tokens of the word that there are
-            uint32_t w = left > 0 ? a.mask[(size_t)(m0 + i / 4) * W + v0 / 32 + j] : 0;
+        for (int i = tid; i < rows * (TOKENS / 32); i += 256) {
+            const int32_t j = i % (TOKENS / 32), left = n_v - 32 * j;        // tokens of the word that there are
+            uint32_t w = left > 0 ? a.mask[(size_t)(m0 + i / (TOKENS / 32)) * W + v0 / 32 + j] : 0;
             if (left < 32 && left > 0) w &= (1u << left) - 1;
-            words[i / 4][j] = w;
+            words[i / (TOKENS / 32)][j] = w;
             if (w) atomicOr(&need[j], w);                                    // the same in any order
         }
         __syncthreads();
-        count = __popc(need[0]) + __popc(need[1]) + __popc(need[2]) + __popc(need[3]);
-        if (tid < SCALE_BLOCK && ((need[tid / 32] >> (tid % 32)) & 1)) {
-            int at = __popc(need[tid / 32] & ((1u << (tid % 32)) - 1));
-            for (int j = 0; j < tid / 32; j++) at += __popc(need[j]);
-            list[at] = (uint8_t)tid;
+        count = 0;
+#pragma unroll
+        for (int j = 0; j < TOKENS / 32; j++) {
+            if (tid < TOKENS && j == tid / 32 && ((need[j] >> (tid % 32)) & 1)) list[count + __popc(need[j] & ((1u << (tid % 32)) - 1))] = (uint8_t)tid;
+            count += __popc(need[j]);
         }
         __syncthreads();
     }
-    const float *const ws = a.ws + (size_t)blockIdx.x * n_k;
-    for (int g = wave * 16; g < count; g += 64) {
-        const int i = g + lane % 16 < count ? g + lane % 16 : count - 1;     // behind the last token: its row once more
-        const uint8_t *const wp = a.w + (int64_t)(v0 + (MASK ? list[i] : i)) * a.w_stride + lane / 16 * 16;
-        const uint8_t *xp[MT];
-        const float *xs[MT];
-        f32x4 acc[MT];
+    const bool shared = count <= 16 * GW;                                    // the wavefronts share the tokens
+    const int first = shared ? 0 : wave * 16 * GW;                           // the wavefront's tokens in the list
+    const bool active = first < count;
+    f32x4 acc[GW][MT];
 #pragma unroll
-        for (int t = 0; t < MT; t++) {
-            const int32_t m = m0 + t * 16 + lane % 16 < a.M ? m0 + t * 16 + lane % 16 : a.M - 1;
-            xp[t] = a.x + m * a.x_stride + lane / 16 * 16;
-            xs[t] = a.xs + (size_t)m * n_k;
-            acc[t] = f32x4{0, 0, 0, 0};
+    for (int g = 0; g < GW; g++)
+#pragma unroll
+        for (int t = 0; t < MT; t++) acc[g][t] = f32x4{0, 0, 0, 0};
+    if (count > 0) {
+        const uint8_t *wp[GW];
+#pragma unroll
+        for (int g = 0; g < GW; g++) {
+            int i = first + g * 16 + lane % 16;
+            if (i >= count) i = count - 1;                                   // behind the last token: its row once more
+            wp[g] = a.w + (int64_t)(v0 + (MASK ? list[i] : i)) * a.w_stride + lane / 16 * 16;
         }
-        for (int32_t k = 0; k < n_k; k++) {
-            Operand<ElemT> w, x;
-            w.take(*reinterpret_cast<const i32x4 *>(wp + (size_t)k * SCALE_BLOCK), *reinterpret_cast<const i32x4 *>(wp + (size_t)k * SCALE_BLOCK + 64));
-            const float s_w = ws[k];
+        // activations of a chunk: 32 pieces a row, piece c of row r at place c ^ (r % 16), so that sixteen rows' pieces of one column lie in different banks
+        constexpr int XN = ROWS * (CHUNK / 16) / 256;
+        i32x4 xr[XN];
+        float sr = 0.0f;
+        const float *const ws = a.ws + (size_t)(v0 / SCALE_BLOCK) * n_k;
+        auto load_x = [&](int32_t c) {
 #pragma unroll
-            for (int t = 0; t < MT; t++) {
-                x.take(*reinterpret_cast<const i32x4 *>(xp[t] + (size_t)k * SCALE_BLOCK), *reinterpret_cast<const i32x4 *>(xp[t] + (size_t)k * SCALE_BLOCK + 64));
-                const f32x4 part = w.times(x);
-                const float s = xs[t][k] * s_w;
-#pragma unroll
-                for (int r = 0; r < 4; r++) acc[t][r] = fmaf(s, part[r], acc[t][r]);
+            for (int i = 0; i < XN; i++) {
+                const int32_t r = (tid + i * 256) / (CHUNK / 16), col = c * CHUNK + (tid + i * 256) % (CHUNK / 16) * 16;
+                xr[i] = i32x4{0, 0, 0, 0};
+                if (col < a.K) xr[i] = piece_at(a.x + (int64_t)(m0 + (r < rows ? r : rows - 1)) * a.x_stride + col);
             }
-        }
+            const int32_t r = tid / CHUNK_BLOCKS, k = c * CHUNK_BLOCKS + tid % CHUNK_BLOCKS;
+            if (r < ROWS) sr = k < n_k ? a.xs[(size_t)(m0 + (r < rows ? r : rows - 1)) * n_k + k] * ws[k] : 0.0f;
+        };
+        auto store_x = [&](int b) {
+            uint8_t *const x = mem + b * Lds::X_BYTES;
 #pragma unroll
-        for (int t = 0; t < MT; t++) {
-            const int m = t * 16 + lane % 16;
-#pragma unroll
-            for (int r = 0; r < 4; r++) {
-                const int j = g + lane / 16 * 4 + r;
-                if (j >= count || m >= rows) continue;
-                const int v = MASK ? list[j] : j;
-                if (!MASK || ((words[m][v / 32] >> (v % 32)) & 1)) tile[m][v] = acc[t][r];
+            for (int i = 0; i < XN; i++) {
+                const int32_t r = (tid + i * 256) / (CHUNK / 16), p = (tid + i * 256) % (CHUNK / 16);
+                *reinterpret_cast<i32x4 *>(x + r * CHUNK + (p ^ (r % 16)) * 16) = xr[i];
             }
+            if (tid < ROWS * CHUNK_BLOCKS) reinterpret_cast<float *>(mem + 2 * Lds::X_BYTES)[b * Lds::S_FLOATS + tid] = sr;
+        };
+        i32x4 now[2][GW][2], next[2][GW][2];
+        auto load_w = [&](i32x4 (&w)[2][GW][2], int32_t h) {                 // two blocks of columns from the 2 h-th on: those that the wavefront takes
+#pragma unroll
+            for (int j = 0; j < 2; j++) {
+                const int32_t k = 2 * h + j;
+                if (!active || k >= n_k || (shared && k % CHUNK_BLOCKS != wave)) continue;
+#pragma unroll
+                for (int g = 0; g < GW; g++) {
+                    w[j][g][0] = __builtin_nontemporal_load(reinterpret_cast<const i32x4 *>(wp[g] + (size_t)k * SCALE_BLOCK));
+                    w[j][g][1] = __builtin_nontemporal_load(reinterpret_cast<const i32x4 *>(wp[g] + (size_t)k * SCALE_BLOCK + 64));
+                }
+            }
+        };
+        const int32_t n_chunks = (n_k + CHUNK_BLOCKS - 1) / CHUNK_BLOCKS;
+        load_x(0);
+        load_w(now, 0);
+        store_x(0);
+        __syncthreads();
+        for (int32_t c = 0; c < n_chunks; c++) {
+            if (c + 1 < n_chunks) load_x(c + 1);
+            const uint8_t *const x = mem + (c & 1) * Lds::X_BYTES;
+            const float *const scales = reinterpret_cast<const float *>(mem + 2 * Lds::X_BYTES) + (c & 1) * Lds::S_FLOATS;
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                load_w(next, 2 * c + h + 1);
+#pragma unroll
+                for (int j = 0; j < 2; j++) {
+                    const int32_t in = 2 * h + j, k = c * CHUNK_BLOCKS + in;
+                    if (!active || k >= n_k || (shared && in != wave)) continue;
+                    Operand<ElemT> w[GW];
+#pragma unroll
+                    for (int g = 0; g < GW; g++) w[g].take(now[j][g][0], now[j][g][1]);
+#pragma unroll
+                    for (int t = 0; t < MT; t++) {
+                        const int r = t * 16 + lane % 16, p = in * 8 + lane / 16;
+                        Operand<ElemT> v;
+                        v.take(*reinterpret_cast<const i32x4 *>(x + r * CHUNK + (p ^ (r % 16)) * 16), *reinterpret_cast<const i32x4 *>(x + r * CHUNK + ((p + 4) ^ (r % 16)) * 16));
+                        const float s = scales[r * CHUNK_BLOCKS + in];
+#pragma unroll
+                        for (int g = 0; g < GW; g++) {
+                            const f32x4 part = w[g].times(v);
+#pragma unroll
+                            for (int e = 0; e < 4; e++) acc[g][t][e] = fmaf(s, part[e], acc[g][t][e]);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < 2; j++)
+#pragma unroll
+                    for (int g = 0; g < GW; g++) { now[j][g][0] = next[j][g][0]; now[j][g][1] = next[j][g][1]; }
+            }
+            if (c + 1 < n_chunks) store_x((c + 1) & 1);
+            __syncthreads();
         }
     }
+    // the loop's memory becomes the logits' and, behind them, that of three wavefronts' sums
+    float *const tile = reinterpret_cast<float *>(mem);
+    f32x4 *const sums = reinterpret_cast<f32x4 *>(mem + Lds::TILE);
+    if (MASK) for (int i = tid; i < ROWS * PITCH; i += 256) tile[i] = -INFINITY;
+    if (shared && wave) {
+#pragma unroll
+        for (int g = 0; g < GW; g++)
+#pragma unroll
+            for (int t = 0; t < MT; t++) sums[((wave - 1) * GW * MT + g * MT + t) * 64 + lane] = acc[g][t];
+    }
     __syncthreads();
-    constexpr int EPV = 16 / sizeof(ElemT), PIECES = SCALE_BLOCK / EPV;
+    if (active && !(shared && wave)) {
+#pragma unroll
+        for (int g = 0; g < GW; g++)
+#pragma unroll
+            for (int t = 0; t < MT; t++) {
+                f32x4 y = acc[g][t];
+                if (shared)
+#pragma unroll
+                    for (int w = 0; w < 3; w++) y += sums[(w * GW * MT + g * MT + t) * 64 + lane];
+                const int m = t * 16 + lane % 16;
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const int j = first + g * 16 + lane / 16 * 4 + e;
+                    if (j >= count || m >= rows) continue;
+                    const int v = MASK ? list[j] : j;
+                    if (!MASK || ((words[m][v / 32] >> (v % 32)) & 1)) tile[m * PITCH + v] = y[e];
+                }
+            }
+    }
+    __syncthreads();
+    constexpr int EPV = 16 / sizeof(ElemT), PIECES = TOKENS / EPV;
     ElemT *const y = (ElemT *)a.y + v0;
     for (int i = tid; i < rows * PIECES; i += 256) {
         const int m = i / PIECES, v = i % PIECES * EPV;
         ElemT *const to = y + (int64_t)(m0 + m) * a.y_stride + v;
         union { ElemT e[EPV]; u32x4 v; } o;
 #pragma unroll
-        for (int k = 0; k < EPV; k++) o.e[k] = sizeof(ElemT) == 4 ? (ElemT)__float_as_uint(tile[m][v + k]) : (ElemT)bf16_of(tile[m][v + k]);
+        for (int k = 0; k < EPV; k++) o.e[k] = sizeof(ElemT) == 4 ? (ElemT)__float_as_uint(tile[m * PITCH + v + k]) : (ElemT)bf16_of(tile[m * PITCH + v + k]);
         if (v + EPV <= n_v) *reinterpret_cast<typename Piece<ElemT>::type *>(to) = o.v;
         else {
 #pragma unroll
@@ -244,16 +347,16 @@ __global__ __launch_bounds__(256) void head_rows_kernel(HeadArgs a) {
     }
 }
 
-template <int MT, bool MASK, typename ElemT>
+template <int MT, int GW, bool MASK, typename ElemT>
 void head_rows(const HeadArgs &a, hipStream_t s) {
-    const dim3 grid((a.V + SCALE_BLOCK - 1) / SCALE_BLOCK, (a.M + MT * 16 - 1) / (MT * 16));
-    hipLaunchKernelGGL((head_rows_kernel<MT, MASK, ElemT>), grid, dim3(256), 0, s, a);
+    const dim3 grid((a.V + 64 * GW - 1) / (64 * GW), (a.M + MT * 16 - 1) / (MT * 16));
+    hipLaunchKernelGGL((head_rows_kernel<MT, GW, MASK, ElemT>), grid, dim3(256), 0, s, a);
 }
 template <bool MASK, typename ElemT>
 void head(const HeadArgs &a, hipStream_t s) {
-    if (a.M <= 16) head_rows<1, MASK, ElemT>(a, s);
-    else if (a.M <= 32) head_rows<2, MASK, ElemT>(a, s);
-    else head_rows<4, MASK, ElemT>(a, s);
+    if (a.M <= 16) head_rows<1, 2, MASK, ElemT>(a, s);
+    else if (a.M <= 32) head_rows<2, 2, MASK, ElemT>(a, s);
+    else head_rows<4, 2, MASK, ElemT>(a, s);
 }
 
 template <typename ElemT>
