@@ -154,7 +154,6 @@ template <> struct Operand<uint32_t> {
     }
 };
 
-// What a lane holds of a 16-byte piece behind the end of its row: nothing.
 __device__ __forceinline__ i32x4 piece_at(const uint8_t *p) { return *reinterpret_cast<const i32x4 *>(p); }
 
 // ---- few rows: the weight streams past them ----
@@ -347,16 +346,168 @@ __global__ __launch_bounds__(256) void head_rows_kernel(HeadArgs a) {
     }
 }
 
+// ---- many rows: tiles of both operands in LDS ----
+//
+// A workgroup of eight wavefronts has 256 tokens and 32 MJ rows of the batch, a wavefront 64 tokens and 16 MJ rows.  A block of columns of both operands, 128 bytes a
+// row, comes from memory straight into LDS while the block before is multiplied: two buffers, one barrier a block.  Piece c of row r lies at place c ^ (r % 8), so
+// that eight rows' pieces of one column lie in different banks; the loads write LDS in lanes' order, so it is their addresses in memory that are exchanged.
+//   Rows behind the last one are the last one again; their results are not stored.
+static const int TILE_TOKENS = 256;
+
+template <int MJ>
+struct TileLds {
+    static constexpr int ROWS = 32 * MJ, W_BYTES = TILE_TOKENS * SCALE_BLOCK, X_BYTES = ROWS * SCALE_BLOCK, BUFFER = W_BYTES + X_BYTES;
+    static constexpr int SCALES = 2 * BUFFER, LOOP = SCALES + 2 * 512 * 4;
+};
+
+// 64 lanes' 16 bytes, `off` behind `base`, to 1 KB of LDS from `at` on.  As an instruction: it has no register for a result, and the compiler, which does not see
+// it, leaves the waits to the caller (arrived(), then a barrier) instead of waiting in front of every read of the other buffer.
+__device__ __forceinline__ void to_lds(const uint8_t *base, uint32_t off, uint32_t at) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(off), "s"(base) : "memory");
+}
+__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ uint32_t lds_at(const void *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t *)p; }
+
+template <int MJ, bool MASK, typename ElemT>
+__global__ __launch_bounds__(512, 2) void head_tile_kernel(HeadArgs a, int32_t tiles_m, int32_t n_tiles) {
+    typedef TileLds<MJ> Lds;
+    extern __shared__ __align__(16) uint8_t mem[];
+    const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64), wv = wave % 4, wm = wave / 4;
+    // workgroups go to the eight XCDs in turn: an XCD takes consecutive tiles, those of the same tokens one after the other, so that its L2 has a weight's rows once
+    const int32_t per = n_tiles / 8, over = n_tiles % 8, xcd = blockIdx.x % 8;
+    const int32_t tile = xcd * per + (xcd < over ? xcd : over) + blockIdx.x / 8;
+    const int32_t v0 = tile / tiles_m * TILE_TOKENS, m0 = tile % tiles_m * Lds::ROWS, n_k = a.K / SCALE_BLOCK;
+    // a wavefront brings eight rows at a time: 32 rows of the weight, 4 MJ of the activations, a block
+    const int32_t place = lane % 8 ^ lane / 8;
+    const uint8_t *const w0 = a.w + (int64_t)v0 * a.w_stride, *const x0 = a.x + (int64_t)m0 * a.x_stride;
+    uint32_t off[4 + MJ / 2], at[4 + MJ / 2];                                // the host checks that a tile's rows lie within 32 bits
+#pragma unroll
+    for (int i = 0; i < 4 + MJ / 2; i++) {
+        const int32_t r = i < 4 ? (wave * 4 + i) * 8 : (wave * (MJ / 2) + i - 4) * 8, left = i < 4 ? a.V - v0 : a.M - m0;
+        off[i] = (uint32_t)(r + lane / 8 < left ? r + lane / 8 : left - 1) * (uint32_t)(i < 4 ? a.w_stride : a.x_stride) + place * 16;
+        at[i] = lds_at(mem) + (i < 4 ? 0 : Lds::W_BYTES) + r * SCALE_BLOCK;
+    }
+    float *const scales = reinterpret_cast<float *>(mem + Lds::SCALES);
+    // a thread's scales: those of one row times the weight's of the first or the second 128 tokens (the threads behind these two have them once more)
+    const int32_t n_vb = (a.V + SCALE_BLOCK - 1) / SCALE_BLOCK, row = m0 + tid % Lds::ROWS, vb = v0 / SCALE_BLOCK + tid / Lds::ROWS % 2;
+    const float *const xs = a.xs + (size_t)(row < a.M ? row : a.M - 1) * n_k, *const ws = a.ws + (size_t)(vb < n_vb ? vb : n_vb - 1) * n_k;
+    auto fetch = [&](int32_t k, int b) {
+#pragma unroll
+        for (int i = 0; i < 4 + MJ / 2; i++) to_lds((i < 4 ? w0 : x0) + (size_t)k * SCALE_BLOCK, off[i], at[i] + b * Lds::BUFFER);
+    };
+    f32x4 acc[MJ][4];
+#pragma unroll
+    for (int j = 0; j < MJ; j++)
+#pragma unroll
+        for (int i = 0; i < 4; i++) acc[j][i] = f32x4{0, 0, 0, 0};
+    scales[tid] = xs[0] * ws[0];
+    fetch(0, 0);
+    arrived();
+    __syncthreads();
+    const int32_t c0 = (lane / 16 ^ lane % 8) * 16, c1 = ((lane / 16 + 4) ^ lane % 8) * 16;   // the lane's two pieces of a row that is lane % 8 modulo 8
+    for (int32_t k = 0; k < n_k; k++) {
+        const int b = k & 1;
+        const int32_t k_next = k + 1 < n_k ? k + 1 : k;
+        const float next_x = xs[k_next], next_w = ws[k_next];
+        if (k + 1 < n_k) fetch(k + 1, b ^ 1);
+        const uint8_t *const w_at = mem + b * Lds::BUFFER + (wv * 64 + lane % 16) * SCALE_BLOCK;
+        const uint8_t *const x_at = mem + b * Lds::BUFFER + Lds::W_BYTES + (wm * 16 * MJ + lane % 16) * SCALE_BLOCK;
+        const float *const s_at = scales + b * 512 + wv / 2 * Lds::ROWS + wm * 16 * MJ + lane % 16;
+        Operand<ElemT> w[4];
+#pragma unroll
+        for (int i = 0; i < 4; i++) w[i].take(piece_at(w_at + i * 16 * SCALE_BLOCK + c0), piece_at(w_at + i * 16 * SCALE_BLOCK + c1));
+        // a step behind: the scaled sums of sixteen rows are added while the next rows' products run
+        f32x4 part[4], last[4];
+        float s = 0.0f, s_last = 0.0f;
+        Operand<ElemT> x, x_next;
+        x_next.take(piece_at(x_at + c0), piece_at(x_at + c1));
+#pragma unroll
+        for (int j = 0; j <= MJ; j++) {
+            if (j < MJ) {
+                x = x_next;
+                s = s_at[j * 16];
+                if (j + 1 < MJ) x_next.take(piece_at(x_at + (j + 1) * 16 * SCALE_BLOCK + c0), piece_at(x_at + (j + 1) * 16 * SCALE_BLOCK + c1));
+            }
+#pragma unroll
+            for (int i = 0; i < 4; i++) {
+                if (j < MJ) part[i] = w[i].times(x);
+                if (j > 0)
+#pragma unroll
+                    for (int e = 0; e < 4; e++) acc[j - 1][i][e] = fmaf(s_last, last[i][e], acc[j - 1][i][e]);
+                last[i] = part[i];
+            }
+            s_last = s;
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        scales[(b ^ 1) * 512 + tid] = next_x * next_w;
+        arrived();
+        __syncthreads();
+    }
+    // sixteen rows at a time through the wavefront's own part of LDS, from four tokens a lane to whole lines of 64 tokens
+    constexpr int EPV = 16 / sizeof(ElemT), PITCH = 64 * sizeof(ElemT) + 16, PIECES = 64 / EPV;
+    uint8_t *const own = mem + wave * (16 * PITCH);
+    const int32_t W = (a.V + 31) / 32, v_w = v0 + wv * 64;
+#pragma unroll
+    for (int j = 0; j < MJ; j++) {
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+            union { ElemT e[4]; uint64_t q; u32x4 v; } o;
+#pragma unroll
+            for (int e = 0; e < 4; e++) o.e[e] = sizeof(ElemT) == 4 ? (ElemT)__float_as_uint(acc[j][i][e]) : (ElemT)bf16_of(acc[j][i][e]);
+            uint8_t *const to = own + lane % 16 * PITCH + (i * 16 + lane / 16 * 4) * sizeof(ElemT);
+            if (sizeof(ElemT) == 4) *reinterpret_cast<u32x4 *>(to) = o.v;
+            else *reinterpret_cast<uint64_t *>(to) = o.q;
+        }
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int i = 0; i < 16 * PIECES / 64; i++) {
+            const int r = (i * 64 + lane) / PIECES, p = (i * 64 + lane) % PIECES;
+            const int32_t m = m0 + wm * 16 * MJ + j * 16 + r, v = v_w + p * EPV;
+            union { ElemT e[EPV]; u32x4 v; } o;
+            o.v = *reinterpret_cast<const u32x4 *>(own + r * PITCH + p * 16);
+            if (m >= a.M || v >= a.V) continue;
+            if (MASK) {
+                const uint32_t bits = a.mask[(size_t)m * W + (v >> 5)] >> (v & 31);
+#pragma unroll
+                for (int e = 0; e < EPV; e++) if (!((bits >> e) & 1)) o.e[e] = sizeof(ElemT) == 4 ? (ElemT)0xFF800000u : (ElemT)0xFF80u;
+            }
+            ElemT *const to = (ElemT *)a.y + (int64_t)m * a.y_stride + v;
+            if (v + EPV <= a.V) *reinterpret_cast<typename Piece<ElemT>::type *>(to) = o.v;
+            else {
+#pragma unroll
+                for (int e = 0; e < EPV; e++) if (v + e < a.V) to[e] = o.e[e];
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+template <int MJ, bool MASK, typename ElemT>
+hipError_t head_tile(const HeadArgs &a, hipStream_t s) {
+    typedef TileLds<MJ> Lds;
+    static const hipError_t ready = hipFuncSetAttribute((const void *)head_tile_kernel<MJ, MASK, ElemT>, hipFuncAttributeMaxDynamicSharedMemorySize, Lds::LOOP);
+    if (ready != hipSuccess) return ready;
+    const int32_t tiles_m = (a.M + Lds::ROWS - 1) / Lds::ROWS;
+    const int64_t n = (int64_t)tiles_m * ((a.V + TILE_TOKENS - 1) / TILE_TOKENS);
+    hipLaunchKernelGGL((head_tile_kernel<MJ, MASK, ElemT>), dim3((uint32_t)n), dim3(512), Lds::LOOP, s, a, tiles_m, (int32_t)n);
+    return hipSuccess;
+}
+
 template <int MT, int GW, bool MASK, typename ElemT>
-void head_rows(const HeadArgs &a, hipStream_t s) {
+hipError_t head_rows(const HeadArgs &a, hipStream_t s) {
     const dim3 grid((a.V + 64 * GW - 1) / (64 * GW), (a.M + MT * 16 - 1) / (MT * 16));
     hipLaunchKernelGGL((head_rows_kernel<MT, GW, MASK, ElemT>), grid, dim3(256), 0, s, a);
+    return hipSuccess;
 }
 template <bool MASK, typename ElemT>
-void head(const HeadArgs &a, hipStream_t s) {
-    if (a.M <= 16) head_rows<1, 2, MASK, ElemT>(a, s);
-    else if (a.M <= 32) head_rows<2, 2, MASK, ElemT>(a, s);
-    else head_rows<4, 2, MASK, ElemT>(a, s);
+hipError_t head(const HeadArgs &a, hipStream_t s) {
+    if (a.M <= 16) return head_rows<1, 2, MASK, ElemT>(a, s);
+    if (a.M <= 32) return head_rows<2, 2, MASK, ElemT>(a, s);
+    if (a.M <= 64) return head_rows<4, 2, MASK, ElemT>(a, s);
+    if ((a.w_stride | a.x_stride) >= (1 << 24)) return head_rows<4, 2, MASK, ElemT>(a, s);   // a tile's rows would not lie within 32 bits
+    // operands in bf16 take twice the registers: half the rows
+    if (sizeof(ElemT) == 4 || a.M <= 128) return head_tile<4, MASK, ElemT>(a, s);
+    return head_tile<8, MASK, ElemT>(a, s);
 }
 
 template <typename ElemT>
@@ -377,9 +528,8 @@ hipError_t launch_quantize(const void *x, int dtype, int64_t rows, int32_t cols,
 }
 
 hipError_t launch_head(const HeadArgs &a, hipStream_t s) {
-    if (a.mask) a.dtype == 0 ? head<true, uint32_t>(a, s) : head<true, uint16_t>(a, s);
-    else a.dtype == 0 ? head<false, uint32_t>(a, s) : head<false, uint16_t>(a, s);
-    return hipGetLastError();
+    const hipError_t e = a.mask ? (a.dtype == 0 ? head<true, uint32_t>(a, s) : head<true, uint16_t>(a, s)) : (a.dtype == 0 ? head<false, uint32_t>(a, s) : head<false, uint16_t>(a, s));
+    return e != hipSuccess ? e : hipGetLastError();
 }
 
 }  // namespace zf
