@@ -13,10 +13,17 @@ from typing import NamedTuple, Optional
 
 import torch
 
+from . import _native_ops
 from .binding import ZF_ERR_INVALID_ARG, LogprobsArgs, ZfError, _check, load_library
 
 BLOCK = 128                                        # columns that share a scale, and rows of a weight that do
 _DTYPES = {torch.float32: 0, torch.bfloat16: 1}
+
+
+_lib = load_library()
+_native_ops.bind({n: ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in (
+    "zf_quantize_blocks", "zf_head_logits", "zf_token_logprobs_workspace", "zf_token_logprobs", "zf_token_logprobs_backward", "zf_last_error")}, _check)
+# The ordinary call is _native_ops' (csrc/zf_py_ops.cpp); what it does not take it answers with None, and the code here, its definition, does or refuses it.
 
 
 class TokenLogprobs(NamedTuple):
@@ -59,6 +66,9 @@ def _stream(device):
 def quantize_blocks(x, *, block_rows=1):
     """x (fp32 or bf16 [rows, cols]) as (q, scale): e4m3 [rows, cols padded with zeros to a multiple of 128] and fp32 scales, one for 128 columns
     of block_rows = 1 row (activations) or of 128 rows (a head's weight)."""
+    got = _native_ops.quantize_blocks(x, block_rows)
+    if got is not None:
+        return got
     _matrix(x, "x", _DTYPES, contiguous=False)
     _need(block_rows in (1, BLOCK), "block_rows must be 1 or 128")
     rows, cols = x.shape
@@ -66,7 +76,7 @@ def quantize_blocks(x, *, block_rows=1):
     blocks = -(-cols // BLOCK)
     q = torch.empty((rows, blocks * BLOCK), dtype=torch.float8_e4m3fn, device=x.device)
     scale = torch.empty((-(-rows // block_rows), blocks), dtype=torch.float32, device=x.device)
-    _check(load_library().zf_quantize_blocks(x.data_ptr(), _DTYPES[x.dtype], rows, cols, _row_stride(x), block_rows, q.data_ptr(), scale.data_ptr(), x.device.index, _stream(x.device)))
+    _check(_lib.zf_quantize_blocks(x.data_ptr(), _DTYPES[x.dtype], rows, cols, _row_stride(x), block_rows, q.data_ptr(), scale.data_ptr(), x.device.index, _stream(x.device)))
     return q, scale
 
 
@@ -74,6 +84,10 @@ def head_logits(q, q_scale, weight, weight_scale, mask=None, *, dtype=torch.bflo
     """Logits [batch, V] of activations q [batch, K] against a head's weight [V, K], both e4m3 with K a multiple of 128, scales [batch, K / 128] and
     [ceil(V / 128), K / 128] (quantize_blocks makes all four).  Under a mask the logits of tokens that it does not allow are -inf, and
     rows of the weight that no row of the batch allows are not read.  dtype: fp32 or bf16; out: rows of the result without gaps."""
+    if out is None:
+        got = _native_ops.head_logits(q, q_scale, weight, weight_scale, mask, _DTYPES.get(dtype, -1))
+        if got is not None:
+            return got
     for t, what in ((q, "q"), (weight, "weight")):
         _matrix(t, what, (torch.float8_e4m3fn,), contiguous=False)
     batch, K, V = q.shape[0], q.shape[1], weight.shape[0]
@@ -88,7 +102,7 @@ def head_logits(q, q_scale, weight, weight_scale, mask=None, *, dtype=torch.bflo
         _matrix(out, "out", _DTYPES, batch, V, contiguous=False)
     for t, what in ((q_scale, "q_scale"), (weight, "weight"), (weight_scale, "weight_scale"), (out, "out")):
         _need(t.device == q.device, f"{what}: on another device than q")
-    _check(load_library().zf_head_logits(q.data_ptr(), _row_stride(q), q_scale.data_ptr(), weight.data_ptr(), _row_stride(weight), weight_scale.data_ptr(),
+    _check(_lib.zf_head_logits(q.data_ptr(), _row_stride(q), q_scale.data_ptr(), weight.data_ptr(), _row_stride(weight), weight_scale.data_ptr(),
                                          batch, V, K, _mask_ptr(mask, batch, V, q.device), out.data_ptr(), _DTYPES[out.dtype], _row_stride(out), q.device.index, _stream(q.device)))
     return out
 
@@ -105,7 +119,7 @@ def _logprobs_args(logits, tokens, mask, temperature, top):
 
 def _forward(logits, tokens, mask, temperature, entropy, top, stats):
     """(logprobs, entropy, top_ids, top_logprobs, stats), each None where it is not wanted."""
-    lib, rows, dev = load_library(), logits.shape[0], logits.device
+    lib, rows, dev = _lib, logits.shape[0], logits.device
     a = _logprobs_args(logits, tokens, mask, temperature, top)
     f32 = dict(dtype=torch.float32, device=dev)
     out = (torch.empty(tokens.shape, **f32) if tokens is not None else None, torch.empty(rows, **f32) if entropy else None,
@@ -142,7 +156,7 @@ def _backward(logits, tokens, mask, lp, H, ids, top_lp, stats, temperature, g_lp
     a.logprobs, a.entropy, a.top_ids, a.top_logprobs, a.stats = (t.data_ptr() if t is not None else None for t in (lp, H, ids, top_lp, stats))
     g = [t.to(torch.float32).contiguous() if t is not None else None for t in (g_lp, g_H, g_top)]
     grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
-    _check(load_library().zf_token_logprobs_backward(ctypes.byref(a), *(t.data_ptr() if t is not None else None for t in g), grad.data_ptr(), grad.shape[1],
+    _check(_lib.zf_token_logprobs_backward(ctypes.byref(a), *(t.data_ptr() if t is not None else None for t in g), grad.data_ptr(), grad.shape[1],
                                                      logits.device.index, _stream(logits.device)))
     return grad
 
@@ -153,6 +167,9 @@ def token_logprobs(logits, tokens=None, mask=None, *, temperature=1.0, entropy=F
 
     -inf for a token that the mask does not allow, 0 and no gradient for a negative id (padding), NaN for an id beyond V.  Alternatives that there are
     not: id -1, -inf.  logprobs, entropy and top_logprobs have gradients for the logits (once; not to be differentiated again)."""
+    got = _native_ops.token_logprobs(logits, tokens, mask, float(temperature), bool(entropy), top)
+    if got is not None:
+        return TokenLogprobs(*got)
     _matrix(logits, "logits", _DTYPES, contiguous=False)
     rows, V = logits.shape
     _need(V > 0, "logits: no columns")
