@@ -47,30 +47,42 @@ __device__ __forceinline__ void to_bits(float x, uint16_t *out) {       // to ne
     const uint32_t u = __float_as_uint(x);
     *out = (u & 0x7FFFFFFFu) > 0x7F800000u ? (uint16_t)((u >> 16) | 0x40u) : (uint16_t)((u + 0x7FFFu + ((u >> 16) & 1u)) >> 16);
 }
+__device__ __forceinline__ uint32_t in_order(float x) {                  // bits that compare as the values do; NaN and -inf: 0
+    const uint32_t u = __float_as_uint(x + 0.0f);
+    return x > -INFINITY ? u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u) : 0u;
+}
 __device__ __forceinline__ Key key_of(float x, uint32_t v) {
-    const uint32_t u = __float_as_uint(x + 0.0f);                        // the two zeros are equal
-    if (!(x > -INFINITY)) return 0;                                      // neither -inf nor NaN
-    return (Key)(u ^ ((u >> 31) ? 0xFFFFFFFFu : 0x80000000u)) << 32 | (uint32_t)~v;
+    const uint32_t o = in_order(x);
+    return o ? (Key)o << 32 | (uint32_t)~v : 0;
 }
 __device__ __forceinline__ float logit_of(Key k) {
     const uint32_t o = (uint32_t)(k >> 32);
     return __uint_as_float(o ^ ((o >> 31) ? 0x80000000u : 0xFFFFFFFFu));
 }
-__device__ __forceinline__ Key wave_max(Key k) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) { const Key o = __shfl_xor(k, d); if (o > k) k = o; }
-    return k;
+// Over a wavefront, to all lanes, by moves between lanes of 1, 2, 4, 8, 16 and 32; sums in this order, whatever the timing.
+template <int CTRL, int ROWS = 0xF> __device__ __forceinline__ uint32_t moved(uint32_t none, uint32_t x) { return (uint32_t)__builtin_amdgcn_update_dpp((int)none, (int)x, CTRL, ROWS, 0xF, false); }
+template <class F>
+__device__ __forceinline__ uint32_t over_wave(uint32_t x, uint32_t none, F f) {
+    x = f(x, moved<0x111>(none, x));           // the lane one below, of the same sixteen
+    x = f(x, moved<0x112>(none, x));
+    x = f(x, moved<0x114>(none, x));
+    x = f(x, moved<0x118>(none, x));
+    x = f(x, moved<0x142, 0xA>(none, x));      // lane 15 of each sixteen to the next
+    x = f(x, moved<0x143, 0xC>(none, x));      // lane 31 to the upper half
+    return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
 }
 __device__ __forceinline__ float wave_max(float x) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) x = fmaxf(x, __shfl_xor(x, d));
-    return x;
+    return __uint_as_float(over_wave(__float_as_uint(x), 0xFF800000u, [](uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }));
 }
 __device__ __forceinline__ float wave_sum(float x) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
-    return x;
+    return __uint_as_float(over_wave(__float_as_uint(x), 0u, [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
 }
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) { return over_wave(x, 0u, [](uint32_t a, uint32_t b) { return a > b ? a : b; }); }
+__device__ __forceinline__ Key wave_max(Key k) {
+    const uint32_t high = wave_max((uint32_t)(k >> 32));
+    return (Key)high << 32 | wave_max((uint32_t)(k >> 32) == high ? (uint32_t)k : 0u);
+}
+__device__ __forceinline__ float two_to(float x) { return __builtin_amdgcn_exp2f(x); }   // below 2^-126 nothing
 // A finite logit has a finite log probability (the type's lowest value divided by a temperature below one is beyond 32 bits).
 __device__ __forceinline__ float logprob_of(float x, float m, float temperature, float ln_S) {
     const float lp = (x - m) / temperature - ln_S;
@@ -80,7 +92,7 @@ __device__ __forceinline__ float logprob_of(float x, float m, float temperature,
 __device__ __forceinline__ void join(Part &a, const Part &b, float c) {
     const float m = fmaxf(a.m, b.m);
     const float da = a.m == m ? 0.0f : fmaxf((a.m - m) * c, -1e4f), db = b.m == m ? 0.0f : fmaxf((b.m - m) * c, -1e4f);
-    const float fa = exp2f(da), fb = exp2f(db);
+    const float fa = two_to(da), fb = two_to(db);
     a.T = fa * (a.T + a.S * da) + fb * (b.T + b.S * db);
     a.S = fa * a.S + fb * b.S;
     a.m = m;
@@ -92,46 +104,60 @@ __device__ __forceinline__ bool allowed(const uint32_t *mask, int64_t row, int32
 // Piece of a row from token v on: its logits, -inf where there is no token or none that is allowed.
 template <typename ElemT, int EPV>
 __device__ __forceinline__ void load_piece(const ElemT *row, const uint32_t *mask_row, int32_t v, int32_t V, float (&x)[EPV]) {
-    uint32_t bits = v < V ? (V - v >= EPV ? (1u << EPV) - 1u : (1u << (V - v)) - 1u) : 0u;
-    if (mask_row && bits) bits &= mask_row[v >> 5] >> (v & 31);
-    if (v + EPV <= V) {
-        union { u32x4 v; ElemT e[EPV]; } p;
-        p.v = *reinterpret_cast<const typename Piece<ElemT>::type *>(row + v);
+    constexpr uint32_t FULL = (1u << EPV) - 1u;
+    const int32_t left = V - v;
+    uint32_t bits = left >= EPV ? FULL : left > 0 ? (1u << left) - 1u : 0u;
+    if (mask_row && left > 0) bits &= mask_row[v >> 5] >> (v & 31);
+    if (left >= EPV) {
+        const u32x4 p = *reinterpret_cast<const typename Piece<ElemT>::type *>(row + v);
 #pragma unroll
-        for (int k = 0; k < EPV; k++) x[k] = (bits >> k) & 1u ? of_bits(p.e[k]) : -INFINITY;
+        for (int k = 0; k < EPV; k++) x[k] = __uint_as_float(sizeof(ElemT) == 4 ? p[k] : k & 1 ? p[k / 2] & 0xFFFF0000u : p[k / 2] << 16);
     } else {
 #pragma unroll
-        for (int k = 0; k < EPV; k++) x[k] = (bits >> k) & 1u ? of_bits(row[v + k]) : -INFINITY;
+        for (int k = 0; k < EPV; k++) x[k] = k < left ? of_bits(row[v + k]) : 0.0f;
+    }
+    if (__any(bits != FULL)) {
+#pragma unroll
+        for (int k = 0; k < EPV; k++) {
+            const uint32_t yes = (uint32_t)__builtin_amdgcn_sbfe((int)bits, k, 1);
+            x[k] = __uint_as_float((__float_as_uint(x[k]) & yes) | (0xFF800000u & ~yes));
+        }
     }
 }
 
-template <bool TOP, typename ElemT>
+// The alternatives of a segment.  Every wavefront takes the `top`-th largest of its lanes' largest logits (by their bits in order, the upper sixteen of them): its
+// part of the segment's alternatives lies at or above it, and little else does.  What does is listed, and of all lists together the rank of each is the number of keys above it.  When a list
+// overflows (many equal logits) the keys are found one by one, each the largest below the last.
+static const int LISTED = 128;                // keys a wavefront lists
+
+template <bool ENT, bool TOP, typename ElemT>
 __global__ __launch_bounds__(THREADS) void logprobs_part_kernel(LogprobsArgs A) {
     constexpr int EPV = 16 / sizeof(ElemT);
     __shared__ Part part[WAVES];
-    __shared__ Key best[WAVES];
+    __shared__ Key best[WAVES], listed[TOP ? WAVES * LISTED : 1];
+    __shared__ int n_listed[WAVES];
     const int tid = threadIdx.x, wave = tid / 64;
     const int64_t row = blockIdx.x / (uint32_t)A.n_seg;
     const int32_t seg = blockIdx.x % (uint32_t)A.n_seg, V = A.a.V, v0 = seg * (THREADS * PIECES * EPV) + tid * EPV;
     const ElemT *const logits = (const ElemT *)A.a.logits + row * A.a.row_stride_elems;
     const uint32_t *const mask = A.a.mask ? A.a.mask + row * A.W : nullptr;
-    float x[PIECES][EPV], m = -INFINITY;
+    float x[PIECES][EPV], most = -INFINITY;
 #pragma unroll
     for (int p = 0; p < PIECES; p++) load_piece<ElemT, EPV>(logits, mask, v0 + p * (THREADS * EPV), V, x[p]);
 #pragma unroll
     for (int p = 0; p < PIECES; p++)
 #pragma unroll
-        for (int k = 0; k < EPV; k++) m = fmaxf(m, x[p][k]);
-    m = wave_max(m);
+        for (int k = 0; k < EPV; k++) most = fmaxf(most, x[p][k]);
+    const float m = wave_max(most);
     float S = 0.0f, T = 0.0f;
     if (m > -INFINITY) {
 #pragma unroll
         for (int p = 0; p < PIECES; p++)
 #pragma unroll
             for (int k = 0; k < EPV; k++) {
-                const float z = (x[p][k] - m) * A.c, e = exp2f(z);
+                const float z = (x[p][k] - m) * A.c, e = two_to(z);
                 S += e;
-                T = fmaf(e, fmaxf(z, -1e4f), T);           // nothing times -inf is nothing
+                if (ENT) T = fmaf(e, fmaxf(z, -1e4f), T);  // nothing times -inf is nothing
             }
     } else {
 #pragma unroll
@@ -140,15 +166,56 @@ __global__ __launch_bounds__(THREADS) void logprobs_part_kernel(LogprobsArgs A) 
             for (int k = 0; k < EPV; k++) if (x[p][k] != x[p][k]) S = T = x[p][k];
     }
     S = wave_sum(S);
-    T = wave_sum(T);
+    if (ENT) T = wave_sum(T);
     if (tid % 64 == 0) part[wave] = Part{m, S, T, 0.0f};
+    if (TOP) {
+        const uint32_t mine = in_order(most);
+        uint32_t line = 0;                                 // the largest multiple of 2^16 that `top` lanes reach
+#pragma unroll
+        for (int bit = 31; bit >= 16; bit--) {
+            const uint32_t up = line | 1u << bit;
+            if (__popcll(__ballot(mine >= up)) >= A.a.top) line = up;
+        }
+        if (line == 0) line = 1;                           // 0 stands for no logit
+        int n = 0;
+#pragma unroll
+        for (int p = 0; p < PIECES; p++)
+#pragma unroll
+            for (int k = 0; k < EPV; k++) {
+                const uint32_t o = in_order(x[p][k]);
+                const unsigned long long who = __ballot(o >= line);
+                if (!who) continue;
+                const int at = n + __popcll(who & ((1ull << (tid % 64)) - 1));
+                if (o >= line && at < LISTED) listed[wave * LISTED + at] = (Key)o << 32 | (uint32_t)~(uint32_t)(v0 + p * (THREADS * EPV) + k);
+                n += __popcll(who);
+            }
+        if (tid % 64 == 0) n_listed[wave] = n;
+    }
     __syncthreads();
     if (tid == 0) {
         Part all = part[0];
+#pragma unroll
         for (int w = 1; w < WAVES; w++) join(all, part[w], A.c);
         A.parts[blockIdx.x] = all;
     }
     if (!TOP) return;
+    Key *const out = A.keys + (int64_t)blockIdx.x * A.a.top;
+    int n_all = 0;
+    bool fits = true;
+#pragma unroll
+    for (int w = 0; w < WAVES; w++) { n_all += n_listed[w]; fits = fits && n_listed[w] <= LISTED; }
+    if (fits) {
+        for (int i = tid; i < WAVES * LISTED; i += THREADS) {
+            if (i % LISTED >= n_listed[i / LISTED]) continue;
+            const Key mine = listed[i];
+            int rank = 0;
+            for (int w = 0; w < WAVES; w++)
+                for (int j = 0; j < n_listed[w]; j++) rank += listed[w * LISTED + j] > mine;
+            if (rank < A.a.top) out[rank] = mine;
+        }
+        if (tid < A.a.top && tid >= n_all) out[tid] = 0;
+        return;
+    }
     Key last = ~(Key)0;
     for (int i = 0; i < A.a.top; i++) {                    // the largest below the last one
         Key k0 = 0;
@@ -164,15 +231,21 @@ __global__ __launch_bounds__(THREADS) void logprobs_part_kernel(LogprobsArgs A) 
         __syncthreads();
         k0 = best[0];
         for (int w = 1; w < WAVES; w++) if (best[w] > k0) k0 = best[w];
-        if (tid == 0) A.keys[(int64_t)blockIdx.x * A.a.top + i] = k0;
+        if (tid == 0) out[i] = k0;
         last = k0 ? k0 : 1;                                // none left: no key is below 1 but 0
         __syncthreads();
     }
 }
 
+// A row's parts, by one wavefront; the alternatives are merged from the segments' sorted lists, a lane at the head of each.
+static const int JOINED_KEYS = 1024;                       // so many of a row are brought to LDS (a step to the next of a list in memory takes ten times as long)
+__host__ __device__ __forceinline__ int32_t join_bytes(int32_t n_seg, int32_t top) {
+    return ((top && n_seg * top <= JOINED_KEYS ? n_seg * top * (int32_t)sizeof(Key) : 0) + n_seg + 7) / 8 * 8;
+}
+
 template <typename ElemT>
 __global__ __launch_bounds__(ROWS_JOINED * 64) void logprobs_join_kernel(LogprobsArgs A) {
-    extern __shared__ uint8_t taken[];                     // [ROWS_JOINED][n_seg]: keys of a segment that are out
+    extern __shared__ __align__(8) uint8_t lds[];          // of each row: its segments' keys where they fit, then how many of each are out
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int64_t row = (int64_t)blockIdx.x * ROWS_JOINED + wave;
     if (row >= A.a.rows) return;                           // whole wavefronts, and no barrier below
@@ -203,9 +276,18 @@ __global__ __launch_bounds__(ROWS_JOINED * 64) void logprobs_join_kernel(Logprob
         A.a.logprobs[at] = lp;
     }
     if (!A.a.top) return;
-    uint8_t *const out = taken + wave * A.n_seg;
+    const int32_t n_keys = A.n_seg * A.a.top;
+    const bool near = n_keys <= JOINED_KEYS;
+    uint8_t *const own = lds + wave * join_bytes(A.n_seg, A.a.top), *const out = own + (near ? n_keys * sizeof(Key) : 0);
+    const Key *keys = A.keys + row * n_keys;
+    if (near) {
+        Key *const copy = reinterpret_cast<Key *>(own);
+        for (int i = lane; i < n_keys; i += 64) copy[i] = keys[i];
+        keys = copy;
+    }
     for (int s = lane; s < A.n_seg; s += 64) out[s] = 0;
-    const Key *const keys = A.keys + row * A.n_seg * A.a.top;
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     Key mine = 0;
     int from = -1;
     bool look = true;
@@ -284,7 +366,7 @@ __global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(GradArgs A) {
         float d[EPV];
 #pragma unroll
         for (int k = 0; k < EPV; k++) {
-            const float y = fmaxf((x[p][k] - m) * A.l.c, -1e4f) - log2_S, e = exp2f(y);
+            const float y = fmaxf((x[p][k] - m) * A.l.c, -1e4f) - log2_S, e = two_to(y);
             d[k] = nothing || x[p][k] == -INFINITY ? 0.0f : e * (-G - gh * (y * LN_2 + H));
             if (x[p][k] != x[p][k]) d[k] = x[p][k];
         }
@@ -322,10 +404,12 @@ LogprobsArgs with_plan(const zf_logprobs_args &a, void *workspace) {
 template <typename ElemT>
 void forward(const LogprobsArgs &A, hipStream_t s) {
     const dim3 grid((uint32_t)(A.a.rows * A.n_seg));
-    if (A.a.top) hipLaunchKernelGGL((logprobs_part_kernel<true, ElemT>), grid, dim3(THREADS), 0, s, A);
-    else hipLaunchKernelGGL((logprobs_part_kernel<false, ElemT>), grid, dim3(THREADS), 0, s, A);
+    const bool entropy = A.a.entropy != nullptr;
+    auto *const part = A.a.top ? (entropy ? logprobs_part_kernel<true, true, ElemT> : logprobs_part_kernel<false, true, ElemT>)
+                               : (entropy ? logprobs_part_kernel<true, false, ElemT> : logprobs_part_kernel<false, false, ElemT>);
+    hipLaunchKernelGGL(part, grid, dim3(THREADS), 0, s, A);
     hipLaunchKernelGGL((logprobs_join_kernel<ElemT>), dim3((uint32_t)((A.a.rows + ROWS_JOINED - 1) / ROWS_JOINED)), dim3(ROWS_JOINED * 64),
-                       A.a.top ? ROWS_JOINED * A.n_seg : 0, s, A);
+                       A.a.top ? ROWS_JOINED * join_bytes(A.n_seg, A.a.top) : 0, s, A);
 }
 
 }  // namespace
