@@ -292,7 +292,7 @@ typedef struct {
     float *entropy;            /* device, [rows], or null */
     int32_t *top_ids;          /* device, [rows][top] */
     float *top_logprobs;       /* device, [rows][top] */
-    float *stats;              /* device, [rows][2], or null: what the gradient is made from (the largest logit, ln of the sum) */
+    float *stats;              /* device, [rows][2], or null: what the gradient is made from (the largest logit, log2 of the sum) */
 } zf_logprobs_args;
 int64_t zf_token_logprobs_workspace(const zf_logprobs_args *a); /* bytes of device memory that zf_token_logprobs needs, or a negative error code */
 int zf_token_logprobs(const zf_logprobs_args *a, void *d_workspace, int64_t workspace_bytes, int32_t device, void *hip_stream);

@@ -1,11 +1,12 @@
 // Log probabilities of given tokens under a mask, with entropy and alternatives, and their gradient.
 //
-// Of a row's allowed logits x, with c = log2(e) / temperature and m their largest:
-//   S = sum 2^((x - m) c),  T = sum 2^((x - m) c) (x - m) c
+// Of a row's allowed logits x, with c = log2(e) / temperature, m their largest and z = x c - m c:
+//   S = sum 2^z,  T = sum 2^z z
 //   logprob of t = (x_t - m) / temperature - ln S        entropy = ln S - ln 2 T / S
 //   d logits_v = 1 / temperature (p_v (-G - g_H (ln p_v + H)) + sum of g_j where token j is v),   G = sum of all g_j
-// m, S and T are held in 32 bits, and sums that were taken around another m join by the factor 2^((m' - m) c).  x - m is taken before it is multiplied:
-// logits at the type's lowest value stay finite then, and equal ones equally probable.
+// All of it is held in 32 bits, and sums that were taken around another m join by the factor 2^(m' c - m c).  z is one fused multiply-add to the rounded
+// product R = m c: as a reference any number near it does, so long as everything that is compared was taken against the same, and all who need it
+// work it out from m.  Far out, where m c - R would be more than a sixteenth (or R infinite: logits at the type's lowest value that a program masked with), z is (x - m) c.
 //   A row is read once, in segments, a workgroup each; a second launch joins a row's segments and looks its given tokens up.
 #include <hip/hip_runtime.h>
 #include <algorithm>
@@ -16,13 +17,14 @@ namespace zf {
 namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 template <typename ElemT> struct Piece;       // 16 bytes at any multiple of an element: the memory system takes them there
 template <> struct Piece<uint32_t> { typedef u32x4 type __attribute__((aligned(4))); };
 template <> struct Piece<uint16_t> { typedef u32x4 type __attribute__((aligned(2))); };
 
 static const float LOG2_E = 1.44269504088896340736f, LN_2 = 0.69314718055994530942f;
 static const int THREADS = 256, WAVES = THREADS / 64, ROWS_JOINED = 4;   // rows a workgroup of the joining kernel takes, a wavefront each
-static const int PIECES = 4;                                             // 16-byte pieces of a segment that a thread holds
+static const int PIECES = 4;                                             // 16-byte pieces of a segment that a thread holds; one where that leaves the chip half empty
 
 struct Part { float m, S, T, pad; };          // of one segment of a row
 // What is largest first, among equals the lowest token: the logit's bits in the order of their values, then the token's complement.  0: none.
@@ -42,11 +44,12 @@ struct GradArgs {
 
 __device__ __forceinline__ float of_bits(uint32_t x) { return __uint_as_float(x); }
 __device__ __forceinline__ float of_bits(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
-__device__ __forceinline__ void to_bits(float x, uint32_t *out) { *out = __float_as_uint(x); }
-__device__ __forceinline__ void to_bits(float x, uint16_t *out) {       // to nearest, ties to even
-    const uint32_t u = __float_as_uint(x);
-    *out = (u & 0x7FFFFFFFu) > 0x7F800000u ? (uint16_t)((u >> 16) | 0x40u) : (uint16_t)((u + 0x7FFFu + ((u >> 16) & 1u)) >> 16);
-}
+// What z is taken against.
+struct Reference {
+    float m, R, c;
+    bool far;                                  // the reference is m c itself, not R
+    __device__ __forceinline__ Reference(float m_, float c_) : m(m_), R(m_ * c_), c(c_), far(!(fabsf(R) < 0x1p20f)) {}
+};
 __device__ __forceinline__ uint32_t in_order(float x) {                  // bits that compare as the values do; NaN and -inf: 0
     const uint32_t u = __float_as_uint(x + 0.0f);
     return x > -INFINITY ? u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u) : 0u;
@@ -83,81 +86,121 @@ __device__ __forceinline__ Key wave_max(Key k) {
     return (Key)high << 32 | wave_max((uint32_t)(k >> 32) == high ? (uint32_t)k : 0u);
 }
 __device__ __forceinline__ float two_to(float x) { return __builtin_amdgcn_exp2f(x); }   // below 2^-126 nothing
-// A finite logit has a finite log probability (the type's lowest value divided by a temperature below one is beyond 32 bits).
-__device__ __forceinline__ float logprob_of(float x, float m, float temperature, float ln_S) {
-    const float lp = (x - m) / temperature - ln_S;
-    return lp < -FLT_MAX && x > -INFINITY ? -FLT_MAX : lp;
+// How far the reference of a part lies below the whole's: nothing times -inf is nothing, so -inf is a large number here.
+__device__ __forceinline__ float below(float m, const Reference &whole) {
+    if (m == whole.m) return 0.0f;
+    const Reference part(m, whole.c);
+    const float d = part.far ? (whole.far ? (m - whole.m) * whole.c : fmaf(m, whole.c, -whole.R)) : whole.far ? -fmaf(whole.m, whole.c, -part.R) : part.R - whole.R;
+    return fmaxf(d, -1e4f);
 }
 // b joins a.  A side without anything has m = -inf and sums of zero (or NaN, where it has nothing but NaN).
 __device__ __forceinline__ void join(Part &a, const Part &b, float c) {
-    const float m = fmaxf(a.m, b.m);
-    const float da = a.m == m ? 0.0f : fmaxf((a.m - m) * c, -1e4f), db = b.m == m ? 0.0f : fmaxf((b.m - m) * c, -1e4f);
-    const float fa = two_to(da), fb = two_to(db);
+    const Reference whole(fmaxf(a.m, b.m), c);
+    const float da = below(a.m, whole), db = below(b.m, whole), fa = two_to(da), fb = two_to(db);
     a.T = fa * (a.T + a.S * da) + fb * (b.T + b.S * db);
     a.S = fa * a.S + fb * b.S;
-    a.m = m;
+    a.m = whole.m;
 }
 __device__ __forceinline__ bool allowed(const uint32_t *mask, int64_t row, int32_t W, uint32_t v) {
     return !mask || ((mask[row * W + (v >> 5)] >> (v & 31)) & 1u);
 }
 
-// Piece of a row from token v on: its logits, -inf where there is no token or none that is allowed.
-template <typename ElemT, int EPV>
-__device__ __forceinline__ void load_piece(const ElemT *row, const uint32_t *mask_row, int32_t v, int32_t V, float (&x)[EPV]) {
+// A thread's pieces of a row's segment, PIECES at a distance of THREADS pieces from token v on: their logits, -inf where there is no token or none that is
+// allowed.  `whole`: the segment ends before the row does.  All loads are issued before the first is looked at.
+template <int PIECES, int EPV, typename ElemT>
+__device__ __forceinline__ void load_pieces(const ElemT *row, const uint32_t *mask_row, int32_t v, int32_t V, bool whole, float (&x)[PIECES][EPV]) {
     constexpr uint32_t FULL = (1u << EPV) - 1u;
-    const int32_t left = V - v;
-    uint32_t bits = left >= EPV ? FULL : left > 0 ? (1u << left) - 1u : 0u;
-    if (mask_row && left > 0) bits &= mask_row[v >> 5] >> (v & 31);
-    if (left >= EPV) {
-        const u32x4 p = *reinterpret_cast<const typename Piece<ElemT>::type *>(row + v);
+    u32x4 raw[PIECES];
+    uint32_t bits[PIECES];
 #pragma unroll
-        for (int k = 0; k < EPV; k++) x[k] = __uint_as_float(sizeof(ElemT) == 4 ? p[k] : k & 1 ? p[k / 2] & 0xFFFF0000u : p[k / 2] << 16);
-    } else {
+    for (int p = 0; p < PIECES; p++) {
+        const int32_t at = v + p * (THREADS * EPV), left = V - at;
+        bits[p] = FULL;
+        if (whole || left >= EPV) raw[p] = *reinterpret_cast<const typename Piece<ElemT>::type *>(row + at);
+        else {
+            bits[p] = left > 0 ? (1u << left) - 1u : 0u;
+            union { u32x4 v; ElemT e[EPV]; } o;
+            o.v = u32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int k = 0; k < EPV; k++) x[k] = k < left ? of_bits(row[v + k]) : 0.0f;
+            for (int k = 0; k < EPV; k++) if (k < left) o.e[k] = row[at + k];
+            raw[p] = o.v;
+        }
+        if (mask_row && (whole || left > 0)) bits[p] &= mask_row[at >> 5] >> (at & 31);
     }
-    if (__any(bits != FULL)) {
 #pragma unroll
-        for (int k = 0; k < EPV; k++) {
-            const uint32_t yes = (uint32_t)__builtin_amdgcn_sbfe((int)bits, k, 1);
-            x[k] = __uint_as_float((__float_as_uint(x[k]) & yes) | (0xFF800000u & ~yes));
+    for (int p = 0; p < PIECES; p++) {
+#pragma unroll
+        for (int k = 0; k < EPV; k++) x[p][k] = __uint_as_float(sizeof(ElemT) == 4 ? raw[p][k] : k & 1 ? raw[p][k / 2] & 0xFFFF0000u : raw[p][k / 2] << 16);
+        if (__any(bits[p] != FULL)) {
+#pragma unroll
+            for (int k = 0; k < EPV; k++) {
+                const uint32_t yes = (uint32_t)__builtin_amdgcn_sbfe((int)bits[p], k, 1);
+                x[p][k] = __uint_as_float((__float_as_uint(x[p][k]) & yes) | (0xFF800000u & ~yes));
+            }
         }
     }
 }
 
-// The alternatives of a segment.  Every wavefront takes the `top`-th largest of its lanes' largest logits (by their bits in order, the upper sixteen of them): its
-// part of the segment's alternatives lies at or above it, and little else does.  What does is listed, and of all lists together the rank of each is the number of keys above it.  When a list
-// overflows (many equal logits) the keys are found one by one, each the largest below the last.
-static const int LISTED = 128;                // keys a wavefront lists
+// The `top` largest of many keys.  A line is found that at least `top` of them reach (the upper sixteen bits of the `top`-th largest, a bit a step, with a
+// ballot), what reaches it is listed -- little else does -- and a listed key's rank is the number of keys above it.  A list that overflows (many equal
+// logits) is left to the caller, which takes the keys one by one, each the largest below the last.
+static const int LISTED = 512, LISTED_JOINED = 128;        // keys that a workgroup, a joining wavefront lists
 
-template <bool ENT, bool TOP, typename ElemT>
+// The largest multiple of 2^16 that `top` lanes reach, but at least 1 (0 stands for no logit).
+__device__ __forceinline__ uint32_t line_of(uint32_t o, int top) {
+    uint32_t line = 0;
+#pragma unroll
+    for (int bit = 31; bit >= 16; bit--) {
+        const uint32_t up = line | 1u << bit;
+        if (__popcll(__ballot(o >= up)) >= top) line = up;
+    }
+    return line ? line : 1;
+}
+__device__ __forceinline__ int rank_of(Key mine, const Key *list, int n) {
+    int rank = 0;
+#pragma unroll 8
+    for (int j = 0; j < n; j++) rank += list[j] > mine;
+    return rank;
+}
+
+template <int PIECES, bool ENT, bool TOP, typename ElemT>
 __global__ __launch_bounds__(THREADS) void logprobs_part_kernel(LogprobsArgs A) {
     constexpr int EPV = 16 / sizeof(ElemT);
     __shared__ Part part[WAVES];
-    __shared__ Key best[WAVES], listed[TOP ? WAVES * LISTED : 1];
-    __shared__ int n_listed[WAVES];
+    __shared__ Key best[WAVES], listed[TOP ? LISTED : 1];
+    __shared__ uint32_t lines[2][WAVES];
+    __shared__ int n_listed;
     const int tid = threadIdx.x, wave = tid / 64;
     const int64_t row = blockIdx.x / (uint32_t)A.n_seg;
     const int32_t seg = blockIdx.x % (uint32_t)A.n_seg, V = A.a.V, v0 = seg * (THREADS * PIECES * EPV) + tid * EPV;
     const ElemT *const logits = (const ElemT *)A.a.logits + row * A.a.row_stride_elems;
     const uint32_t *const mask = A.a.mask ? A.a.mask + row * A.W : nullptr;
     float x[PIECES][EPV], most = -INFINITY;
-#pragma unroll
-    for (int p = 0; p < PIECES; p++) load_piece<ElemT, EPV>(logits, mask, v0 + p * (THREADS * EPV), V, x[p]);
+    load_pieces<PIECES, EPV>(logits, mask, v0, V, (seg + 1) * (THREADS * PIECES * EPV) <= V, x);
 #pragma unroll
     for (int p = 0; p < PIECES; p++)
 #pragma unroll
         for (int k = 0; k < EPV; k++) most = fmaxf(most, x[p][k]);
     const float m = wave_max(most);
+    const Reference ref(m, A.c);
     float S = 0.0f, T = 0.0f;
-    if (m > -INFINITY) {
+    if (!ref.far) {
 #pragma unroll
         for (int p = 0; p < PIECES; p++)
 #pragma unroll
             for (int k = 0; k < EPV; k++) {
-                const float z = (x[p][k] - m) * A.c, e = two_to(z);
+                const float z = fmaf(x[p][k], ref.c, -ref.R), e = two_to(z);
                 S += e;
                 if (ENT) T = fmaf(e, fmaxf(z, -1e4f), T);  // nothing times -inf is nothing
+            }
+    } else if (m > -INFINITY) {
+#pragma unroll
+        for (int p = 0; p < PIECES; p++)
+#pragma unroll
+            for (int k = 0; k < EPV; k++) {
+                const float z = (x[p][k] - m) * ref.c, e = two_to(z);
+                S += e;
+                if (ENT) T = fmaf(e, fmaxf(z, -1e4f), T);
             }
     } else {
 #pragma unroll
@@ -169,51 +212,51 @@ __global__ __launch_bounds__(THREADS) void logprobs_part_kernel(LogprobsArgs A) 
     if (ENT) T = wave_sum(T);
     if (tid % 64 == 0) part[wave] = Part{m, S, T, 0.0f};
     if (TOP) {
-        const uint32_t mine = in_order(most);
-        uint32_t line = 0;                                 // the largest multiple of 2^16 that `top` lanes reach
-#pragma unroll
-        for (int bit = 31; bit >= 16; bit--) {
-            const uint32_t up = line | 1u << bit;
-            if (__popcll(__ballot(mine >= up)) >= A.a.top) line = up;
-        }
-        if (line == 0) line = 1;                           // 0 stands for no logit
-        int n = 0;
-#pragma unroll
-        for (int p = 0; p < PIECES; p++)
-#pragma unroll
-            for (int k = 0; k < EPV; k++) {
-                const uint32_t o = in_order(x[p][k]);
-                const unsigned long long who = __ballot(o >= line);
-                if (!who) continue;
-                const int at = n + __popcll(who & ((1ull << (tid % 64)) - 1));
-                if (o >= line && at < LISTED) listed[wave * LISTED + at] = (Key)o << 32 | (uint32_t)~(uint32_t)(v0 + p * (THREADS * EPV) + k);
-                n += __popcll(who);
-            }
-        if (tid % 64 == 0) n_listed[wave] = n;
+        const uint32_t mine = in_order(most);              // as many lanes as reach a line have a logit that does
+        lines[0][wave] = line_of(mine, A.a.top);
+        lines[1][wave] = line_of(mine, (A.a.top + WAVES - 1) / WAVES);
+        if (tid == 0) n_listed = 0;
     }
     __syncthreads();
-    if (tid == 0) {
+    if (tid == THREADS - 1) {
         Part all = part[0];
 #pragma unroll
         for (int w = 1; w < WAVES; w++) join(all, part[w], A.c);
         A.parts[blockIdx.x] = all;
     }
     if (!TOP) return;
-    Key *const out = A.keys + (int64_t)blockIdx.x * A.a.top;
-    int n_all = 0;
-    bool fits = true;
+    // `top` logits of a single wavefront reach the one, a share of them in each wavefront the other: the higher of the two
+    uint32_t line = lines[0][0], share = lines[1][0];
 #pragma unroll
-    for (int w = 0; w < WAVES; w++) { n_all += n_listed[w]; fits = fits && n_listed[w] <= LISTED; }
-    if (fits) {
-        for (int i = tid; i < WAVES * LISTED; i += THREADS) {
-            if (i % LISTED >= n_listed[i / LISTED]) continue;
+    for (int w = 1; w < WAVES; w++) { line = max(line, lines[0][w]); share = min(share, lines[1][w]); }
+    line = max(line, share);
+    const float from = line <= 0x007FFFFFu ? -FLT_MAX : logit_of((Key)line << 32);
+    if (most >= from) {                                    // few lanes; the list's order does not show: keys differ
+        int n = 0;
+#pragma unroll
+        for (int p = 0; p < PIECES; p++)
+#pragma unroll
+            for (int k = 0; k < EPV; k++) n += x[p][k] >= from;
+        int at = atomicAdd(&n_listed, n);
+#pragma unroll
+        for (int p = 0; p < PIECES; p++)
+#pragma unroll
+            for (int k = 0; k < EPV; k++)
+                if (x[p][k] >= from) {
+                    if (at < LISTED) listed[at] = key_of(x[p][k], (uint32_t)(v0 + p * (THREADS * EPV) + k));
+                    at++;
+                }
+    }
+    __syncthreads();
+    Key *const out = A.keys + (int64_t)blockIdx.x * A.a.top;
+    const int n = n_listed;
+    if (n <= LISTED) {
+        for (int i = tid; i < n; i += THREADS) {
             const Key mine = listed[i];
-            int rank = 0;
-            for (int w = 0; w < WAVES; w++)
-                for (int j = 0; j < n_listed[w]; j++) rank += listed[w * LISTED + j] > mine;
+            const int rank = rank_of(mine, listed, n);
             if (rank < A.a.top) out[rank] = mine;
         }
-        if (tid < A.a.top && tid >= n_all) out[tid] = 0;
+        if (tid < A.a.top && tid >= n) out[tid] = 0;
         return;
     }
     Key last = ~(Key)0;
@@ -237,57 +280,100 @@ __global__ __launch_bounds__(THREADS) void logprobs_part_kernel(LogprobsArgs A) 
     }
 }
 
-// A row's parts, by one wavefront; the alternatives are merged from the segments' sorted lists, a lane at the head of each.
-static const int JOINED_KEYS = 1024;                       // so many of a row are brought to LDS (a step to the next of a list in memory takes ten times as long)
-__host__ __device__ __forceinline__ int32_t join_bytes(int32_t n_seg, int32_t top) {
-    return ((top && n_seg * top <= JOINED_KEYS ? n_seg * top * (int32_t)sizeof(Key) : 0) + n_seg + 7) / 8 * 8;
-}
+// A row's parts, by one wavefront.  Its segments' alternatives are listed and ranked as a segment's are, up to JOINED_LANE in a lane; with more of them, or
+// more equal ones than the list takes, they are merged from the segments' sorted lists, a lane at the head of each.
+static const int JOINED_LANE = 16;
 
 template <typename ElemT>
 __global__ __launch_bounds__(ROWS_JOINED * 64) void logprobs_join_kernel(LogprobsArgs A) {
-    extern __shared__ __align__(8) uint8_t lds[];          // of each row: its segments' keys where they fit, then how many of each are out
+    __shared__ Key listed[ROWS_JOINED][LISTED_JOINED];
+    extern __shared__ uint8_t taken[];                     // [ROWS_JOINED][n_seg]: keys of a segment that are out
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int64_t row = (int64_t)blockIdx.x * ROWS_JOINED + wave;
     if (row >= A.a.rows) return;                           // whole wavefronts, and no barrier below
+    // everything that has to come from memory is asked for first
+    const int32_t n_keys = A.n_seg * A.a.top;
+    const Key *const keys = A.keys + row * n_keys;
+    const bool listable = A.a.top && n_keys <= JOINED_LANE * 64;
+    Key own[JOINED_LANE];
+    if (listable)
+#pragma unroll
+        for (int j = 0; j < JOINED_LANE; j++) {
+            own[j] = 0;
+            if (j * 64 + lane < n_keys) own[j] = keys[j * 64 + lane];
+        }
+    const ElemT *const logits = (const ElemT *)A.a.logits + row * A.a.row_stride_elems;
+    int64_t t = -1;                                        // the lane's given token, its logit (-inf where the mask does not allow it)
+    float x = -INFINITY;
+    auto look_up = [&](int j) {
+        const int64_t at = row * A.a.n_tokens + j;
+        t = A.a.token_bytes == 8 ? ((const int64_t *)A.a.tokens)[at] : ((const int32_t *)A.a.tokens)[at];
+        x = -INFINITY;
+        if (t >= 0 && t < A.a.V) {
+            const float logit = of_bits(logits[t]);
+            if (allowed(A.a.mask, row, A.W, (uint32_t)t)) x = logit;
+        }
+    };
+    if (lane < A.a.n_tokens) look_up(lane);
     Part all{-INFINITY, 0.0f, 0.0f, 0.0f};
     for (int s = lane; s < A.n_seg; s += 64) join(all, A.parts[row * A.n_seg + s], A.c);
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const Part o{__shfl_xor(all.m, d), __shfl_xor(all.S, d), __shfl_xor(all.T, d), 0.0f};
-        join(all, o, A.c);
-    }
-    const bool nothing = all.m == -INFINITY && all.S == 0.0f;
-    const float ln_S = nothing ? 0.0f : logf(all.S);
+    const Reference ref(wave_max(all.m), A.c);
+    const float d = below(all.m, ref), f = two_to(d);
+    all.T = wave_sum(f * (all.T + all.S * d));
+    all.S = wave_sum(f * all.S);
+    const bool nothing = ref.m == -INFINITY && all.S == 0.0f;
+    const float log2_S = nothing ? 0.0f : log2f(all.S);
+    const float ln_S = LN_2 * (ref.far ? log2_S : log2_S - fmaf(ref.m, ref.c, -ref.R));      // of the sum around m itself
+    auto logprob_of = [&](float x) {                       // a finite logit has a finite log probability (the type's lowest value divided by a temperature below one is beyond 32 bits)
+        const float lp = (x - ref.m) / A.a.temperature - ln_S;
+        return lp < -FLT_MAX && x > -INFINITY ? -FLT_MAX : lp;
+    };
     if (lane == 0) {
-        if (A.a.entropy) A.a.entropy[row] = nothing ? 0.0f : ln_S - LN_2 * all.T / all.S;
-        if (A.a.stats) { A.a.stats[2 * row] = all.m; A.a.stats[2 * row + 1] = ln_S; }
+        if (A.a.entropy) A.a.entropy[row] = nothing ? 0.0f : LN_2 * (log2_S - all.T / all.S);
+        if (A.a.stats) { A.a.stats[2 * row] = ref.m; A.a.stats[2 * row + 1] = log2_S; }
     }
-    const ElemT *const logits = (const ElemT *)A.a.logits + row * A.a.row_stride_elems;
     for (int j = lane; j < A.a.n_tokens; j += 64) {
-        const int64_t at = row * A.a.n_tokens + j;
-        const int64_t t = A.a.token_bytes == 8 ? ((const int64_t *)A.a.tokens)[at] : ((const int32_t *)A.a.tokens)[at];
+        if (j != lane) look_up(j);
         float lp = 0.0f;
         if (t >= A.a.V) lp = NAN;
-        else if (t >= 0) {
-            lp = -INFINITY;
-            if (!nothing && allowed(A.a.mask, row, A.W, (uint32_t)t)) lp = logprob_of(of_bits(logits[t]), all.m, A.a.temperature, ln_S);
-            else if (all.S != all.S) lp = all.S;
-        }
-        A.a.logprobs[at] = lp;
+        else if (t >= 0) lp = all.S != all.S ? all.S : x == -INFINITY ? -INFINITY : logprob_of(x);
+        A.a.logprobs[row * A.a.n_tokens + j] = lp;
     }
     if (!A.a.top) return;
-    const int32_t n_keys = A.n_seg * A.a.top;
-    const bool near = n_keys <= JOINED_KEYS;
-    uint8_t *const own = lds + wave * join_bytes(A.n_seg, A.a.top), *const out = own + (near ? n_keys * sizeof(Key) : 0);
-    const Key *keys = A.keys + row * n_keys;
-    if (near) {
-        Key *const copy = reinterpret_cast<Key *>(own);
-        for (int i = lane; i < n_keys; i += 64) copy[i] = keys[i];
-        keys = copy;
+    auto store = [&](int i, Key k) {
+        A.a.top_ids[row * A.a.top + i] = k ? (int32_t)~(uint32_t)k : -1;
+        A.a.top_logprobs[row * A.a.top + i] = k ? logprob_of(logit_of(k)) : -INFINITY;
+    };
+    if (listable) {
+        uint32_t most = 0;
+#pragma unroll
+        for (int j = 0; j < JOINED_LANE; j++) most = max(most, (uint32_t)(own[j] >> 32));
+        const uint32_t line = line_of(most, A.a.top);
+        Key *const list = listed[wave];
+        int n = 0;
+#pragma unroll
+        for (int j = 0; j < JOINED_LANE; j++) {
+            const bool in = (uint32_t)(own[j] >> 32) >= line;
+            const unsigned long long who = __ballot(in);
+            if (!who) continue;
+            const int at = n + __popcll(who & ((1ull << lane) - 1));
+            if (in && at < LISTED_JOINED) list[at] = own[j];
+            n += __popcll(who);
+        }
+        if (n <= LISTED_JOINED) {
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+            __builtin_amdgcn_wave_barrier();
+            for (int i = lane; i < n; i += 64) {
+                const Key mine = list[i];
+                const int rank = rank_of(mine, list, n);
+                if (rank < A.a.top) store(rank, mine);
+            }
+            for (int i = n + lane; i < A.a.top; i += 64) store(i, 0);
+            return;
+        }
     }
-    for (int s = lane; s < A.n_seg; s += 64) out[s] = 0;
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    uint8_t *const out = taken + wave * A.n_seg;
+    for (int s = lane; s < A.n_seg; s += 64) out[s] = 0;   // a lane reads what it wrote itself
     Key mine = 0;
     int from = -1;
     bool look = true;
@@ -302,15 +388,12 @@ __global__ __launch_bounds__(ROWS_JOINED * 64) void logprobs_join_kernel(Logprob
         const Key k = wave_max(mine);
         look = k && k == mine;
         if (look) out[from]++;
-        if (lane == 0) {
-            A.a.top_ids[row * A.a.top + i] = k ? (int32_t)~(uint32_t)k : -1;
-            A.a.top_logprobs[row * A.a.top + i] = k ? logprob_of(logit_of(k), all.m, A.a.temperature, ln_S) : -INFINITY;
-        }
+        if (lane == 0) store(i, k);
     }
 }
 
 // The gradient: every thread reads a piece before it writes it, so the two may be the same memory.
-template <typename ElemT>
+template <int PIECES, typename ElemT>
 __global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(GradArgs A) {
     constexpr int EPV = 16 / sizeof(ElemT);
     __shared__ float sums[WAVES];
@@ -323,9 +406,9 @@ __global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(GradArgs A) {
     const int32_t seg = blockIdx.x % (uint32_t)A.l.n_seg, V = a.V, first = seg * (THREADS * PIECES * EPV), v0 = first + tid * EPV;
     const ElemT *const logits = (const ElemT *)a.logits + row * a.row_stride_elems;
     const uint32_t *const mask = a.mask ? a.mask + row * A.l.W : nullptr;
+    const bool whole = first + THREADS * PIECES * EPV <= V;
     float x[PIECES][EPV];
-#pragma unroll
-    for (int p = 0; p < PIECES; p++) load_piece<ElemT, EPV>(logits, mask, v0 + p * (THREADS * EPV), V, x[p]);
+    load_pieces<PIECES, EPV>(logits, mask, v0, V, whole, x);
     float G = 0.0f;
     const int n_given = A.g.g_logprobs ? a.n_tokens : 0, n_all = n_given + (A.g.g_top ? a.top : 0);
     if (wave == 0) {                                       // the first wavefront lists them, in order
@@ -346,7 +429,7 @@ __global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(GradArgs A) {
             G += g;
             const bool here = t >= first && t < first + THREADS * PIECES * EPV;
             const unsigned long long who = __ballot(here);
-            if (here) { const int at = n + __popcll(who & ((1ull << lane) - 1)); mine_v[at] = (int32_t)t; mine_g[at] = g; }
+            if (here) { const int at = n + __popcll(who & ((1ull << lane) - 1)); mine_v[at] = (int32_t)t; mine_g[at] = g * A.l.inv_t; }
             n += __popcll(who);
         }
         G = wave_sum(G);
@@ -354,30 +437,41 @@ __global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(GradArgs A) {
     }
     __syncthreads();
     G = sums[0];
-    const float m = a.stats[2 * row], ln_S = a.stats[2 * row + 1], inv_t = A.l.inv_t;
+    const Reference ref(a.stats[2 * row], A.l.c);
+    const float log2_S = a.stats[2 * row + 1], inv_t = A.l.inv_t;
     const float gh = A.g.g_entropy ? A.g.g_entropy[row] : 0.0f, H = A.g.g_entropy ? a.entropy[row] : 0.0f;
-    const bool nothing = m == -INFINITY;
-    const float log2_S = ln_S * LOG2_E;
+    // d = p (base + slope log2 p), p = 2^y, y = log2 p
+    const float base = inv_t * (-G - gh * H), slope = -inv_t * gh * LN_2;
     const int n = n_mine;
     ElemT *const grad = (ElemT *)A.g.grad + row * A.g.stride;
 #pragma unroll
     for (int p = 0; p < PIECES; p++) {
         const int32_t v = v0 + p * (THREADS * EPV);
         float d[EPV];
+        if (!ref.far) {
 #pragma unroll
-        for (int k = 0; k < EPV; k++) {
-            const float y = fmaxf((x[p][k] - m) * A.l.c, -1e4f) - log2_S, e = two_to(y);
-            d[k] = nothing || x[p][k] == -INFINITY ? 0.0f : e * (-G - gh * (y * LN_2 + H));
-            if (x[p][k] != x[p][k]) d[k] = x[p][k];
+            for (int k = 0; k < EPV; k++) {
+                const float y = fmaxf(fmaf(x[p][k], ref.c, -ref.R), -1e4f) - log2_S;
+                d[k] = two_to(y) * fmaf(slope, y, base);
+            }
+        } else {                                           // nothing that is allowed, NaN alone, or logits that are far out
+#pragma unroll
+            for (int k = 0; k < EPV; k++) {
+                const float y = fmaxf((x[p][k] - ref.m) * ref.c, -1e4f) - log2_S;
+                d[k] = x[p][k] == -INFINITY ? 0.0f : two_to(y) * fmaf(slope, y, base);
+            }
         }
         for (int j = 0; j < n; j++) {
 #pragma unroll
             for (int k = 0; k < EPV; k++) if (mine_v[j] == v + k) d[k] += mine_g[j];
         }
-        union { u32x4 v; ElemT e[EPV]; } o;
+        union { u32x4 v; ElemT e[EPV]; bf16x2 b[4]; } o;
 #pragma unroll
-        for (int k = 0; k < EPV; k++) to_bits(d[k] * inv_t, &o.e[k]);
-        if (v + EPV <= V) *reinterpret_cast<typename Piece<ElemT>::type *>(grad + v) = o.v;
+        for (int k = 0; k < EPV; k += 2) {
+            if (sizeof(ElemT) == 4) { o.v[k % 4] = __float_as_uint(d[k]); o.v[k % 4 + 1] = __float_as_uint(d[k + 1]); }
+            else o.b[k / 2 % 4] = bf16x2{(__bf16)d[k], (__bf16)d[k + 1]};
+        }
+        if (whole || v + EPV <= V) *reinterpret_cast<typename Piece<ElemT>::type *>(grad + v) = o.v;
         else {
 #pragma unroll
             for (int k = 0; k < EPV; k++) if (v + k < V) grad[v + k] = o.e[k];
@@ -385,8 +479,14 @@ __global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(GradArgs A) {
     }
 }
 
+// A thread of a segment holds PIECES pieces, or one where segments of so many would be fewer than two workgroups a compute unit.
+int pieces(const zf_logprobs_args &a) {
+    const int64_t n = THREADS * PIECES * (a.dtype == 0 ? 4 : 8);
+    if (a.rows * ((a.V + n - 1) / n) >= 512) return PIECES;
+    return (int64_t)((a.V + n / PIECES - 1) / (n / PIECES)) * a.top <= JOINED_LANE * 64 ? 1 : PIECES;   // ... and what the joining wavefronts list holds their alternatives
+}
 int32_t segments(const zf_logprobs_args &a) {
-    const int32_t n = THREADS * PIECES * (a.dtype == 0 ? 4 : 8);
+    const int32_t n = THREADS * pieces(a) * (a.dtype == 0 ? 4 : 8);
     return (a.V + n - 1) / n;
 }
 LogprobsArgs with_plan(const zf_logprobs_args &a, void *workspace) {
@@ -401,15 +501,19 @@ LogprobsArgs with_plan(const zf_logprobs_args &a, void *workspace) {
     return A;
 }
 
+template <int PIECES, typename ElemT>
+void parts(const LogprobsArgs &A, hipStream_t s) {
+    const bool entropy = A.a.entropy != nullptr;
+    auto *const part = A.a.top ? (entropy ? logprobs_part_kernel<PIECES, true, true, ElemT> : logprobs_part_kernel<PIECES, false, true, ElemT>)
+                               : (entropy ? logprobs_part_kernel<PIECES, true, false, ElemT> : logprobs_part_kernel<PIECES, false, false, ElemT>);
+    hipLaunchKernelGGL(part, dim3((uint32_t)(A.a.rows * A.n_seg)), dim3(THREADS), 0, s, A);
+}
 template <typename ElemT>
 void forward(const LogprobsArgs &A, hipStream_t s) {
-    const dim3 grid((uint32_t)(A.a.rows * A.n_seg));
-    const bool entropy = A.a.entropy != nullptr;
-    auto *const part = A.a.top ? (entropy ? logprobs_part_kernel<true, true, ElemT> : logprobs_part_kernel<false, true, ElemT>)
-                               : (entropy ? logprobs_part_kernel<true, false, ElemT> : logprobs_part_kernel<false, false, ElemT>);
-    hipLaunchKernelGGL(part, grid, dim3(THREADS), 0, s, A);
+    if (pieces(A.a) == 1) parts<1, ElemT>(A, s);
+    else parts<PIECES, ElemT>(A, s);
     hipLaunchKernelGGL((logprobs_join_kernel<ElemT>), dim3((uint32_t)((A.a.rows + ROWS_JOINED - 1) / ROWS_JOINED)), dim3(ROWS_JOINED * 64),
-                       A.a.top ? ROWS_JOINED * join_bytes(A.n_seg, A.a.top) : 0, s, A);
+                       A.a.top ? ROWS_JOINED * A.n_seg : 0, s, A);
 }
 
 }  // namespace
@@ -426,9 +530,9 @@ hipError_t launch_logprobs(const zf_logprobs_args &a, void *workspace, hipStream
 
 hipError_t launch_logprobs_backward(const zf_logprobs_args &a, const LogprobsGrad &g, hipStream_t s) {
     const GradArgs A{with_plan(a, nullptr), g};
-    const dim3 grid((uint32_t)(a.rows * A.l.n_seg));
-    if (a.dtype == 0) hipLaunchKernelGGL((logprobs_grad_kernel<uint32_t>), grid, dim3(THREADS), 0, s, A);
-    else hipLaunchKernelGGL((logprobs_grad_kernel<uint16_t>), grid, dim3(THREADS), 0, s, A);
+    auto *const kernel = pieces(a) == 1 ? (a.dtype == 0 ? logprobs_grad_kernel<1, uint32_t> : logprobs_grad_kernel<1, uint16_t>)
+                                        : (a.dtype == 0 ? logprobs_grad_kernel<PIECES, uint32_t> : logprobs_grad_kernel<PIECES, uint16_t>);
+    hipLaunchKernelGGL(kernel, dim3((uint32_t)(a.rows * A.l.n_seg)), dim3(THREADS), 0, s, A);
     return hipGetLastError();
 }
 
