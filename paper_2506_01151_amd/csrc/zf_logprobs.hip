@@ -107,7 +107,7 @@ __device__ __forceinline__ bool allowed(const uint32_t *mask, int64_t row, int32
 
 // A thread's pieces of a row's segment, PIECES at a distance of THREADS pieces from token v on: their logits, -inf where there is no token or none that is
 // allowed.  `whole`: the segment ends before the row does.  All loads are issued before the first is looked at.
-template <int PIECES, int EPV, typename ElemT>
+template <int PIECES, int EPV, bool ONCE, typename ElemT>
 __device__ __forceinline__ void load_pieces(const ElemT *row, const uint32_t *mask_row, int32_t v, int32_t V, bool whole, float (&x)[PIECES][EPV]) {
     constexpr uint32_t FULL = (1u << EPV) - 1u;
     u32x4 raw[PIECES];
@@ -116,7 +116,8 @@ __device__ __forceinline__ void load_pieces(const ElemT *row, const uint32_t *ma
     for (int p = 0; p < PIECES; p++) {
         const int32_t at = v + p * (THREADS * EPV), left = V - at;
         bits[p] = FULL;
-        if (whole || left >= EPV) raw[p] = *reinterpret_cast<const typename Piece<ElemT>::type *>(row + at);
+        const typename Piece<ElemT>::type *const from = reinterpret_cast<const typename Piece<ElemT>::type *>(row + at);
+        if (whole || left >= EPV) raw[p] = ONCE ? __builtin_nontemporal_load(from) : *from;
         else {
             bits[p] = left > 0 ? (1u << left) - 1u : 0u;
             union { u32x4 v; ElemT e[EPV]; } o;
@@ -144,7 +145,7 @@ __device__ __forceinline__ void load_pieces(const ElemT *row, const uint32_t *ma
 // The `top` largest of many keys.  A line is found that at least `top` of them reach (the upper sixteen bits of the `top`-th largest, a bit a step, with a
 // ballot), what reaches it is listed -- little else does -- and a listed key's rank is the number of keys above it.  A list that overflows (many equal
 // logits) is left to the caller, which takes the keys one by one, each the largest below the last.
-static const int LISTED = 512, LISTED_JOINED = 128;        // keys that a workgroup, a joining wavefront lists
+static const int LISTED = 128;                             // keys that a wavefront lists
 
 // The largest multiple of 2^16 that `top` lanes reach, but at least 1 (0 stands for no logit).
 __device__ __forceinline__ uint32_t line_of(uint32_t o, int top) {
@@ -163,20 +164,22 @@ __device__ __forceinline__ int rank_of(Key mine, const Key *list, int n) {
     return rank;
 }
 
-template <int PIECES, bool ENT, bool TOP, typename ElemT>
+template <int PIECES, bool ONCE, bool ENT, bool TOP, typename ElemT>
 __global__ __launch_bounds__(THREADS) void logprobs_part_kernel(LogprobsArgs A) {
     constexpr int EPV = 16 / sizeof(ElemT);
     __shared__ Part part[WAVES];
-    __shared__ Key best[WAVES], listed[TOP ? LISTED : 1];
+    __shared__ Key best[WAVES];
+    __shared__ float listed_x[TOP ? WAVES : 1][LISTED];
+    __shared__ uint32_t listed_v[TOP ? WAVES : 1][LISTED];
     __shared__ uint32_t lines[2][WAVES];
-    __shared__ int n_listed;
+    __shared__ int n_listed[WAVES];
     const int tid = threadIdx.x, wave = tid / 64;
     const int64_t row = blockIdx.x / (uint32_t)A.n_seg;
     const int32_t seg = blockIdx.x % (uint32_t)A.n_seg, V = A.a.V, v0 = seg * (THREADS * PIECES * EPV) + tid * EPV;
     const ElemT *const logits = (const ElemT *)A.a.logits + row * A.a.row_stride_elems;
     const uint32_t *const mask = A.a.mask ? A.a.mask + row * A.W : nullptr;
     float x[PIECES][EPV], most = -INFINITY;
-    load_pieces<PIECES, EPV>(logits, mask, v0, V, (seg + 1) * (THREADS * PIECES * EPV) <= V, x);
+    load_pieces<PIECES, EPV, ONCE>(logits, mask, v0, V, (seg + 1) * (THREADS * PIECES * EPV) <= V, x);
 #pragma unroll
     for (int p = 0; p < PIECES; p++)
 #pragma unroll
@@ -215,7 +218,6 @@ __global__ __launch_bounds__(THREADS) void logprobs_part_kernel(LogprobsArgs A) 
         const uint32_t mine = in_order(most);              // as many lanes as reach a line have a logit that does
         lines[0][wave] = line_of(mine, A.a.top);
         lines[1][wave] = line_of(mine, (A.a.top + WAVES - 1) / WAVES);
-        if (tid == 0) n_listed = 0;
     }
     __syncthreads();
     if (tid == THREADS - 1) {
@@ -231,32 +233,44 @@ __global__ __launch_bounds__(THREADS) void logprobs_part_kernel(LogprobsArgs A) 
     for (int w = 1; w < WAVES; w++) { line = max(line, lines[0][w]); share = min(share, lines[1][w]); }
     line = max(line, share);
     const float from = line <= 0x007FFFFFu ? -FLT_MAX : logit_of((Key)line << 32);
-    if (most >= from) {                                    // few lanes; the list's order does not show: keys differ
-        int n = 0;
+    int n = 0;
 #pragma unroll
-        for (int p = 0; p < PIECES; p++)
+    for (int p = 0; p < PIECES; p++)
 #pragma unroll
-            for (int k = 0; k < EPV; k++) n += x[p][k] >= from;
-        int at = atomicAdd(&n_listed, n);
-#pragma unroll
-        for (int p = 0; p < PIECES; p++)
-#pragma unroll
-            for (int k = 0; k < EPV; k++)
-                if (x[p][k] >= from) {
-                    if (at < LISTED) listed[at] = key_of(x[p][k], (uint32_t)(v0 + p * (THREADS * EPV) + k));
-                    at++;
-                }
-    }
+        for (int k = 0; k < EPV; k++) {
+            const unsigned long long who = __ballot(x[p][k] >= from);
+            if (!who) continue;                            // most often
+            const int at = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
+            if (x[p][k] >= from && at < LISTED) { listed_x[wave][at] = x[p][k]; listed_v[wave][at] = (uint32_t)(v0 + p * (THREADS * EPV) + k); }
+            n += __popcll(who);
+        }
+    if (tid % 64 == 0) n_listed[wave] = n;
     __syncthreads();
     Key *const out = A.keys + (int64_t)blockIdx.x * A.a.top;
-    const int n = n_listed;
-    if (n <= LISTED) {
-        for (int i = tid; i < n; i += THREADS) {
-            const Key mine = listed[i];
-            const int rank = rank_of(mine, listed, n);
-            if (rank < A.a.top) out[rank] = mine;
+    int n_all = 0;
+    bool fits = true;
+#pragma unroll
+    for (int w = 0; w < WAVES; w++) { n_all += n_listed[w]; fits = fits && n_listed[w] <= LISTED; }
+    if (fits) {
+        if (wave) return;                                  // the first wavefront ranks them, 64 at a time
+        auto key_at = [&](int i) -> Key {
+            int w = 0;
+#pragma unroll
+            for (int u = 0; u < WAVES - 1; u++) if (w == u && i >= n_listed[u]) { i -= n_listed[u]; w++; }
+            return key_of(listed_x[w][i], listed_v[w][i]);
+        };
+        for (int i0 = 0; i0 < n_all; i0 += 64) {
+            const Key mine = i0 + tid < n_all ? key_at(i0 + tid) : 0;
+            int rank = 0;
+            for (int j0 = 0; j0 < n_all; j0 += 64) {
+                const Key other = j0 == i0 ? mine : j0 + tid < n_all ? key_at(j0 + tid) : 0;
+                const int n_other = n_all - j0 < 64 ? n_all - j0 : 64;
+                for (int j = 0; j < n_other; j++)
+                    rank += ((Key)(uint32_t)__builtin_amdgcn_readlane((int)(other >> 32), j) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)other, j)) > mine;
+            }
+            if (mine && rank < A.a.top) out[rank] = mine;
         }
-        if (tid < A.a.top && tid >= n) out[tid] = 0;
+        for (int i = n_all + tid; i < A.a.top; i += 64) out[i] = 0;
         return;
     }
     Key last = ~(Key)0;
@@ -286,7 +300,7 @@ static const int JOINED_LANE = 16;
 
 template <typename ElemT>
 __global__ __launch_bounds__(ROWS_JOINED * 64) void logprobs_join_kernel(LogprobsArgs A) {
-    __shared__ Key listed[ROWS_JOINED][LISTED_JOINED];
+    __shared__ Key listed[ROWS_JOINED][LISTED];
     extern __shared__ uint8_t taken[];                     // [ROWS_JOINED][n_seg]: keys of a segment that are out
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int64_t row = (int64_t)blockIdx.x * ROWS_JOINED + wave;
@@ -357,10 +371,10 @@ __global__ __launch_bounds__(ROWS_JOINED * 64) void logprobs_join_kernel(Logprob
             const unsigned long long who = __ballot(in);
             if (!who) continue;
             const int at = n + __popcll(who & ((1ull << lane) - 1));
-            if (in && at < LISTED_JOINED) list[at] = own[j];
+            if (in && at < LISTED) list[at] = own[j];
             n += __popcll(who);
         }
-        if (n <= LISTED_JOINED) {
+        if (n <= LISTED) {
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
             for (int i = lane; i < n; i += 64) {
@@ -393,7 +407,7 @@ __global__ __launch_bounds__(ROWS_JOINED * 64) void logprobs_join_kernel(Logprob
 }
 
 // The gradient: every thread reads a piece before it writes it, so the two may be the same memory.
-template <int PIECES, typename ElemT>
+template <int PIECES, bool ONCE, typename ElemT>
 __global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(GradArgs A) {
     constexpr int EPV = 16 / sizeof(ElemT);
     __shared__ float sums[WAVES];
@@ -408,7 +422,7 @@ __global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(GradArgs A) {
     const uint32_t *const mask = a.mask ? a.mask + row * A.l.W : nullptr;
     const bool whole = first + THREADS * PIECES * EPV <= V;
     float x[PIECES][EPV];
-    load_pieces<PIECES, EPV>(logits, mask, v0, V, whole, x);
+    load_pieces<PIECES, EPV, ONCE>(logits, mask, v0, V, whole, x);
     float G = 0.0f;
     const int n_given = A.g.g_logprobs ? a.n_tokens : 0, n_all = n_given + (A.g.g_top ? a.top : 0);
     if (wave == 0) {                                       // the first wavefront lists them, in order
@@ -471,8 +485,11 @@ __global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(GradArgs A) {
             if (sizeof(ElemT) == 4) { o.v[k % 4] = __float_as_uint(d[k]); o.v[k % 4 + 1] = __float_as_uint(d[k + 1]); }
             else o.b[k / 2 % 4] = bf16x2{(__bf16)d[k], (__bf16)d[k + 1]};
         }
-        if (whole || v + EPV <= V) *reinterpret_cast<typename Piece<ElemT>::type *>(grad + v) = o.v;
-        else {
+        typename Piece<ElemT>::type *const to = reinterpret_cast<typename Piece<ElemT>::type *>(grad + v);
+        if (whole || v + EPV <= V) {
+            if (ONCE) __builtin_nontemporal_store(o.v, to);
+            else *to = o.v;
+        } else {
 #pragma unroll
             for (int k = 0; k < EPV; k++) if (v + k < V) grad[v + k] = o.e[k];
         }
@@ -501,17 +518,25 @@ LogprobsArgs with_plan(const zf_logprobs_args &a, void *workspace) {
     return A;
 }
 
-template <int PIECES, typename ElemT>
+// Rows that the last-level cache (256 MB) cannot hold until somebody reads them again pass it by.  4,096 x 128,256 bf16: the sums 187 us without, 181 so, the
+// gradient 399 and 352; 2,000 x 128,256 fp32 177 and 162, 394 and 372; but 300 x 32,000 fp32 14.8 and 15.1, 16.5 and 17.4, and rows at odd
+// elements (1,030 x 40,037 bf16) 19.5 and 21.0.
+bool once(const zf_logprobs_args &a) {
+    const int64_t size = a.dtype == 0 ? 4 : 2;
+    return a.rows * a.V * size > (256ll << 20) && (uintptr_t)a.logits % 16 == 0 && a.row_stride_elems * size % 16 == 0;
+}
+template <int PIECES, bool ONCE, typename ElemT>
 void parts(const LogprobsArgs &A, hipStream_t s) {
     const bool entropy = A.a.entropy != nullptr;
-    auto *const part = A.a.top ? (entropy ? logprobs_part_kernel<PIECES, true, true, ElemT> : logprobs_part_kernel<PIECES, false, true, ElemT>)
-                               : (entropy ? logprobs_part_kernel<PIECES, true, false, ElemT> : logprobs_part_kernel<PIECES, false, false, ElemT>);
+    auto *const part = A.a.top ? (entropy ? logprobs_part_kernel<PIECES, ONCE, true, true, ElemT> : logprobs_part_kernel<PIECES, ONCE, false, true, ElemT>)
+                               : (entropy ? logprobs_part_kernel<PIECES, ONCE, true, false, ElemT> : logprobs_part_kernel<PIECES, ONCE, false, false, ElemT>);
     hipLaunchKernelGGL(part, dim3((uint32_t)(A.a.rows * A.n_seg)), dim3(THREADS), 0, s, A);
 }
 template <typename ElemT>
 void forward(const LogprobsArgs &A, hipStream_t s) {
-    if (pieces(A.a) == 1) parts<1, ElemT>(A, s);
-    else parts<PIECES, ElemT>(A, s);
+    if (pieces(A.a) == 1) parts<1, false, ElemT>(A, s);
+    else if (once(A.a)) parts<PIECES, true, ElemT>(A, s);
+    else parts<PIECES, false, ElemT>(A, s);
     hipLaunchKernelGGL((logprobs_join_kernel<ElemT>), dim3((uint32_t)((A.a.rows + ROWS_JOINED - 1) / ROWS_JOINED)), dim3(ROWS_JOINED * 64),
                        A.a.top ? ROWS_JOINED * A.n_seg : 0, s, A);
 }
@@ -530,8 +555,10 @@ hipError_t launch_logprobs(const zf_logprobs_args &a, void *workspace, hipStream
 
 hipError_t launch_logprobs_backward(const zf_logprobs_args &a, const LogprobsGrad &g, hipStream_t s) {
     const GradArgs A{with_plan(a, nullptr), g};
-    auto *const kernel = pieces(a) == 1 ? (a.dtype == 0 ? logprobs_grad_kernel<1, uint32_t> : logprobs_grad_kernel<1, uint16_t>)
-                                        : (a.dtype == 0 ? logprobs_grad_kernel<PIECES, uint32_t> : logprobs_grad_kernel<PIECES, uint16_t>);
+    const bool pass = once(a) && (uintptr_t)g.grad % 16 == 0 && g.stride * (a.dtype == 0 ? 4 : 2) % 16 == 0;
+    auto *const kernel = pieces(a) == 1 ? (a.dtype == 0 ? logprobs_grad_kernel<1, false, uint32_t> : logprobs_grad_kernel<1, false, uint16_t>)
+                         : pass         ? (a.dtype == 0 ? logprobs_grad_kernel<PIECES, true, uint32_t> : logprobs_grad_kernel<PIECES, true, uint16_t>)
+                                        : (a.dtype == 0 ? logprobs_grad_kernel<PIECES, false, uint32_t> : logprobs_grad_kernel<PIECES, false, uint16_t>);
     hipLaunchKernelGGL(kernel, dim3((uint32_t)(a.rows * A.l.n_seg)), dim3(THREADS), 0, s, A);
     return hipGetLastError();
 }
