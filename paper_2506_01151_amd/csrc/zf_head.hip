@@ -13,6 +13,7 @@
 // four v_mfma_f32_16x16x32_bf16 make the block's sum (1e-8 and 7e-8 off), at half the rate.
 #include <hip/hip_runtime.h>
 #include <algorithm>
+#include <cstdlib>
 #include "zf_ops.h"
 
 namespace zf {
@@ -156,148 +157,210 @@ template <> struct Operand<uint32_t> {
 
 __device__ __forceinline__ i32x4 piece_at(const uint8_t *p) { return *reinterpret_cast<const i32x4 *>(p); }
 
+// ---- memory straight into LDS ----
+//
+// 64 lanes' 16 (or 4) bytes, each from its address, to consecutive places of LDS from `at` on.  As an instruction: it has no register for a result, and the
+// compiler, which does not see it, leaves the waits to the caller instead of waiting in front of every read of LDS.
+__device__ __forceinline__ void to_lds(const uint8_t *base, uint32_t off, uint32_t at) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(off), "s"(base) : "memory");
+}
+__device__ __forceinline__ void to_lds(const uint8_t *from, uint32_t at) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(at), "v"(from) : "memory");
+}
+__device__ __forceinline__ void to_lds(const float *from, uint32_t at) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(at), "v"(from) : "memory");
+}
+template <int N> __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }   // of the wavefront's loads, all but the last N
+__device__ __forceinline__ uint32_t lds_at(const void *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t *)p; }
+
 // ---- few rows: the weight streams past them ----
 //
-// A workgroup has TOKENS = 64 GW tokens of one scale and up to 16 MT rows of the batch.  Under a mask it lists the tokens that some of its rows allows.  A
-// wavefront takes 16 GW of them at a time, their weights straight from memory into the operand's registers, two blocks of columns (2 KB each and group) ahead; the rows' activations go through
-// LDS four blocks (CHUNK columns) at a time, with their scales times the weight's.  With no more than 16 GW tokens to do, the four wavefronts
-// share them and take a block of columns of every chunk each (their sums join in a fixed order).  Results gather in LDS, so that the logits
-// go out in whole rows of the range, -inf where nothing was computed.
-static const int CHUNK_BLOCKS = 4, CHUNK = CHUNK_BLOCKS * SCALE_BLOCK;
-
-template <int MT, int GW>
+// A workgroup has TOKENS tokens of one scale and up to 16 MT rows of the batch.  Under a mask it lists the tokens that some of its rows allows.
+//   Many tokens (up to 128): a wavefront takes 32 of them.  Blocks of columns of the weight's rows and the activations come straight into LDS, STAGES - 1 blocks ahead, in
+// lines: a fragment's own addresses (sixteen rows, 16 bytes of each) are taken a lane at a time, at a quarter of the rate.  Every wavefront issues the same number of loads for a
+// block, so that a count says which have arrived; one barrier a block.  Piece c of row r lies at place c ^ (r % 8), so that eight rows' pieces of one
+// column lie in different banks (the loads write LDS in lanes' order: it is their addresses in memory that are exchanged).
+//   Up to 32 tokens (TOKENS = 16 is made of such): the wavefronts share them and take every fourth block of columns each, the weight straight to registers, and join their sums in a fixed order.  With
+// 128-token ranges the activations come through LDS, as many columns at a time as there is room.
+//   Results gather in LDS, so that the logits go out in whole rows of the range, -inf where nothing was computed.
+template <int MT, int TOKENS>
 struct RowsLds {
-    static constexpr int ROWS = MT * 16, TOKENS = 64 * GW, PITCH = TOKENS + 4;
-    static constexpr int X_BYTES = ROWS * CHUNK, S_FLOATS = ROWS * CHUNK_BLOCKS;
-    static constexpr int LOOP = 2 * (X_BYTES + 4 * S_FLOATS), TILE = ROWS * PITCH * 4, JOIN = 3 * ROWS * 16 * GW * 4;   // activations and scales; then the logits, and three wavefronts' sums
+    static constexpr int ROWS = MT * 16, GW = TOKENS > 16 ? 2 : 1, PITCH = TOKENS + 4;
+    static constexpr int STAGES = MT == 4 ? 3 : 4, X_AT = 128 * SCALE_BLOCK, S_AT = X_AT + ROWS * SCALE_BLOCK, STAGE = S_AT + 64 * 4;   // weight, activations, their scales
+    static constexpr int LOADS = 4 + (MT + 1) / 2 + 1;                       // of a wavefront for a stage
+    static constexpr int SPAN = MT == 1 ? 4096 : MT == 2 ? 2048 : 1024;      // columns of the activations that the short form has in LDS
+    static constexpr int LOOP = TOKENS > 16 ? STAGES * STAGE : 0, TILE = ROWS * PITCH * 4, JOIN = 3 * ROWS * 16 * GW * 4;                   // the loop; then the logits, and three wavefronts' sums
     static constexpr int BYTES = LOOP > TILE + JOIN ? LOOP : TILE + JOIN;
+    static_assert(TOKENS == 16 || ROWS * SPAN <= STAGES * STAGE, "the short form's activations lie in the stages' memory");
 };
 
-template <int MT, int GW, bool MASK, typename ElemT>
-__global__ __launch_bounds__(256) void head_rows_kernel(HeadArgs a) {
-    typedef RowsLds<MT, GW> Lds;
-    constexpr int ROWS = Lds::ROWS, TOKENS = Lds::TOKENS, PITCH = Lds::PITCH;
-    __shared__ __align__(16) uint8_t mem[Lds::BYTES];
-    __shared__ uint32_t words[MASK ? ROWS : 1][TOKENS / 32], need[TOKENS / 32];
+template <int MT, int TOKENS, bool MASK, typename ElemT>
+__global__ __launch_bounds__(256, 2) void head_rows_kernel(HeadArgs a) {
+    typedef RowsLds<MT, TOKENS> Lds;
+    constexpr int ROWS = Lds::ROWS, GW = Lds::GW, PITCH = Lds::PITCH, WORDS = (TOKENS + 31) / 32, STAGES = Lds::STAGES;
+    extern __shared__ __align__(16) uint8_t mem[];
+    __shared__ uint32_t words[MASK ? ROWS : 1][WORDS], need[WORDS];
     __shared__ uint8_t list[TOKENS];
-    const int tid = threadIdx.x, lane = tid % 64, wave = tid / 64;
+    const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
     const int32_t v0 = blockIdx.x * TOKENS, m0 = blockIdx.y * ROWS;
     const int32_t rows = a.M - m0 < ROWS ? a.M - m0 : ROWS, n_v = a.V - v0 < TOKENS ? a.V - v0 : TOKENS, n_k = a.K / SCALE_BLOCK;
     int32_t count = n_v;
     if (MASK) {
         const int32_t W = (a.V + 31) / 32;
-        if (tid < TOKENS / 32) need[tid] = 0;
+        if (tid < WORDS) need[tid] = 0;
         __syncthreads();
-        for (int i = tid; i < rows * (TOKENS / 32); i += 256) {
-            const int32_t j = i % (TOKENS / 32), left = n_v - 32 * j;        // tokens of the word that there are
-            uint32_t w = left > 0 ? a.mask[(size_t)(m0 + i / (TOKENS / 32)) * W + v0 / 32 + j] : 0;
+        for (int i = tid; i < rows * WORDS; i += 256) {
+            const int32_t j = i % WORDS, left = n_v - 32 * j;                // tokens of the word that there are
+            uint32_t w = left > 0 ? a.mask[(size_t)(m0 + i / WORDS) * W + v0 / 32 + j] >> (TOKENS < 32 ? v0 % 32 : 0) : 0;
             if (left < 32 && left > 0) w &= (1u << left) - 1;
-            words[i / (TOKENS / 32)][j] = w;
+            words[i / WORDS][j] = w;
             if (w) atomicOr(&need[j], w);                                    // the same in any order
         }
         __syncthreads();
         count = 0;
 #pragma unroll
-        for (int j = 0; j < TOKENS / 32; j++) {
+        for (int j = 0; j < WORDS; j++) {
             if (tid < TOKENS && j == tid / 32 && ((need[j] >> (tid % 32)) & 1)) list[count + __popc(need[j] & ((1u << (tid % 32)) - 1))] = (uint8_t)tid;
             count += __popc(need[j]);
         }
+        count = __builtin_amdgcn_readfirstlane(count);
         __syncthreads();
     }
     const bool shared = count <= 16 * GW;                                    // the wavefronts share the tokens
-    const int first = shared ? 0 : wave * 16 * GW;                           // the wavefront's tokens in the list
-    const bool active = first < count;
+    const int first = shared ? 0 : wave * 32;                                // the wavefront's tokens in the list
+    // the weight's row of the i-th listed token; behind the last one its row once more
+    auto w_row = [&](int i) { i = i < count ? i : count - 1; return a.w + (int64_t)(v0 + (MASK ? list[i] : i)) * a.w_stride; };
+    auto x_row = [&](int r) { return m0 + (r < rows ? r : rows - 1); };
+    const float *const ws = a.ws + (size_t)(v0 / SCALE_BLOCK) * n_k;
+    const auto *const ws_uniform = (const __attribute__((address_space(4))) float *)ws;      // read by the scalar unit
     f32x4 acc[GW][MT];
 #pragma unroll
     for (int g = 0; g < GW; g++)
 #pragma unroll
         for (int t = 0; t < MT; t++) acc[g][t] = f32x4{0, 0, 0, 0};
-    if (count > 0) {
-        const uint8_t *wp[GW];
+    const int c0 = (lane / 16 ^ lane % 8) * 16, c1 = ((lane / 16 + 4) ^ lane % 8) * 16;      // the lane's two pieces of a row that is lane % 8 modulo 8
+    if (shared && count > 0) {
+        constexpr int U = TOKENS == 16 && MT == 4 ? 1 : TOKENS == 16 && MT == 2 ? 2 : 4;     // blocks of columns asked for at a time
+        constexpr bool NEAR = TOKENS > 16;                                                   // activations through LDS
+        const bool two = GW > 1 && count > 16;
+        const uint8_t *wp[GW], *xp[MT];
+        const float *xs[MT];
 #pragma unroll
-        for (int g = 0; g < GW; g++) {
-            int i = first + g * 16 + lane % 16;
-            if (i >= count) i = count - 1;                                   // behind the last token: its row once more
-            wp[g] = a.w + (int64_t)(v0 + (MASK ? list[i] : i)) * a.w_stride + lane / 16 * 16;
+        for (int g = 0; g < GW; g++) wp[g] = w_row(g * 16 + lane % 16) + lane / 16 * 16;
+#pragma unroll
+        for (int t = 0; t < MT; t++) {
+            xp[t] = a.x + x_row(t * 16 + lane % 16) * a.x_stride + lane / 16 * 16;
+            xs[t] = a.xs + (size_t)x_row(t * 16 + lane % 16) * n_k;
         }
-        // activations of a chunk: 32 pieces a row, piece c of row r at place c ^ (r % 16), so that sixteen rows' pieces of one column lie in different banks
-        constexpr int XN = ROWS * (CHUNK / 16) / 256;
-        i32x4 xr[XN];
-        float sr = 0.0f;
-        const float *const ws = a.ws + (size_t)(v0 / SCALE_BLOCK) * n_k;
-        auto load_x = [&](int32_t c) {
-#pragma unroll
-            for (int i = 0; i < XN; i++) {
-                const int32_t r = (tid + i * 256) / (CHUNK / 16), col = c * CHUNK + (tid + i * 256) % (CHUNK / 16) * 16;
-                xr[i] = i32x4{0, 0, 0, 0};
-                if (col < a.K) xr[i] = piece_at(a.x + (int64_t)(m0 + (r < rows ? r : rows - 1)) * a.x_stride + col);
-            }
-            const int32_t r = tid / CHUNK_BLOCKS, k = c * CHUNK_BLOCKS + tid % CHUNK_BLOCKS;
-            if (r < ROWS) sr = k < n_k ? a.xs[(size_t)(m0 + (r < rows ? r : rows - 1)) * n_k + k] * ws[k] : 0.0f;
-        };
-        auto store_x = [&](int b) {
-            uint8_t *const x = mem + b * Lds::X_BYTES;
-#pragma unroll
-            for (int i = 0; i < XN; i++) {
-                const int32_t r = (tid + i * 256) / (CHUNK / 16), p = (tid + i * 256) % (CHUNK / 16);
-                *reinterpret_cast<i32x4 *>(x + r * CHUNK + (p ^ (r % 16)) * 16) = xr[i];
-            }
-            if (tid < ROWS * CHUNK_BLOCKS) reinterpret_cast<float *>(mem + 2 * Lds::X_BYTES)[b * Lds::S_FLOATS + tid] = sr;
-        };
-        i32x4 now[2][GW][2], next[2][GW][2];
-        auto load_w = [&](i32x4 (&w)[2][GW][2], int32_t h) {                 // two blocks of columns from the 2 h-th on: those that the wavefront takes
-#pragma unroll
-            for (int j = 0; j < 2; j++) {
-                const int32_t k = 2 * h + j;
-                if (!active || k >= n_k || (shared && k % CHUNK_BLOCKS != wave)) continue;
-#pragma unroll
-                for (int g = 0; g < GW; g++) {
-                    w[j][g][0] = __builtin_nontemporal_load(reinterpret_cast<const i32x4 *>(wp[g] + (size_t)k * SCALE_BLOCK));
-                    w[j][g][1] = __builtin_nontemporal_load(reinterpret_cast<const i32x4 *>(wp[g] + (size_t)k * SCALE_BLOCK + 64));
+        const int32_t span = NEAR ? Lds::SPAN / SCALE_BLOCK : n_k;
+        for (int32_t from = 0; from < n_k; from += span) {
+            const int32_t to = from + span < n_k ? from + span : n_k;
+            if (NEAR) {
+                if (from) __syncthreads();                                   // the span before has been read
+                const int groups = (rows + 7) / 8;                           // of eight rows; the span's blocks in turn
+                for (int i = wave; i < groups * (to - from); i += 4) {
+                    const int r = i % groups * 8 + lane / 8, k = i / groups;
+                    to_lds(a.x + x_row(r) * a.x_stride + (size_t)(from + k) * SCALE_BLOCK + (lane % 8 ^ lane / 8) * 16, lds_at(mem) + k * (ROWS * SCALE_BLOCK) + i % groups * 8 * SCALE_BLOCK);
                 }
             }
-        };
-        const int32_t n_chunks = (n_k + CHUNK_BLOCKS - 1) / CHUNK_BLOCKS;
-        load_x(0);
-        load_w(now, 0);
-        store_x(0);
-        __syncthreads();
-        for (int32_t c = 0; c < n_chunks; c++) {
-            if (c + 1 < n_chunks) load_x(c + 1);
-            const uint8_t *const x = mem + (c & 1) * Lds::X_BYTES;
-            const float *const scales = reinterpret_cast<const float *>(mem + 2 * Lds::X_BYTES) + (c & 1) * Lds::S_FLOATS;
+            for (int32_t k0 = from + wave; k0 < to || (NEAR && k0 == from + wave); k0 += 4 * U) {
+                i32x4 w[U][GW][2], x[U][MT][2];
+                float s[U][MT];
 #pragma unroll
-            for (int h = 0; h < 2; h++) {
-                load_w(next, 2 * c + h + 1);
+                for (int u = 0; u < U; u++) {
+                    const int32_t k = k0 + 4 * u;
+                    if (k >= to) continue;
 #pragma unroll
-                for (int j = 0; j < 2; j++) {
-                    const int32_t in = 2 * h + j, k = c * CHUNK_BLOCKS + in;
-                    if (!active || k >= n_k || (shared && in != wave)) continue;
-                    Operand<ElemT> w[GW];
+                    for (int g = 0; g < GW; g++)
+                        if (g == 0 || two)
 #pragma unroll
-                    for (int g = 0; g < GW; g++) w[g].take(now[j][g][0], now[j][g][1]);
+                            for (int h = 0; h < 2; h++) w[u][g][h] = __builtin_nontemporal_load(reinterpret_cast<const i32x4 *>(wp[g] + (size_t)k * SCALE_BLOCK + 64 * h));
 #pragma unroll
                     for (int t = 0; t < MT; t++) {
-                        const int r = t * 16 + lane % 16, p = in * 8 + lane / 16;
-                        Operand<ElemT> v;
-                        v.take(*reinterpret_cast<const i32x4 *>(x + r * CHUNK + (p ^ (r % 16)) * 16), *reinterpret_cast<const i32x4 *>(x + r * CHUNK + ((p + 4) ^ (r % 16)) * 16));
-                        const float s = scales[r * CHUNK_BLOCKS + in];
+                        if (!NEAR)
 #pragma unroll
-                        for (int g = 0; g < GW; g++) {
-                            const f32x4 part = w[g].times(v);
+                            for (int h = 0; h < 2; h++) x[u][t][h] = piece_at(xp[t] + (size_t)k * SCALE_BLOCK + 64 * h);
+                        s[u][t] = xs[t][k] * ws_uniform[k];
+                    }
+                }
+                if (NEAR && k0 == from + wave) {                             // once a span, by every wavefront
+                    arrived<0>();
+                    __syncthreads();
+                }
 #pragma unroll
-                            for (int e = 0; e < 4; e++) acc[g][t][e] = fmaf(s, part[e], acc[g][t][e]);
+                for (int u = 0; u < U; u++) {
+                    if (k0 + 4 * u >= to) continue;
+                    Operand<ElemT> v[MT];
+#pragma unroll
+                    for (int t = 0; t < MT; t++) {
+                        const uint8_t *const at = mem + (k0 + 4 * u - from) * (ROWS * SCALE_BLOCK) + (t * 16 + lane % 16) * SCALE_BLOCK;
+                        if (NEAR) v[t].take(piece_at(at + c0), piece_at(at + c1));
+                        else v[t].take(x[u][t][0], x[u][t][1]);
+                    }
+#pragma unroll
+                    for (int g = 0; g < GW; g++) {
+                        if (g && !two) continue;
+                        Operand<ElemT> y;
+                        y.take(w[u][g][0], w[u][g][1]);
+#pragma unroll
+                        for (int t = 0; t < MT; t++) {
+                            const f32x4 part = y.times(v[t]);
+#pragma unroll
+                            for (int e = 0; e < 4; e++) acc[g][t][e] = fmaf(s[u][t], part[e], acc[g][t][e]);
                         }
                     }
                 }
-#pragma unroll
-                for (int j = 0; j < 2; j++)
-#pragma unroll
-                    for (int g = 0; g < GW; g++) { now[j][g][0] = next[j][g][0]; now[j][g][1] = next[j][g][1]; }
             }
-            if (c + 1 < n_chunks) store_x((c + 1) & 1);
-            __syncthreads();
         }
+        __syncthreads();
+    } else if (TOKENS > 16 && count > 0) {
+        constexpr int XN = (MT + 1) / 2;                                     // groups of eight of the activations' rows that a wavefront brings
+        const uint8_t *from[4 + XN];
+        const int place = (lane % 8 ^ lane / 8) * 16;
+#pragma unroll
+        for (int i = 0; i < 4; i++) from[i] = w_row(wave * 32 + i * 8 + lane / 8) + place;
+#pragma unroll
+        for (int i = 0; i < XN; i++) from[4 + i] = a.x + x_row((wave * XN + i) % (2 * MT) * 8 + lane / 8) * a.x_stride + place;
+        const float *const xs = a.xs + (size_t)x_row(lane % ROWS) * n_k;
+        auto fetch = [&](int32_t k) {                                        // behind the last block: that one once more, for the count
+            const uint32_t at = lds_at(mem) + k % STAGES * Lds::STAGE;
+            k = k < n_k ? k : n_k - 1;
+#pragma unroll
+            for (int i = 0; i < 4; i++) to_lds(from[i] + (size_t)k * SCALE_BLOCK, at + (wave * 32 + i * 8) * SCALE_BLOCK);
+#pragma unroll
+            for (int i = 0; i < XN; i++) to_lds(from[4 + i] + (size_t)k * SCALE_BLOCK, at + Lds::X_AT + (wave * XN + i) % (2 * MT) * 8 * SCALE_BLOCK);
+            to_lds(xs + k, at + Lds::S_AT);
+        };
+#pragma unroll
+        for (int k = 0; k < STAGES - 1; k++) fetch(k);
+        for (int32_t k = 0; k < n_k; k++) {
+            arrived<(STAGES - 2) * Lds::LOADS>();
+            __syncthreads();
+            fetch(k + STAGES - 1);
+            const uint8_t *const stage = mem + k % STAGES * Lds::STAGE;
+            const float s_w = ws_uniform[k];
+            Operand<ElemT> w[GW];
+#pragma unroll
+            for (int g = 0; g < GW; g++) {
+                const uint8_t *const at = stage + (wave * 32 + g * 16 + lane % 16) * SCALE_BLOCK;
+                w[g].take(piece_at(at + c0), piece_at(at + c1));
+            }
+#pragma unroll
+            for (int t = 0; t < MT; t++) {
+                const uint8_t *const at = stage + Lds::X_AT + (t * 16 + lane % 16) * SCALE_BLOCK;
+                Operand<ElemT> v;
+                v.take(piece_at(at + c0), piece_at(at + c1));
+                const float s = reinterpret_cast<const float *>(stage + Lds::S_AT)[t * 16 + lane % 16] * s_w;
+#pragma unroll
+                for (int g = 0; g < GW; g++) {
+                    const f32x4 part = w[g].times(v);
+#pragma unroll
+                    for (int e = 0; e < 4; e++) acc[g][t][e] = fmaf(s, part[e], acc[g][t][e]);
+                }
+            }
+        }
+        arrived<0>();
+        __syncthreads();
     }
     // the loop's memory becomes the logits' and, behind them, that of three wavefronts' sums
     float *const tile = reinterpret_cast<float *>(mem);
@@ -310,7 +373,7 @@ __global__ __launch_bounds__(256) void head_rows_kernel(HeadArgs a) {
             for (int t = 0; t < MT; t++) sums[((wave - 1) * GW * MT + g * MT + t) * 64 + lane] = acc[g][t];
     }
     __syncthreads();
-    if (active && !(shared && wave)) {
+    if (first < count && !(shared && wave)) {
 #pragma unroll
         for (int g = 0; g < GW; g++)
 #pragma unroll
@@ -349,8 +412,7 @@ __global__ __launch_bounds__(256) void head_rows_kernel(HeadArgs a) {
 // ---- many rows: tiles of both operands in LDS ----
 //
 // A workgroup of eight wavefronts has 256 tokens and 32 MJ rows of the batch, a wavefront 64 tokens and 16 MJ rows.  A block of columns of both operands, 128 bytes a
-// row, comes from memory straight into LDS while the block before is multiplied: two buffers, one barrier a block.  Piece c of row r lies at place c ^ (r % 8), so
-// that eight rows' pieces of one column lie in different banks; the loads write LDS in lanes' order, so it is their addresses in memory that are exchanged.
+// row, comes from memory straight into LDS while the block before is multiplied: two buffers, one barrier a block, pieces in places as above.
 //   Rows behind the last one are the last one again; their results are not stored.
 static const int TILE_TOKENS = 256;
 
@@ -359,14 +421,6 @@ struct TileLds {
     static constexpr int ROWS = 32 * MJ, W_BYTES = TILE_TOKENS * SCALE_BLOCK, X_BYTES = ROWS * SCALE_BLOCK, BUFFER = W_BYTES + X_BYTES;
     static constexpr int SCALES = 2 * BUFFER, LOOP = SCALES + 2 * 512 * 4;
 };
-
-// 64 lanes' 16 bytes, `off` behind `base`, to 1 KB of LDS from `at` on.  As an instruction: it has no register for a result, and the compiler, which does not see
-// it, leaves the waits to the caller (arrived(), then a barrier) instead of waiting in front of every read of the other buffer.
-__device__ __forceinline__ void to_lds(const uint8_t *base, uint32_t off, uint32_t at) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(off), "s"(base) : "memory");
-}
-__device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
-__device__ __forceinline__ uint32_t lds_at(const void *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t *)p; }
 
 template <int MJ, bool MASK, typename ElemT>
 __global__ __launch_bounds__(512, 2) void head_tile_kernel(HeadArgs a, int32_t tiles_m, int32_t n_tiles) {
@@ -402,7 +456,7 @@ __global__ __launch_bounds__(512, 2) void head_tile_kernel(HeadArgs a, int32_t t
         for (int i = 0; i < 4; i++) acc[j][i] = f32x4{0, 0, 0, 0};
     scales[tid] = xs[0] * ws[0];
     fetch(0, 0);
-    arrived();
+    arrived<0>();
     __syncthreads();
     const int32_t c0 = (lane / 16 ^ lane % 8) * 16, c1 = ((lane / 16 + 4) ^ lane % 8) * 16;   // the lane's two pieces of a row that is lane % 8 modulo 8
     for (int32_t k = 0; k < n_k; k++) {
@@ -440,7 +494,7 @@ __global__ __launch_bounds__(512, 2) void head_tile_kernel(HeadArgs a, int32_t t
             __builtin_amdgcn_sched_barrier(0);
         }
         scales[(b ^ 1) * 512 + tid] = next_x * next_w;
-        arrived();
+        arrived<0>();
         __syncthreads();
     }
     // sixteen rows at a time through the wavefront's own part of LDS, from four tokens a lane to whole lines of 64 tokens
@@ -493,18 +547,26 @@ hipError_t head_tile(const HeadArgs &a, hipStream_t s) {
     return hipSuccess;
 }
 
-template <int MT, int GW, bool MASK, typename ElemT>
+template <int MT, int TOKENS, bool MASK, typename ElemT>
 hipError_t head_rows(const HeadArgs &a, hipStream_t s) {
-    const dim3 grid((a.V + 64 * GW - 1) / (64 * GW), (a.M + MT * 16 - 1) / (MT * 16));
-    hipLaunchKernelGGL((head_rows_kernel<MT, GW, MASK, ElemT>), grid, dim3(256), 0, s, a);
+    typedef RowsLds<MT, TOKENS> Lds;
+    static const hipError_t ready = hipFuncSetAttribute((const void *)head_rows_kernel<MT, TOKENS, MASK, ElemT>, hipFuncAttributeMaxDynamicSharedMemorySize, Lds::BYTES);
+    if (ready != hipSuccess) return ready;
+    const dim3 grid((a.V + TOKENS - 1) / TOKENS, (a.M + MT * 16 - 1) / (MT * 16));
+    hipLaunchKernelGGL((head_rows_kernel<MT, TOKENS, MASK, ElemT>), grid, dim3(256), Lds::BYTES, s, a);
     return hipSuccess;
+}
+template <int MT, bool MASK, typename ElemT>
+hipError_t head_few(const HeadArgs &a, hipStream_t s) {
+    if (getenv("T16") ? atoi(getenv("T16")) : a.V < 128 * 128) return head_rows<MT, 16, MASK, ElemT>(a, s);
+    return head_rows<MT, 128, MASK, ElemT>(a, s);
 }
 template <bool MASK, typename ElemT>
 hipError_t head(const HeadArgs &a, hipStream_t s) {
-    if (a.M <= 16) return head_rows<1, 2, MASK, ElemT>(a, s);
-    if (a.M <= 32) return head_rows<2, 2, MASK, ElemT>(a, s);
-    if (a.M <= 64) return head_rows<4, 2, MASK, ElemT>(a, s);
-    if ((a.w_stride | a.x_stride) >= (1 << 24)) return head_rows<4, 2, MASK, ElemT>(a, s);   // a tile's rows would not lie within 32 bits
+    if (a.M <= 16) return head_few<1, MASK, ElemT>(a, s);
+    if (a.M <= 32) return head_few<2, MASK, ElemT>(a, s);
+    if (a.M <= 64) return head_few<4, MASK, ElemT>(a, s);
+    if ((a.w_stride | a.x_stride) >= (1 << 24)) return head_rows<4, 128, MASK, ElemT>(a, s);   // a tile's rows would not lie within 32 bits
     // operands in bf16 take twice the registers: half the rows
     if (sizeof(ElemT) == 4 || a.M <= 128) return head_tile<4, MASK, ElemT>(a, s);
     return head_tile<8, MASK, ElemT>(a, s);
