@@ -137,7 +137,8 @@ template <typename ElemT> struct Operand;
 template <> struct Operand<uint16_t> {
     i32x8 v;
     __device__ __forceinline__ void take(i32x4 a, i32x4 b) { v = i32x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]}; }
-    __device__ __forceinline__ f32x4 times(const Operand &o) const { return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(v, o.v, f32x4{0, 0, 0, 0}, 0, 0, 0, 0, 0, 0); }
+    static constexpr int STEPS = 1;
+    template <int H> __device__ __forceinline__ f32x4 times(const Operand &o, f32x4 d) const { return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(v, o.v, d, 0, 0, 0, 0, 0, 0); }
 };
 template <> struct Operand<uint32_t> {
     bf16x8 v[4];
@@ -147,13 +148,18 @@ template <> struct Operand<uint32_t> {
         return bf16x8{p[0], p[1], q[0], q[1], r[0], r[1], t[0], t[1]};
     }
     __device__ __forceinline__ void take(i32x4 a, i32x4 b) { v[0] = wide(a[0], a[1]); v[1] = wide(a[2], a[3]); v[2] = wide(b[0], b[1]); v[3] = wide(b[2], b[3]); }
-    __device__ __forceinline__ f32x4 times(const Operand &o) const {
-        f32x4 d{0, 0, 0, 0};
-#pragma unroll
-        for (int h = 0; h < 4; h++) d = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[h], o.v[h], d, 0, 0, 0);
-        return d;
-    }
+    static constexpr int STEPS = 4;
+    template <int H> __device__ __forceinline__ f32x4 times(const Operand &o, f32x4 d) const { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(v[H], o.v[H], d, 0, 0, 0); }
 };
+// The sums of a block of A's tokens against B's rows: all products of a step before those of the next, which add to them.
+template <int A, int B, typename ElemT, int H = 0>
+__device__ __forceinline__ void multiply(const Operand<ElemT> (&a)[A], const Operand<ElemT> (&b)[B], f32x4 (&d)[A][B]) {
+#pragma unroll
+    for (int i = 0; i < A; i++)
+#pragma unroll
+        for (int j = 0; j < B; j++) d[i][j] = a[i].template times<H>(b[j], H ? d[i][j] : f32x4{0, 0, 0, 0});
+    if constexpr (H + 1 < Operand<ElemT>::STEPS) multiply<A, B, ElemT, H + 1>(a, b, d);
+}
 
 __device__ __forceinline__ i32x4 piece_at(const uint8_t *p) { return *reinterpret_cast<const i32x4 *>(p); }
 
@@ -240,8 +246,8 @@ __global__ __launch_bounds__(256, 2) void head_rows_kernel(HeadArgs a) {
         for (int t = 0; t < MT; t++) acc[g][t] = f32x4{0, 0, 0, 0};
     const int c0 = (lane / 16 ^ lane % 8) * 16, c1 = ((lane / 16 + 4) ^ lane % 8) * 16;      // the lane's two pieces of a row that is lane % 8 modulo 8
     if (shared && count > 0) {
-        constexpr int U = TOKENS == 16 && MT == 4 ? 1 : TOKENS == 16 && MT == 2 ? 2 : 4;     // blocks of columns asked for at a time
         constexpr bool NEAR = TOKENS > 16;                                                   // activations through LDS
+        constexpr int U = NEAR ? Lds::SPAN / SCALE_BLOCK / 4 : MT == 4 ? 1 : MT == 2 ? 2 : 4;   // blocks of columns a wavefront asks for at a time
         const bool two = GW > 1 && count > 16;
         const uint8_t *wp[GW], *xp[MT];
         const float *xs[MT];
@@ -252,63 +258,59 @@ __global__ __launch_bounds__(256, 2) void head_rows_kernel(HeadArgs a) {
             xp[t] = a.x + x_row(t * 16 + lane % 16) * a.x_stride + lane / 16 * 16;
             xs[t] = a.xs + (size_t)x_row(t * 16 + lane % 16) * n_k;
         }
-        const int32_t span = NEAR ? Lds::SPAN / SCALE_BLOCK : n_k;
-        for (int32_t from = 0; from < n_k; from += span) {
-            const int32_t to = from + span < n_k ? from + span : n_k;
+        for (int32_t from = 0; from < n_k; from += 4 * U) {
+            i32x4 w[U][GW][2] = {}, x[U][MT][2];
+            float s[U][MT];
             if (NEAR) {
                 if (from) __syncthreads();                                   // the span before has been read
-                const int groups = (rows + 7) / 8;                           // of eight rows; the span's blocks in turn
-                for (int i = wave; i < groups * (to - from); i += 4) {
+                const int groups = (rows + 7) / 8, n = n_k - from < 4 * U ? n_k - from : 4 * U;   // of eight rows; the span's blocks in turn
+                for (int i = wave; i < groups * n; i += 4) {
                     const int r = i % groups * 8 + lane / 8, k = i / groups;
                     to_lds(a.x + x_row(r) * a.x_stride + (size_t)(from + k) * SCALE_BLOCK + (lane % 8 ^ lane / 8) * 16, lds_at(mem) + k * (ROWS * SCALE_BLOCK) + i % groups * 8 * SCALE_BLOCK);
                 }
             }
-            for (int32_t k0 = from + wave; k0 < to || (NEAR && k0 == from + wave); k0 += 4 * U) {
-                i32x4 w[U][GW][2], x[U][MT][2];
-                float s[U][MT];
 #pragma unroll
-                for (int u = 0; u < U; u++) {
-                    const int32_t k = k0 + 4 * u;
-                    if (k >= to) continue;
+            for (int u = 0; u < U; u++) {
+                const int32_t k = from + wave + 4 * u;
+                if (k >= n_k) continue;
 #pragma unroll
-                    for (int g = 0; g < GW; g++)
-                        if (g == 0 || two)
+                for (int g = 0; g < GW; g++)
+                    if (g * 16 + lane % 16 < count)                          // (a lane with nothing to ask for takes its turn all the same: 16 rows x 200 tokens each, 22 us when all asked)
 #pragma unroll
-                            for (int h = 0; h < 2; h++) w[u][g][h] = __builtin_nontemporal_load(reinterpret_cast<const i32x4 *>(wp[g] + (size_t)k * SCALE_BLOCK + 64 * h));
+                        for (int h = 0; h < 2; h++) w[u][g][h] = __builtin_nontemporal_load(reinterpret_cast<const i32x4 *>(wp[g] + (size_t)k * SCALE_BLOCK + 64 * h));
 #pragma unroll
-                    for (int t = 0; t < MT; t++) {
-                        if (!NEAR)
+                for (int t = 0; t < MT; t++) {
+                    if (!NEAR)
 #pragma unroll
-                            for (int h = 0; h < 2; h++) x[u][t][h] = piece_at(xp[t] + (size_t)k * SCALE_BLOCK + 64 * h);
-                        s[u][t] = xs[t][k] * ws_uniform[k];
-                    }
+                        for (int h = 0; h < 2; h++) x[u][t][h] = piece_at(xp[t] + (size_t)k * SCALE_BLOCK + 64 * h);
+                    s[u][t] = xs[t][k] * ws_uniform[k];
                 }
-                if (NEAR && k0 == from + wave) {                             // once a span, by every wavefront
-                    arrived<0>();
-                    __syncthreads();
+            }
+            if (NEAR) {
+                arrived<0>();
+                __syncthreads();
+            }
+#pragma unroll
+            for (int u = 0; u < U; u++) {
+                if (from + wave + 4 * u >= n_k) continue;
+                Operand<ElemT> v[MT];
+                f32x4 part[1][MT];
+#pragma unroll
+                for (int t = 0; t < MT; t++) {
+                    const uint8_t *const at = mem + (wave + 4 * u) * (ROWS * SCALE_BLOCK) + (t * 16 + lane % 16) * SCALE_BLOCK;
+                    if (NEAR) v[t].take(piece_at(at + c0), piece_at(at + c1));
+                    else v[t].take(x[u][t][0], x[u][t][1]);
                 }
 #pragma unroll
-                for (int u = 0; u < U; u++) {
-                    if (k0 + 4 * u >= to) continue;
-                    Operand<ElemT> v[MT];
+                for (int g = 0; g < GW; g++) {
+                    if (g && !two) continue;
+                    Operand<ElemT> y[1];
+                    y[0].take(w[u][g][0], w[u][g][1]);
+                    multiply(y, v, part);
 #pragma unroll
-                    for (int t = 0; t < MT; t++) {
-                        const uint8_t *const at = mem + (k0 + 4 * u - from) * (ROWS * SCALE_BLOCK) + (t * 16 + lane % 16) * SCALE_BLOCK;
-                        if (NEAR) v[t].take(piece_at(at + c0), piece_at(at + c1));
-                        else v[t].take(x[u][t][0], x[u][t][1]);
-                    }
+                    for (int t = 0; t < MT; t++)
 #pragma unroll
-                    for (int g = 0; g < GW; g++) {
-                        if (g && !two) continue;
-                        Operand<ElemT> y;
-                        y.take(w[u][g][0], w[u][g][1]);
-#pragma unroll
-                        for (int t = 0; t < MT; t++) {
-                            const f32x4 part = y.times(v[t]);
-#pragma unroll
-                            for (int e = 0; e < 4; e++) acc[g][t][e] = fmaf(s[u][t], part[e], acc[g][t][e]);
-                        }
-                    }
+                        for (int e = 0; e < 4; e++) acc[g][t][e] = fmaf(s[u][t], part[0][t][e], acc[g][t][e]);
                 }
             }
         }
@@ -322,9 +324,13 @@ __global__ __launch_bounds__(256, 2) void head_rows_kernel(HeadArgs a) {
 #pragma unroll
         for (int i = 0; i < XN; i++) from[4 + i] = a.x + x_row((wave * XN + i) % (2 * MT) * 8 + lane / 8) * a.x_stride + place;
         const float *const xs = a.xs + (size_t)x_row(lane % ROWS) * n_k;
+        // Workgroups begin at blocks of columns of their own: rows lie at multiples of a power of two, and who reads the same columns of many rows asks
+        // few of the memory's channels (16 x 128,256 x 4,096: 113 us when all begin at the first, 103 so).
+        const int32_t turn = (int32_t)(blockIdx.x * 5u % (uint32_t)n_k);
+        auto turned = [&](int32_t k) { return k + turn < n_k ? k + turn : k + turn - n_k; };
         auto fetch = [&](int32_t k) {                                        // behind the last block: that one once more, for the count
             const uint32_t at = lds_at(mem) + k % STAGES * Lds::STAGE;
-            k = k < n_k ? k : n_k - 1;
+            k = turned(k < n_k ? k : n_k - 1);
 #pragma unroll
             for (int i = 0; i < 4; i++) to_lds(from[i] + (size_t)k * SCALE_BLOCK, at + (wave * 32 + i * 8) * SCALE_BLOCK);
 #pragma unroll
@@ -338,25 +344,32 @@ __global__ __launch_bounds__(256, 2) void head_rows_kernel(HeadArgs a) {
             __syncthreads();
             fetch(k + STAGES - 1);
             const uint8_t *const stage = mem + k % STAGES * Lds::STAGE;
-            const float s_w = ws_uniform[k];
+            const float s_w = ws_uniform[turned(k)];
             Operand<ElemT> w[GW];
 #pragma unroll
             for (int g = 0; g < GW; g++) {
                 const uint8_t *const at = stage + (wave * 32 + g * 16 + lane % 16) * SCALE_BLOCK;
                 w[g].take(piece_at(at + c0), piece_at(at + c1));
             }
+            constexpr int PAIR = MT > 1 ? 2 : 1;                             // sixteens of rows at a time
 #pragma unroll
-            for (int t = 0; t < MT; t++) {
-                const uint8_t *const at = stage + Lds::X_AT + (t * 16 + lane % 16) * SCALE_BLOCK;
-                Operand<ElemT> v;
-                v.take(piece_at(at + c0), piece_at(at + c1));
-                const float s = reinterpret_cast<const float *>(stage + Lds::S_AT)[t * 16 + lane % 16] * s_w;
+            for (int t0 = 0; t0 < MT; t0 += PAIR) {
+                Operand<ElemT> v[PAIR];
+                float s[PAIR];
+                f32x4 part[GW][PAIR];
 #pragma unroll
-                for (int g = 0; g < GW; g++) {
-                    const f32x4 part = w[g].times(v);
-#pragma unroll
-                    for (int e = 0; e < 4; e++) acc[g][t][e] = fmaf(s, part[e], acc[g][t][e]);
+                for (int t = 0; t < PAIR; t++) {
+                    const int r = (t0 + t) * 16 + lane % 16;
+                    v[t].take(piece_at(stage + Lds::X_AT + r * SCALE_BLOCK + c0), piece_at(stage + Lds::X_AT + r * SCALE_BLOCK + c1));
+                    s[t] = reinterpret_cast<const float *>(stage + Lds::S_AT)[r] * s_w;
                 }
+                multiply(w, v, part);
+#pragma unroll
+                for (int t = 0; t < PAIR; t++)
+#pragma unroll
+                    for (int g = 0; g < GW; g++)
+#pragma unroll
+                        for (int e = 0; e < 4; e++) acc[g][t0 + t][e] = fmaf(s[t], part[g][t][e], acc[g][t0 + t][e]);
             }
         }
         arrived<0>();
@@ -471,24 +484,24 @@ __global__ __launch_bounds__(512, 2) void head_tile_kernel(HeadArgs a, int32_t t
 #pragma unroll
         for (int i = 0; i < 4; i++) w[i].take(piece_at(w_at + i * 16 * SCALE_BLOCK + c0), piece_at(w_at + i * 16 * SCALE_BLOCK + c1));
         // a step behind: the scaled sums of sixteen rows are added while the next rows' products run
-        f32x4 part[4], last[4];
+        f32x4 part[4][1], last[4];
         float s = 0.0f, s_last = 0.0f;
-        Operand<ElemT> x, x_next;
+        Operand<ElemT> x[1], x_next;
         x_next.take(piece_at(x_at + c0), piece_at(x_at + c1));
 #pragma unroll
         for (int j = 0; j <= MJ; j++) {
             if (j < MJ) {
-                x = x_next;
+                x[0] = x_next;
                 s = s_at[j * 16];
                 if (j + 1 < MJ) x_next.take(piece_at(x_at + (j + 1) * 16 * SCALE_BLOCK + c0), piece_at(x_at + (j + 1) * 16 * SCALE_BLOCK + c1));
+                multiply(w, x, part);
             }
 #pragma unroll
             for (int i = 0; i < 4; i++) {
-                if (j < MJ) part[i] = w[i].times(x);
                 if (j > 0)
 #pragma unroll
                     for (int e = 0; e < 4; e++) acc[j - 1][i][e] = fmaf(s_last, last[i][e], acc[j - 1][i][e]);
-                last[i] = part[i];
+                last[i] = part[i][0];
             }
             s_last = s;
             __builtin_amdgcn_sched_barrier(0);
@@ -568,8 +581,8 @@ hipError_t head(const HeadArgs &a, hipStream_t s) {
     if (a.M <= 64) return head_few<4, MASK, ElemT>(a, s);
     if ((a.w_stride | a.x_stride) >= (1 << 24)) return head_rows<4, 128, MASK, ElemT>(a, s);   // a tile's rows would not lie within 32 bits
     // operands in bf16 take twice the registers: half the rows
-    if (sizeof(ElemT) == 4 || a.M <= 128) return head_tile<4, MASK, ElemT>(a, s);
-    return head_tile<8, MASK, ElemT>(a, s);
+    if constexpr (sizeof(ElemT) == 2) { if (a.M > 128) return head_tile<8, MASK, ElemT>(a, s); }
+    return head_tile<4, MASK, ElemT>(a, s);
 }
 
 template <typename ElemT>
