@@ -23,7 +23,7 @@ template <> struct Piece<uint32_t> { typedef u32x4 type __attribute__((aligned(4
 template <> struct Piece<uint16_t> { typedef u32x4 type __attribute__((aligned(2))); };
 
 static const float LOG2_E = 1.44269504088896340736f, LN_2 = 0.69314718055994530942f;
-static const int THREADS = 256, WAVES = THREADS / 64, ROWS_JOINED = 4;   // rows a workgroup of the joining kernel takes, a wavefront each
+static const int THREADS = 256, ROWS_JOINED = 4;  // rows a workgroup of the joining kernel takes, a wavefront each
 static const int PIECES = 4;                                             // 16-byte pieces of a segment that a thread holds; one where that leaves the chip half empty
 
 struct Part { float m, S, T, pad; };          // of one segment of a row
@@ -101,13 +101,58 @@ __device__ __forceinline__ void join(Part &a, const Part &b, float c) {
     a.S = fa * a.S + fb * b.S;
     a.m = whole.m;
 }
+// The parts that the lanes of a wavefront hold (m = -inf, S = T = 0 in the others), joined, and what follows from the whole of a row.
+struct RowEnd {
+    Reference ref;
+    float S, T, log2_S, ln_S;                  // ln_S: of the sum around m itself
+    bool nothing;
+    __device__ __forceinline__ RowEnd() : ref(0.0f, 0.0f) {}
+    __device__ __forceinline__ RowEnd(const Part &mine, float c) : ref(wave_max(mine.m), c) {
+        const float d = below(mine.m, ref), f = two_to(d);
+        T = wave_sum(f * (mine.T + mine.S * d));
+        S = wave_sum(f * mine.S);
+        nothing = ref.m == -INFINITY && S == 0.0f;
+        log2_S = nothing ? 0.0f : log2f(S);
+        ln_S = LN_2 * (ref.far ? log2_S : log2_S - fmaf(ref.m, ref.c, -ref.R));
+    }
+    __device__ __forceinline__ float entropy() const { return nothing ? 0.0f : LN_2 * (log2_S - T / S); }
+    // A finite logit has a finite log probability (the type's lowest value divided by a temperature below one is beyond 32 bits).
+    __device__ __forceinline__ float logprob(float x, float temperature) const {
+        const float lp = (x - ref.m) / temperature - ln_S;
+        return lp < -FLT_MAX && x > -INFINITY ? -FLT_MAX : lp;
+    }
+    // Of a given token whose logit is x, -inf where the mask does not allow it.
+    __device__ __forceinline__ float given(int64_t t, float x, const zf_logprobs_args &a) const {
+        return t >= a.V ? NAN : t < 0 ? 0.0f : S != S ? S : x == -INFINITY ? -INFINITY : logprob(x, a.temperature);
+    }
+    __device__ __forceinline__ void store_row(const zf_logprobs_args &a, int64_t row) const {
+        if (a.entropy) a.entropy[row] = entropy();
+        if (a.stats) { a.stats[2 * row] = ref.m; a.stats[2 * row + 1] = log2_S; }
+    }
+    __device__ __forceinline__ void store_top(const zf_logprobs_args &a, int64_t row, int i, Key k) const {
+        a.top_ids[row * a.top + i] = k ? (int32_t)~(uint32_t)k : -1;
+        a.top_logprobs[row * a.top + i] = k ? logprob(logit_of(k), a.temperature) : -INFINITY;
+    }
+};
 __device__ __forceinline__ bool allowed(const uint32_t *mask, int64_t row, int32_t W, uint32_t v) {
     return !mask || ((mask[row * W + (v >> 5)] >> (v & 31)) & 1u);
 }
 
+// A row's given token j: the token, and its logit (-inf where the mask does not allow it, or there is none such).
+template <typename ElemT>
+__device__ __forceinline__ void look_up(const LogprobsArgs &A, int64_t row, int j, int64_t *t, float *x) {
+    const int64_t at = row * A.a.n_tokens + j;
+    *t = A.a.token_bytes == 8 ? ((const int64_t *)A.a.tokens)[at] : ((const int32_t *)A.a.tokens)[at];
+    *x = -INFINITY;
+    if (*t >= 0 && *t < A.a.V) {
+        const float logit = of_bits(((const ElemT *)A.a.logits)[row * A.a.row_stride_elems + *t]);
+        if (allowed(A.a.mask, row, A.W, (uint32_t)*t)) *x = logit;
+    }
+}
+
 // A thread's pieces of a row's segment, PIECES at a distance of THREADS pieces from token v on: their logits, -inf where there is no token or none that is
 // allowed.  `whole`: the segment ends before the row does.  All loads are issued before the first is looked at.
-template <int PIECES, int EPV, bool ONCE, typename ElemT>
+template <int THREADS, int PIECES, int EPV, bool ONCE, typename ElemT>
 __device__ __forceinline__ void load_pieces(const ElemT *row, const uint32_t *mask_row, int32_t v, int32_t V, bool whole, float (&x)[PIECES][EPV]) {
     constexpr uint32_t FULL = (1u << EPV) - 1u;
     u32x4 raw[PIECES];
@@ -164,22 +209,27 @@ __device__ __forceinline__ int rank_of(Key mine, const Key *list, int n) {
     return rank;
 }
 
-template <int PIECES, bool ONCE, bool ENT, bool TOP, typename ElemT>
+// A segment of a row, or (n_seg = 1) the whole of it, to the end.
+template <int THREADS, int PIECES, bool ONCE, bool ENT, bool TOP, typename ElemT>
 __global__ __launch_bounds__(THREADS) void logprobs_part_kernel(LogprobsArgs A) {
-    constexpr int EPV = 16 / sizeof(ElemT);
+    constexpr int EPV = 16 / sizeof(ElemT), WAVES = THREADS / 64;
     __shared__ Part part[WAVES];
     __shared__ Key best[WAVES];
     __shared__ float listed_x[TOP ? WAVES : 1][LISTED];
     __shared__ uint32_t listed_v[TOP ? WAVES : 1][LISTED];
     __shared__ uint32_t lines[2][WAVES];
     __shared__ int n_listed[WAVES];
-    const int tid = threadIdx.x, wave = tid / 64;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64;
     const int64_t row = blockIdx.x / (uint32_t)A.n_seg;
     const int32_t seg = blockIdx.x % (uint32_t)A.n_seg, V = A.a.V, v0 = seg * (THREADS * PIECES * EPV) + tid * EPV;
     const ElemT *const logits = (const ElemT *)A.a.logits + row * A.a.row_stride_elems;
     const uint32_t *const mask = A.a.mask ? A.a.mask + row * A.W : nullptr;
     float x[PIECES][EPV], most = -INFINITY;
-    load_pieces<PIECES, EPV, ONCE>(logits, mask, v0, V, (seg + 1) * (THREADS * PIECES * EPV) <= V, x);
+    load_pieces<THREADS, PIECES, EPV, ONCE>(logits, mask, v0, V, (seg + 1) * (THREADS * PIECES * EPV) <= V, x);
+    const bool row_ends = A.n_seg == 1;                    // here; the last wavefront looks the given tokens up
+    int64_t given = -1;
+    float given_x = -INFINITY;
+    if (row_ends && wave == WAVES - 1 && lane < A.a.n_tokens) look_up<ElemT>(A, row, lane, &given, &given_x);
 #pragma unroll
     for (int p = 0; p < PIECES; p++)
 #pragma unroll
@@ -220,11 +270,18 @@ __global__ __launch_bounds__(THREADS) void logprobs_part_kernel(LogprobsArgs A) 
         lines[1][wave] = line_of(mine, (A.a.top + WAVES - 1) / WAVES);
     }
     __syncthreads();
-    if (tid == THREADS - 1) {
-        Part all = part[0];
-#pragma unroll
-        for (int w = 1; w < WAVES; w++) join(all, part[w], A.c);
-        A.parts[blockIdx.x] = all;
+    const Part mine = lane < WAVES ? part[lane] : Part{-INFINITY, 0.0f, 0.0f, 0.0f};
+    if (wave == WAVES - 1) {
+        const RowEnd end(mine, A.c);                       // (of the segment)
+        if (!row_ends) {
+            if (lane == 0) A.parts[blockIdx.x] = Part{end.ref.m, end.S, end.T, 0.0f};
+        } else {
+            if (lane == 0) end.store_row(A.a, row);
+            for (int j = lane; j < A.a.n_tokens; j += 64) {
+                if (j != lane) look_up<ElemT>(A, row, j, &given, &given_x);
+                A.a.logprobs[row * A.a.n_tokens + j] = end.given(given, given_x, A.a);
+            }
+        }
     }
     if (!TOP) return;
     // `top` logits of a single wavefront reach the one, a share of them in each wavefront the other: the higher of the two
@@ -246,7 +303,12 @@ __global__ __launch_bounds__(THREADS) void logprobs_part_kernel(LogprobsArgs A) 
         }
     if (tid % 64 == 0) n_listed[wave] = n;
     __syncthreads();
-    Key *const out = A.keys + (int64_t)blockIdx.x * A.a.top;
+    RowEnd end;
+    if (wave == 0 && row_ends) end = RowEnd(mine, A.c);    // the first wavefront stores
+    auto store = [&](int i, Key k) {
+        if (row_ends) end.store_top(A.a, row, i, k);
+        else A.keys[(int64_t)blockIdx.x * A.a.top + i] = k;
+    };
     int n_all = 0;
     bool fits = true;
 #pragma unroll
@@ -268,9 +330,9 @@ __global__ __launch_bounds__(THREADS) void logprobs_part_kernel(LogprobsArgs A) 
                 for (int j = 0; j < n_other; j++)
                     rank += ((Key)(uint32_t)__builtin_amdgcn_readlane((int)(other >> 32), j) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)other, j)) > mine;
             }
-            if (mine && rank < A.a.top) out[rank] = mine;
+            if (mine && rank < A.a.top) store(rank, mine);
         }
-        for (int i = n_all + tid; i < A.a.top; i += 64) out[i] = 0;
+        for (int i = n_all + tid; i < A.a.top; i += 64) store(i, 0);
         return;
     }
     Key last = ~(Key)0;
@@ -288,7 +350,7 @@ __global__ __launch_bounds__(THREADS) void logprobs_part_kernel(LogprobsArgs A) 
         __syncthreads();
         k0 = best[0];
         for (int w = 1; w < WAVES; w++) if (best[w] > k0) k0 = best[w];
-        if (tid == 0) out[i] = k0;
+        if (tid == 0) store(i, k0);
         last = k0 ? k0 : 1;                                // none left: no key is below 1 but 0
         __syncthreads();
     }
@@ -316,48 +378,19 @@ __global__ __launch_bounds__(ROWS_JOINED * 64) void logprobs_join_kernel(Logprob
             own[j] = 0;
             if (j * 64 + lane < n_keys) own[j] = keys[j * 64 + lane];
         }
-    const ElemT *const logits = (const ElemT *)A.a.logits + row * A.a.row_stride_elems;
-    int64_t t = -1;                                        // the lane's given token, its logit (-inf where the mask does not allow it)
+    int64_t t = -1;
     float x = -INFINITY;
-    auto look_up = [&](int j) {
-        const int64_t at = row * A.a.n_tokens + j;
-        t = A.a.token_bytes == 8 ? ((const int64_t *)A.a.tokens)[at] : ((const int32_t *)A.a.tokens)[at];
-        x = -INFINITY;
-        if (t >= 0 && t < A.a.V) {
-            const float logit = of_bits(logits[t]);
-            if (allowed(A.a.mask, row, A.W, (uint32_t)t)) x = logit;
-        }
-    };
-    if (lane < A.a.n_tokens) look_up(lane);
-    Part all{-INFINITY, 0.0f, 0.0f, 0.0f};
-    for (int s = lane; s < A.n_seg; s += 64) join(all, A.parts[row * A.n_seg + s], A.c);
-    const Reference ref(wave_max(all.m), A.c);
-    const float d = below(all.m, ref), f = two_to(d);
-    all.T = wave_sum(f * (all.T + all.S * d));
-    all.S = wave_sum(f * all.S);
-    const bool nothing = ref.m == -INFINITY && all.S == 0.0f;
-    const float log2_S = nothing ? 0.0f : log2f(all.S);
-    const float ln_S = LN_2 * (ref.far ? log2_S : log2_S - fmaf(ref.m, ref.c, -ref.R));      // of the sum around m itself
-    auto logprob_of = [&](float x) {                       // a finite logit has a finite log probability (the type's lowest value divided by a temperature below one is beyond 32 bits)
-        const float lp = (x - ref.m) / A.a.temperature - ln_S;
-        return lp < -FLT_MAX && x > -INFINITY ? -FLT_MAX : lp;
-    };
-    if (lane == 0) {
-        if (A.a.entropy) A.a.entropy[row] = nothing ? 0.0f : LN_2 * (log2_S - all.T / all.S);
-        if (A.a.stats) { A.a.stats[2 * row] = ref.m; A.a.stats[2 * row + 1] = log2_S; }
-    }
+    if (lane < A.a.n_tokens) look_up<ElemT>(A, row, lane, &t, &x);
+    Part mine_part{-INFINITY, 0.0f, 0.0f, 0.0f};
+    for (int s = lane; s < A.n_seg; s += 64) join(mine_part, A.parts[row * A.n_seg + s], A.c);
+    const RowEnd end(mine_part, A.c);
+    if (lane == 0) end.store_row(A.a, row);
     for (int j = lane; j < A.a.n_tokens; j += 64) {
-        if (j != lane) look_up(j);
-        float lp = 0.0f;
-        if (t >= A.a.V) lp = NAN;
-        else if (t >= 0) lp = all.S != all.S ? all.S : x == -INFINITY ? -INFINITY : logprob_of(x);
-        A.a.logprobs[row * A.a.n_tokens + j] = lp;
+        if (j != lane) look_up<ElemT>(A, row, j, &t, &x);
+        A.a.logprobs[row * A.a.n_tokens + j] = end.given(t, x, A.a);
     }
     if (!A.a.top) return;
-    auto store = [&](int i, Key k) {
-        A.a.top_ids[row * A.a.top + i] = k ? (int32_t)~(uint32_t)k : -1;
-        A.a.top_logprobs[row * A.a.top + i] = k ? logprob_of(logit_of(k)) : -INFINITY;
-    };
+    auto store = [&](int i, Key k) { end.store_top(A.a, row, i, k); };
     if (listable) {
         uint32_t most = 0;
 #pragma unroll
@@ -410,7 +443,7 @@ __global__ __launch_bounds__(ROWS_JOINED * 64) void logprobs_join_kernel(Logprob
 template <int PIECES, bool ONCE, typename ElemT>
 __global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(GradArgs A) {
     constexpr int EPV = 16 / sizeof(ElemT);
-    __shared__ float sums[WAVES];
+    __shared__ float sum;
     __shared__ int n_mine;
     __shared__ int32_t mine_v[GIVEN_MAX + TOP_MAX];        // tokens of the segment that have a gradient of their own
     __shared__ float mine_g[GIVEN_MAX + TOP_MAX];
@@ -422,7 +455,7 @@ __global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(GradArgs A) {
     const uint32_t *const mask = a.mask ? a.mask + row * A.l.W : nullptr;
     const bool whole = first + THREADS * PIECES * EPV <= V;
     float x[PIECES][EPV];
-    load_pieces<PIECES, EPV, ONCE>(logits, mask, v0, V, whole, x);
+    load_pieces<THREADS, PIECES, EPV, ONCE>(logits, mask, v0, V, whole, x);
     float G = 0.0f;
     const int n_given = A.g.g_logprobs ? a.n_tokens : 0, n_all = n_given + (A.g.g_top ? a.top : 0);
     if (wave == 0) {                                       // the first wavefront lists them, in order
@@ -447,10 +480,10 @@ __global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(GradArgs A) {
             n += __popcll(who);
         }
         G = wave_sum(G);
-        if (lane == 0) { sums[0] = G; n_mine = n; }
+        if (lane == 0) { sum = G; n_mine = n; }
     }
     __syncthreads();
-    G = sums[0];
+    G = sum;
     const Reference ref(a.stats[2 * row], A.l.c);
     const float log2_S = a.stats[2 * row + 1], inv_t = A.l.inv_t;
     const float gh = A.g.g_entropy ? A.g.g_entropy[row] : 0.0f, H = A.g.g_entropy ? a.entropy[row] : 0.0f;
@@ -496,21 +529,27 @@ __global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(GradArgs A) {
     }
 }
 
-// A thread of a segment holds PIECES pieces, or one where segments of so many would be fewer than two workgroups a compute unit.
-int pieces(const zf_logprobs_args &a) {
-    const int64_t n = THREADS * PIECES * (a.dtype == 0 ? 4 : 8);
-    if (a.rows * ((a.V + n - 1) / n) >= 512) return PIECES;
-    return (int64_t)((a.V + n / PIECES - 1) / (n / PIECES)) * a.top <= JOINED_LANE * 64 ? 1 : PIECES;   // ... and what the joining wavefronts list holds their alternatives
+int64_t blocks_of(const zf_logprobs_args &a, int threads, int pieces) {
+    const int32_t n = threads * pieces * (a.dtype == 0 ? 4 : 8);
+    return a.rows * ((a.V + n - 1) / n);
 }
-int32_t segments(const zf_logprobs_args &a) {
-    const int32_t n = THREADS * pieces(a) * (a.dtype == 0 ? 4 : 8);
-    return (a.V + n - 1) / n;
+// Threads of a workgroup and 16-byte pieces that each holds.  A row of up to 32,768 logits is one workgroup's, which ends it: no second launch, no workspace
+// (300 x 32,000 fp32 12.2 us, in segments 14.8; one such row 9.7 and 8.9, but its call 7 us of the host and 11).  Longer rows are cut into segments of four pieces a thread, or of one where that would be fewer than two workgroups a compute unit and the joining
+// wavefronts' lists hold the alternatives of so many.
+struct Plan { int threads, pieces; int32_t n_seg; };
+Plan plan_of(const zf_logprobs_args &a) {
+    const int epv = a.dtype == 0 ? 4 : 8;
+    const Plan whole[] = {{256, 1, 1}, {256, 4, 1}, {1024, 4, 1}, {1024, 8, 1}};
+    for (const Plan &p : whole) if (a.V <= p.threads * p.pieces * epv && (a.dtype == 0 || p.pieces < 8)) return p;
+    int pieces = PIECES;
+    if (blocks_of(a, THREADS, PIECES) < 512 && blocks_of(a, THREADS, 1) / a.rows * a.top <= JOINED_LANE * 64) pieces = 1;
+    return Plan{THREADS, pieces, (int32_t)(blocks_of(a, THREADS, pieces) / a.rows)};
 }
-LogprobsArgs with_plan(const zf_logprobs_args &a, void *workspace) {
+LogprobsArgs args_of(const zf_logprobs_args &a, int32_t n_seg, void *workspace) {
     LogprobsArgs A{};
     A.a = a;
     A.W = (a.V + 31) / 32;
-    A.n_seg = segments(a);
+    A.n_seg = n_seg;
     A.c = LOG2_E / a.temperature;
     A.inv_t = 1.0f / a.temperature;
     A.parts = (Part *)workspace;
@@ -525,38 +564,49 @@ bool once(const zf_logprobs_args &a) {
     const int64_t size = a.dtype == 0 ? 4 : 2;
     return a.rows * a.V * size > (256ll << 20) && (uintptr_t)a.logits % 16 == 0 && a.row_stride_elems * size % 16 == 0;
 }
-template <int PIECES, bool ONCE, typename ElemT>
+template <int THREADS, int PIECES, bool ONCE, typename ElemT>
 void parts(const LogprobsArgs &A, hipStream_t s) {
     const bool entropy = A.a.entropy != nullptr;
-    auto *const part = A.a.top ? (entropy ? logprobs_part_kernel<PIECES, ONCE, true, true, ElemT> : logprobs_part_kernel<PIECES, ONCE, false, true, ElemT>)
-                               : (entropy ? logprobs_part_kernel<PIECES, ONCE, true, false, ElemT> : logprobs_part_kernel<PIECES, ONCE, false, false, ElemT>);
+    auto *const part = A.a.top ? (entropy ? logprobs_part_kernel<THREADS, PIECES, ONCE, true, true, ElemT> : logprobs_part_kernel<THREADS, PIECES, ONCE, false, true, ElemT>)
+                               : (entropy ? logprobs_part_kernel<THREADS, PIECES, ONCE, true, false, ElemT> : logprobs_part_kernel<THREADS, PIECES, ONCE, false, false, ElemT>);
     hipLaunchKernelGGL(part, dim3((uint32_t)(A.a.rows * A.n_seg)), dim3(THREADS), 0, s, A);
 }
 template <typename ElemT>
-void forward(const LogprobsArgs &A, hipStream_t s) {
-    if (pieces(A.a) == 1) parts<1, false, ElemT>(A, s);
-    else if (once(A.a)) parts<PIECES, true, ElemT>(A, s);
-    else parts<PIECES, false, ElemT>(A, s);
-    hipLaunchKernelGGL((logprobs_join_kernel<ElemT>), dim3((uint32_t)((A.a.rows + ROWS_JOINED - 1) / ROWS_JOINED)), dim3(ROWS_JOINED * 64),
-                       A.a.top ? ROWS_JOINED * A.n_seg : 0, s, A);
+void forward(const LogprobsArgs &A, const Plan &p, hipStream_t s) {
+    const bool pass = once(A.a);
+    if (p.threads == 1024) {
+        if constexpr (sizeof(ElemT) == 4) { if (p.pieces == 8) return pass ? parts<1024, 8, true, ElemT>(A, s) : parts<1024, 8, false, ElemT>(A, s); }
+        return pass ? parts<1024, 4, true, ElemT>(A, s) : parts<1024, 4, false, ElemT>(A, s);
+    }
+    if (p.pieces == 1) parts<THREADS, 1, false, ElemT>(A, s);
+    else if (pass) parts<THREADS, PIECES, true, ElemT>(A, s);
+    else parts<THREADS, PIECES, false, ElemT>(A, s);
+    if (A.n_seg > 1)
+        hipLaunchKernelGGL((logprobs_join_kernel<ElemT>), dim3((uint32_t)((A.a.rows + ROWS_JOINED - 1) / ROWS_JOINED)), dim3(ROWS_JOINED * 64),
+                           A.a.top ? ROWS_JOINED * A.n_seg : 0, s, A);
 }
 
 }  // namespace
 
-int64_t logprobs_workspace(const zf_logprobs_args &a) { return a.rows * segments(a) * (int64_t)(sizeof(Part) + a.top * sizeof(Key)); }
-int64_t logprobs_blocks(const zf_logprobs_args &a) { return a.rows * segments(a); }
+int64_t logprobs_workspace(const zf_logprobs_args &a) {
+    const int64_t n = plan_of(a).n_seg;
+    return n > 1 ? a.rows * n * (int64_t)(sizeof(Part) + a.top * sizeof(Key)) : 0;
+}
+int64_t logprobs_blocks(const zf_logprobs_args &a) { return blocks_of(a, THREADS, 1); }   // at most
 
 hipError_t launch_logprobs(const zf_logprobs_args &a, void *workspace, hipStream_t s) {
-    const LogprobsArgs A = with_plan(a, workspace);
-    if (a.dtype == 0) forward<uint32_t>(A, s);
-    else forward<uint16_t>(A, s);
+    const Plan p = plan_of(a);
+    const LogprobsArgs A = args_of(a, p.n_seg, workspace);
+    if (a.dtype == 0) forward<uint32_t>(A, p, s);
+    else forward<uint16_t>(A, p, s);
     return hipGetLastError();
 }
 
 hipError_t launch_logprobs_backward(const zf_logprobs_args &a, const LogprobsGrad &g, hipStream_t s) {
-    const GradArgs A{with_plan(a, nullptr), g};
+    const int n = blocks_of(a, THREADS, PIECES) < 512 ? 1 : PIECES;       // pieces
+    const GradArgs A{args_of(a, (int32_t)(blocks_of(a, THREADS, n) / a.rows), nullptr), g};
     const bool pass = once(a) && (uintptr_t)g.grad % 16 == 0 && g.stride * (a.dtype == 0 ? 4 : 2) % 16 == 0;
-    auto *const kernel = pieces(a) == 1 ? (a.dtype == 0 ? logprobs_grad_kernel<1, false, uint32_t> : logprobs_grad_kernel<1, false, uint16_t>)
+    auto *const kernel = n == 1 ? (a.dtype == 0 ? logprobs_grad_kernel<1, false, uint32_t> : logprobs_grad_kernel<1, false, uint16_t>)
                          : pass         ? (a.dtype == 0 ? logprobs_grad_kernel<PIECES, true, uint32_t> : logprobs_grad_kernel<PIECES, true, uint16_t>)
                                         : (a.dtype == 0 ? logprobs_grad_kernel<PIECES, false, uint32_t> : logprobs_grad_kernel<PIECES, false, uint16_t>);
     hipLaunchKernelGGL(kernel, dim3((uint32_t)(a.rows * A.l.n_seg)), dim3(THREADS), 0, s, A);

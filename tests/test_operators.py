@@ -527,11 +527,12 @@ def test_library_refuses_before_it_touches_a_device():
                 dict(n_tokens=1025), dict(top=-1), dict(top=65), dict(temperature=0.0), dict(temperature=-1.0), dict(temperature=math.nan), dict(temperature=INF), dict(logprobs=None), dict(top_ids=None), dict(top_logprobs=None),
                 dict(logits=one + 2)):
         assert logprobs(**bad) == zf.ZF_ERR_INVALID_ARG and L.zf_last_error(), bad
-    need = L.zf_token_logprobs_workspace(args())
+    wide = dict(V=100000, row_stride=100000)               # rows that one workgroup does not take
+    need = L.zf_token_logprobs_workspace(args(**wide))
     assert need > 0
-    assert L.zf_token_logprobs(args(), one, need - 1, 0, None) == zf.ZF_ERR_INVALID_ARG
-    assert L.zf_token_logprobs(args(), None, need, 0, None) == zf.ZF_ERR_INVALID_ARG
-    assert L.zf_token_logprobs(args(), one + 8, need, 0, None) == zf.ZF_ERR_INVALID_ARG
+    assert L.zf_token_logprobs(args(**wide), one, need - 1, 0, None) == zf.ZF_ERR_INVALID_ARG
+    assert L.zf_token_logprobs(args(**wide), None, need, 0, None) == zf.ZF_ERR_INVALID_ARG
+    assert L.zf_token_logprobs(args(**wide), one + 8, need, 0, None) == zf.ZF_ERR_INVALID_ARG
     assert L.zf_token_logprobs(None, one, 1 << 40, 0, None) == zf.ZF_ERR_INVALID_ARG and L.zf_token_logprobs_workspace(None) == zf.ZF_ERR_INVALID_ARG
     assert L.zf_token_logprobs(args(rows=0, logits=None), None, 0, 0, None) == 0 and L.zf_token_logprobs_workspace(args(rows=0)) == 0
     for kw, g in ((dict(stats=None), (one, one, one, one, 10)), ({}, (one, one, one, None, 10)), ({}, (one, one, one, one, 9)), ({}, (one, one, one, one + 2, 10)), (dict(entropy=None), (one, one, one, one, 10))):
