@@ -13,6 +13,7 @@
 // four v_mfma_f32_16x16x32_bf16 make the block's sum (1e-8 and 7e-8 off), at half the rate.
 #include <hip/hip_runtime.h>
 #include <algorithm>
+#include <atomic>
 #include <cstdlib>
 #include "zf_ops.h"
 
@@ -34,9 +35,9 @@ template <> struct Piece<uint16_t> { typedef u32x4 type __attribute__((aligned(2
 __device__ __forceinline__ float of_bits(uint32_t x) { return __uint_as_float(x); }
 __device__ __forceinline__ float of_bits(uint16_t x) { return __uint_as_float((uint32_t)x << 16); }
 __device__ __forceinline__ uint16_t bf16_of(float x) {             // to nearest, ties to even
-    uint32_t u = __float_as_uint(x);
-    if ((u & 0x7FFFFFFFu) > 0x7F800000u) return (uint16_t)((u >> 16) | 0x40u);
-    return (uint16_t)((u + 0x7FFFu + ((u >> 16) & 1u)) >> 16);
+    union { __bf16 b; uint16_t u; } o;
+    o.b = (__bf16)x;
+    return o.u;
 }
 
 // ---- to 8 bits ----
@@ -424,147 +425,181 @@ __global__ __launch_bounds__(256, 2) void head_rows_kernel(HeadArgs a) {
 
 // ---- many rows: tiles of both operands in LDS ----
 //
-// A workgroup of eight wavefronts has 256 tokens and 32 MJ rows of the batch, a wavefront 64 tokens and 16 MJ rows.  A block of columns of both operands, 128 bytes a
-// row, comes from memory straight into LDS while the block before is multiplied: two buffers, one barrier a block, pieces in places as above.
+// A workgroup of eight wavefronts takes tiles of 256 tokens and 32 MJ rows of the batch, one after the other, a wavefront 64 tokens and 16 MJ rows.  A block of columns of both
+// operands, 128 bytes a row, comes from memory straight into LDS while the block before is multiplied, the next tile's first one while this one's last is: two buffers, one
+// barrier a block, pieces in places as above.  While sixteen rows' products run the sixteen before them are scaled and added.
 //   Rows behind the last one are the last one again; their results are not stored.
-static const int TILE_TOKENS = 256;
+static const int TILE_TOKENS = 256, COMPUTE_UNITS = 256;
 
-template <int MJ>
+template <int MJ, typename ElemT>
 struct TileLds {
     static constexpr int ROWS = 32 * MJ, W_BYTES = TILE_TOKENS * SCALE_BLOCK, X_BYTES = ROWS * SCALE_BLOCK, BUFFER = W_BYTES + X_BYTES;
-    static constexpr int SCALES = 2 * BUFFER, LOOP = SCALES + 2 * 512 * 4;
+    static constexpr int SCALES = 2 * BUFFER, OUT = SCALES + 2 * 512 * 4, PITCH = 64 * sizeof(ElemT) + 16, BYTES = OUT + 8 * 16 * PITCH;
 };
 
 template <int MJ, bool MASK, typename ElemT>
 __global__ __launch_bounds__(512, 2) void head_tile_kernel(HeadArgs a, int32_t tiles_m, int32_t n_tiles) {
-    typedef TileLds<MJ> Lds;
+    typedef TileLds<MJ, ElemT> Lds;
+    constexpr int LOADS = 4 + MJ / 2;                                        // of a wavefront for a block: eight rows each, 32 of the weight, 4 MJ of the activations
     extern __shared__ __align__(16) uint8_t mem[];
     const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64), wv = wave % 4, wm = wave / 4;
+    const int32_t n_k = a.K / SCALE_BLOCK, n_vb = (a.V + SCALE_BLOCK - 1) / SCALE_BLOCK, W = (a.V + 31) / 32;
     // workgroups go to the eight XCDs in turn: an XCD takes consecutive tiles, those of the same tokens one after the other, so that its L2 has a weight's rows once
-    const int32_t per = n_tiles / 8, over = n_tiles % 8, xcd = blockIdx.x % 8;
-    const int32_t tile = xcd * per + (xcd < over ? xcd : over) + blockIdx.x / 8;
-    const int32_t v0 = tile / tiles_m * TILE_TOKENS, m0 = tile % tiles_m * Lds::ROWS, n_k = a.K / SCALE_BLOCK;
-    // a wavefront brings eight rows at a time: 32 rows of the weight, 4 MJ of the activations, a block
-    const int32_t place = lane % 8 ^ lane / 8;
-    const uint8_t *const w0 = a.w + (int64_t)v0 * a.w_stride, *const x0 = a.x + (int64_t)m0 * a.x_stride;
-    uint32_t off[4 + MJ / 2], at[4 + MJ / 2];                                // the host checks that a tile's rows lie within 32 bits
+    const int32_t per = n_tiles / 8, over = n_tiles % 8, xcd = blockIdx.x % 8, stride = (gridDim.x - xcd + 7) / 8;
+    const int32_t end = (xcd + 1) * per + (xcd < over ? xcd + 1 : over);
+    int32_t tile = xcd * per + (xcd < over ? xcd : over) + blockIdx.x / 8;
+    if (tile >= end) return;
+    const uint8_t *w0, *x0;                                                  // of the tile that is being brought
+    uint32_t off[LOADS];                                                     // the host checks that a tile's rows lie within 32 bits
+    const float *xs, *ws;                                                    // a thread's scales: of one row, and of the weight's first or second 128 tokens (the threads behind these two have them once more)
+    auto aim = [&](int32_t t) {
+        const int32_t v0 = t / tiles_m * TILE_TOKENS, m0 = t % tiles_m * Lds::ROWS;
+        w0 = a.w + (int64_t)v0 * a.w_stride;
+        x0 = a.x + (int64_t)m0 * a.x_stride;
 #pragma unroll
-    for (int i = 0; i < 4 + MJ / 2; i++) {
-        const int32_t r = i < 4 ? (wave * 4 + i) * 8 : (wave * (MJ / 2) + i - 4) * 8, left = i < 4 ? a.V - v0 : a.M - m0;
-        off[i] = (uint32_t)(r + lane / 8 < left ? r + lane / 8 : left - 1) * (uint32_t)(i < 4 ? a.w_stride : a.x_stride) + place * 16;
-        at[i] = lds_at(mem) + (i < 4 ? 0 : Lds::W_BYTES) + r * SCALE_BLOCK;
-    }
-    float *const scales = reinterpret_cast<float *>(mem + Lds::SCALES);
-    // a thread's scales: those of one row times the weight's of the first or the second 128 tokens (the threads behind these two have them once more)
-    const int32_t n_vb = (a.V + SCALE_BLOCK - 1) / SCALE_BLOCK, row = m0 + tid % Lds::ROWS, vb = v0 / SCALE_BLOCK + tid / Lds::ROWS % 2;
-    const float *const xs = a.xs + (size_t)(row < a.M ? row : a.M - 1) * n_k, *const ws = a.ws + (size_t)(vb < n_vb ? vb : n_vb - 1) * n_k;
+        for (int i = 0; i < LOADS; i++) {
+            const int32_t r = (i < 4 ? wave * 4 + i : wave * (MJ / 2) + i - 4) * 8 + lane / 8, left = i < 4 ? a.V - v0 : a.M - m0;
+            off[i] = (uint32_t)(r < left ? r : left - 1) * (uint32_t)(i < 4 ? a.w_stride : a.x_stride) + (lane % 8 ^ lane / 8) * 16;
+        }
+        const int32_t row = m0 + tid % Lds::ROWS, vb = v0 / SCALE_BLOCK + tid / Lds::ROWS % 2;
+        xs = a.xs + (size_t)(row < a.M ? row : a.M - 1) * n_k;
+        ws = a.ws + (size_t)(vb < n_vb ? vb : n_vb - 1) * n_k;
+    };
     auto fetch = [&](int32_t k, int b) {
 #pragma unroll
-        for (int i = 0; i < 4 + MJ / 2; i++) to_lds((i < 4 ? w0 : x0) + (size_t)k * SCALE_BLOCK, off[i], at[i] + b * Lds::BUFFER);
+        for (int i = 0; i < LOADS; i++)
+            to_lds((i < 4 ? w0 : x0) + (size_t)k * SCALE_BLOCK, off[i], lds_at(mem) + b * Lds::BUFFER + (i < 4 ? (wave * 4 + i) * 8 * SCALE_BLOCK : Lds::W_BYTES + (wave * (MJ / 2) + i - 4) * 8 * SCALE_BLOCK));
     };
-    f32x4 acc[MJ][4];
-#pragma unroll
-    for (int j = 0; j < MJ; j++)
-#pragma unroll
-        for (int i = 0; i < 4; i++) acc[j][i] = f32x4{0, 0, 0, 0};
+    float *const scales = reinterpret_cast<float *>(mem + Lds::SCALES);
+    uint8_t *const own = mem + Lds::OUT + wave * (16 * Lds::PITCH);
+    const int32_t c0 = (lane / 16 ^ lane % 8) * 16, c1 = ((lane / 16 + 4) ^ lane % 8) * 16;   // the lane's two pieces of a row that is lane % 8 modulo 8
+    aim(tile);
     scales[tid] = xs[0] * ws[0];
     fetch(0, 0);
     arrived<0>();
     __syncthreads();
-    const int32_t c0 = (lane / 16 ^ lane % 8) * 16, c1 = ((lane / 16 + 4) ^ lane % 8) * 16;   // the lane's two pieces of a row that is lane % 8 modulo 8
-    for (int32_t k = 0; k < n_k; k++) {
-        const int b = k & 1;
-        const int32_t k_next = k + 1 < n_k ? k + 1 : k;
-        const float next_x = xs[k_next], next_w = ws[k_next];
-        if (k + 1 < n_k) fetch(k + 1, b ^ 1);
-        const uint8_t *const w_at = mem + b * Lds::BUFFER + (wv * 64 + lane % 16) * SCALE_BLOCK;
-        const uint8_t *const x_at = mem + b * Lds::BUFFER + Lds::W_BYTES + (wm * 16 * MJ + lane % 16) * SCALE_BLOCK;
-        const float *const s_at = scales + b * 512 + wv / 2 * Lds::ROWS + wm * 16 * MJ + lane % 16;
-        Operand<ElemT> w[4];
+    int b = 0;
+    for (; tile < end; tile += stride) {
+        f32x4 acc[MJ][4];
 #pragma unroll
-        for (int i = 0; i < 4; i++) w[i].take(piece_at(w_at + i * 16 * SCALE_BLOCK + c0), piece_at(w_at + i * 16 * SCALE_BLOCK + c1));
-        // a step behind: the scaled sums of sixteen rows are added while the next rows' products run
-        f32x4 part[4][1], last[4];
-        float s = 0.0f, s_last = 0.0f;
-        Operand<ElemT> x[1], x_next;
-        x_next.take(piece_at(x_at + c0), piece_at(x_at + c1));
+        for (int j = 0; j < MJ; j++)
 #pragma unroll
-        for (int j = 0; j <= MJ; j++) {
-            if (j < MJ) {
-                x[0] = x_next;
-                s = s_at[j * 16];
-                if (j + 1 < MJ) x_next.take(piece_at(x_at + (j + 1) * 16 * SCALE_BLOCK + c0), piece_at(x_at + (j + 1) * 16 * SCALE_BLOCK + c1));
-                multiply(w, x, part);
+            for (int i = 0; i < 4; i++) acc[j][i] = f32x4{0, 0, 0, 0};
+        for (int32_t k = 0; k < n_k; k++, b ^= 1) {
+            int32_t k_next = k + 1;
+            if (k_next == n_k) {                                             // behind the last block: the next tile's first (behind the last tile: this one's, which nobody reads)
+                k_next = 0;
+                if (tile + stride < end) aim(tile + stride);
             }
+            const float next_x = xs[k_next], next_w = ws[k_next];
+            const uint8_t *const w_at = mem + b * Lds::BUFFER + (wv * 64 + lane % 16) * SCALE_BLOCK;
+            const uint8_t *const x_at = mem + b * Lds::BUFFER + Lds::W_BYTES + (wm * 16 * MJ + lane % 16) * SCALE_BLOCK;
+            const float *const s_at = scales + b * 512 + wv / 2 * Lds::ROWS + wm * 16 * MJ + lane % 16;
+            Operand<ElemT> w[4];
+#pragma unroll
+            for (int i = 0; i < 4; i++) w[i].take(piece_at(w_at + i * 16 * SCALE_BLOCK + c0), piece_at(w_at + i * 16 * SCALE_BLOCK + c1));
+            f32x4 part[4][1], last[4];
+            float s = 0.0f, s_last = 0.0f;
+            Operand<ElemT> x[1], x_next;
+            x_next.take(piece_at(x_at + c0), piece_at(x_at + c1));
+#pragma unroll
+            for (int j = 0; j <= MJ; j++) {
+                if (j < MJ) {
+                    x[0] = x_next;
+                    s = s_at[j * 16];
+                    if (j + 1 < MJ) x_next.take(piece_at(x_at + (j + 1) * 16 * SCALE_BLOCK + c0), piece_at(x_at + (j + 1) * 16 * SCALE_BLOCK + c1));
+                    multiply(w, x, part);
+                    if (j == 0) fetch(k_next, b ^ 1);                        // behind the reads that the first products wait for
+                }
+#pragma unroll
+                for (int i = 0; i < 4; i++) {
+                    if (j > 0)
+#pragma unroll
+                        for (int e = 0; e < 4; e++) acc[j - 1][i][e] = fmaf(s_last, last[i][e], acc[j - 1][i][e]);
+                    last[i] = part[i][0];
+                }
+                s_last = s;
+                if (j > 0 && j < MJ)
+#pragma unroll
+                    for (int i = 0; i < 4; i++) {                            // a product, four sums, a product, ...
+                        __builtin_amdgcn_sched_group_barrier(0x8, Operand<ElemT>::STEPS, 0);
+                        __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);
+                    }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            scales[(b ^ 1) * 512 + tid] = next_x * next_w;
+            arrived<0>();
+            __syncthreads();
+        }
+        // sixteen rows at a time through the wavefront's own part of LDS, from four tokens a lane to whole lines of 64 tokens
+        constexpr int EPV = 16 / sizeof(ElemT), PIECES = 64 / EPV;
+        const int32_t v_w = tile / tiles_m * TILE_TOKENS + wv * 64, m_w = tile % tiles_m * Lds::ROWS + wm * 16 * MJ;
+#pragma unroll
+        for (int j = 0; j < MJ; j++) {
 #pragma unroll
             for (int i = 0; i < 4; i++) {
-                if (j > 0)
+                union { ElemT e[4]; uint64_t q; u32x4 v; } o;
 #pragma unroll
-                    for (int e = 0; e < 4; e++) acc[j - 1][i][e] = fmaf(s_last, last[i][e], acc[j - 1][i][e]);
-                last[i] = part[i][0];
+                for (int e = 0; e < 4; e++) o.e[e] = sizeof(ElemT) == 4 ? (ElemT)__float_as_uint(acc[j][i][e]) : (ElemT)bf16_of(acc[j][i][e]);
+                uint8_t *const to = own + lane % 16 * Lds::PITCH + (i * 16 + lane / 16 * 4) * sizeof(ElemT);
+                if (sizeof(ElemT) == 4) *reinterpret_cast<u32x4 *>(to) = o.v;
+                else *reinterpret_cast<uint64_t *>(to) = o.q;
             }
-            s_last = s;
-            __builtin_amdgcn_sched_barrier(0);
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int i = 0; i < 16 * PIECES / 64; i++) {
+                const int r = (i * 64 + lane) / PIECES, p = (i * 64 + lane) % PIECES;
+                const int32_t m = m_w + j * 16 + r, v = v_w + p * EPV;
+                union { ElemT e[EPV]; u32x4 v; } o;
+                o.v = *reinterpret_cast<const u32x4 *>(own + r * Lds::PITCH + p * 16);
+                if (m >= a.M || v >= a.V) continue;
+                if (MASK) {
+                    const uint32_t bits = a.mask[(size_t)m * W + (v >> 5)] >> (v & 31);
+#pragma unroll
+                    for (int e = 0; e < EPV; e++) if (!((bits >> e) & 1)) o.e[e] = sizeof(ElemT) == 4 ? (ElemT)0xFF800000u : (ElemT)0xFF80u;
+                }
+                ElemT *const to = (ElemT *)a.y + (int64_t)m * a.y_stride + v;
+                if (v + EPV <= a.V) *reinterpret_cast<typename Piece<ElemT>::type *>(to) = o.v;
+                else {
+#pragma unroll
+                    for (int e = 0; e < EPV; e++) if (v + e < a.V) to[e] = o.e[e];
+                }
+            }
+            __builtin_amdgcn_wave_barrier();
         }
-        scales[(b ^ 1) * 512 + tid] = next_x * next_w;
-        arrived<0>();
-        __syncthreads();
     }
-    // sixteen rows at a time through the wavefront's own part of LDS, from four tokens a lane to whole lines of 64 tokens
-    constexpr int EPV = 16 / sizeof(ElemT), PITCH = 64 * sizeof(ElemT) + 16, PIECES = 64 / EPV;
-    uint8_t *const own = mem + wave * (16 * PITCH);
-    const int32_t W = (a.V + 31) / 32, v_w = v0 + wv * 64;
-#pragma unroll
-    for (int j = 0; j < MJ; j++) {
-#pragma unroll
-        for (int i = 0; i < 4; i++) {
-            union { ElemT e[4]; uint64_t q; u32x4 v; } o;
-#pragma unroll
-            for (int e = 0; e < 4; e++) o.e[e] = sizeof(ElemT) == 4 ? (ElemT)__float_as_uint(acc[j][i][e]) : (ElemT)bf16_of(acc[j][i][e]);
-            uint8_t *const to = own + lane % 16 * PITCH + (i * 16 + lane / 16 * 4) * sizeof(ElemT);
-            if (sizeof(ElemT) == 4) *reinterpret_cast<u32x4 *>(to) = o.v;
-            else *reinterpret_cast<uint64_t *>(to) = o.q;
-        }
-        __builtin_amdgcn_wave_barrier();
-#pragma unroll
-        for (int i = 0; i < 16 * PIECES / 64; i++) {
-            const int r = (i * 64 + lane) / PIECES, p = (i * 64 + lane) % PIECES;
-            const int32_t m = m0 + wm * 16 * MJ + j * 16 + r, v = v_w + p * EPV;
-            union { ElemT e[EPV]; u32x4 v; } o;
-            o.v = *reinterpret_cast<const u32x4 *>(own + r * PITCH + p * 16);
-            if (m >= a.M || v >= a.V) continue;
-            if (MASK) {
-                const uint32_t bits = a.mask[(size_t)m * W + (v >> 5)] >> (v & 31);
-#pragma unroll
-                for (int e = 0; e < EPV; e++) if (!((bits >> e) & 1)) o.e[e] = sizeof(ElemT) == 4 ? (ElemT)0xFF800000u : (ElemT)0xFF80u;
-            }
-            ElemT *const to = (ElemT *)a.y + (int64_t)m * a.y_stride + v;
-            if (v + EPV <= a.V) *reinterpret_cast<typename Piece<ElemT>::type *>(to) = o.v;
-            else {
-#pragma unroll
-                for (int e = 0; e < EPV; e++) if (v + e < a.V) to[e] = o.e[e];
-            }
-        }
-        __builtin_amdgcn_wave_barrier();
-    }
+}
+
+// LDS beyond 64 KB has to be allowed for a kernel, once on every device.
+hipError_t allow_lds(const void *kernel, int bytes, std::atomic<uint64_t> &allowed) {
+    int device = 0;
+    hipError_t e = hipGetDevice(&device);
+    if (e != hipSuccess) return e;
+    const uint64_t bit = device < 64 ? 1ull << device : 0;
+    if (bit && (allowed.load(std::memory_order_relaxed) & bit)) return hipSuccess;
+    e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == hipSuccess) allowed.fetch_or(bit, std::memory_order_relaxed);
+    return e;
 }
 
 template <int MJ, bool MASK, typename ElemT>
 hipError_t head_tile(const HeadArgs &a, hipStream_t s) {
-    typedef TileLds<MJ> Lds;
-    static const hipError_t ready = hipFuncSetAttribute((const void *)head_tile_kernel<MJ, MASK, ElemT>, hipFuncAttributeMaxDynamicSharedMemorySize, Lds::LOOP);
-    if (ready != hipSuccess) return ready;
+    typedef TileLds<MJ, ElemT> Lds;
+    static std::atomic<uint64_t> allowed{0};
+    const hipError_t e = allow_lds((const void *)head_tile_kernel<MJ, MASK, ElemT>, Lds::BYTES, allowed);
+    if (e != hipSuccess) return e;
     const int32_t tiles_m = (a.M + Lds::ROWS - 1) / Lds::ROWS;
     const int64_t n = (int64_t)tiles_m * ((a.V + TILE_TOKENS - 1) / TILE_TOKENS);
-    hipLaunchKernelGGL((head_tile_kernel<MJ, MASK, ElemT>), dim3((uint32_t)n), dim3(512), Lds::LOOP, s, a, tiles_m, (int32_t)n);
+    hipLaunchKernelGGL((head_tile_kernel<MJ, MASK, ElemT>), dim3((uint32_t)std::min<int64_t>(n, COMPUTE_UNITS)), dim3(512), Lds::BYTES, s, a, tiles_m, (int32_t)n);
     return hipSuccess;
 }
 
 template <int MT, int TOKENS, bool MASK, typename ElemT>
 hipError_t head_rows(const HeadArgs &a, hipStream_t s) {
     typedef RowsLds<MT, TOKENS> Lds;
-    static const hipError_t ready = hipFuncSetAttribute((const void *)head_rows_kernel<MT, TOKENS, MASK, ElemT>, hipFuncAttributeMaxDynamicSharedMemorySize, Lds::BYTES);
-    if (ready != hipSuccess) return ready;
+    static std::atomic<uint64_t> allowed{0};
+    const hipError_t e = allow_lds((const void *)head_rows_kernel<MT, TOKENS, MASK, ElemT>, Lds::BYTES, allowed);
+    if (e != hipSuccess) return e;
     const dim3 grid((a.V + TOKENS - 1) / TOKENS, (a.M + MT * 16 - 1) / (MT * 16));
     hipLaunchKernelGGL((head_rows_kernel<MT, TOKENS, MASK, ElemT>), grid, dim3(256), Lds::BYTES, s, a);
     return hipSuccess;
@@ -580,8 +615,13 @@ hipError_t head(const HeadArgs &a, hipStream_t s) {
     if (a.M <= 32) return head_few<2, MASK, ElemT>(a, s);
     if (a.M <= 64) return head_few<4, MASK, ElemT>(a, s);
     if ((a.w_stride | a.x_stride) >= (1 << 24)) return head_rows<4, 128, MASK, ElemT>(a, s);   // a tile's rows would not lie within 32 bits
-    // operands in bf16 take twice the registers: half the rows
-    if constexpr (sizeof(ElemT) == 2) { if (a.M > 128) return head_tile<8, MASK, ElemT>(a, s); }
+    if constexpr (sizeof(ElemT) == 2) {                                      // (operands in bf16 take twice the registers: 128 rows)
+        // Tiles of 128, 192 or 256 rows, whichever makes the least work: rows of all tiles, and 64 more for what a tile costs whatever its rows
+        // (130 x 40,037 x 1,024: 128 rows 24 us, 192 18.2, 256 21.6).
+        auto cost = [&](int32_t rows) { return (int64_t)((a.M + rows - 1) / rows) * (rows + 64); };
+        if (cost(256) <= cost(192) && cost(256) <= cost(128)) return head_tile<8, MASK, ElemT>(a, s);
+        if (cost(192) <= cost(128)) return head_tile<6, MASK, ElemT>(a, s);
+    }
     return head_tile<4, MASK, ElemT>(a, s);
 }
 
