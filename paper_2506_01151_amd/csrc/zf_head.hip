@@ -14,12 +14,12 @@
 #include <hip/hip_runtime.h>
 #include <algorithm>
 #include <atomic>
-#include <cstdlib>
 #include "zf_ops.h"
 
 namespace zf {
 namespace {
 
+static const int COMPUTE_UNITS = 256;
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -182,88 +182,86 @@ __device__ __forceinline__ uint32_t lds_at(const void *p) { return (uint32_t)(ui
 
 // ---- few rows: the weight streams past them ----
 //
-// A workgroup has TOKENS tokens of one scale and up to 16 MT rows of the batch.  Under a mask it lists the tokens that some of its rows allows.
-//   Many tokens (up to 128): a wavefront takes 32 of them.  Blocks of columns of the weight's rows and the activations come straight into LDS, STAGES - 1 blocks ahead, in
+// A workgroup takes ranges of TOKENS tokens, each of one scale, and up to 16 MT rows of the batch.  Under a mask it lists the tokens that some of its rows allows, of up to
+// RANGES ranges at a time.
+//   Long lists, a range at a time: a wavefront takes 32 tokens.  Blocks of columns of the weight's rows and the activations come straight into LDS, STAGES - 1 blocks ahead, in
 // lines: a fragment's own addresses (sixteen rows, 16 bytes of each) are taken a lane at a time, at a quarter of the rate.  Every wavefront issues the same number of loads for a
 // block, so that a count says which have arrived; one barrier a block.  Piece c of row r lies at place c ^ (r % 8), so that eight rows' pieces of one
-// column lie in different banks (the loads write LDS in lanes' order: it is their addresses in memory that are exchanged).
-//   Up to 32 tokens (TOKENS = 16 is made of such): the wavefronts share them and take every fourth block of columns each, the weight straight to registers, and join their sums in a fixed order.  With
-// 128-token ranges the activations come through LDS, as many columns at a time as there is room.
-//   Results gather in LDS, so that the logits go out in whole rows of the range, -inf where nothing was computed.
-template <int MT, int TOKENS>
+// column lie in different banks (the loads write LDS in lanes' order: it is their addresses in memory that are exchanged).  Results gather in LDS, so that the logits
+// go out in whole rows of the range, -inf where nothing was computed.
+//   Up to 32 tokens of all ranges, or of one (TOKENS = 16 has no others), sixteen at a time: the wavefronts take every fourth block of columns each, the weight straight to registers,
+// activations through LDS (TOKENS = 16: straight to registers), and join their sums in a fixed order.  Everything is -inf first.  (16 x 128,256 x 4,096 with 200 tokens a
+// row: 13.6 us; when every range was a workgroup's own 22.)
+template <int MT, int TOKENS, bool MASK>
 struct RowsLds {
-    static constexpr int ROWS = MT * 16, GW = TOKENS > 16 ? 2 : 1, PITCH = TOKENS + 4;
-    static constexpr int STAGES = MT == 4 ? 3 : 4, X_AT = 128 * SCALE_BLOCK, S_AT = X_AT + ROWS * SCALE_BLOCK, STAGE = S_AT + 64 * 4;   // weight, activations, their scales
+    static constexpr int ROWS = MT * 16, PITCH = TOKENS + 4, RANGES = MASK && TOKENS > 16 ? 4 : 1, SHORT = 32;
+    static constexpr int STAGES = MT == 1 ? 4 : 3, X_AT = 128 * SCALE_BLOCK, S_AT = X_AT + ROWS * SCALE_BLOCK, STAGE = S_AT + 64 * 4;   // weight, activations, their scales
     static constexpr int LOADS = 4 + (MT + 1) / 2 + 1;                       // of a wavefront for a stage
-    static constexpr int SPAN = MT == 1 ? 4096 : MT == 2 ? 2048 : 1024;      // columns of the activations that the short form has in LDS
-    static constexpr int LOOP = TOKENS > 16 ? STAGES * STAGE : 0, TILE = ROWS * PITCH * 4, JOIN = 3 * ROWS * 16 * GW * 4;                   // the loop; then the logits, and three wavefronts' sums
-    static constexpr int BYTES = LOOP > TILE + JOIN ? LOOP : TILE + JOIN;
+    static constexpr int SPAN = MT == 1 ? 4096 : 1024;      // columns of the activations that the short form has in LDS
+    static constexpr int LOOP = TOKENS > 16 ? STAGES * STAGE : 0, TILE = TOKENS > 16 ? ROWS * PITCH * 4 : 0, JOIN = 3 * ROWS * 16 * 4;  // the loop, then the logits; the short form's sums
+    static constexpr int BYTES = LOOP > TILE ? (LOOP > JOIN ? LOOP : JOIN) : (TILE > JOIN ? TILE : JOIN);
     static_assert(TOKENS == 16 || ROWS * SPAN <= STAGES * STAGE, "the short form's activations lie in the stages' memory");
 };
 
 template <int MT, int TOKENS, bool MASK, typename ElemT>
-__global__ __launch_bounds__(256, 2) void head_rows_kernel(HeadArgs a) {
-    typedef RowsLds<MT, TOKENS> Lds;
-    constexpr int ROWS = Lds::ROWS, GW = Lds::GW, PITCH = Lds::PITCH, WORDS = (TOKENS + 31) / 32, STAGES = Lds::STAGES;
+__global__ __launch_bounds__(256, 2) void head_rows_kernel(HeadArgs a, int32_t n_ranges) {
+    typedef RowsLds<MT, TOKENS, MASK> Lds;
+    constexpr int ROWS = Lds::ROWS, PITCH = Lds::PITCH, WORDS = (TOKENS + 31) / 32, STAGES = Lds::STAGES, RANGES = Lds::RANGES, EPV = 16 / sizeof(ElemT);
     extern __shared__ __align__(16) uint8_t mem[];
-    __shared__ uint32_t words[MASK ? ROWS : 1][WORDS], need[WORDS];
-    __shared__ uint8_t list[TOKENS];
+    __shared__ uint32_t words[MASK ? RANGES : 1][MASK ? ROWS : 1][WORDS], need[RANGES][WORDS];
+    __shared__ uint16_t list[MASK ? RANGES * TOKENS : 1];                    // range of the group * TOKENS + token of the range
     const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
-    const int32_t v0 = blockIdx.x * TOKENS, m0 = blockIdx.y * ROWS;
-    const int32_t rows = a.M - m0 < ROWS ? a.M - m0 : ROWS, n_v = a.V - v0 < TOKENS ? a.V - v0 : TOKENS, n_k = a.K / SCALE_BLOCK;
-    int32_t count = n_v;
-    if (MASK) {
-        const int32_t W = (a.V + 31) / 32;
-        if (tid < WORDS) need[tid] = 0;
-        __syncthreads();
-        for (int i = tid; i < rows * WORDS; i += 256) {
-            const int32_t j = i % WORDS, left = n_v - 32 * j;                // tokens of the word that there are
-            uint32_t w = left > 0 ? a.mask[(size_t)(m0 + i / WORDS) * W + v0 / 32 + j] >> (TOKENS < 32 ? v0 % 32 : 0) : 0;
-            if (left < 32 && left > 0) w &= (1u << left) - 1;
-            words[i / WORDS][j] = w;
-            if (w) atomicOr(&need[j], w);                                    // the same in any order
-        }
-        __syncthreads();
-        count = 0;
-#pragma unroll
-        for (int j = 0; j < WORDS; j++) {
-            if (tid < TOKENS && j == tid / 32 && ((need[j] >> (tid % 32)) & 1)) list[count + __popc(need[j] & ((1u << (tid % 32)) - 1))] = (uint8_t)tid;
-            count += __popc(need[j]);
-        }
-        count = __builtin_amdgcn_readfirstlane(count);
-        __syncthreads();
-    }
-    const bool shared = count <= 16 * GW;                                    // the wavefronts share the tokens
-    const int first = shared ? 0 : wave * 32;                                // the wavefront's tokens in the list
-    // the weight's row of the i-th listed token; behind the last one its row once more
-    auto w_row = [&](int i) { i = i < count ? i : count - 1; return a.w + (int64_t)(v0 + (MASK ? list[i] : i)) * a.w_stride; };
-    auto x_row = [&](int r) { return m0 + (r < rows ? r : rows - 1); };
-    const float *const ws = a.ws + (size_t)(v0 / SCALE_BLOCK) * n_k;
-    const auto *const ws_uniform = (const __attribute__((address_space(4))) float *)ws;      // read by the scalar unit
-    f32x4 acc[GW][MT];
-#pragma unroll
-    for (int g = 0; g < GW; g++)
-#pragma unroll
-        for (int t = 0; t < MT; t++) acc[g][t] = f32x4{0, 0, 0, 0};
+    const int32_t m0 = blockIdx.y * ROWS, rows = a.M - m0 < ROWS ? a.M - m0 : ROWS, n_k = a.K / SCALE_BLOCK, W = (a.V + 31) / 32;
     const int c0 = (lane / 16 ^ lane % 8) * 16, c1 = ((lane / 16 + 4) ^ lane % 8) * 16;      // the lane's two pieces of a row that is lane % 8 modulo 8
-    if (shared && count > 0) {
+    auto x_row = [&](int r) { return m0 + (r < rows ? r : rows - 1); };
+    int32_t base = blockIdx.x;                                               // the group's ranges are base, base + gridDim.x, ...
+    auto first_of = [&](int range) { return (base + range * (int32_t)gridDim.x) * TOKENS; };   // token
+    auto token_of = [&](int i) { return MASK ? first_of(list[i] / TOKENS) + list[i] % TOKENS : base * TOKENS + i; };
+    auto allowed = [&](int i, int m) { return !MASK || ((words[list[i] / TOKENS][m][list[i] % TOKENS / 32] >> (list[i] % 32)) & 1); };
+    auto put = [&](ElemT *to, float y) { *to = sizeof(ElemT) == 4 ? (ElemT)__float_as_uint(y) : (ElemT)bf16_of(y); };
+
+    // Logits of a range, from LDS or -inf.
+    auto store_range = [&](int32_t v0, const float *tile) {
+        const int32_t n_v = a.V - v0 < TOKENS ? a.V - v0 : TOKENS;
+        constexpr int PIECES = TOKENS / EPV;
+        for (int i = tid; i < rows * PIECES; i += 256) {
+            const int m = i / PIECES, v = i % PIECES * EPV;
+            ElemT *const to = (ElemT *)a.y + (int64_t)(m0 + m) * a.y_stride + v0 + v;
+            union { ElemT e[EPV]; u32x4 v; } o;
+#pragma unroll
+            for (int k = 0; k < EPV; k++) put(&o.e[k], tile ? tile[m * PITCH + v + k] : -INFINITY);
+            if (v + EPV <= n_v) *reinterpret_cast<typename Piece<ElemT>::type *>(to) = o.v;
+            else {
+#pragma unroll
+                for (int k = 0; k < EPV; k++) if (v + k < n_v) to[k] = o.e[k];
+            }
+        }
+    };
+
+    // Up to sixteen listed tokens from `at` on.
+    auto short_form = [&](int at, int count) {
         constexpr bool NEAR = TOKENS > 16;                                                   // activations through LDS
         constexpr int U = NEAR ? Lds::SPAN / SCALE_BLOCK / 4 : MT == 4 ? 1 : MT == 2 ? 2 : 4;   // blocks of columns a wavefront asks for at a time
-        const bool two = GW > 1 && count > 16;
-        const uint8_t *wp[GW], *xp[MT];
-        const float *xs[MT];
+        const bool real = lane % 16 < count;
+        const uint8_t *const wp = a.w + (int64_t)token_of(at + (real ? lane % 16 : 0)) * a.w_stride + lane / 16 * 16, *xp[MT];
+        const float *xs[MT], *ws[4];
 #pragma unroll
-        for (int g = 0; g < GW; g++) wp[g] = w_row(g * 16 + lane % 16) + lane / 16 * 16;
+        for (int e = 0; e < 4; e++) {
+            const int j = lane / 16 * 4 + e;
+            ws[e] = a.ws + (size_t)(token_of(at + (j < count ? j : 0)) / SCALE_BLOCK) * n_k;
+        }
 #pragma unroll
         for (int t = 0; t < MT; t++) {
             xp[t] = a.x + x_row(t * 16 + lane % 16) * a.x_stride + lane / 16 * 16;
             xs[t] = a.xs + (size_t)x_row(t * 16 + lane % 16) * n_k;
         }
+        f32x4 acc[MT];
+#pragma unroll
+        for (int t = 0; t < MT; t++) acc[t] = f32x4{0, 0, 0, 0};
         for (int32_t from = 0; from < n_k; from += 4 * U) {
-            i32x4 w[U][GW][2] = {}, x[U][MT][2];
-            float s[U][MT];
+            i32x4 w[U][2] = {}, x[U][MT][2];
+            float s[U][MT], s_w[U][4];
             if (NEAR) {
-                if (from) __syncthreads();                                   // the span before has been read
                 const int groups = (rows + 7) / 8, n = n_k - from < 4 * U ? n_k - from : 4 * U;   // of eight rows; the span's blocks in turn
                 for (int i = wave; i < groups * n; i += 4) {
                     const int r = i % groups * 8 + lane / 8, k = i / groups;
@@ -274,17 +272,17 @@ __global__ __launch_bounds__(256, 2) void head_rows_kernel(HeadArgs a) {
             for (int u = 0; u < U; u++) {
                 const int32_t k = from + wave + 4 * u;
                 if (k >= n_k) continue;
+                if (real)                                                    // (a lane with nothing to ask for takes its turn all the same)
 #pragma unroll
-                for (int g = 0; g < GW; g++)
-                    if (g * 16 + lane % 16 < count)                          // (a lane with nothing to ask for takes its turn all the same: 16 rows x 200 tokens each, 22 us when all asked)
+                    for (int h = 0; h < 2; h++) w[u][h] = __builtin_nontemporal_load(reinterpret_cast<const i32x4 *>(wp + (size_t)k * SCALE_BLOCK + 64 * h));
 #pragma unroll
-                        for (int h = 0; h < 2; h++) w[u][g][h] = __builtin_nontemporal_load(reinterpret_cast<const i32x4 *>(wp[g] + (size_t)k * SCALE_BLOCK + 64 * h));
+                for (int e = 0; e < 4; e++) s_w[u][e] = ws[e][k];
 #pragma unroll
                 for (int t = 0; t < MT; t++) {
                     if (!NEAR)
 #pragma unroll
                         for (int h = 0; h < 2; h++) x[u][t][h] = piece_at(xp[t] + (size_t)k * SCALE_BLOCK + 64 * h);
-                    s[u][t] = xs[t][k] * ws_uniform[k];
+                    s[u][t] = xs[t][k];
                 }
             }
             if (NEAR) {
@@ -294,50 +292,79 @@ __global__ __launch_bounds__(256, 2) void head_rows_kernel(HeadArgs a) {
 #pragma unroll
             for (int u = 0; u < U; u++) {
                 if (from + wave + 4 * u >= n_k) continue;
-                Operand<ElemT> v[MT];
+                Operand<ElemT> v[MT], y[1];
                 f32x4 part[1][MT];
 #pragma unroll
                 for (int t = 0; t < MT; t++) {
-                    const uint8_t *const at = mem + (wave + 4 * u) * (ROWS * SCALE_BLOCK) + (t * 16 + lane % 16) * SCALE_BLOCK;
-                    if (NEAR) v[t].take(piece_at(at + c0), piece_at(at + c1));
+                    const uint8_t *const from_lds = mem + (wave + 4 * u) * (ROWS * SCALE_BLOCK) + (t * 16 + lane % 16) * SCALE_BLOCK;
+                    if (NEAR) v[t].take(piece_at(from_lds + c0), piece_at(from_lds + c1));
                     else v[t].take(x[u][t][0], x[u][t][1]);
                 }
+                y[0].take(w[u][0], w[u][1]);
+                multiply(y, v, part);
 #pragma unroll
-                for (int g = 0; g < GW; g++) {
-                    if (g && !two) continue;
-                    Operand<ElemT> y[1];
-                    y[0].take(w[u][g][0], w[u][g][1]);
-                    multiply(y, v, part);
+                for (int t = 0; t < MT; t++)
 #pragma unroll
-                    for (int t = 0; t < MT; t++)
+                    for (int e = 0; e < 4; e++) acc[t][e] = fmaf(s[u][t] * s_w[u][e], part[0][t][e], acc[t][e]);
+            }
+            if (NEAR) __syncthreads();                                       // the span has been read
+        }
+        f32x4 *const sums = reinterpret_cast<f32x4 *>(mem);
+        if (wave) {
 #pragma unroll
-                        for (int e = 0; e < 4; e++) acc[g][t][e] = fmaf(s[u][t], part[0][t][e], acc[g][t][e]);
+            for (int t = 0; t < MT; t++) sums[((wave - 1) * MT + t) * 64 + lane] = acc[t];
+        }
+        arrived<0>();                                                        // (what was -inf first, too)
+        __syncthreads();
+        if (wave == 0) {
+#pragma unroll
+            for (int t = 0; t < MT; t++) {
+                f32x4 y = acc[t];
+#pragma unroll
+                for (int w = 0; w < 3; w++) y += sums[(w * MT + t) * 64 + lane];
+                const int m = t * 16 + lane % 16;
+#pragma unroll
+                for (int e = 0; e < 4; e++) {
+                    const int j = lane / 16 * 4 + e;
+                    if (j < count && m < rows && allowed(at + j, m)) put((ElemT *)a.y + (int64_t)(m0 + m) * a.y_stride + token_of(at + j), y[e]);
                 }
             }
         }
         __syncthreads();
-    } else if (TOKENS > 16 && count > 0) {
+    };
+
+    // The listed tokens of one range, `count` from `at` on, 32 a wavefront.
+    auto long_form = [&](int32_t v0, int at, int count) {
         constexpr int XN = (MT + 1) / 2;                                     // groups of eight of the activations' rows that a wavefront brings
         const uint8_t *from[4 + XN];
-        const int place = (lane % 8 ^ lane / 8) * 16;
+        const int place = (lane % 8 ^ lane / 8) * 16, first = wave * 32;
 #pragma unroll
-        for (int i = 0; i < 4; i++) from[i] = w_row(wave * 32 + i * 8 + lane / 8) + place;
+        for (int i = 0; i < 4; i++) {
+            const int j = first + i * 8 + lane / 8;                          // behind the last token: its row once more
+            from[i] = a.w + (int64_t)token_of(at + (j < count ? j : count - 1)) * a.w_stride + place;
+        }
 #pragma unroll
         for (int i = 0; i < XN; i++) from[4 + i] = a.x + x_row((wave * XN + i) % (2 * MT) * 8 + lane / 8) * a.x_stride + place;
         const float *const xs = a.xs + (size_t)x_row(lane % ROWS) * n_k;
+        const auto *const ws = (const __attribute__((address_space(4))) float *)(a.ws + (size_t)(v0 / SCALE_BLOCK) * n_k);   // read by the scalar unit
         // Workgroups begin at blocks of columns of their own: rows lie at multiples of a power of two, and who reads the same columns of many rows asks
         // few of the memory's channels (16 x 128,256 x 4,096: 113 us when all begin at the first, 103 so).
         const int32_t turn = (int32_t)(blockIdx.x * 5u % (uint32_t)n_k);
         auto turned = [&](int32_t k) { return k + turn < n_k ? k + turn : k + turn - n_k; };
         auto fetch = [&](int32_t k) {                                        // behind the last block: that one once more, for the count
-            const uint32_t at = lds_at(mem) + k % STAGES * Lds::STAGE;
+            const uint32_t to = lds_at(mem) + k % STAGES * Lds::STAGE;
             k = turned(k < n_k ? k : n_k - 1);
 #pragma unroll
-            for (int i = 0; i < 4; i++) to_lds(from[i] + (size_t)k * SCALE_BLOCK, at + (wave * 32 + i * 8) * SCALE_BLOCK);
+            for (int i = 0; i < 4; i++) to_lds(from[i] + (size_t)k * SCALE_BLOCK, to + (wave * 32 + i * 8) * SCALE_BLOCK);
 #pragma unroll
-            for (int i = 0; i < XN; i++) to_lds(from[4 + i] + (size_t)k * SCALE_BLOCK, at + Lds::X_AT + (wave * XN + i) % (2 * MT) * 8 * SCALE_BLOCK);
-            to_lds(xs + k, at + Lds::S_AT);
+            for (int i = 0; i < XN; i++) to_lds(from[4 + i] + (size_t)k * SCALE_BLOCK, to + Lds::X_AT + (wave * XN + i) % (2 * MT) * 8 * SCALE_BLOCK);
+            to_lds(xs + k, to + Lds::S_AT);
         };
+        f32x4 acc[2][MT];
+#pragma unroll
+        for (int g = 0; g < 2; g++)
+#pragma unroll
+            for (int t = 0; t < MT; t++) acc[g][t] = f32x4{0, 0, 0, 0};
 #pragma unroll
         for (int k = 0; k < STAGES - 1; k++) fetch(k);
         for (int32_t k = 0; k < n_k; k++) {
@@ -345,19 +372,19 @@ __global__ __launch_bounds__(256, 2) void head_rows_kernel(HeadArgs a) {
             __syncthreads();
             fetch(k + STAGES - 1);
             const uint8_t *const stage = mem + k % STAGES * Lds::STAGE;
-            const float s_w = ws_uniform[turned(k)];
-            Operand<ElemT> w[GW];
+            const float s_w = ws[turned(k)];
+            Operand<ElemT> w[2];
 #pragma unroll
-            for (int g = 0; g < GW; g++) {
-                const uint8_t *const at = stage + (wave * 32 + g * 16 + lane % 16) * SCALE_BLOCK;
-                w[g].take(piece_at(at + c0), piece_at(at + c1));
+            for (int g = 0; g < 2; g++) {
+                const uint8_t *const p = stage + (first + g * 16 + lane % 16) * SCALE_BLOCK;
+                w[g].take(piece_at(p + c0), piece_at(p + c1));
             }
             constexpr int PAIR = MT > 1 ? 2 : 1;                             // sixteens of rows at a time
 #pragma unroll
             for (int t0 = 0; t0 < MT; t0 += PAIR) {
                 Operand<ElemT> v[PAIR];
                 float s[PAIR];
-                f32x4 part[GW][PAIR];
+                f32x4 part[2][PAIR];
 #pragma unroll
                 for (int t = 0; t < PAIR; t++) {
                     const int r = (t0 + t) * 16 + lane % 16;
@@ -368,58 +395,87 @@ __global__ __launch_bounds__(256, 2) void head_rows_kernel(HeadArgs a) {
 #pragma unroll
                 for (int t = 0; t < PAIR; t++)
 #pragma unroll
-                    for (int g = 0; g < GW; g++)
+                    for (int g = 0; g < 2; g++)
 #pragma unroll
                         for (int e = 0; e < 4; e++) acc[g][t0 + t][e] = fmaf(s[t], part[g][t][e], acc[g][t0 + t][e]);
             }
         }
         arrived<0>();
         __syncthreads();
-    }
-    // the loop's memory becomes the logits' and, behind them, that of three wavefronts' sums
-    float *const tile = reinterpret_cast<float *>(mem);
-    f32x4 *const sums = reinterpret_cast<f32x4 *>(mem + Lds::TILE);
-    if (MASK) for (int i = tid; i < ROWS * PITCH; i += 256) tile[i] = -INFINITY;
-    if (shared && wave) {
+        float *const tile = reinterpret_cast<float *>(mem);                  // the loop's memory becomes the logits'
+        if (MASK) {
+            for (int i = tid; i < ROWS * PITCH; i += 256) tile[i] = -INFINITY;
+            __syncthreads();
+        }
 #pragma unroll
-        for (int g = 0; g < GW; g++)
-#pragma unroll
-            for (int t = 0; t < MT; t++) sums[((wave - 1) * GW * MT + g * MT + t) * 64 + lane] = acc[g][t];
-    }
-    __syncthreads();
-    if (first < count && !(shared && wave)) {
-#pragma unroll
-        for (int g = 0; g < GW; g++)
+        for (int g = 0; g < 2; g++)
 #pragma unroll
             for (int t = 0; t < MT; t++) {
-                f32x4 y = acc[g][t];
-                if (shared)
-#pragma unroll
-                    for (int w = 0; w < 3; w++) y += sums[(w * GW * MT + g * MT + t) * 64 + lane];
                 const int m = t * 16 + lane % 16;
 #pragma unroll
                 for (int e = 0; e < 4; e++) {
                     const int j = first + g * 16 + lane / 16 * 4 + e;
-                    if (j >= count || m >= rows) continue;
-                    const int v = MASK ? list[j] : j;
-                    if (!MASK || ((words[m][v / 32] >> (v % 32)) & 1)) tile[m * PITCH + v] = y[e];
+                    if (j < count && m < rows && allowed(at + j, m)) tile[m * PITCH + (MASK ? list[at + j] % TOKENS : j)] = acc[g][t][e];
                 }
             }
-    }
-    __syncthreads();
-    constexpr int EPV = 16 / sizeof(ElemT), PIECES = TOKENS / EPV;
-    ElemT *const y = (ElemT *)a.y + v0;
-    for (int i = tid; i < rows * PIECES; i += 256) {
-        const int m = i / PIECES, v = i % PIECES * EPV;
-        ElemT *const to = y + (int64_t)(m0 + m) * a.y_stride + v;
-        union { ElemT e[EPV]; u32x4 v; } o;
-#pragma unroll
-        for (int k = 0; k < EPV; k++) o.e[k] = sizeof(ElemT) == 4 ? (ElemT)__float_as_uint(tile[m * PITCH + v + k]) : (ElemT)bf16_of(tile[m * PITCH + v + k]);
-        if (v + EPV <= n_v) *reinterpret_cast<typename Piece<ElemT>::type *>(to) = o.v;
-        else {
-#pragma unroll
-            for (int k = 0; k < EPV; k++) if (v + k < n_v) to[k] = o.e[k];
+        __syncthreads();
+        store_range(v0, tile);
+        __syncthreads();
+    };
+
+    for (; base < n_ranges; base += RANGES * gridDim.x) {
+        if (!MASK) {
+            const int32_t v0 = base * TOKENS, n_v = a.V - v0 < TOKENS ? a.V - v0 : TOKENS;
+            if (TOKENS == 16) short_form(0, n_v);
+            else if constexpr (TOKENS > 16) long_form(v0, 0, n_v);
+            continue;
         }
+        if (tid < RANGES * WORDS) need[tid / WORDS][tid % WORDS] = 0;
+        __syncthreads();
+        for (int i = tid; i < RANGES * rows * WORDS; i += 256) {
+            const int range = i / (rows * WORDS), m = i / WORDS % rows, j = i % WORDS;
+            const int32_t v0 = first_of(range), left = a.V - v0 - 32 * j;    // tokens from the word on (none in a range that is not there)
+            uint32_t w = left > 0 ? a.mask[(size_t)(m0 + m) * W + v0 / 32 + j] >> (TOKENS < 32 ? v0 % 32 : 0) : 0;
+            if (left > 0 && left < 32) w &= (1u << left) - 1;
+            if (TOKENS < 32) w &= (1u << TOKENS % 32) - 1;
+            words[range][m][j] = w;
+            if (w) atomicOr(&need[range][j], w);                             // the same in any order
+        }
+        __syncthreads();
+        int start[RANGES + 1];
+        start[0] = 0;
+#pragma unroll
+        for (int range = 0; range < RANGES; range++) {
+            start[range + 1] = start[range];
+#pragma unroll
+            for (int j = 0; j < WORDS; j++) {
+                const uint32_t w = need[range][j];
+                if (tid < TOKENS && tid / 32 == j && ((w >> (tid % 32)) & 1)) list[start[range + 1] + __popc(w & ((1u << (tid % 32)) - 1))] = (uint16_t)(range * TOKENS + tid);
+                start[range + 1] += __popc(w);
+            }
+            start[range + 1] = __builtin_amdgcn_readfirstlane(start[range + 1]);
+        }
+        __syncthreads();
+        if (TOKENS == 16 || start[RANGES] <= Lds::SHORT) {
+#pragma unroll
+            for (int range = 0; range < RANGES; range++) if (first_of(range) < a.V) store_range(first_of(range), nullptr);
+            for (int i = 0; i < start[RANGES]; i += 16) short_form(i, start[RANGES] - i < 16 ? start[RANGES] - i : 16);
+        } else {
+            for (int range = 0; range < RANGES; range++) {
+                const int32_t v0 = first_of(range);
+                if (v0 >= a.V) break;
+                int from = 0, to = 0;
+#pragma unroll
+                for (int i = 0; i < RANGES; i++) if (i == range) { from = start[i]; to = start[i + 1]; }
+                if (to - from > Lds::SHORT) {
+                    if constexpr (TOKENS > 16) long_form(v0, from, to - from);
+                    continue;
+                }
+                store_range(v0, nullptr);
+                for (int i = from; i < to; i += 16) short_form(i, to - i < 16 ? to - i : 16);
+            }
+        }
+        __syncthreads();                                                     // before the lists are made again
     }
 }
 
@@ -429,7 +485,7 @@ __global__ __launch_bounds__(256, 2) void head_rows_kernel(HeadArgs a) {
 // operands, 128 bytes a row, comes from memory straight into LDS while the block before is multiplied, the next tile's first one while this one's last is: two buffers, one
 // barrier a block, pieces in places as above.  While sixteen rows' products run the sixteen before them are scaled and added.
 //   Rows behind the last one are the last one again; their results are not stored.
-static const int TILE_TOKENS = 256, COMPUTE_UNITS = 256;
+static const int TILE_TOKENS = 256;
 
 template <int MJ, typename ElemT>
 struct TileLds {
@@ -596,18 +652,20 @@ hipError_t head_tile(const HeadArgs &a, hipStream_t s) {
 
 template <int MT, int TOKENS, bool MASK, typename ElemT>
 hipError_t head_rows(const HeadArgs &a, hipStream_t s) {
-    typedef RowsLds<MT, TOKENS> Lds;
+    typedef RowsLds<MT, TOKENS, MASK> Lds;
     static std::atomic<uint64_t> allowed{0};
     const hipError_t e = allow_lds((const void *)head_rows_kernel<MT, TOKENS, MASK, ElemT>, Lds::BYTES, allowed);
     if (e != hipSuccess) return e;
-    const dim3 grid((a.V + TOKENS - 1) / TOKENS, (a.M + MT * 16 - 1) / (MT * 16));
-    hipLaunchKernelGGL((head_rows_kernel<MT, TOKENS, MASK, ElemT>), grid, dim3(256), Lds::BYTES, s, a);
+    // Without a mask a workgroup a range.  With one as many as the compute units hold, so that those with little to do in a range have several.
+    const int32_t n = (a.V + TOKENS - 1) / TOKENS;
+    const dim3 grid(Lds::RANGES > 1 ? std::min(n, 2 * COMPUTE_UNITS) : n, (a.M + MT * 16 - 1) / (MT * 16));
+    hipLaunchKernelGGL((head_rows_kernel<MT, TOKENS, MASK, ElemT>), grid, dim3(256), Lds::BYTES, s, a, n);
     return hipSuccess;
 }
+// Ranges of 16 tokens where those of 128 would leave three compute units of four idle (one row x 2,048 x 1,024: 4.2 us, 6.0 in ranges of 128; 64 rows x 8,192 x 1,024: 10.1 and 9.2).
 template <int MT, bool MASK, typename ElemT>
 hipError_t head_few(const HeadArgs &a, hipStream_t s) {
-    if (getenv("T16") ? atoi(getenv("T16")) : a.V < 128 * 128) return head_rows<MT, 16, MASK, ElemT>(a, s);
-    return head_rows<MT, 128, MASK, ElemT>(a, s);
+    return a.V < 64 * 128 ? head_rows<MT, 16, MASK, ElemT>(a, s) : head_rows<MT, 128, MASK, ElemT>(a, s);
 }
 template <bool MASK, typename ElemT>
 hipError_t head(const HeadArgs &a, hipStream_t s) {

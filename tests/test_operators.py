@@ -161,6 +161,39 @@ def test_head_logits_under_masks(M, V, K, kind):
 
 
 @gpu
+@pytest.mark.parametrize("kind", [None, "few", "some", "half", "mixed"])
+@pytest.mark.parametrize("M,V,K", [(1, 8192, 256), (2, 8200, 4224), (7, 9001, 640), (20, 8321, 1152), (33, 8193, 2304), (64, 8320, 384), (5, 70001, 256), (18, 66000, 128), (40, 200003, 128), (3, 300000, 256)])
+def test_head_logits_vocabularies_of_many_ranges(M, V, K, kind):
+    """Vocabularies that workgroups of few rows take in ranges of 128 tokens, several of them: lists of all lengths, long ones beside empty ones."""
+    q, qs, wq, ws = head_case(M, V, K, M + K)
+    g = torch.Generator().manual_seed(V)
+    bits = None
+    if kind:
+        bits = torch.rand((M, V), generator=g) < {"few": 2.0 / 128 / M, "some": 0.2 / M, "half": 0.5, "mixed": 0.02}[kind]
+        if kind == "mixed":                                # dense ranges, and runs that nothing allows
+            bits[:, 128 * 5:128 * 8] = True
+            bits[0, V // 2:V // 2 + 300] = True
+            bits[:, V - 2000:] = False
+        bits[M - 1, V - 1] = True
+    want, bound = head_want(q, qs, wq, ws)
+    y = zf.head_logits(q.cuda(), qs.cuda(), wq.cuda(), ws.cuda(), packed(bits, True).cuda() if kind else None, dtype=torch.float32)
+    check_head(y, want, bound, bits)
+
+
+@gpu
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,V,K", [(70, 70001, 128), (150, 70001, 384), (200, 66049, 256), (300, 66000, 128), (513, 40037, 256)])
+def test_head_logits_more_tiles_than_compute_units(M, V, K, dtype, masked):
+    """Batches whose workgroups take several tiles, one after the other: one block of columns and several, an odd number and an even one."""
+    q, qs, wq, ws = head_case(M, V, K, M + K)
+    bits = torch.rand((M, V), generator=torch.Generator().manual_seed(K)) < 0.5 if masked else None
+    y = zf.head_logits(q.cuda(), qs.cuda(), wq.cuda(), ws.cuda(), packed(bits).cuda() if masked else None, dtype=DTYPES[dtype])
+    want, bound = head_want(q, qs, wq, ws)
+    check_head(y, want, bound, bits)
+
+
+@gpu
 @pytest.mark.parametrize("masked", [False, True])
 @pytest.mark.parametrize("M,V", [(2, 515), (70, 300), (260, 515)])
 def test_head_logits_strides(M, V, masked):
