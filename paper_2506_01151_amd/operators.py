@@ -6,7 +6,8 @@
     got.logprobs.sum().backward()                                 # the logits' gradient under the same mask
 
 Masks are those of compute_mask.  Every call is enqueued on torch's current stream of the tensors' device, waits for nothing and
-allocates through torch only, so it can be captured into a graph.  Arguments that do not fit raise ZfError (ZF_ERR_INVALID_ARG).
+allocates through torch only, so it can be captured into a graph (a backward pass as any of torch's: from leaves made for the
+capture, no eager graph of theirs alive).  Arguments that do not fit raise ZfError (ZF_ERR_INVALID_ARG).
 """
 import ctypes
 from typing import NamedTuple, Optional

@@ -33,8 +33,14 @@ def packed(bits, padding=False):
 
 
 def rows_of(x, layout):
-    """x on the GPU: its rows one behind the other; at the next multiple of 64 elements; or from an odd element on, at odd distances, among other numbers."""
+    """x on the GPU: its rows one behind the other; at the next multiple of 64 elements; from an odd element on, at odd distances, among other numbers; or 2^30
+    elements (and a few) apart, so that the third begins beyond what 31 bits count."""
     rows, V = x.shape
+    if layout == "far":
+        pitch = 2 ** 30 + 24
+        y = torch.empty(((rows - 1) * pitch + V,), dtype=x.dtype, device="cuda").as_strided((rows, V), (pitch, 1))
+        y.copy_(x.cuda())
+        return y
     if layout == "packed":
         return x.cuda()
     if layout == "padded":
@@ -214,6 +220,29 @@ def test_head_logits_strides(M, V, masked):
         check_head(out, want, bound, bits)
         assert buf[0] == 7.0 and (buf[1:].view(M, V + 2)[:, V:] == 7.0).all()
     assert zf.head_logits(q_on[:0], qs.cuda()[:0], w_on, ws.cuda()).shape == (0, V)
+
+
+@gpu
+@pytest.mark.parametrize("M", [3, 70])
+def test_head_logits_weight_of_more_than_two_gibibytes(M):
+    """The last rows of the weight lie beyond 2^31 bytes, the last rows of the result beyond 2^31 elements."""
+    V, K = 300001, 7424
+    q, qs, wq, ws = head_case(M, 384, K, M)                # (its scales are the last three blocks of the weight's, whose last one is not full)
+    first = V - 1 - (V - 1) % 128 - 256
+    weight = torch.zeros((V, K), dtype=torch.float8_e4m3fn, device="cuda")
+    weight[first:] = wq[:V - first].cuda()
+    scales = torch.full((-(-V // 128), K // 128), math.nan, device="cuda")
+    scales[-3:] = ws.cuda()
+    bits = torch.zeros((M, V), dtype=torch.bool)
+    bits[:, first:] = True
+    out = None
+    if M == 3:
+        out = torch.empty(((M - 1) * (2 ** 30 + 24) + V,), dtype=torch.bfloat16, device="cuda").as_strided((M, V), (2 ** 30 + 24, 1))
+    want, bound = head_want(q, qs, wq, ws)
+    y = zf.head_logits(q.cuda(), qs.cuda(), weight, scales, packed(bits).cuda(), out=out)
+    assert (y[:, :first] == -INF).all()
+    n = V - first
+    check_head(y[:, first:], want[:, :n], bound[:, :n])
 
 
 # ---- log probabilities -------------------------------------------------------------------------------
@@ -428,6 +457,63 @@ def test_alternatives_with_many_equal_logits(dtype, top):
 
 
 @gpu
+@pytest.mark.parametrize("top", [1, 5, 64])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [8193, 20000, 32768])
+def test_alternatives_of_equal_logits_in_rows_of_one_workgroup(V, dtype, top):
+    """Rows that are all one value, two values, the smaller first, or rise: more candidates than a list holds."""
+    x = torch.zeros((5, V))
+    x[1, V // 2:] = 1.0
+    x[2] = torch.arange(V).float() / 256
+    x[3] = -torch.arange(V).float()
+    x[4, -1] = -0.0
+    bits = torch.ones((5, V), dtype=torch.bool)
+    bits[4, :-3] = False
+    x = x.to(DTYPES[dtype])
+    got = zf.token_logprobs(x.cuda(), mask=packed(bits).cuda(), top=top)
+    assert torch.equal(got.top_ids.cpu().long(), top_of(x.double().masked_fill(~bits, -INF) + 0.0, top))
+
+
+@gpu
+@pytest.mark.parametrize("V,top", [(40037, 20), (9001, 3), (511, 0)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_token_logprobs_rows_far_apart(V, top, dtype):
+    g = torch.Generator().manual_seed(V + 1)
+    x = torch.randn((4, V), generator=g).to(DTYPES[dtype])
+    bits = torch.rand((4, V), generator=g) < 0.5
+    check_logprobs(x, some_tokens(4, V, 5, bits, g, torch.int64), bits, 0.9, top, layout="far")
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_quantize_rows_far_apart(dtype):
+    x = torch.randn((4, 300), generator=torch.Generator().manual_seed(9)).to(DTYPES[dtype])
+    for block_rows in (1, 128):
+        q, scale = zf.quantize_blocks(rows_of(x, "far"), block_rows=block_rows)
+        want_q, want_scale = quantized(x, block_rows)
+        assert torch.equal(q.cpu().float(), want_q.float()) and torch.equal(scale.cpu(), want_scale)
+
+
+@gpu
+def test_calls_with_nothing_to_do():
+    """No rows, no given tokens in a row, neither tokens nor anything else."""
+    x = torch.randn((3, 50)).cuda()
+    for grad in (False, True):
+        on = x.clone().requires_grad_(grad)
+        got = zf.token_logprobs(on, torch.empty((3, 0), dtype=torch.int64, device="cuda"), entropy=True)
+        assert got.logprobs.shape == (3, 0) and got.entropy.shape == (3,)
+        if grad:
+            (got.entropy.sum() + got.logprobs.sum()).backward()
+            want = zf.token_logprobs(on.detach(), entropy=True).entropy
+            assert torch.equal(got.entropy.detach(), want) and on.grad.shape == on.shape
+        got = zf.token_logprobs(on[:0], torch.empty(0, dtype=torch.int64, device="cuda"), entropy=True, top=2)
+        assert got.logprobs.shape == got.entropy.shape == (0,) and got.top_ids.shape == got.top_logprobs.shape == (0, 2)
+        assert zf.token_logprobs(on) == (None, None, None, None)
+    q, scale = zf.quantize_blocks(x[:0])
+    assert q.shape == (0, 128) and scale.shape == (0, 1)
+
+
+@gpu
 def test_gradient_against_differences():
     """The forward call's own differences in 32 bits: a step of h = 2^-5 leaves h^2 / 6 times the third derivative (each factor's share of it is below 1, times what the
     gradients add up to), and twice a value's error over 2 h."""
@@ -509,6 +595,57 @@ def test_gradient_may_overwrite_the_logits():
     a.logprobs, a.entropy, a.stats = lp.data_ptr(), H.data_ptr(), stats.data_ptr()
     assert zf.load_library().zf_token_logprobs_backward(ctypes.byref(a), g.data_ptr(), g.data_ptr(), None, x.data_ptr(), V, 0, torch.cuda.current_stream().cuda_stream) == 0
     assert torch.equal(x, want)
+
+
+@gpu
+def test_example_draws_under_the_grammar_and_learns():
+    """examples/decode_and_train.py: what it draws parses, what it reports is what the definitions say of the logits' own product, the gradient is that of its loss."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "decode_and_train.py")
+    spec = importlib.util.spec_from_file_location("decode_and_train", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    from workloads import configs
+    cfg = configs.CONFIGS[1]
+    engine = zf.Engine(cfg.grammar(), cfg.vocab())
+    model = example.Model(engine.V, 256, "cuda:0")
+    steps = example.decode(engine, model, 3, 12)
+    assert len(steps) == 12
+    for r in range(3):
+        state = engine.new_state()
+        for _, mask, tokens, got in steps:
+            bits = np.unpackbits(mask[r].cpu().numpy().view(np.uint8), bitorder="little")[:engine.V]
+            token = int(tokens[r])
+            if token < 0:
+                assert not bits.any() and float(got.logprobs[r]) == 0.0
+                state.reset()
+                continue
+            assert bits[token]
+            state.advance(token)                           # (raises where the grammar does not go on so)
+            assert 0 <= float(got.entropy[r]) <= math.log(bits.sum()) + 1e-3 and float(got.logprobs[r]) <= 0
+            best = [i for i in got.top_ids[r].tolist() if i >= 0]
+            assert len(best) == min(5, int(bits.sum())) and all(bits[i] for i in best)
+    served = torch.cat([s[3].logprobs for s in steps])
+    advantage = torch.linspace(-1, 1, len(served)).cuda()
+    loss, g_hidden, g_head, learnt = example.train_step(model, steps, advantage)
+    # the loss in 64 bits from the same logits, and its gradient for them by torch
+    hidden = torch.cat([s[0] for s in steps]).to(torch.bfloat16)
+    head = model.head.to(torch.bfloat16)
+    logits = (hidden @ head.t()).cpu().double().requires_grad_()
+    mask, tokens = torch.cat([s[1] for s in steps]).cpu(), torch.cat([s[2] for s in steps]).cpu().long()
+    bits = torch.from_numpy(np.unpackbits(mask.numpy().view(np.uint8), axis=1, bitorder="little")[:, :engine.V].astype(bool))
+    drawn = tokens >= 0
+    z = torch.where(drawn[:, None], logits.masked_fill(~bits, -INF), 0.0) / 0.8
+    lp = torch.log_softmax(z, dim=1)
+    own = torch.where(drawn, lp.gather(1, tokens.clamp(min=0)[:, None])[:, 0], 0.0)
+    entropy = -(lp.exp() * lp.masked_fill(lp == -INF, 0.0)).sum(dim=1) * drawn
+    want = -(advantage.cpu().double() * own + 0.01 * entropy).sum() / drawn.sum()
+    grad, = torch.autograd.grad(want, logits)
+    assert (learnt.cpu().double() - own.detach()).abs().max() < 1e-4 and abs(float(loss) - float(want.detach())) < 1e-4
+    # the logits' gradient is in bf16, and so are its two products with the model: three roundings of half a step relative to the terms
+    for got, by_hand, terms in ((g_hidden, grad @ head.cpu().double(), grad.abs() @ head.cpu().double().abs()), (g_head, grad.t() @ hidden.cpu().double(), grad.abs().t() @ hidden.cpu().double().abs())):
+        assert ((got.cpu().double() - by_hand.detach()).abs() <= 3 * half_step(torch.bfloat16) * terms + 1e-6).all()
 
 
 # ---- refusals ----------------------------------------------------------------------------------------
