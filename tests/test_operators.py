@@ -103,6 +103,27 @@ def test_quantize_zeros_tiny_infinite_and_nan(block_rows):
 
 
 # ---- the head's product ------------------------------------------------------------------------------
+@gpu
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_quantize_next_to_ties(block_rows):
+    """Scales of all sizes, elements within three steps of e4m3's numbers and of the middles between them, zeros of both signs: the bytes themselves."""
+    g = torch.Generator().manual_seed(21)
+    rows, cols = 512, 2048
+    e = torch.randint(-126, 119, (rows // block_rows, 1, cols // 128, 1), generator=g).double()
+    scale = (1 + torch.rand(e.shape, generator=g, dtype=torch.float64)) * 2.0 ** e
+    few = torch.randint(16, 32, (rows // block_rows, block_rows, cols // 128, 128), generator=g) * 2.0 ** torch.randint(-15, 4, (rows // block_rows, block_rows, cols // 128, 128), generator=g)
+    x = (few.double() * scale).float()
+    x = (x.view(torch.int32) + torch.randint(-3, 4, x.shape, generator=g, dtype=torch.int32)).view(torch.float32)
+    x = torch.where(torch.rand(x.shape, generator=g) < 0.5, -x, x)
+    x[..., 5], x[..., 77] = 0.0, -0.0
+    x[..., 0:1, :, 9] = (448.0 * scale[..., 0]).float()                       # the largest, so that the scale is near what it was made with
+    x = x.reshape(rows, cols)
+    want_q, want_scale = quantized(x, block_rows)
+    got_q, got_scale = zf.quantize_blocks(x.cuda(), block_rows=block_rows)
+    assert torch.equal(got_scale.cpu(), want_scale)
+    assert torch.equal(got_q.cpu().view(torch.uint8), want_q.to(torch.float8_e4m3fn).view(torch.uint8))
+
+
 def head_case(M, V, K, seed):
     g = torch.Generator().manual_seed(seed)
     x = torch.randn((M, K), generator=g) * torch.exp(torch.randn((M, 1), generator=g))
