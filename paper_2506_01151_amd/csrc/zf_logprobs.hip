@@ -215,8 +215,7 @@ __global__ __launch_bounds__(THREADS) void logprobs_part_kernel(LogprobsArgs A) 
     constexpr int EPV = 16 / sizeof(ElemT), WAVES = THREADS / 64;
     __shared__ Part part[WAVES];
     __shared__ Key best[WAVES];
-    __shared__ float listed_x[TOP ? WAVES : 1][LISTED];
-    __shared__ uint32_t listed_v[TOP ? WAVES : 1][LISTED];
+    __shared__ Key listed[TOP ? WAVES : 1][LISTED];
     __shared__ uint32_t lines[2][WAVES];
     __shared__ int n_listed[WAVES];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64;
@@ -298,13 +297,13 @@ __global__ __launch_bounds__(THREADS) void logprobs_part_kernel(LogprobsArgs A) 
             const unsigned long long who = __ballot(x[p][k] >= from);
             if (!who) continue;                            // most often
             const int at = n + __builtin_amdgcn_mbcnt_hi((uint32_t)(who >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)who, 0));
-            if (x[p][k] >= from && at < LISTED) { listed_x[wave][at] = x[p][k]; listed_v[wave][at] = (uint32_t)(v0 + p * (THREADS * EPV) + k); }
+            if (x[p][k] >= from && at < LISTED) listed[wave][at] = key_of(x[p][k], (uint32_t)(v0 + p * (THREADS * EPV) + k));
             n += __popcll(who);
         }
     if (tid % 64 == 0) n_listed[wave] = n;
     __syncthreads();
     RowEnd end;
-    if (wave == 0 && row_ends) end = RowEnd(mine, A.c);    // the first wavefront stores
+    if (row_ends) end = RowEnd(mine, A.c);
     auto store = [&](int i, Key k) {
         if (row_ends) end.store_top(A.a, row, i, k);
         else A.keys[(int64_t)blockIdx.x * A.a.top + i] = k;
@@ -314,25 +313,29 @@ __global__ __launch_bounds__(THREADS) void logprobs_part_kernel(LogprobsArgs A) 
 #pragma unroll
     for (int w = 0; w < WAVES; w++) { n_all += n_listed[w]; fits = fits && n_listed[w] <= LISTED; }
     if (fits) {
-        if (wave) return;                                  // the first wavefront ranks them, 64 at a time
-        auto key_at = [&](int i) -> Key {
-            int w = 0;
-#pragma unroll
-            for (int u = 0; u < WAVES - 1; u++) if (w == u && i >= n_listed[u]) { i -= n_listed[u]; w++; }
-            return key_of(listed_x[w][i], listed_v[w][i]);
-        };
-        for (int i0 = 0; i0 < n_all; i0 += 64) {
-            const Key mine = i0 + tid < n_all ? key_at(i0 + tid) : 0;
-            int rank = 0;
-            for (int j0 = 0; j0 < n_all; j0 += 64) {
-                const Key other = j0 == i0 ? mine : j0 + tid < n_all ? key_at(j0 + tid) : 0;
-                const int n_other = n_all - j0 < 64 ? n_all - j0 : 64;
-                for (int j = 0; j < n_other; j++)
-                    rank += ((Key)(uint32_t)__builtin_amdgcn_readlane((int)(other >> 32), j) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)other, j)) > mine;
+        // Few keys are the first wavefront's, a lane each, which hears of the others' by lane moves; of more of them each wavefront ranks its own against the lists
+        // (64 x 128,256 bf16 with 64 alternatives: 14 us, by the first wavefront alone 28).
+        if (n_all > 64) {
+            for (int i = lane; i < n_listed[wave]; i += 64) {
+                const Key mine = listed[wave][i];
+                int rank = 0;
+                for (int w = 0; w < WAVES; w++) rank += rank_of(mine, listed[w], n_listed[w]);
+                if (rank < A.a.top) store(rank, mine);
             }
+        } else if (wave == 0) {
+            Key mine = 0;
+            if (tid < n_all) {
+                int w = 0, i = tid;
+#pragma unroll
+                for (int u = 0; u < WAVES - 1; u++) if (w == u && i >= n_listed[u]) { i -= n_listed[u]; w++; }
+                mine = listed[w][i];
+            }
+            int rank = 0;
+            for (int j = 0; j < n_all; j++)
+                rank += ((Key)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), j) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)mine, j)) > mine;
             if (mine && rank < A.a.top) store(rank, mine);
+            for (int i = n_all + tid; i < A.a.top; i += 64) store(i, 0);
         }
-        for (int i = n_all + tid; i < A.a.top; i += 64) store(i, 0);
         return;
     }
     Key last = ~(Key)0;
@@ -358,11 +361,11 @@ __global__ __launch_bounds__(THREADS) void logprobs_part_kernel(LogprobsArgs A) 
 
 // A row's parts, by one wavefront.  Its segments' alternatives are listed and ranked as a segment's are, up to JOINED_LANE in a lane; with more of them, or
 // more equal ones than the list takes, they are merged from the segments' sorted lists, a lane at the head of each.
-static const int JOINED_LANE = 16;
+static const int JOINED_LANE = 16, JOINED = 256;           // keys of a lane, of the list
 
 template <typename ElemT>
 __global__ __launch_bounds__(ROWS_JOINED * 64) void logprobs_join_kernel(LogprobsArgs A) {
-    __shared__ Key listed[ROWS_JOINED][LISTED];
+    __shared__ Key listed[ROWS_JOINED][JOINED];
     extern __shared__ uint8_t taken[];                     // [ROWS_JOINED][n_seg]: keys of a segment that are out
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
     const int64_t row = (int64_t)blockIdx.x * ROWS_JOINED + wave;
@@ -372,11 +375,16 @@ __global__ __launch_bounds__(ROWS_JOINED * 64) void logprobs_join_kernel(Logprob
     const Key *const keys = A.keys + row * n_keys;
     const bool listable = A.a.top && n_keys <= JOINED_LANE * 64;
     Key own[JOINED_LANE];
+    // A segment's keys lie sorted.  Each 64 of them go to the lanes from another one on, so that every lane has some of the first and the line, which a lane's
+    // largest stands for, is not that of the last of a segment (64 alternatives of 16 segments: all would reach it;
+    // 64 x 128,256 bf16: the whole kernel 42 us then, 11.6 so).
+    const int turn = 64 / ((n_keys + 63) / 64 + !n_keys);
     if (listable)
 #pragma unroll
         for (int j = 0; j < JOINED_LANE; j++) {
+            const int i = j * 64 + ((lane + j * turn) & 63);
             own[j] = 0;
-            if (j * 64 + lane < n_keys) own[j] = keys[j * 64 + lane];
+            if (i < n_keys) own[j] = keys[i];
         }
     int64_t t = -1;
     float x = -INFINITY;
@@ -404,10 +412,10 @@ __global__ __launch_bounds__(ROWS_JOINED * 64) void logprobs_join_kernel(Logprob
             const unsigned long long who = __ballot(in);
             if (!who) continue;
             const int at = n + __popcll(who & ((1ull << lane) - 1));
-            if (in && at < LISTED) list[at] = own[j];
+            if (in && at < JOINED) list[at] = own[j];
             n += __popcll(who);
         }
-        if (n <= LISTED) {
+        if (n <= JOINED) {
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             __builtin_amdgcn_wave_barrier();
             for (int i = lane; i < n; i += 64) {
