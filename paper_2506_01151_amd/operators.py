@@ -84,7 +84,7 @@ def quantize_blocks(x, *, block_rows=1):
 def head_logits(q, q_scale, weight, weight_scale, mask=None, *, dtype=torch.bfloat16, out=None):
     """Logits [batch, V] of activations q [batch, K] against a head's weight [V, K], both e4m3 with K a multiple of 128, scales [batch, K / 128] and
     [ceil(V / 128), K / 128] (quantize_blocks makes all four).  Under a mask the logits of tokens that it does not allow are -inf, and
-    rows of the weight that no row of the batch allows are not read.  dtype: fp32 or bf16; out: rows of the result without gaps."""
+    rows of the weight that none of a batch of up to 64 allows are not read.  dtype: fp32 or bf16; out: rows of the result without gaps."""
     if out is None:
         got = _native_ops.head_logits(q, q_scale, weight, weight_scale, mask, _DTYPES.get(dtype, -1))
         if got is not None:
