@@ -501,27 +501,34 @@ __global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(GradArgs A) {
     // d = p (base + slope log2 p), p = 2^y, y = log2 p
     const float base = inv_t * (-G - gh * H), slope = -inv_t * gh * LN_2;
     const int n = n_mine;
+    // p may be 0, and 0 times what is not finite is NaN: rows with a NaN, infinite gradients, factors near 32 bits' limit (y is -1e4 at least, less log2 S).
+    // There, and far out, where there may be nothing but -inf, every element is looked at.
+    const bool look = ref.far || !(fabsf(base) + 2e4f * fabsf(slope) + fabsf(log2_S) < INFINITY);
     ElemT *const grad = (ElemT *)A.g.grad + row * A.g.stride;
 #pragma unroll
     for (int p = 0; p < PIECES; p++) {
         const int32_t v = v0 + p * (THREADS * EPV);
         float d[EPV];
-        if (!ref.far) {
+        if (!look) {
 #pragma unroll
             for (int k = 0; k < EPV; k++) {
                 const float y = fmaxf(fmaf(x[p][k], ref.c, -ref.R), -1e4f) - log2_S;
                 d[k] = two_to(y) * fmaf(slope, y, base);
             }
-        } else {                                           // nothing that is allowed, NaN alone, or logits that are far out
+        } else {
 #pragma unroll
             for (int k = 0; k < EPV; k++) {
-                const float y = fmaxf((x[p][k] - ref.m) * ref.c, -1e4f) - log2_S;
-                d[k] = x[p][k] == -INFINITY ? 0.0f : two_to(y) * fmaf(slope, y, base);
+                const float y = fmaxf(ref.far ? (x[p][k] - ref.m) * ref.c : fmaf(x[p][k], ref.c, -ref.R), -1e4f) - log2_S, e = two_to(y);
+                d[k] = fmaf(e * y, slope, e * base);
             }
         }
         for (int j = 0; j < n; j++) {
 #pragma unroll
             for (int k = 0; k < EPV; k++) if (mine_v[j] == v + k) d[k] += mine_g[j];
+        }
+        if (look) {
+#pragma unroll
+            for (int k = 0; k < EPV; k++) d[k] = x[p][k] == -INFINITY ? 0.0f : d[k];
         }
         union { u32x4 v; ElemT e[EPV]; bf16x2 b[4]; } o;
 #pragma unroll

@@ -455,6 +455,33 @@ def test_token_logprobs_forbidden_values_are_not_looked_at(dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [40, 9001, 40037])
+def test_gradient_of_forbidden_tokens_is_zero_whatever_comes_in(V, dtype):
+    """Rows with a NaN, with +inf, with NaN alone, of logits far out, and ordinary ones with infinite and NaN gradients: what the mask forbids has gradient 0, given or not; the row
+    beside them is what it is without them."""
+    g = torch.Generator().manual_seed(V)
+    x = torch.randn((7, V), generator=g).to(DTYPES[dtype])
+    bits = torch.rand((7, V), generator=g) < 0.4
+    tokens = torch.stack([bits.float().argmax(dim=1), (~bits).float().argmax(dim=1)], dim=1)      # an allowed one and one that is not
+    x[0, tokens[0, 0]] = math.nan
+    x[1, tokens[1, 0]] = INF
+    x[2] = torch.where(bits[2], math.nan, x[2].float()).to(x.dtype)
+    x[3] = x[3] * 1e30
+    g_lp, g_H = torch.randn((7, 2), generator=g), torch.randn(7, generator=g)
+    g_lp[4, 0], g_H[5], g_lp[6, 1] = INF, math.nan, INF    # the last one's token is not allowed: nobody takes it
+    grads = []
+    for rows in (torch.arange(7), torch.tensor([6])):
+        on = x[rows].cuda().requires_grad_()
+        got = zf.token_logprobs(on, tokens[rows].cuda(), packed(bits[rows]).cuda(), entropy=True)
+        grad, = torch.autograd.grad((got.logprobs, got.entropy), on, (g_lp[rows].cuda(), g_H[rows].cuda()))
+        grads.append(grad.cpu())
+    assert (grads[0][~bits] == 0).all()
+    assert torch.equal(grads[0][6:], grads[1]) and torch.isfinite(grads[1]).all()
+    assert grads[0][0][bits[0]].isnan().all() and grads[0][2][bits[2]].isnan().all() and torch.isfinite(grads[0][3]).all()
+
+
+@gpu
 @pytest.mark.parametrize("top", [1, 20, 64])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_alternatives_with_many_equal_logits(dtype, top):
