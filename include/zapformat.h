@@ -275,8 +275,8 @@ int zf_head_logits(const uint8_t *d_x, int64_t x_row_stride, const float *d_x_sc
  *                     at least the lowest finite number for a finite logit
  *   entropy[b]      = - sum p ln p
  *   top_ids, top_logprobs [b][i]: the i-th largest logit's token (equal ones by the lower id) and its log probability; -1 and -inf behind the last one
- * A row that allows nothing, or whose allowed logits are all -inf, has logprobs -inf, entropy 0 and no alternatives; a NaN among the
- * allowed logits makes the row's logprobs and entropy NaN (it is no alternative).  What a mask forbids is not looked at. */
+ * A row that allows nothing, or whose allowed logits are all -inf, has logprobs -inf, entropy 0 and no alternatives; a NaN or +inf among the
+ * allowed logits makes the row's logprobs and entropy NaN (a NaN is no alternative).  What a mask forbids is not looked at. */
 typedef struct {
     const void *logits;        /* device, [rows][row_stride_elems], V valid elements per row */
     int32_t dtype;
@@ -287,7 +287,7 @@ typedef struct {
     int32_t token_bytes;       /* 4 or 8: the ids' type */
     int32_t n_tokens;          /* 0 .. 1024 */
     int32_t top;               /* 0 .. 64 alternatives */
-    float temperature;         /* > 0 */
+    float temperature;         /* 2^-126 at least, finite */
     float *logprobs;           /* device, [rows][n_tokens] */
     float *entropy;            /* device, [rows], or null */
     int32_t *top_ids;          /* device, [rows][top] */

@@ -1,4 +1,5 @@
 // The C boundary of the calls at the two ends of a step's logits: argument checks, then the kernels' launches.
+#include <cfloat>
 #include <cmath>
 #include <new>
 #include <string>
@@ -39,7 +40,7 @@ int check_logprobs(const zf_logprobs_args *a, bool backward) {
     if (a->n_tokens < 0 || a->n_tokens > GIVEN_MAX) return refuse("n_tokens must be 0..1024");
     if (a->top < 0 || a->top > TOP_MAX) return refuse("top must be 0..64");
     if (a->n_tokens && a->token_bytes != 4 && a->token_bytes != 8) return refuse("token_bytes must be 4 or 8");
-    if (!(a->temperature > 0.0f) || !std::isfinite(a->temperature)) return refuse("temperature must be positive and finite");
+    if (!(a->temperature >= FLT_MIN) || !std::isfinite(a->temperature)) return refuse("temperature must be finite, at least 2^-126");   // (its reciprocal is finite)
     if (a->rows == 0) return ZF_OK;
     if (logprobs_blocks(*a) > BLOCKS_MAX) return refuse("more logits than a call takes: split the rows");
     if (!a->logits || (a->n_tokens && (!a->tokens || !a->logprobs)) || (a->top && (!a->top_ids || !a->top_logprobs))) return refuse("null argument");

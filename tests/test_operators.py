@@ -482,6 +482,27 @@ def test_gradient_of_forbidden_tokens_is_zero_whatever_comes_in(V, dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [40, 9001, 40037])
+@pytest.mark.parametrize("exponent", [-120, -20, 20, 120])
+def test_token_logprobs_temperatures_far_from_one(exponent, V, dtype):
+    g = torch.Generator().manual_seed(V)
+    x = torch.randn((3, V), generator=g).to(DTYPES[dtype])
+    bits = torch.rand((3, V), generator=g) < 0.5
+    bits[:, 1] = True
+    check_logprobs(x, torch.tensor([1, 1, -1]), bits, 2.0 ** exponent, 3)
+
+
+def test_library_refuses_temperatures_whose_reciprocal_is_infinite():
+    from paper_2506_01151_amd.binding import LogprobsArgs
+    a = LogprobsArgs()
+    a.logits, a.V, a.rows, a.row_stride = 4096, 10, 2, 10                     # (an address that nothing reads)
+    for t, code in ((2.0 ** -149, zf.ZF_ERR_INVALID_ARG), (2.0 ** -126 - 2.0 ** -149, zf.ZF_ERR_INVALID_ARG), (2.0 ** -126, 0), (3e38, 0)):
+        a.temperature = t
+        assert min(zf.load_library().zf_token_logprobs_workspace(ctypes.byref(a)), 0) == code, t
+
+
+@gpu
 @pytest.mark.parametrize("top", [1, 20, 64])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_alternatives_with_many_equal_logits(dtype, top):
