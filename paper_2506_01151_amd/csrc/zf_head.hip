@@ -207,6 +207,11 @@ __device__ __forceinline__ void to_lds(const float *from, uint32_t at) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(at), "v"(from) : "memory");
 }
 template <int N> __device__ __forceinline__ void arrived() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }   // of the wavefront's loads, all but the last N
+// What a wavefront's lanes wrote to LDS before it is what they read behind it: LDS takes a wavefront's accesses in turn, the compiler has to leave them so.
+__device__ __forceinline__ void in_turn() {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
 __device__ __forceinline__ uint32_t lds_at(const void *p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) uint8_t *)p; }
 
 // ---- few rows: the weight streams past them ----
@@ -640,7 +645,7 @@ __global__ __launch_bounds__(512, 2) void head_tile_kernel(HeadArgs a, int32_t t
                 if (sizeof(ElemT) == 4) *reinterpret_cast<u32x4 *>(to) = o.v;
                 else *reinterpret_cast<uint64_t *>(to) = o.q;
             }
-            __builtin_amdgcn_wave_barrier();
+            in_turn();
 #pragma unroll
             for (int i = 0; i < 16 * PIECES / 64; i++) {
                 const int r = (i * 64 + lane) / PIECES, p = (i * 64 + lane) % PIECES;
@@ -660,7 +665,7 @@ __global__ __launch_bounds__(512, 2) void head_tile_kernel(HeadArgs a, int32_t t
                     for (int e = 0; e < EPV; e++) if (v + e < a.V) to[e] = o.e[e];
                 }
             }
-            __builtin_amdgcn_wave_barrier();
+            in_turn();
         }
     }
 }
