@@ -208,6 +208,26 @@ def test_head_logits_vocabularies_of_many_ranges(M, V, K, kind):
 
 
 @gpu
+@pytest.mark.parametrize("kind", [None, "few", "half", "mixed"])
+@pytest.mark.parametrize("M,V,K", [(2, 16384, 256), (17, 16385, 384), (50, 16321, 640), (40, 16449, 256), (3, 28737, 4224), (30, 32768, 4096), (20, 30001, 4224), (1, 32769, 4096), (9, 33000, 4352), (18, 33000, 4096), (64, 28800, 4096)])
+def test_head_logits_where_ranges_change(M, V, K, kind):
+    """Vocabularies on both sides of where ranges of tokens get wider, rows of an odd number of blocks where they are taken in pairs; "mixed": some ranges are allowed whole."""
+    q, qs, wq, ws = head_case(M, V, K, M + V)
+    want, bound = head_want(q, qs, wq, ws)
+    bits = None
+    if kind:
+        g = torch.Generator().manual_seed(K)
+        bits = torch.rand((M, V), generator=g) < {"few": 0.002, "half": 0.5, "mixed": 0.0005}[kind]
+        if kind == "mixed":
+            for v in (0, 320, 8192, V - 200):
+                bits[:, v:v + 200] = True
+        bits[M // 2] = False
+    mask = None if bits is None else packed(bits, padding=True).cuda()
+    for dtype in (torch.float32, torch.bfloat16):
+        check_head(zf.head_logits(q.cuda(), qs.cuda(), wq.cuda(), ws.cuda(), mask, dtype=dtype), want, bound, bits)
+
+
+@gpu
 @pytest.mark.parametrize("masked", [False, True])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("M,V,K", [(70, 70001, 128), (150, 70001, 384), (200, 66049, 256), (300, 66000, 128), (513, 40037, 256)])
