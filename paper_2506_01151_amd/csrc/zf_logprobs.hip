@@ -483,7 +483,7 @@ __global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(GradArgs A) {
                 const int64_t at = row * a.top + j - n_given;
                 t = a.top_ids[at]; g = A.g.g_top[at]; lp = a.top_logprobs[at];
             }
-            if (t < 0 || t >= V || lp == -INFINITY) g = 0.0f, t = -1;
+            if (t < 0 || t >= V || !(lp > -INFINITY)) g = 0.0f, t = -1;      // (in a row with a NaN every token that is allowed has NaN anyway)
             G += g;
             const bool here = t >= first && t < first + THREADS * PIECES * EPV;
             const unsigned long long who = __ballot(here);
@@ -519,16 +519,12 @@ __global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(GradArgs A) {
 #pragma unroll
             for (int k = 0; k < EPV; k++) {
                 const float y = fmaxf(ref.far ? (x[p][k] - ref.m) * ref.c : fmaf(x[p][k], ref.c, -ref.R), -1e4f) - log2_S, e = two_to(y);
-                d[k] = fmaf(e * y, slope, e * base);
+                d[k] = x[p][k] == -INFINITY ? 0.0f : fmaf(e * y, slope, e * base);
             }
         }
         for (int j = 0; j < n; j++) {
 #pragma unroll
             for (int k = 0; k < EPV; k++) if (mine_v[j] == v + k) d[k] += mine_g[j];
-        }
-        if (look) {
-#pragma unroll
-            for (int k = 0; k < EPV; k++) d[k] = x[p][k] == -INFINITY ? 0.0f : d[k];
         }
         union { u32x4 v; ElemT e[EPV]; bf16x2 b[4]; } o;
 #pragma unroll
