@@ -37,7 +37,7 @@ def _extension_jobs(force):
         torch_flags += ["-isystem", p]
     libs = [f for p in library_paths() if os.path.isdir(p) for f in ["-L" + p]] + ["-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python"]
     jobs = []
-    for src, name, flags, link in (("zf_py.cpp", "_native.so", [], []), ("zf_py_torch.cpp", "_native_torch.so", torch_flags, libs), ("zf_py_ops.cpp", "_native_ops.so", torch_flags, libs)):
+    for src, name, flags, link in (("zf_py.cpp", "_native.so", [], []), ("zf_py_torch.cpp", "_native_torch.so", torch_flags, libs), ("zf_py_ops.cpp", "_native_ops.so", torch_flags, libs + ["-ltorch_hip"])):
         path, out = os.path.join(CSRC, src), os.path.join(HERE, name)
         newest = max(os.path.getmtime(p) for p in (path, os.path.join(CSRC, "zf_py.h"), os.path.join(HERE, "..", "include", "zapformat.h")))
         if force or not os.path.exists(out) or os.path.getmtime(out) < newest:
