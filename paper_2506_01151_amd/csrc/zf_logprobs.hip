@@ -85,6 +85,16 @@ __device__ __forceinline__ Key wave_max(Key k) {
     const uint32_t high = wave_max((uint32_t)(k >> 32));
     return (Key)high << 32 | wave_max((uint32_t)(k >> 32) == high ? (uint32_t)k : 0u);
 }
+__device__ __forceinline__ int four_sum(int x) {           // over four neighbouring lanes, to all of them
+    x += (int)moved<0xB1>(0, x);                           // lanes 1 0 3 2 of each four
+    return x + (int)moved<0x4E>(0, x);                     // lanes 2 3 0 1
+}
+__device__ __forceinline__ int sum_up_to(int x) {          // of sixteen lanes, each with those below it
+    x += (int)moved<0x111>(0, x);
+    x += (int)moved<0x112>(0, x);
+    x += (int)moved<0x114>(0, x);
+    return x + (int)moved<0x118>(0, x);
+}
 __device__ __forceinline__ float two_to(float x) { return __builtin_amdgcn_exp2f(x); }   // below 2^-126 nothing
 // How far the reference of a part lies below the whole's: nothing times -inf is nothing, so -inf is a large number here.
 __device__ __forceinline__ float below(float m, const Reference &whole) {
@@ -192,15 +202,21 @@ __device__ __forceinline__ void load_pieces(const ElemT *row, const uint32_t *ma
 // logits) is left to the caller, which takes the keys one by one, each the largest below the last.
 static const int LISTED = 128;                             // keys that a wavefront lists
 
-// The largest multiple of 2^16 that `top` lanes reach, but at least 1 (0 stands for no logit).
-__device__ __forceinline__ uint32_t line_of(uint32_t o, int top) {
-    uint32_t line = 0;
+// The largest multiples of 2^16 that so many lanes reach, but at least 1 (0 stands for no logit).
+template <int N>
+__device__ __forceinline__ void lines_of(uint32_t o, const int (&lanes)[N], uint32_t (&line)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; i++) line[i] = 0;
 #pragma unroll
     for (int bit = 31; bit >= 16; bit--) {
-        const uint32_t up = line | 1u << bit;
-        if (__popcll(__ballot(o >= up)) >= top) line = up;
+#pragma unroll
+        for (int i = 0; i < N; i++) {
+            const uint32_t up = line[i] | 1u << bit;
+            if (__popcll(__ballot(o >= up)) >= lanes[i]) line[i] = up;
+        }
     }
-    return line ? line : 1;
+#pragma unroll
+    for (int i = 0; i < N; i++) line[i] = line[i] ? line[i] : 1;
 }
 __device__ __forceinline__ int rank_of(Key mine, const Key *list, int n) {
     int rank = 0;
@@ -211,14 +227,14 @@ __device__ __forceinline__ int rank_of(Key mine, const Key *list, int n) {
 
 // A segment of a row, or (n_seg = 1) the whole of it, to the end.
 //   Large inputs are bound by memory: 4,096 x 128,256 bf16 with entropy 181 us (5.8 TB/s; now and then 160 or 207), 1,030 x 40,037 bf16 at odd elements 15.6 (5.3).  Small ones by
-// what follows in turn: 64 x 128,256 bf16 6.4 us without alternatives, of which 2.7 are its bytes; with 20 of them 12 (lines 0.7, lists 2, ranks and stores 2.5),
-// one row of 32,000 fp32 with 5 8.4.
+// what follows in turn: 64 x 128,256 bf16 6.0 us without alternatives, of which 2.7 are its bytes; with 20 of them 10.5, with 64 12.3; one row of 32,000 fp32 4.5 without, with 5 7.0, with 64 8.2
+// (of the 2.5 a fifth is the lines, a half the lists and the waits for the slowest wavefront's, the rest ranks and stores); 64 x 32,000 bf16 5.1, with 20 9.0.
 template <int THREADS, int PIECES, bool ONCE, bool ENT, bool TOP, typename ElemT>
 __global__ __launch_bounds__(THREADS) void logprobs_part_kernel(LogprobsArgs A) {
     constexpr int EPV = 16 / sizeof(ElemT), WAVES = THREADS / 64;
     __shared__ Part part[WAVES];
     __shared__ Key best[WAVES];
-    __shared__ Key listed[TOP ? WAVES : 1][LISTED];
+    __shared__ Key listed[TOP ? WAVES : 1][LISTED], all[TOP ? WAVES * LISTED + 32 : 1];
     __shared__ uint32_t lines[2][WAVES];
     __shared__ int n_listed[WAVES];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64;
@@ -268,33 +284,37 @@ __global__ __launch_bounds__(THREADS) void logprobs_part_kernel(LogprobsArgs A) 
     if (tid % 64 == 0) part[wave] = Part{m, S, T, 0.0f};
     if (TOP) {
         const uint32_t mine = in_order(most);              // as many lanes as reach a line have a logit that does
-        lines[0][wave] = line_of(mine, A.a.top);
-        lines[1][wave] = line_of(mine, (A.a.top + WAVES - 1) / WAVES);
+        uint32_t line[2];
+        lines_of<2>(mine, {A.a.top, (A.a.top + WAVES - 1) / WAVES}, line);
+        if (lane < 2) lines[lane][wave] = lane ? line[1] : line[0];
     }
     __syncthreads();
     const Part mine = lane < WAVES ? part[lane] : Part{-INFINITY, 0.0f, 0.0f, 0.0f};
-    if (wave == WAVES - 1) {
-        const RowEnd end(mine, A.c);                       // (of the segment)
+    auto finish = [&](const RowEnd &end) {                 // (of the segment)
         if (!row_ends) {
             if (lane == 0) A.parts[blockIdx.x] = Part{end.ref.m, end.S, end.T, 0.0f};
-        } else {
-            if (lane == 0) end.store_row(A.a, row);
-            for (int j = lane; j < A.a.n_tokens; j += 64) {
-                if (j != lane) look_up<ElemT>(A, row, j, &given, &given_x);
-                A.a.logprobs[row * A.a.n_tokens + j] = end.given(given, given_x, A.a);
-            }
+            return;
         }
+        if (lane == 0) end.store_row(A.a, row);
+        for (int j = lane; j < A.a.n_tokens; j += 64) {
+            if (j != lane) look_up<ElemT>(A, row, j, &given, &given_x);
+            A.a.logprobs[row * A.a.n_tokens + j] = end.given(given, given_x, A.a);
+        }
+    };
+    if (!TOP) {
+        if (wave == WAVES - 1) finish(RowEnd(mine, A.c));
+        return;
     }
-    if (!TOP) return;
     // `top` logits of a single wavefront reach the one, a share of them in each wavefront the other: the higher of the two
-    uint32_t line = lines[0][0], share = lines[1][0];
-#pragma unroll
-    for (int w = 1; w < WAVES; w++) { line = max(line, lines[0][w]); share = min(share, lines[1][w]); }
-    line = max(line, share);
+    const uint32_t line = max(wave_max(lines[0][lane % WAVES]), ~wave_max(~lines[1][lane % WAVES]));
     const float from = line <= 0x007FFFFFu ? -FLT_MAX : logit_of((Key)line << 32);
     int n = 0;
 #pragma unroll
-    for (int p = 0; p < PIECES; p++)
+    for (int p = 0; p < PIECES; p++) {
+        float largest = x[p][0];
+#pragma unroll
+        for (int k = 1; k < EPV; k++) largest = fmaxf(largest, x[p][k]);
+        if (!__any(largest >= from)) continue;             // most often
 #pragma unroll
         for (int k = 0; k < EPV; k++) {
             const unsigned long long who = __ballot(x[p][k] >= from);
@@ -303,44 +323,39 @@ __global__ __launch_bounds__(THREADS) void logprobs_part_kernel(LogprobsArgs A) 
             if (x[p][k] >= from && at < LISTED) listed[wave][at] = key_of(x[p][k], (uint32_t)(v0 + p * (THREADS * EPV) + k));
             n += __popcll(who);
         }
+    }
     if (tid % 64 == 0) n_listed[wave] = n;
     __syncthreads();
     RowEnd end;
-    if (row_ends) end = RowEnd(mine, A.c);
+    if (row_ends || wave == WAVES - 1) end = RowEnd(mine, A.c);
     auto store = [&](int i, Key k) {
         if (row_ends) end.store_top(A.a, row, i, k);
         else A.keys[(int64_t)blockIdx.x * A.a.top + i] = k;
     };
-    int n_all = 0;
-    bool fits = true;
-#pragma unroll
-    for (int w = 0; w < WAVES; w++) { n_all += n_listed[w]; fits = fits && n_listed[w] <= LISTED; }
-    if (fits) {
-        // Few keys are the first wavefront's, a lane each, which hears of the others' by lane moves; of more of them each wavefront ranks its own against the lists
-        // (64 x 128,256 bf16 with 64 alternatives: 14 us, by the first wavefront alone 28).
-        if (n_all > 64) {
-            for (int i = lane; i < n_listed[wave]; i += 64) {
-                const Key mine = listed[wave][i];
-                int rank = 0;
-                for (int w = 0; w < WAVES; w++) rank += rank_of(mine, listed[w], n_listed[w]);
-                if (rank < A.a.top) store(rank, mine);
-            }
-        } else if (wave == 0) {
-            Key mine = 0;
-            if (tid < n_all) {
-                int w = 0, i = tid;
-#pragma unroll
-                for (int u = 0; u < WAVES - 1; u++) if (w == u && i >= n_listed[u]) { i -= n_listed[u]; w++; }
-                mine = listed[w][i];
-            }
+    const int counts = lane < WAVES ? n_listed[lane] : 0, up_to = sum_up_to(counts);
+    if (!__any(counts > LISTED)) {
+        // All lists become one, and each key's rank the sum of what four lanes find above it, each in a quarter of the list: all wavefronts take part (64 x 32,000 bf16 with 20
+        // alternatives 9.0 us; by the first wavefront alone, or by each against the others' lists in turn, 16.2).
+        const int n_all = __builtin_amdgcn_readlane(up_to, WAVES - 1), before = __builtin_amdgcn_readlane(up_to, wave) - n;
+        for (int i = lane; i < n; i += 64) all[before + i] = listed[wave][i];
+        if (tid < 32) all[n_all + tid] = 0;                // nothing is below it: the list is taken 32 at a time
+        __syncthreads();
+        if (wave == WAVES - 1) finish(end);
+        for (int i0 = wave * 16; i0 < n_all; i0 += THREADS / 4) {
+            const int i = i0 + lane / 4;
+            const Key mine = all[i < n_all ? i : 0];
             int rank = 0;
-            for (int j = 0; j < n_all; j++)
-                rank += ((Key)(uint32_t)__builtin_amdgcn_readlane((int)(mine >> 32), j) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)mine, j)) > mine;
-            if (mine && rank < A.a.top) store(rank, mine);
-            for (int i = n_all + tid; i < A.a.top; i += 64) store(i, 0);
+            for (int j = 0; j < n_all; j += 32) {
+#pragma unroll
+                for (int u = 0; u < 8; u++) rank += all[j + 4 * u + lane % 4] > mine;
+            }
+            rank = four_sum(rank);
+            if (lane % 4 == 0 && i < n_all && rank < A.a.top) store(rank, mine);
         }
+        for (int i = n_all + tid; i < A.a.top; i += THREADS) store(i, 0);
         return;
     }
+    if (wave == WAVES - 1) finish(end);
     Key last = ~(Key)0;
     for (int i = 0; i < A.a.top; i++) {                    // the largest below the last one
         Key k0 = 0;
@@ -406,12 +421,13 @@ __global__ __launch_bounds__(ROWS_JOINED * 64) void logprobs_join_kernel(Logprob
         uint32_t most = 0;
 #pragma unroll
         for (int j = 0; j < JOINED_LANE; j++) most = max(most, (uint32_t)(own[j] >> 32));
-        const uint32_t line = line_of(most, A.a.top);
+        uint32_t line[1];
+        lines_of<1>(most, {A.a.top}, line);
         Key *const list = listed[wave];
         int n = 0;
 #pragma unroll
         for (int j = 0; j < JOINED_LANE; j++) {
-            const bool in = (uint32_t)(own[j] >> 32) >= line;
+            const bool in = (uint32_t)(own[j] >> 32) >= line[0];
             const unsigned long long who = __ballot(in);
             if (!who) continue;
             const int at = n + __popcll(who & ((1ull << lane) - 1));
