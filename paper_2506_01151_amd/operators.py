@@ -167,7 +167,7 @@ def token_logprobs(logits, tokens=None, mask=None, *, temperature=1.0, entropy=F
     entropies and their `top` (up to 64) most probable tokens, as TokenLogprobs.  logits: fp32 or bf16 [rows, V], rows without gaps.
 
     -inf for a token that the mask does not allow, 0 and no gradient for a negative id (padding), NaN for an id beyond V.  Alternatives that there are
-    not: id -1, -inf.  logprobs, entropy and top_logprobs have gradients for the logits (once; not to be differentiated again)."""
+    not: id -1, -inf.  temperature: 2^-126 at least.  logprobs, entropy and top_logprobs have gradients for the logits (once; not to be differentiated again)."""
     got = _native_ops.token_logprobs(logits, tokens, mask, float(temperature), bool(entropy), top)
     if got is not None:
         return TokenLogprobs(*got)
