@@ -539,7 +539,7 @@ __global__ __launch_bounds__(256, 2) void head_rows_kernel(HeadArgs a, int32_t n
 
 // ---- many rows: tiles of both operands in LDS ----
 //
-// A workgroup of eight wavefronts takes tiles of 256 tokens and 32 MJ rows of the batch, one after the other, a wavefront 64 tokens and 16 MJ rows.  A block of columns of both
+// A workgroup of eight wavefronts takes tiles of 64 MI tokens and 32 MJ rows of the batch, one after the other, a wavefront 16 MI tokens and 16 MJ rows.  A block of columns of both
 // operands, 128 bytes a row, comes from memory straight into LDS while the block before is multiplied, the next tile's first one while this one's last is: two buffers, one
 // barrier a block, pieces in places as above.  While sixteen rows' products run the sixteen before them are scaled and added.
 //   2,048 x 128,256 x 4,096 bf16: 1,040 to 1,080 us, 2.0 PFLOP/s.  The matrix units are busy for 51 % of it, the other vector instructions (the scales, mostly) would be for 30 %
@@ -547,18 +547,17 @@ __global__ __launch_bounds__(256, 2) void head_rows_kernel(HeadArgs a, int32_t n
 // of the bf16 instructions' rate and the operands' conversion beside them.
 //   Under a mask a tile is computed whole: of more than 64 rows some most often allow each of its ranges of tokens.
 //   Rows behind the last one are the last one again; their results are not stored.
-static const int TILE_TOKENS = 256;
-
-template <int MJ, typename ElemT>
+template <int MJ, int MI, typename ElemT>
 struct TileLds {
-    static constexpr int ROWS = 32 * MJ, W_BYTES = TILE_TOKENS * SCALE_BLOCK, X_BYTES = ROWS * SCALE_BLOCK, BUFFER = W_BYTES + X_BYTES;
-    static constexpr int SCALES = 2 * BUFFER, OUT = SCALES + 2 * 512 * 4, PITCH = 64 * sizeof(ElemT) + 16, BYTES = OUT + 8 * 16 * PITCH;
+    static constexpr int ROWS = 32 * MJ, TOKENS = 64 * MI, W_BYTES = TOKENS * SCALE_BLOCK, X_BYTES = ROWS * SCALE_BLOCK, BUFFER = W_BYTES + X_BYTES;
+    static constexpr int SCALES = 2 * BUFFER, OUT = SCALES + 2 * 512 * 4, PITCH = 16 * MI * sizeof(ElemT) + 16, BYTES = OUT + 8 * 16 * PITCH;
 };
 
-template <int MJ, bool MASK, typename ElemT>
+template <int MJ, int MI, bool MASK, typename ElemT>
 __global__ __launch_bounds__(512, 2) void head_tile_kernel(HeadArgs a, int32_t tiles_m, int32_t n_tiles) {
-    typedef TileLds<MJ, ElemT> Lds;
-    constexpr int LOADS = 4 + MJ / 2;                                        // of a wavefront for a block: eight rows each, 32 of the weight, 4 MJ of the activations
+    typedef TileLds<MJ, MI, ElemT> Lds;
+    constexpr int LOADS = MI + MJ / 2;                                       // of a wavefront for a block: eight rows each, 8 MI of the weight, 4 MJ of the activations
+    constexpr bool SPLIT = Lds::TOKENS % SCALE_BLOCK != 0;                   // tiles begin in the middle of 128 tokens, and wavefronts have some of both
     extern __shared__ __align__(16) uint8_t mem[];
     const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64), wv = wave % 4, wm = wave / 4;
     const int32_t n_k = a.K / SCALE_BLOCK, n_vb = (a.V + SCALE_BLOCK - 1) / SCALE_BLOCK, W = (a.V + 31) / 32;
@@ -571,13 +570,13 @@ __global__ __launch_bounds__(512, 2) void head_tile_kernel(HeadArgs a, int32_t t
     uint32_t off[LOADS];                                                     // the host checks that a tile's rows lie within 32 bits
     const float *xs, *ws;                                                    // a thread's scales: of one row, and of the weight's first or second 128 tokens (the threads behind these two have them once more)
     auto aim = [&](int32_t t) {
-        const int32_t v0 = t / tiles_m * TILE_TOKENS, m0 = t % tiles_m * Lds::ROWS;
+        const int32_t v0 = t / tiles_m * Lds::TOKENS, m0 = t % tiles_m * Lds::ROWS;
         w0 = a.w + (int64_t)v0 * a.w_stride;
         x0 = a.x + (int64_t)m0 * a.x_stride;
 #pragma unroll
         for (int i = 0; i < LOADS; i++) {
-            const int32_t r = (i < 4 ? wave * 4 + i : wave * (MJ / 2) + i - 4) * 8 + lane / 8, left = i < 4 ? a.V - v0 : a.M - m0;
-            off[i] = (uint32_t)(r < left ? r : left - 1) * (uint32_t)(i < 4 ? a.w_stride : a.x_stride) + (lane % 8 ^ lane / 8) * 16;
+            const int32_t r = (i < MI ? wave * MI + i : wave * (MJ / 2) + i - MI) * 8 + lane / 8, left = i < MI ? a.V - v0 : a.M - m0;
+            off[i] = (uint32_t)(r < left ? r : left - 1) * (uint32_t)(i < MI ? a.w_stride : a.x_stride) + (lane % 8 ^ lane / 8) * 16;
         }
         const int32_t row = m0 + tid % Lds::ROWS, vb = v0 / SCALE_BLOCK + tid / Lds::ROWS % 2;
         xs = a.xs + (size_t)(row < a.M ? row : a.M - 1) * n_k;
@@ -586,7 +585,7 @@ __global__ __launch_bounds__(512, 2) void head_tile_kernel(HeadArgs a, int32_t t
     auto fetch = [&](int32_t k, int b) {
 #pragma unroll
         for (int i = 0; i < LOADS; i++)
-            to_lds((i < 4 ? w0 : x0) + (size_t)k * SCALE_BLOCK, off[i], lds_at(mem) + b * Lds::BUFFER + (i < 4 ? (wave * 4 + i) * 8 * SCALE_BLOCK : Lds::W_BYTES + (wave * (MJ / 2) + i - 4) * 8 * SCALE_BLOCK));
+            to_lds((i < MI ? w0 : x0) + (size_t)k * SCALE_BLOCK, off[i], lds_at(mem) + b * Lds::BUFFER + (i < MI ? (wave * MI + i) * 8 * SCALE_BLOCK : Lds::W_BYTES + (wave * (MJ / 2) + i - MI) * 8 * SCALE_BLOCK));
     };
     float *const scales = reinterpret_cast<float *>(mem + Lds::SCALES);
     uint8_t *const own = mem + Lds::OUT + wave * (16 * Lds::PITCH);
@@ -598,11 +597,12 @@ __global__ __launch_bounds__(512, 2) void head_tile_kernel(HeadArgs a, int32_t t
     __syncthreads();
     int b = 0;
     for (; tile < end; tile += stride) {
-        f32x4 acc[MJ][4];
+        const int second = (SCALE_BLOCK - tile / tiles_m * Lds::TOKENS % SCALE_BLOCK - wv * 16 * MI) / 16;   // sixteens of the wavefront before the second 128 tokens (or none)
+        f32x4 acc[MJ][MI];
 #pragma unroll
         for (int j = 0; j < MJ; j++)
 #pragma unroll
-            for (int i = 0; i < 4; i++) acc[j][i] = f32x4{0, 0, 0, 0};
+            for (int i = 0; i < MI; i++) acc[j][i] = f32x4{0, 0, 0, 0};
         for (int32_t k = 0; k < n_k; k++, b ^= 1) {
             int32_t k_next = k + 1;
             if (k_next == n_k) {                                             // behind the last block: the next tile's first (behind the last tile: this one's, which nobody reads)
@@ -610,36 +610,38 @@ __global__ __launch_bounds__(512, 2) void head_tile_kernel(HeadArgs a, int32_t t
                 if (tile + stride < end) aim(tile + stride);
             }
             const float next_x = xs[k_next], next_w = ws[k_next];
-            const uint8_t *const w_at = mem + b * Lds::BUFFER + (wv * 64 + lane % 16) * SCALE_BLOCK;
+            const uint8_t *const w_at = mem + b * Lds::BUFFER + (wv * 16 * MI + lane % 16) * SCALE_BLOCK;
             const uint8_t *const x_at = mem + b * Lds::BUFFER + Lds::W_BYTES + (wm * 16 * MJ + lane % 16) * SCALE_BLOCK;
-            const float *const s_at = scales + b * 512 + wv / 2 * Lds::ROWS + wm * 16 * MJ + lane % 16;
-            Operand<ElemT> w[4];
+            const float *const s_at = scales + b * 512 + (SPLIT ? 0 : wv * 16 * MI / SCALE_BLOCK) * Lds::ROWS + wm * 16 * MJ + lane % 16;
+            Operand<ElemT> w[MI];
 #pragma unroll
-            for (int i = 0; i < 4; i++) w[i].take(piece_at(w_at + i * 16 * SCALE_BLOCK + c0), piece_at(w_at + i * 16 * SCALE_BLOCK + c1));
-            f32x4 part[4][1], last[4];
-            float s = 0.0f, s_last = 0.0f;
+            for (int i = 0; i < MI; i++) w[i].take(piece_at(w_at + i * 16 * SCALE_BLOCK + c0), piece_at(w_at + i * 16 * SCALE_BLOCK + c1));
+            f32x4 part[MI][1], last[MI];
+            float s[2] = {0.0f, 0.0f}, s_last[2] = {0.0f, 0.0f};             // of the weight's first and second 128 tokens, where a wavefront may have some of both
             Operand<ElemT> x[1], x_next;
             x_next.take(piece_at(x_at + c0), piece_at(x_at + c1));
 #pragma unroll
             for (int j = 0; j <= MJ; j++) {
                 if (j < MJ) {
                     x[0] = x_next;
-                    s = s_at[j * 16];
+                    s[0] = s_at[j * 16];
+                    if (SPLIT) s[1] = s_at[Lds::ROWS + j * 16];
                     if (j + 1 < MJ) x_next.take(piece_at(x_at + (j + 1) * 16 * SCALE_BLOCK + c0), piece_at(x_at + (j + 1) * 16 * SCALE_BLOCK + c1));
                     multiply(w, x, part);
                     if (j == 0) fetch(k_next, b ^ 1);                        // behind the reads that the first products wait for
                 }
 #pragma unroll
-                for (int i = 0; i < 4; i++) {
+                for (int i = 0; i < MI; i++) {
                     if (j > 0)
 #pragma unroll
-                        for (int e = 0; e < 4; e++) acc[j - 1][i][e] = fmaf(s_last, last[i][e], acc[j - 1][i][e]);
+                        for (int e = 0; e < 4; e++) acc[j - 1][i][e] = fmaf(SPLIT && i >= second ? s_last[1] : s_last[0], last[i][e], acc[j - 1][i][e]);
                     last[i] = part[i][0];
                 }
-                s_last = s;
+                s_last[0] = s[0];
+                if (SPLIT) s_last[1] = s[1];
                 if (j > 0 && j < MJ)
 #pragma unroll
-                    for (int i = 0; i < 4; i++) {                            // a product, four sums, a product, ...
+                    for (int i = 0; i < MI; i++) {                            // a product, four sums, a product, ...
                         __builtin_amdgcn_sched_group_barrier(0x8, Operand<ElemT>::STEPS, 0);
                         __builtin_amdgcn_sched_group_barrier(0x2, 4, 0);
                     }
@@ -650,12 +652,12 @@ __global__ __launch_bounds__(512, 2) void head_tile_kernel(HeadArgs a, int32_t t
             __syncthreads();
         }
         // sixteen rows at a time through the wavefront's own part of LDS, from four tokens a lane to whole lines of 64 tokens
-        constexpr int EPV = 16 / sizeof(ElemT), PIECES = 64 / EPV;
-        const int32_t v_w = tile / tiles_m * TILE_TOKENS + wv * 64, m_w = tile % tiles_m * Lds::ROWS + wm * 16 * MJ;
+        constexpr int EPV = 16 / sizeof(ElemT), PIECES = 16 * MI / EPV;
+        const int32_t v_w = tile / tiles_m * Lds::TOKENS + wv * 16 * MI, m_w = tile % tiles_m * Lds::ROWS + wm * 16 * MJ;
 #pragma unroll
         for (int j = 0; j < MJ; j++) {
 #pragma unroll
-            for (int i = 0; i < 4; i++) {
+            for (int i = 0; i < MI; i++) {
                 union { ElemT e[4]; uint64_t q; u32x4 v; } o;
 #pragma unroll
                 for (int e = 0; e < 4; e++) o.e[e] = sizeof(ElemT) == 4 ? (ElemT)__float_as_uint(acc[j][i][e]) : (ElemT)bf16_of(acc[j][i][e]);
@@ -665,7 +667,8 @@ __global__ __launch_bounds__(512, 2) void head_tile_kernel(HeadArgs a, int32_t t
             }
             in_turn();
 #pragma unroll
-            for (int i = 0; i < 16 * PIECES / 64; i++) {
+            for (int i = 0; i < (16 * PIECES + 63) / 64; i++) {
+                if (16 * PIECES % 64 && i * 64 + lane >= 16 * PIECES) continue;
                 const int r = (i * 64 + lane) / PIECES, p = (i * 64 + lane) % PIECES;
                 const int32_t m = m_w + j * 16 + r, v = v_w + p * EPV;
                 union { ElemT e[EPV]; u32x4 v; } o;
@@ -700,16 +703,21 @@ hipError_t allow_lds(const void *kernel, int bytes, std::atomic<uint64_t> &allow
     return e;
 }
 
-template <int MJ, bool MASK, typename ElemT>
+template <int MJ, int MI, bool MASK, typename ElemT>
 hipError_t head_tile(const HeadArgs &a, hipStream_t s) {
-    typedef TileLds<MJ, ElemT> Lds;
+    typedef TileLds<MJ, MI, ElemT> Lds;
     static std::atomic<uint64_t> allowed{0};
-    const hipError_t e = allow_lds((const void *)head_tile_kernel<MJ, MASK, ElemT>, Lds::BYTES, allowed);
+    const hipError_t e = allow_lds((const void *)head_tile_kernel<MJ, MI, MASK, ElemT>, Lds::BYTES, allowed);
     if (e != hipSuccess) return e;
     const int32_t tiles_m = (a.M + Lds::ROWS - 1) / Lds::ROWS;
-    const int64_t n = (int64_t)tiles_m * ((a.V + TILE_TOKENS - 1) / TILE_TOKENS);
-    hipLaunchKernelGGL((head_tile_kernel<MJ, MASK, ElemT>), dim3((uint32_t)std::min<int64_t>(n, COMPUTE_UNITS)), dim3(512), Lds::BYTES, s, a, tiles_m, (int32_t)n);
+    const int64_t n = (int64_t)tiles_m * ((a.V + Lds::TOKENS - 1) / Lds::TOKENS);
+    hipLaunchKernelGGL((head_tile_kernel<MJ, MI, MASK, ElemT>), dim3((uint32_t)std::min<int64_t>(n, COMPUTE_UNITS)), dim3(512), Lds::BYTES, s, a, tiles_m, (int32_t)n);
     return hipSuccess;
+}
+
+template <int MJ, bool MASK, typename ElemT>
+hipError_t head_tile_of(const HeadArgs &a, int tokens, hipStream_t s) {
+    return tokens == 256 ? head_tile<MJ, 4, MASK, ElemT>(a, s) : tokens == 192 ? head_tile<MJ, 3, MASK, ElemT>(a, s) : head_tile<MJ, 2, MASK, ElemT>(a, s);
 }
 
 template <int MT, int TOKENS, bool PAIRS, bool MASK, typename ElemT>
@@ -745,14 +753,22 @@ hipError_t head(const HeadArgs &a, hipStream_t s) {
     if (a.M <= 32) return head_few<2, MASK, ElemT>(a, s);
     if (a.M <= 64) return head_few<4, MASK, ElemT>(a, s);
     if ((a.w_stride | a.x_stride) >= (1 << 24)) return head_rows<4, 128, false, MASK, ElemT>(a, s);   // a tile's rows would not lie within 32 bits
-    if constexpr (sizeof(ElemT) == 2) {                                      // (operands in bf16 take twice the registers: 128 rows)
-        // Tiles of 128, 192 or 256 rows, whichever makes the least work: rows of all tiles, and 64 more for what a tile costs whatever its rows
-        // (130 x 40,037 x 1,024: 128 rows 24 us, 192 18.2, 256 21.6).
-        auto cost = [&](int32_t rows) { return (int64_t)((a.M + rows - 1) / rows) * (rows + 64); };
-        if (cost(256) <= cost(192) && cost(256) <= cost(128)) return head_tile<8, MASK, ElemT>(a, s);
-        if (cost(192) <= cost(128)) return head_tile<6, MASK, ElemT>(a, s);
+    // Tiles of 128, 192 or 256 rows (operands in bf16 take twice the registers: 128) and as many tokens, whichever are done first: tiles that a compute unit has, a tile's work and 64 more
+    // in each direction for what it costs whatever its size; smaller ones have to promise a twentieth (1,030 x 32,000 x 4,096 fp32 283 us, with 192 tokens 289).  With 256 tokens alone and
+    // so: 70 x 32,000 x 1,024 bf16 16.9 and 13.4 us, fp32 20.5 and 15.7; 130 x 32,000 x 4,096 bf16 58.3 and 47.0; 256 rows 65.0 and 57.5; 100 x 8,192 x 2,048 18.3 and 14.7; 300 x 32,000 x 4,096
+    // fp32 116 and 102.
+    int rows = 128, tokens = 256;
+    int64_t least = INT64_MAX;
+    for (int r = sizeof(ElemT) == 2 ? 256 : 128; r >= 128; r -= 64)
+        for (int t = 256; t >= 128; t -= 64) {
+            const int64_t tiles = (int64_t)((a.M + r - 1) / r) * ((a.V + t - 1) / t), cost = (tiles + COMPUTE_UNITS - 1) / COMPUTE_UNITS * (r + 64) * (t + 64);
+            if (least == INT64_MAX || cost * 20 < least * 19) least = cost, rows = r, tokens = t;
+        }
+    if constexpr (sizeof(ElemT) == 2) {
+        if (rows == 256) return head_tile_of<8, MASK, ElemT>(a, tokens, s);
+        if (rows == 192) return head_tile_of<6, MASK, ElemT>(a, tokens, s);
     }
-    return head_tile<4, MASK, ElemT>(a, s);
+    return head_tile_of<4, MASK, ElemT>(a, tokens, s);
 }
 
 template <typename ElemT>

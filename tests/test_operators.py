@@ -242,6 +242,19 @@ def test_head_logits_more_tiles_than_compute_units(M, V, K, dtype, masked):
 
 @gpu
 @pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,V,K", [(70, 65000, 128), (180, 60001, 256), (256, 50257, 384), (100, 40037, 256), (185, 49001, 128), (250, 33001, 384), (128, 32768, 256), (520, 20003, 128), (700, 24001, 256), (66, 191, 640), (66, 193, 128)])
+def test_head_logits_tiles_of_all_sizes(M, V, K, dtype, masked):
+    """Batches and vocabularies that tiles of 128, 192 and 256 tokens are chosen for, in one round of the compute units and in several."""
+    q, qs, wq, ws = head_case(M, V, K, M + V)
+    bits = torch.rand((M, V), generator=torch.Generator().manual_seed(K)) < 0.5 if masked else None
+    y = zf.head_logits(q.cuda(), qs.cuda(), wq.cuda(), ws.cuda(), packed(bits, padding=True).cuda() if masked else None, dtype=DTYPES[dtype])
+    want, bound = head_want(q, qs, wq, ws)
+    check_head(y, want, bound, bits)
+
+
+@gpu
+@pytest.mark.parametrize("masked", [False, True])
 @pytest.mark.parametrize("M,V", [(2, 515), (70, 300), (260, 515)])
 def test_head_logits_strides(M, V, masked):
     """Operands among others, a result at odd elements and distances that leaves what is around it alone, a result of the other type."""
