@@ -31,7 +31,8 @@ struct Failed { int rc; };             // a code of the library
 
 const int64_t BLOCK = 128;
 int logit_type(const Tensor &t) { return t.scalar_type() == at::kFloat ? 0 : t.scalar_type() == at::kBFloat16 ? 1 : -1; }
-bool plain(const Tensor &t) { return t.layout() == at::kStrided && t.is_cuda() && !t.is_nested() && !t.unsafeGetTensorImpl()->has_symbolic_sizes_strides() && !t.is_neg() && !t.is_conj(); }
+bool has_tangent(const Tensor &t) { return t._fw_grad(0).defined(); }
+bool plain(const Tensor &t) { return t.layout() == at::kStrided && t.is_cuda() && !t.is_nested() && !t.unsafeGetTensorImpl()->has_symbolic_sizes_strides() && !t.is_neg() && !t.is_conj() && !has_tangent(t); }
 bool matrix(const Tensor &t) { return plain(t) && t.dim() == 2; }
 bool rows_without_gaps(const Tensor &t) { return t.size(1) <= 1 || t.stride(1) == 1; }
 int64_t row_stride(const Tensor &t) { return t.size(0) > 1 ? t.stride(0) : t.size(1); }
@@ -135,6 +136,7 @@ struct TokenLogprobs : public torch::autograd::Function<TokenLogprobs> {
         size_t at = 0;
         auto next = [&](bool there) {
             const Tensor g = there ? grads[at++] : Tensor();
+            TORCH_CHECK(!g.defined() || !has_tangent(g), "token_logprobs: its gradient has no forward-mode derivative");
             return !g.defined() || (g.scalar_type() == at::kFloat && g.is_contiguous() && plain(g)) ? g : g.detach().to(at::kFloat).contiguous();
         };
         const Tensor g_lp = next(r.logprobs.has_value()), g_H = next(r.entropy.has_value());

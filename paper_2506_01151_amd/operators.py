@@ -7,12 +7,14 @@
 
 Masks are those of compute_mask.  Every call is enqueued on torch's current stream of the tensors' device, waits for nothing and
 allocates through torch only, so it can be captured into a graph (a backward pass as any of torch's: from leaves made for the
-capture, no eager graph of theirs alive).  Arguments that do not fit raise ZfError (ZF_ERR_INVALID_ARG).
+capture, no eager graph of theirs alive).  Arguments that do not fit raise ZfError (ZF_ERR_INVALID_ARG), tensors with a tangent among them: there are no
+forward-mode derivatives.
 """
 import ctypes
 from typing import NamedTuple, Optional
 
 import torch
+from torch.autograd import forward_ad
 
 from . import _native_ops
 from .binding import ZF_ERR_INVALID_ARG, LogprobsArgs, ZfError, _check, load_library
@@ -39,8 +41,14 @@ def _need(ok, why):
         raise ZfError(ZF_ERR_INVALID_ARG, why)
 
 
+def _plain(t, what):
+    """A kernel is given the tensor's address: what else there is to a tensor would be lost."""
+    _need(not torch._C._functorch.is_functorch_wrapped_tensor(t) and forward_ad.unpack_dual(t).tangent is None, f"{what}: there is no forward-mode derivative, nor another of torch.func's transforms")
+
+
 def _matrix(t, what, dtypes, rows=None, cols=None, contiguous=True):
     _need(isinstance(t, torch.Tensor) and t.layout == torch.strided and t.is_cuda, f"{what}: a tensor on the GPU is wanted")
+    _plain(t, what)
     _need(t.dtype in dtypes, f"{what}: {t.dtype} is none of {', '.join(map(str, dtypes))}")
     _need(t.dim() == 2 and (rows is None or t.shape[0] == rows) and (cols is None or t.shape[1] == cols),
           f"{what}: a matrix of {'any' if rows is None else rows} x {'any' if cols is None else cols} is wanted, not {tuple(t.shape)}")
@@ -155,6 +163,9 @@ class _TokenLogprobs(torch.autograd.Function):
 def _backward(logits, tokens, mask, lp, H, ids, top_lp, stats, temperature, g_lp, g_H, g_top):
     a = _logprobs_args(logits, tokens, mask, temperature, ids.shape[1] if ids is not None else 0)
     a.logprobs, a.entropy, a.top_ids, a.top_logprobs, a.stats = (t.data_ptr() if t is not None else None for t in (lp, H, ids, top_lp, stats))
+    for t in (g_lp, g_H, g_top):
+        if t is not None:
+            _plain(t, "incoming gradient")
     g = [t.to(torch.float32).contiguous() if t is not None else None for t in (g_lp, g_H, g_top)]
     grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
     _check(_lib.zf_token_logprobs_backward(ctypes.byref(a), *(t.data_ptr() if t is not None else None for t in g), grad.data_ptr(), grad.shape[1],
@@ -176,6 +187,7 @@ def token_logprobs(logits, tokens=None, mask=None, *, temperature=1.0, entropy=F
     _need(V > 0, "logits: no columns")
     if tokens is not None:
         _need(isinstance(tokens, torch.Tensor) and tokens.device == logits.device and tokens.dtype in (torch.int32, torch.int64), "tokens: int32 or int64 on the logits' device are wanted")
+        _plain(tokens, "tokens")
         _need(tokens.dim() in (1, 2) and tokens.shape[0] == rows and tokens.is_contiguous(), f"tokens: a contiguous [{rows}] or [{rows}, n] is wanted, not {tuple(tokens.shape)}")
     _need(isinstance(top, int) and 0 <= top <= 64, "top must be 0..64")
     if torch.is_grad_enabled() and logits.requires_grad:
