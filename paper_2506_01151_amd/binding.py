@@ -398,6 +398,7 @@ def _compute_mask_twin(engine: Engine, states, mask_tensor):
     _look_at_tensors()
     assert mask_tensor.is_cuda and mask_tensor.is_contiguous() and mask_tensor.dtype == torch.int32
     assert tuple(mask_tensor.shape) == (len(states), engine.W)
+    torch.autograd.graph.increment_version(mask_tensor)
     engine.compute_mask(states, mask_tensor.data_ptr(), _current_stream(engine))
     return mask_tensor
 
@@ -408,6 +409,7 @@ def _compute_mask_noalloc_twin(engine: Engine, states, mask_tensor):
     _look_at_tensors()
     assert mask_tensor.is_cuda and mask_tensor.is_contiguous() and mask_tensor.dtype == torch.int32
     assert tuple(mask_tensor.shape) == (len(states), engine.W)
+    torch.autograd.graph.increment_version(mask_tensor)
     engine.compute_mask_noalloc(states, mask_tensor.data_ptr(), _current_stream(engine))
     return mask_tensor
 
@@ -418,6 +420,7 @@ def _compute_mask_async_twin(engine: Engine, states, mask_tensor):
     _look_at_tensors()
     assert mask_tensor.is_cuda and mask_tensor.is_contiguous() and mask_tensor.dtype == torch.int32
     assert tuple(mask_tensor.shape) == (len(states), engine.W)
+    torch.autograd.graph.increment_version(mask_tensor)
     engine.compute_mask_async(states, mask_tensor.data_ptr(), _current_stream(engine))
     return mask_tensor
 
@@ -433,6 +436,7 @@ def _compute_mask_apply_async_twin(engine: Engine, states, mask_tensor, logits, 
     if out is None:
         out = logits
     assert out.dtype == logits.dtype and out.shape == logits.shape and out.stride() == logits.stride()
+    torch.autograd.graph.increment_version((mask_tensor, out))   # the tensors are written by their addresses: what a backward pass has kept of them is no longer there
     engine.compute_mask_apply_async(states, mask_tensor.data_ptr(), logits.data_ptr(), out.data_ptr(), dtype, logits.stride(0), _current_stream(engine))
     return out
 
@@ -451,6 +455,7 @@ def _apply_mask_twin(engine: Engine, logits, mask_tensor, out=None):
     if out is None:
         out = logits
     assert out.dtype == logits.dtype and out.shape == logits.shape and out.stride() == logits.stride()
+    torch.autograd.graph.increment_version(out)
     engine.apply_mask(logits.data_ptr(), out.data_ptr(), dtype, logits.shape[0], logits.stride(0),
                       mask_tensor.data_ptr(), _current_stream(engine))
     return out

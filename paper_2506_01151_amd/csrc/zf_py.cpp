@@ -198,6 +198,7 @@ PyObject *mask_call(const char *name, MaskCall call, PyObject *const *args, Py_s
     zfpy::TensorInfo m;
     void *s;
     if (!T || n != 3 || kw || !engine_of(args[0], &e) || !rows.take(args[1]) || !mask_of(args[2], e, rows.n, &m) || !T->stream(e->device, &s)) return twin(name, args, n, kw);
+    T->written(args[2]);
     const int rc = unlocked([&] { return call(e->h, rows.p, (int32_t)rows.n, (uint32_t *)m.data, s); });
     return itself(args[2], rc);
 }
@@ -214,6 +215,8 @@ PyObject *compute_mask_apply_async(PyObject *, PyObject *const *args, Py_ssize_t
         !logits_of(args[3], e, &x) || x.size[0] != rows.n || (out && (!T->look(out, &y) || y.device < 0 || !same_shape(x, y))) || !T->stream(e->device, &s))
         return twin("compute_mask_apply_async", args, n, kw);
     if (!out) { out = args[3]; y = x; }
+    T->written(args[2]);
+    T->written(out);
     const int rc = unlocked([&] { return L.compute_mask_apply_async(e->h, rows.p, (int32_t)rows.n, (uint32_t *)m.data, x.data, y.data, x.dtype, x.stride[0], s); });
     return itself(out, rc);
 }
@@ -226,6 +229,7 @@ PyObject *apply_mask(PyObject *, PyObject *const *args, Py_ssize_t n, PyObject *
         !T->look(args[2], &m) || m.device < 0 || (out && (!T->look(out, &y) || y.device < 0 || !same_shape(x, y))) || !T->stream(e->device, &s))
         return twin("apply_mask", args, n, kw);
     if (!out) { out = args[1]; y = x; }
+    T->written(out);
     const int rc = unlocked([&] { return L.apply_mask(e->h, x.data, y.data, x.dtype, (int32_t)x.size[0], x.stride[0], (const uint32_t *)m.data, s); });
     return itself(out, rc);
 }

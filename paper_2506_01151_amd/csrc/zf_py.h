@@ -14,6 +14,7 @@ struct TensorInfo {
 struct TensorCalls {
     bool (*look)(void *obj, TensorInfo *out) noexcept;      // false: not a plain torch.Tensor, or one that cannot be looked at
     bool (*stream)(int32_t device, void **out) noexcept;    // torch's current stream there; false: torch has none to give
+    void (*written)(void *obj) noexcept;                    // a tensor that was looked at is written by its address: tells autograd, which may have kept it
 };
 static const char *const TENSOR_CALLS_NAME = "paper_2506_01151_amd._native_torch.calls";
 

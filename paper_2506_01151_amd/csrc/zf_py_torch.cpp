@@ -31,7 +31,15 @@ bool stream(int32_t device, void **out) noexcept {
     return true;
 }
 
-zfpy::TensorCalls calls = {look, stream};
+// What torch's own in-place operations do: a backward pass that needs the tensor as it was then raises.  (Tensors of inference mode are not kept, and have no count.)
+void written(void *o) noexcept {
+    try {
+        const at::Tensor &t = THPVariable_Unpack((PyObject *)o);
+        if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+    } catch (...) {}
+}
+
+zfpy::TensorCalls calls = {look, stream, written};
 
 PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_native_torch", "Access to torch tensors for the _native module.", -1, nullptr, nullptr, nullptr, nullptr, nullptr};
 

@@ -111,6 +111,7 @@ def head_logits(q, q_scale, weight, weight_scale, mask=None, *, dtype=torch.bflo
         _matrix(out, "out", _DTYPES, batch, V, contiguous=False)
     for t, what in ((q_scale, "q_scale"), (weight, "weight"), (weight_scale, "weight_scale"), (out, "out")):
         _need(t.device == q.device, f"{what}: on another device than q")
+    torch.autograd.graph.increment_version(out)        # written by its address: a backward pass that has kept it is told
     _check(_lib.zf_head_logits(q.data_ptr(), _row_stride(q), q_scale.data_ptr(), weight.data_ptr(), _row_stride(weight), weight_scale.data_ptr(),
                                          batch, V, K, _mask_ptr(mask, batch, V, q.device), out.data_ptr(), _DTYPES[out.dtype], _row_stride(out), q.device.index, _stream(q.device)))
     return out
@@ -178,7 +179,8 @@ def token_logprobs(logits, tokens=None, mask=None, *, temperature=1.0, entropy=F
     entropies and their `top` (up to 64) most probable tokens, as TokenLogprobs.  logits: fp32 or bf16 [rows, V], rows without gaps.
 
     -inf for a token that the mask does not allow, 0 and no gradient for a negative id (padding), NaN for an id beyond V.  Alternatives that there are
-    not: id -1, -inf.  temperature: 2^-126 at least.  logprobs, entropy and top_logprobs have gradients for the logits (once; not to be differentiated again)."""
+    not: id -1, -inf.  temperature: 2^-126 at least.  logprobs, entropy and top_logprobs have gradients for the logits (once; not to be differentiated again).  The backward pass
+    reads logits, tokens and mask again: written meanwhile by torch or by this package's calls on tensors, it raises; what is written by a raw address (Engine's methods, other libraries) torch does not see."""
     got = _native_ops.token_logprobs(logits, tokens, mask, float(temperature), bool(entropy), top)
     if got is not None:
         return TokenLogprobs(*got)

@@ -60,3 +60,54 @@ def test_forward_mode_is_refused(path):
     for f, at in ((lambda v: zf.token_logprobs(v, tokens).logprobs, logits), (lambda v: zf.quantize_blocks(v)[1], x), (lambda v: zf.head_logits(q, v, w, ws, dtype=torch.float32), s)):
         with pytest.raises(RuntimeError):
             torch.func.jvp(f, (at,), (torch.ones_like(at),))
+
+
+@gpu
+@pytest.mark.parametrize("by", ["position", "name"])       # by name: the binding's own code does it, not the extension module
+def test_buffers_that_are_written_again_are_noticed(path, by):
+    """A mask or logits that a backward pass still needs, written by this package's own calls: torch's error of such buffers, no gradient under another mask."""
+    from workloads import configs
+    cfg = configs.CONFIGS[1]
+    engine = zf.Engine(cfg.grammar(), cfg.vocab())
+    states = zf.StateBatch([engine.new_state() for _ in range(2)])
+    x = torch.randn((2, engine.V), generator=torch.Generator().manual_seed(5)).cuda()
+    tokens = torch.zeros(2, dtype=torch.int64, device="cuda")
+    _, q, s, w, ws, _, _ = operands(rows=2, V=engine.V)
+
+    def call(f, *args, **kw):
+        names = {"compute_mask": ("engine", "states", "mask_tensor"), "compute_mask_noalloc": ("engine", "states", "mask_tensor"), "compute_mask_async": ("engine", "states", "mask_tensor"),
+                 "compute_mask_apply_async": ("engine", "states", "mask_tensor", "logits"), "apply_mask": ("engine", "logits", "mask_tensor")}[f]
+        getattr(zf, f)(**dict(zip(names, args)), **kw) if by == "name" else getattr(zf, f)(*args, **kw)
+        if "async" in f:
+            zf.mask_wait(engine)
+
+    spare = torch.empty((2, engine.W), dtype=torch.int32, device="cuda")
+    writers = {"mask": lambda mask, on: call("compute_mask", engine, states, mask), "noalloc": lambda mask, on: call("compute_mask_noalloc", engine, states, mask),
+               "async": lambda mask, on: call("compute_mask_async", engine, states, mask), "apply_async": lambda mask, on: call("compute_mask_apply_async", engine, states, mask, torch.zeros_like(x)),
+               "apply_async logits": lambda mask, on: call("compute_mask_apply_async", engine, states, spare, on.detach()),
+               "apply_async out": lambda mask, on: call("compute_mask_apply_async", engine, states, spare, torch.zeros_like(x), out=on.detach()),
+               "apply": lambda mask, on: call("apply_mask", engine, on.detach(), mask), "apply out": lambda mask, on: call("apply_mask", engine, torch.zeros_like(x), mask, out=on.detach()),
+               "head": lambda mask, on: zf.head_logits(q, s, w, ws, out=on.detach())}
+    for name, write in writers.items():
+        for another in (False, True):                      # the buffers themselves, or others
+            mask = torch.empty((2, engine.W), dtype=torch.int32, device="cuda")
+            zf.compute_mask(engine, states, mask)
+            on = x.clone().requires_grad_()
+            loss = zf.token_logprobs(on, tokens, mask, entropy=True).entropy.sum()
+            write(*(mask.clone(), on.detach().clone()) if another else (mask, on))
+            if another:
+                loss.backward()
+                assert torch.isfinite(on.grad).all()
+            else:
+                with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+                    loss.backward()
+    # tensors of inference mode have no such count, inside it and outside
+    with torch.inference_mode():
+        mask, on = torch.empty((2, engine.W), dtype=torch.int32, device="cuda"), x.clone()
+        call("compute_mask", engine, states, mask)
+        call("apply_mask", engine, on, mask)
+        zf.head_logits(q, s, w, ws, out=on)
+    call("compute_mask", engine, states, mask)
+    call("compute_mask_apply_async", engine, states, mask, on)
+    zf.head_logits(q, s, w, ws, mask, out=on)
+    assert torch.equal(on, zf.head_logits(q, s, w, ws, mask, dtype=torch.float32))
