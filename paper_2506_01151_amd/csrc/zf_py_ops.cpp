@@ -75,7 +75,8 @@ PyObject *head_logits(PyObject *const *args, Py_ssize_t n) {           // (q, q_
     const int64_t batch = q->size(0), K = q->size(1), V = w->size(0), k = K / BLOCK;
     if (batch < 1 || V < 1 || V > INT32_MAX || K < BLOCK || K % BLOCK || K > INT32_MAX || batch > INT32_MAX || w->size(1) != K || !rows_without_gaps(*q) || !rows_without_gaps(*w) || !qs->is_contiguous() || !ws->is_contiguous() ||
         qs->size(0) != batch || qs->size(1) != k || ws->size(0) != (V + BLOCK - 1) / BLOCK || ws->size(1) != k || w->device() != q->device() || qs->device() != q->device() ||
-        ws->device() != q->device() || !mask_fits(mask, batch, V, *q)) return nullptr;
+        ws->device() != q->device() || !mask_fits(mask, batch, V, *q) ||
+        (at::GradMode::is_enabled() && (q->requires_grad() || qs->requires_grad() || w->requires_grad() || ws->requires_grad()))) return nullptr;
     const Tensor out = fresh({batch, V}, type == 0 ? at::kFloat : at::kBFloat16, *q);
     must(L.head_logits((const uint8_t *)q->data_ptr(), row_stride(*q), qs->data_ptr<float>(), (const uint8_t *)w->data_ptr(), row_stride(*w), ws->data_ptr<float>(), (int32_t)batch, (int32_t)V, (int32_t)K,
                        mask ? (const uint32_t *)mask->data_ptr() : nullptr, out.data_ptr(), (int32_t)type, V, q->get_device(), stream_of(*q)));

@@ -74,7 +74,7 @@ def _stream(device):
 
 def quantize_blocks(x, *, block_rows=1):
     """x (fp32 or bf16 [rows, cols]) as (q, scale): e4m3 [rows, cols padded with zeros to a multiple of 128] and fp32 scales, one for 128 columns
-    of block_rows = 1 row (activations) or of 128 rows (a head's weight)."""
+    of block_rows = 1 row (activations) or of 128 rows (a head's weight).  Both are constants to autograd, as those of x.detach(), also where x requires grad."""
     got = _native_ops.quantize_blocks(x, block_rows)
     if got is not None:
         return got
@@ -89,10 +89,23 @@ def quantize_blocks(x, *, block_rows=1):
     return q, scale
 
 
+class _NoDerivative(torch.autograd.Function):
+    """The result of a call, tied to its operands by a node that raises when it is followed back."""
+
+    @staticmethod
+    def forward(ctx, call, *operands):
+        return call()
+
+    @staticmethod
+    def backward(ctx, *g):
+        raise ZfError(ZF_ERR_INVALID_ARG, "head_logits: there is no derivative; detach its operands, or take the product in another type")
+
+
 def head_logits(q, q_scale, weight, weight_scale, mask=None, *, dtype=torch.bfloat16, out=None):
     """Logits [batch, V] of activations q [batch, K] against a head's weight [V, K], both e4m3 with K a multiple of 128, scales [batch, K / 128] and
     [ceil(V / 128), K / 128] (quantize_blocks makes all four).  Under a mask the logits of tokens that it does not allow are -inf, and
-    rows of the weight that none of a batch of up to 64 allows are not read.  dtype: fp32 or bf16; out: rows of the result without gaps."""
+    rows of the weight that none of a batch of up to 64 allows are not read.  dtype: fp32 or bf16; out: rows of the result without gaps.  There is no derivative: where an operand requires grad the result does,
+    and a backward pass that reaches it raises; out= is refused then, and an out that requires grad itself, as torch's own calls do."""
     if out is None:
         got = _native_ops.head_logits(q, q_scale, weight, weight_scale, mask, _DTYPES.get(dtype, -1))
         if got is not None:
@@ -104,17 +117,25 @@ def head_logits(q, q_scale, weight, weight_scale, mask=None, *, dtype=torch.bflo
     _need(V > 0, "weight: no rows")
     _matrix(q_scale, "q_scale", (torch.float32,), batch, K // BLOCK)
     _matrix(weight_scale, "weight_scale", (torch.float32,), -(-V // BLOCK), K // BLOCK)
+    followed = torch.is_grad_enabled() and any(t.requires_grad for t in (q, q_scale, weight, weight_scale))
     if out is None:
         _need(dtype in _DTYPES, f"dtype: {dtype} is neither fp32 nor bf16")
-        out = torch.empty((batch, V), dtype=dtype, device=q.device)
     else:
         _matrix(out, "out", _DTYPES, batch, V, contiguous=False)
-    for t, what in ((q_scale, "q_scale"), (weight, "weight"), (weight_scale, "weight_scale"), (out, "out")):
+        _need(not followed and not (torch.is_grad_enabled() and out.requires_grad), "out: there is no derivative, and it or an operand requires grad")
+    for t, what in ((q_scale, "q_scale"), (weight, "weight"), (weight_scale, "weight_scale"), (q if out is None else out, "out")):
         _need(t.device == q.device, f"{what}: on another device than q")
-    torch.autograd.graph.increment_version(out)        # written by its address: a backward pass that has kept it is told
-    _check(_lib.zf_head_logits(q.data_ptr(), _row_stride(q), q_scale.data_ptr(), weight.data_ptr(), _row_stride(weight), weight_scale.data_ptr(),
-                                         batch, V, K, _mask_ptr(mask, batch, V, q.device), out.data_ptr(), _DTYPES[out.dtype], _row_stride(out), q.device.index, _stream(q.device)))
-    return out
+    mask_ptr = _mask_ptr(mask, batch, V, q.device)
+
+    def call():
+        y = torch.empty((batch, V), dtype=dtype, device=q.device) if out is None else out
+        if out is not None:
+            torch.autograd.graph.increment_version(out)    # written by its address: a backward pass that has kept it is told
+        _check(_lib.zf_head_logits(q.data_ptr(), _row_stride(q), q_scale.data_ptr(), weight.data_ptr(), _row_stride(weight), weight_scale.data_ptr(),
+                                   batch, V, K, mask_ptr, y.data_ptr(), _DTYPES[y.dtype], _row_stride(y), q.device.index, _stream(q.device)))
+        return y
+
+    return _NoDerivative.apply(call, q, q_scale, weight, weight_scale) if followed else call()
 
 
 def _logprobs_args(logits, tokens, mask, temperature, top):

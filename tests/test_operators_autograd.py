@@ -111,3 +111,28 @@ def test_buffers_that_are_written_again_are_noticed(path, by):
     call("compute_mask_apply_async", engine, states, mask, on)
     zf.head_logits(q, s, w, ws, mask, out=on)
     assert torch.equal(on, zf.head_logits(q, s, w, ws, mask, dtype=torch.float32))
+
+
+@gpu
+def test_head_logits_has_no_derivative(path):
+    """Operands that require grad: the result does too, and who follows it back is told.  A result's memory that requires grad, or has to for its operands, is refused.
+    quantize_blocks rounds: its results are constants."""
+    x, q, s, w, ws, logits, tokens = operands()
+    want = zf.head_logits(q, s, w, ws, dtype=torch.float32)
+    for k in range(4):
+        args = [q, s, w, ws]
+        args[k] = args[k].clone().requires_grad_()
+        y = zf.head_logits(*args, dtype=torch.float32)
+        assert y.requires_grad and torch.equal(y.detach(), want)
+        with pytest.raises(RuntimeError, match="no derivative"):
+            y.sum().backward()
+        refused(lambda: zf.head_logits(*args, out=logits.clone()), "derivative")
+        with torch.no_grad():
+            assert not zf.head_logits(*args).requires_grad
+            out = logits.clone().requires_grad_()
+            assert zf.head_logits(*args, out=out) is out
+        assert torch.equal(out.detach(), want)
+    kept = logits.clone().requires_grad_()
+    refused(lambda: zf.head_logits(q, s, w, ws, out=kept), "derivative")
+    assert torch.equal(kept.detach(), logits)
+    assert not any(t.requires_grad for t in zf.quantize_blocks(x.clone().requires_grad_()))
