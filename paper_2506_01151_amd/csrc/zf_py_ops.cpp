@@ -6,7 +6,9 @@
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/functions/basic_ops.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <ATen/TracerMode.h>
 #include <ATen/hip/EmptyTensor.h>
+#include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPStream.h>
 #include <optional>
 #include <string>
@@ -186,11 +188,17 @@ PyObject *token_logprobs(PyObject *const *args, Py_ssize_t n) {        // (logit
     return t;
 }
 
+// Somebody watches what torch is asked for on this thread: a tracer, which operators.py refuses, or a dispatch mode that wants to see the allocations.
+bool watched() {
+    return at::tracer::impl::is_dispatch_enabled() || c10::impl::tls_is_dispatch_key_included(at::DispatchKey::PreDispatch) || c10::impl::TorchDispatchModeTLS::any_modes_set();
+}
+
 // Python calls C: no C++ exception goes that way.
 typedef PyObject *(*Call)(PyObject *const *, Py_ssize_t);
 template <Call F>
 PyObject *guarded(PyObject *, PyObject *const *args, Py_ssize_t n) {
     try {
+        if (watched()) Py_RETURN_NONE;
         PyObject *r = F(args, n);
         if (r || PyErr_Occurred()) return r;
     } catch (const Failed &e) {

@@ -8,9 +8,10 @@
 Masks are those of compute_mask.  Every call is enqueued on torch's current stream of the tensors' device, waits for nothing and
 allocates through torch only, so it can be captured into a graph (a backward pass as any of torch's: from leaves made for the
 capture, no eager graph of theirs alive).  Arguments that do not fit raise ZfError (ZF_ERR_INVALID_ARG), tensors with a tangent among them: there are no
-forward-mode derivatives.
+forward-mode derivatives.  Nor can the calls be traced (torch.jit.trace, make_fx): they refuse.
 """
 import ctypes
+import sys
 from typing import NamedTuple, Optional
 
 import torch
@@ -46,6 +47,12 @@ def _plain(t, what):
     _need(not torch._C._functorch.is_functorch_wrapped_tensor(t) and forward_ad.unpack_dual(t).tangent is None, f"{what}: there is no forward-mode derivative, nor another of torch.func's transforms")
 
 
+def _not_traced():
+    """torch.jit.trace and make_fx see none of what these calls do, and would keep the results as constants."""
+    proxies = sys.modules.get("torch.fx.experimental.proxy_tensor")
+    _need(not torch.jit.is_tracing() and (proxies is None or proxies.get_proxy_mode() is None), "these calls cannot be traced")
+
+
 def _matrix(t, what, dtypes, rows=None, cols=None, contiguous=True):
     _need(isinstance(t, torch.Tensor) and t.layout == torch.strided and t.is_cuda, f"{what}: a tensor on the GPU is wanted")
     _plain(t, what)
@@ -78,6 +85,7 @@ def quantize_blocks(x, *, block_rows=1):
     got = _native_ops.quantize_blocks(x, block_rows)
     if got is not None:
         return got
+    _not_traced()
     _matrix(x, "x", _DTYPES, contiguous=False)
     _need(block_rows in (1, BLOCK), "block_rows must be 1 or 128")
     rows, cols = x.shape
@@ -110,6 +118,7 @@ def head_logits(q, q_scale, weight, weight_scale, mask=None, *, dtype=torch.bflo
         got = _native_ops.head_logits(q, q_scale, weight, weight_scale, mask, _DTYPES.get(dtype, -1))
         if got is not None:
             return got
+    _not_traced()
     for t, what in ((q, "q"), (weight, "weight")):
         _matrix(t, what, (torch.float8_e4m3fn,), contiguous=False)
     batch, K, V = q.shape[0], q.shape[1], weight.shape[0]
@@ -205,6 +214,7 @@ def token_logprobs(logits, tokens=None, mask=None, *, temperature=1.0, entropy=F
     got = _native_ops.token_logprobs(logits, tokens, mask, float(temperature), bool(entropy), top)
     if got is not None:
         return TokenLogprobs(*got)
+    _not_traced()
     _matrix(logits, "logits", _DTYPES, contiguous=False)
     rows, V = logits.shape
     _need(V > 0, "logits: no columns")

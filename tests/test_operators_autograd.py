@@ -136,3 +136,38 @@ def test_head_logits_has_no_derivative(path):
     refused(lambda: zf.head_logits(q, s, w, ws, out=kept), "derivative")
     assert torch.equal(kept.detach(), logits)
     assert not any(t.requires_grad for t in zf.quantize_blocks(x.clone().requires_grad_()))
+
+
+@gpu
+def test_tracing_is_refused(path):
+    """A traced program would hold the results of the example's inputs as constants."""
+    from torch.fx.experimental.proxy_tensor import make_fx
+    x, q, s, w, ws, logits, tokens = operands()
+    for f, at in ((lambda v: zf.quantize_blocks(v)[1], x), (lambda v: zf.head_logits(q, v, w, ws), s), (lambda v: zf.token_logprobs(v, tokens).logprobs, logits)):
+        refused(lambda: make_fx(f)(at), "trace")
+        refused(lambda: make_fx(f, pre_dispatch=True)(at), "trace")
+        refused(lambda: make_fx(f, tracing_mode="fake")(at), "trace")
+        refused(lambda: torch.jit.trace(f, (at,), check_trace=False), "trace")
+        f(at)
+
+
+@gpu
+def test_other_dispatch_modes_change_nothing(path):
+    from torch.utils._python_dispatch import TorchDispatchMode
+
+    class Through(TorchDispatchMode):
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            return func(*args, **(kwargs or {}))
+
+    x, q, s, w, ws, logits, tokens = operands()
+
+    def calls():
+        on = logits.clone().requires_grad_()
+        got = zf.token_logprobs(on, tokens, entropy=True, top=3)
+        grad, = torch.autograd.grad(got.logprobs.sum() + got.entropy.sum(), on)
+        return [t.detach() for t in (*zf.quantize_blocks(x), zf.head_logits(q, s, w, ws), *got, grad)]
+
+    want = calls()
+    with Through():
+        got = calls()
+    assert all(torch.equal(a.float(), b.float()) for a, b in zip(got, want))
