@@ -117,6 +117,15 @@ Results forward(const Tensor &logits, const std::optional<Tensor> &tokens, const
     return r;
 }
 
+// A saved tensor, or an incoming gradient, for a kernel to read: what hooks on saved tensors give back may lie anywhere, in any order.
+Tensor kept(const Tensor &t, const char *what, const Tensor &with, at::ScalarType type, c10::IntArrayRef size, bool rows_apart = false) {
+    TORCH_CHECK(t.layout() == at::kStrided && t.is_cuda() && !t.is_nested() && t.device() == with.device() && t.scalar_type() == type && t.sizes() == size, "token_logprobs: saved ", what,
+                " came back with another device, type or shape: ", t.toString(), " ", t.sizes(), " on ", t.device(), " instead of ", size, " on ", with.device());
+    TORCH_CHECK(!has_tangent(t), "token_logprobs: its gradient has no forward-mode derivative");
+    const bool as_it_is = rows_apart ? t.dim() == 2 && t.stride(1) == 1 && row_stride(t) >= t.size(1) : t.is_contiguous();
+    return as_it_is && plain(t) ? t : t.detach().contiguous();
+}
+
 struct TokenLogprobs : public torch::autograd::Function<TokenLogprobs> {
     static torch::autograd::variable_list forward(torch::autograd::AutogradContext *ctx, const Tensor &logits, const std::optional<Tensor> &tokens, const std::optional<Tensor> &mask,
                                                   double temperature, bool entropy, int64_t top) {
@@ -132,20 +141,25 @@ struct TokenLogprobs : public torch::autograd::Function<TokenLogprobs> {
     }
     static torch::autograd::variable_list backward(torch::autograd::AutogradContext *ctx, torch::autograd::variable_list grads) {
         const auto saved = ctx->get_saved_variables();
-        auto some = [](const Tensor &t) { return t.defined() ? std::optional<Tensor>(t) : std::nullopt; };
-        const Tensor logits = saved[0];
-        const Results r{some(saved[3]), some(saved[4]), some(saved[5]), some(saved[6]), some(saved[7])};
+        const Tensor logits = kept(saved[0], "logits", saved[0], saved[0].scalar_type(), saved[0].sizes(), true);
+        TORCH_CHECK(logits.dim() == 2 && logit_type(logits) >= 0, "token_logprobs: saved logits came back as others");
+        const int64_t rows = logits.size(0), V = logits.size(1);
+        auto some = [&](int i, const char *what, at::ScalarType type, c10::IntArrayRef size) { return saved[i].defined() ? std::optional<Tensor>(kept(saved[i], what, logits, type, size)) : std::nullopt; };
+        auto width = [&](int i) { return saved[i].defined() && saved[i].dim() == 2 ? saved[i].size(1) : 0; };
+        const int64_t of_rows[] = {rows, width(3)}, of_top[] = {rows, width(5)};
+        const c10::IntArrayRef given(of_rows, saved[3].defined() && saved[3].dim() == 2 ? 2 : 1);
+        const std::optional<Tensor> tokens = some(1, "tokens", saved[1].defined() && saved[1].scalar_type() == at::kInt ? at::kInt : at::kLong, given), mask = some(2, "mask", at::kInt, {rows, (V + 31) / 32});
+        const Results r{some(3, "logprobs", at::kFloat, given), some(4, "entropy", at::kFloat, {rows}), some(5, "top_ids", at::kInt, of_top), some(6, "top_logprobs", at::kFloat, of_top), some(7, "stats", at::kFloat, {rows, 2})};
         const double temperature = ctx->saved_data["temperature"].toDouble();
         size_t at = 0;
-        auto next = [&](bool there) {
-            const Tensor g = there ? grads[at++] : Tensor();
-            TORCH_CHECK(!g.defined() || !has_tangent(g), "token_logprobs: its gradient has no forward-mode derivative");
-            return !g.defined() || (g.scalar_type() == at::kFloat && g.is_contiguous() && plain(g)) ? g : g.detach().to(at::kFloat).contiguous();
+        auto next = [&](const std::optional<Tensor> &of) {
+            const Tensor g = of ? grads[at++] : Tensor();
+            return g.defined() ? kept(g.scalar_type() == at::kFloat ? g : g.detach().to(at::kFloat), "gradient", logits, at::kFloat, of->sizes()) : g;
         };
-        const Tensor g_lp = next(r.logprobs.has_value()), g_H = next(r.entropy.has_value());
-        (void)next(r.ids.has_value());
-        const Tensor g_top = next(r.top.has_value());
-        zf_logprobs_args a = args_of(logits, some(saved[1]), some(saved[2]), temperature, r.ids ? r.ids->size(1) : 0);
+        const Tensor g_lp = next(r.logprobs), g_H = next(r.entropy);
+        (void)next(r.ids);
+        const Tensor g_top = next(r.top);
+        zf_logprobs_args a = args_of(logits, tokens, mask, temperature, r.ids ? r.ids->size(1) : 0);
         point(&a, r);
         auto ptr = [](const Tensor &t) { return t.defined() ? t.data_ptr<float>() : nullptr; };
         Tensor grad = fresh(logits.sizes(), logits.scalar_type(), logits);

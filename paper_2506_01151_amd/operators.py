@@ -191,13 +191,32 @@ class _TokenLogprobs(torch.autograd.Function):
         return _backward(*ctx.saved_tensors, ctx.temperature, g_lp, g_H, g_top), None, None, None, None, None
 
 
+def _kept(t, what, dtypes, shape, device, rows_apart=False):
+    """A saved tensor, or an incoming gradient, for a kernel to read: what hooks on saved tensors give back may lie anywhere, in any order."""
+    _need(t.layout == torch.strided and t.device == device and t.dtype in dtypes and tuple(t.shape) == tuple(shape), f"saved {what}: {tuple(t.shape)} of {t.dtype} on {t.device} came back instead of {tuple(shape)} on {device}")
+    _plain(t, f"saved {what}")
+    as_it_is = t.stride(1) == 1 and _row_stride(t) >= t.shape[1] if rows_apart else t.is_contiguous()
+    return t if as_it_is else t.contiguous()
+
+
 def _backward(logits, tokens, mask, lp, H, ids, top_lp, stats, temperature, g_lp, g_H, g_top):
+    _need(logits.is_cuda and logits.dim() == 2, "saved logits: a matrix on the GPU is wanted")
+    (rows, V), dev, f32 = logits.shape, logits.device, (torch.float32,)
+    logits = _kept(logits, "logits", _DTYPES, (rows, V), dev, rows_apart=True)
+    if tokens is not None:
+        tokens = _kept(tokens, "tokens", (torch.int32, torch.int64), lp.shape, dev)
+        lp = _kept(lp, "logprobs", f32, (rows, *lp.shape[1:2]), dev)
+    if mask is not None:
+        mask = _kept(mask, "mask", (torch.int32,), (rows, (V + 31) // 32), dev)
+    if H is not None:
+        H = _kept(H, "entropy", f32, (rows,), dev)
+    if ids is not None:
+        ids = _kept(ids, "top_ids", (torch.int32,), (rows, *ids.shape[1:2]), dev)
+        top_lp = _kept(top_lp, "top_logprobs", f32, ids.shape, dev)
+    stats = _kept(stats, "stats", f32, (rows, 2), dev)
     a = _logprobs_args(logits, tokens, mask, temperature, ids.shape[1] if ids is not None else 0)
     a.logprobs, a.entropy, a.top_ids, a.top_logprobs, a.stats = (t.data_ptr() if t is not None else None for t in (lp, H, ids, top_lp, stats))
-    for t in (g_lp, g_H, g_top):
-        if t is not None:
-            _plain(t, "incoming gradient")
-    g = [t.to(torch.float32).contiguous() if t is not None else None for t in (g_lp, g_H, g_top)]
+    g = [_kept(t.to(torch.float32), "gradient", f32, of.shape, dev) if t is not None else None for t, of in ((g_lp, lp), (g_H, H), (g_top, top_lp))]
     grad = torch.empty(logits.shape, dtype=logits.dtype, device=logits.device)
     _check(_lib.zf_token_logprobs_backward(ctypes.byref(a), *(t.data_ptr() if t is not None else None for t in g), grad.data_ptr(), grad.shape[1],
                                                      logits.device.index, _stream(logits.device)))

@@ -171,3 +171,61 @@ def test_other_dispatch_modes_change_nothing(path):
     with Through():
         got = calls()
     assert all(torch.equal(a.float(), b.float()) for a, b in zip(got, want))
+
+
+class Spread:
+    """Saved tensors in every other place of a larger one, the places between filled with something else."""
+
+    def __enter__(self):
+        def pack(t):
+            big = torch.full((*t.shape[:-1], 2 * t.shape[-1]), 77, dtype=t.dtype, device=t.device)
+            big[..., ::2] = t
+            return big
+        self.hooks = torch.autograd.graph.saved_tensors_hooks(pack, lambda big: big[..., ::2])
+        return self.hooks.__enter__()
+
+    def __exit__(self, *e):
+        return self.hooks.__exit__(*e)
+
+
+@gpu
+def test_saved_tensors_come_back_as_their_hooks_give_them(path):
+    """In another layout, or by way of the host: the same gradient."""
+    _, _, _, _, _, logits, tokens = operands(rows=4, V=1001)
+    mask = torch.randint(-2 ** 31, 2 ** 31 - 1, (4, 32), generator=torch.Generator().manual_seed(3), dtype=torch.int32).cuda()
+
+    def grad():
+        on = logits.clone().requires_grad_()
+        got = zf.token_logprobs(on, tokens[:, None].repeat(1, 3), mask, entropy=True, top=4)
+        return on, (got.logprobs.nan_to_num(0, 0, 0).sum() * 0.5 + got.entropy.square().sum() + got.top_logprobs.sum())
+
+    on, loss = grad()
+    want, = torch.autograd.grad(loss, on)
+    for hooks in (Spread(), torch.autograd.graph.save_on_cpu(), torch.autograd.graph.save_on_cpu(pin_memory=True)):
+        with hooks:
+            on, loss = grad()
+        got, = torch.autograd.grad(loss, on)
+        assert torch.equal(got, want)
+
+
+@gpu
+def test_saved_tensors_that_came_back_as_others_are_refused(path):
+    """Left on the host, of another type or shape: an error before anything is read."""
+    _, _, _, _, _, logits, tokens = operands(rows=4, V=1001)
+    mask = torch.full((4, 32), -1, dtype=torch.int32, device="cuda")
+
+    def only(pick, change):
+        return torch.autograd.graph.saved_tensors_hooks(lambda t: t, lambda t: change(t) if pick(t) else t)
+
+    def lost(pick, change):
+        on = logits.clone().requires_grad_()
+        with only(pick, change):
+            got = zf.token_logprobs(on, tokens, mask, entropy=True, top=4)
+            loss = got.logprobs.sum() + got.entropy.sum() + got.top_logprobs.sum()
+        with pytest.raises(RuntimeError, match="saved"):
+            loss.backward()
+
+    for pick in (lambda t: tuple(t.shape) == (4, 1001), lambda t: tuple(t.shape) == (4, 32), lambda t: t.dtype == torch.int64, lambda t: tuple(t.shape) == (4,) and t.dtype == torch.float32,
+                 lambda t: tuple(t.shape) == (4, 4) and t.dtype == torch.int32, lambda t: tuple(t.shape) == (4, 4) and t.dtype == torch.float32, lambda t: tuple(t.shape) == (4, 2)):
+        for change in (lambda t: t.cpu(), lambda t: t[:2], lambda t: t.to(torch.float16), lambda t: t.to_sparse(), lambda t: t[..., :1] if t.dim() > 1 else t[:1]):
+            lost(pick, change)
