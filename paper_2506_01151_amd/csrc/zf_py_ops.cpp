@@ -123,7 +123,7 @@ Tensor kept(const Tensor &t, const char *what, const Tensor &with, at::ScalarTyp
                 " came back with another device, type or shape: ", t.toString(), " ", t.sizes(), " on ", t.device(), " instead of ", size, " on ", with.device());
     TORCH_CHECK(!has_tangent(t), "token_logprobs: its gradient has no forward-mode derivative");
     const bool as_it_is = rows_apart ? t.dim() == 2 && t.stride(1) == 1 && row_stride(t) >= t.size(1) : t.is_contiguous();
-    return as_it_is && plain(t) ? t : t.detach().contiguous();
+    return as_it_is && plain(t) ? t : t.detach().resolve_neg().contiguous();
 }
 
 struct TokenLogprobs : public torch::autograd::Function<TokenLogprobs> {

@@ -44,6 +44,7 @@ def _need(ok, why):
 
 def _plain(t, what):
     """A kernel is given the tensor's address: what else there is to a tensor would be lost."""
+    _need(not t.is_neg(), f"{what}: a negated view is not taken (resolve_neg makes a tensor of it)")
     _need(not torch._C._functorch.is_functorch_wrapped_tensor(t) and forward_ad.unpack_dual(t).tangent is None, f"{what}: there is no forward-mode derivative, nor another of torch.func's transforms")
 
 
@@ -194,6 +195,7 @@ class _TokenLogprobs(torch.autograd.Function):
 def _kept(t, what, dtypes, shape, device, rows_apart=False):
     """A saved tensor, or an incoming gradient, for a kernel to read: what hooks on saved tensors give back may lie anywhere, in any order."""
     _need(t.layout == torch.strided and t.device == device and t.dtype in dtypes and tuple(t.shape) == tuple(shape), f"saved {what}: {tuple(t.shape)} of {t.dtype} on {t.device} came back instead of {tuple(shape)} on {device}")
+    t = t.resolve_neg()
     _plain(t, f"saved {what}")
     as_it_is = t.stride(1) == 1 and _row_stride(t) >= t.shape[1] if rows_apart else t.is_contiguous()
     return t if as_it_is else t.contiguous()

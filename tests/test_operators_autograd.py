@@ -229,3 +229,21 @@ def test_saved_tensors_that_came_back_as_others_are_refused(path):
                  lambda t: tuple(t.shape) == (4, 4) and t.dtype == torch.int32, lambda t: tuple(t.shape) == (4, 4) and t.dtype == torch.float32, lambda t: tuple(t.shape) == (4, 2)):
         for change in (lambda t: t.cpu(), lambda t: t[:2], lambda t: t.to(torch.float16), lambda t: t.to_sparse(), lambda t: t[..., :1] if t.dim() > 1 else t[:1]):
             lost(pick, change)
+
+
+@gpu
+def test_negated_views_are_refused_or_resolved(path):
+    """A view that stands for its memory's negative (torch's imaginary parts of conjugates are such): refused as an input, its values taken as a gradient."""
+    x, q, s, w, ws, logits, tokens = operands()
+    mask = torch.full((3, 10), -1, dtype=torch.int32, device="cuda")
+    neg = torch._neg_view
+    for call in (lambda: zf.quantize_blocks(neg(x)), lambda: zf.head_logits(q, neg(s), w, ws), lambda: zf.head_logits(q, s, w, neg(ws)), lambda: zf.head_logits(q, s, w, ws, neg(mask)), lambda: zf.head_logits(q, s, w, ws, out=neg(logits)),
+                 lambda: zf.token_logprobs(neg(logits), tokens), lambda: zf.token_logprobs(logits, neg(tokens)), lambda: zf.token_logprobs(logits, tokens, neg(mask))):
+        refused(call, "negated")
+    on = logits.clone().requires_grad_()
+    got = zf.token_logprobs(on, tokens, entropy=True, top=2)
+    gs = [torch.randn(t.shape, generator=torch.Generator().manual_seed(9)).cuda() for t in (got.logprobs, got.entropy, got.top_logprobs)]
+    outs = (got.logprobs, got.entropy, got.top_logprobs)
+    want, = torch.autograd.grad(outs, on, [-g for g in gs], retain_graph=True)
+    grad, = torch.autograd.grad(outs, on, [neg(g) for g in gs])
+    assert torch.equal(grad, want)
