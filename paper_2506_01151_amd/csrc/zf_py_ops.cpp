@@ -223,10 +223,7 @@ PyObject *guarded(PyObject *, PyObject *const *args, Py_ssize_t n) {
         Py_XDECREF(r);
         if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, "an error code that raises nothing");
         return nullptr;
-    } catch (const c10::OutOfMemoryError &e) {
-        PyErr_SetString(PyExc_MemoryError, e.what_without_backtrace());
-        return nullptr;
-    } catch (...) {}                   // a tensor that torch does not let be looked at
+    } catch (...) {}                   // a tensor that torch does not let be looked at, no memory: operators.py meets the same and raises what torch raises
     Py_RETURN_NONE;
 }
 

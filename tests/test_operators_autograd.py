@@ -247,3 +247,21 @@ def test_negated_views_are_refused_or_resolved(path):
     want, = torch.autograd.grad(outs, on, [-g for g in gs], retain_graph=True)
     grad, = torch.autograd.grad(outs, on, [neg(g) for g in gs])
     assert torch.equal(grad, want)
+
+
+@gpu
+def test_no_memory_is_torch_s_own_error(path):
+    """What torch's other calls raise then, which programs catch to try a smaller batch."""
+    x, q, s, w, ws, logits, _ = operands()
+    x, many = torch.zeros((1 << 22, 1), device="cuda"), torch.zeros((1 << 17, 128), device="cuda").to(torch.float8_e4m3fn)
+    scale = torch.ones((1 << 17, 1), device="cuda")
+    torch.cuda.empty_cache()
+    free, total = torch.cuda.mem_get_info()
+    torch.cuda.set_per_process_memory_fraction((torch.cuda.memory_reserved() + (64 << 20)) / total)      # (a limit of torch's allocator: the device is not asked)
+    try:
+        for call in (lambda: zf.quantize_blocks(x), lambda: zf.head_logits(many, scale, many[:4096], scale[:32])):
+            with pytest.raises(torch.OutOfMemoryError):
+                call()
+    finally:
+        torch.cuda.set_per_process_memory_fraction(1.0)
+    assert zf.quantize_blocks(x[:128])[0].shape == (128, 128)
