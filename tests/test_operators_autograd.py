@@ -265,3 +265,69 @@ def test_no_memory_is_torch_s_own_error(path):
     finally:
         torch.cuda.set_per_process_memory_fraction(1.0)
     assert zf.quantize_blocks(x[:128])[0].shape == (128, 128)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("grad", [False, True])
+def test_the_extension_module_does_what_the_definition_does(monkeypatch, dtype, grad):
+    """The same bits of every result and gradient, with everything asked for and with parts of it; the same refusals."""
+    from paper_2506_01151_amd import operators as ops
+    taken = ops._native_ops
+    g = torch.Generator().manual_seed(31)
+
+    class Untaken:
+        quantize_blocks = head_logits = token_logprobs = staticmethod(lambda *a: None)
+
+    def both(call):
+        res = []
+        for module in (taken, Untaken):
+            monkeypatch.setattr(ops, "_native_ops", module)
+            try:
+                res.append([t if t is None else t.detach().float().cpu() for t in call()])
+            except zf.ZfError as e:
+                res.append((e.code, str(e)))
+        monkeypatch.setattr(ops, "_native_ops", taken)
+        assert len(res[0]) == len(res[1])
+        for a, b in zip(*res):
+            assert type(a) is type(b) and (torch.equal(a.nan_to_num(9.0, 8.0, 7.0), b.nan_to_num(9.0, 8.0, 7.0)) if isinstance(a, torch.Tensor) else a == b), (a, b)
+
+    for rows, V, n, top, entropy, masked, layout in ((1, 1, 0, 1, True, False, "packed"), (5, 700, 1, 0, True, True, "padded"), (3, 40037, 4, 7, False, True, "odd"), (2, 9001, None, 3, True, True, "packed"), (33, 515, 0, 0, False, False, "odd"),
+                                                     (4, 32768, 70, 64, True, False, "padded"), (6, 33, None, 0, True, False, "packed")):
+        buf = torch.randn((rows * (V + 5) + 1,), generator=g).to(dtype).cuda()
+        x = buf[1:].view(rows, V + 5)[:, :V] if layout != "packed" else buf[:rows * V].view(rows, V)
+        if layout == "padded":
+            x = torch.nn.functional.pad(x, (0, 64 - V % 64))[:, :V]
+        tokens = None if n is None else torch.randint(-1, V + 1, (rows, n) if n else (rows,), generator=g).to(torch.int32 if V % 2 else torch.int64).cuda()
+        mask = torch.randint(-2 ** 31, 2 ** 31 - 1, (rows, (V + 31) // 32), generator=g, dtype=torch.int32).cuda() if masked else None
+
+        def call():
+            on = x.detach().requires_grad_(grad)
+            got = zf.token_logprobs(on, tokens, mask, temperature=0.7, entropy=entropy, top=top)
+            if not grad:
+                return got
+            outs = [t for t in (got.logprobs, got.entropy, got.top_logprobs) if t is not None]
+            res = list(got)
+            for some in [outs] + ([[t] for t in outs] if outs else []):
+                if some:
+                    ws = [torch.linspace(-1, 2, t.numel(), device="cuda").view(t.shape) for t in some]
+                    res += torch.autograd.grad(some, on, ws, retain_graph=True)
+            return res
+
+        both(call)
+    for rows, cols in ((1, 1), (130, 300), (5, 4096), (257, 1000)):
+        x = torch.randn((rows, cols), generator=g).to(dtype).cuda()
+        for block_rows in (1, 128):
+            both(lambda: [t.view(torch.uint8) if t.dtype == torch.float8_e4m3fn else t for t in zf.quantize_blocks(x, block_rows=block_rows)])
+    for M, V, K in ((1, 300, 256), (33, 9001, 384), (130, 515, 128)):
+        q, s = zf.quantize_blocks(torch.randn((M, K), generator=g).cuda())
+        w, ws = zf.quantize_blocks(torch.randn((V, K), generator=g).cuda(), block_rows=128)
+        mask = torch.randint(-2 ** 31, 2 ** 31 - 1, (M, (V + 31) // 32), generator=g, dtype=torch.int32).cuda()
+        both(lambda: [zf.head_logits(q, s, w, ws, dtype=dtype)])
+        both(lambda: [zf.head_logits(q, s, w, ws, mask, dtype=dtype)])
+    x = torch.zeros((2, 256), device="cuda", dtype=dtype, requires_grad=grad)
+    t, m = torch.zeros(2, dtype=torch.int64, device="cuda"), torch.zeros((2, 8), dtype=torch.int32, device="cuda")
+    for bad in (lambda: zf.quantize_blocks(x, block_rows=2), lambda: zf.quantize_blocks(x.half()), lambda: zf.quantize_blocks(x.t()), lambda: zf.quantize_blocks(x.detach()[:1].expand(3, 256)), lambda: zf.token_logprobs(x, t, m[:, :7]),
+                lambda: zf.token_logprobs(x, t, top=65), lambda: zf.token_logprobs(x, t, temperature=0.0), lambda: zf.token_logprobs(x, t, temperature=1e-40), lambda: zf.token_logprobs(x, t, temperature=1e39), lambda: zf.token_logprobs(x, t.float()),
+                lambda: zf.token_logprobs(x, t.cpu()), lambda: zf.token_logprobs(x, t[:1]), lambda: zf.token_logprobs(x, torch.zeros((2, 1025), dtype=torch.int64, device="cuda"))):
+        both(bad)
