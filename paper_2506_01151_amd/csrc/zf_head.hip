@@ -196,7 +196,8 @@ __device__ __forceinline__ i32x4 piece_at(const uint8_t *p) { return *reinterpre
 // ---- memory straight into LDS ----
 //
 // 64 lanes' 16 (or 4) bytes, each from its address, to consecutive places of LDS from `at` on.  As an instruction: it has no register for a result, and the
-// compiler, which does not see it, leaves the waits to the caller instead of waiting in front of every read of LDS.
+// compiler, which does not see it, leaves the waits to the caller instead of waiting in front of every read of LDS.  Its place comes from m0, which the compiler allots to
+// nothing and, being reserved, is not to be named as overwritten: no other instruction of these kernels may use it (a test reads the assembly).
 __device__ __forceinline__ void to_lds(const uint8_t *base, uint32_t off, uint32_t at) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(at), "v"(off), "s"(base) : "memory");
 }
