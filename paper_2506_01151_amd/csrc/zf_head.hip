@@ -4,13 +4,14 @@
 //   y[m][v] = sum_k xs[m][k] ws[v / 128][k] (sum over the 128 columns of block k of x[m][..] w[v][..])
 //
 // One v_mfma_f32_16x16x128_f8f6f4 takes 16 tokens, 16 rows of the batch and exactly one block of columns, so a block's inner sum
-// is one instruction from zero and its scale one fused multiply-add for each of the four results that a lane holds.  Sums are held in 32 bits.  The order of
+// is one instruction from zero and its scale one fused multiply-add for each of the four results that a lane holds.  The sum over the blocks is held in 32 bits.  The order of
 // the 128 columns within the instruction's operands does not matter as long as it is the same for both: a lane takes bytes 16 c .. 16 c + 15 and
 // 64 + 16 c .. 64 + 16 c + 15 of a block, c = lane / 16, of the row that is its lane % 16.
-//   The 8-bit instructions are not exact to 32 bits, whatever their shape: of eight neighbouring products they keep what lies less than about 2^-14
-// below the largest (measured: blocks of normal numbers come out 1.3e-5 off relative to their norm, of numbers spread over e^2 5e-5).  For logits in bf16, which are
-// rounded by up to 2^-9 anyway, that is nothing.  For fp32 logits the operands are brought to bf16, which holds every e4m3 number, and
-// four v_mfma_f32_16x16x32_bf16 make the block's sum (1e-8 and 7e-8 off), at half the rate.
+//   The 8-bit instructions do not hold a block's sum in 32 bits, whatever their shape: of eight neighbouring products each is cut, towards zero, to a multiple of 2^-13 of the largest one's power of
+// two (measured: one of 2^-14 beside it is gone; the largest itself is exact).  So a logit is off by less than 7 x 2^-13 of the sum of its products' sizes; blocks of normal numbers come out 1.3e-5
+// off relative to their norm, of numbers spread over e^2 5e-5, root of the mean square.  Logits in bf16 take them: one about as large as its norm is rounded by up to 2^-8 of itself anyway, 300 times
+// that; one whose products cancel to a hundredth of their norm or less carries more of this than of its rounding.  The same product in bf16 instructions would take twice the time where the product
+// bounds it.  For fp32 logits the operands are brought to bf16, which holds every e4m3 number, and four v_mfma_f32_16x16x32_bf16 make the block's sum (1e-8 and 7e-8 off), at half the rate.
 #include <hip/hip_runtime.h>
 #include <algorithm>
 #include <atomic>
