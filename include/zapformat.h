@@ -256,7 +256,7 @@ int zf_apply_mask(zf_engine *e, const void *d_logits, void *d_out, int32_t dtype
  * max(largest |x| of the block / 448, 2^-126).  A block is 128 columns of block_rows = 1 row (activations) or of block_rows = 128
  * rows (weights).  x: device, [rows][row_stride_elems], cols valid elements per row.  q: device, [rows][P], P = cols rounded
  * up to a multiple of 128, the columns from cols on zero; scale: device, [ceil(rows / block_rows)][P / 128].  A block with
- * an infinity has an infinite scale (the infinity becomes NaN, the others 0); a NaN stays one. */
+ * an infinity has an infinite scale (the infinity becomes NaN, the others 0); a NaN stays one.  Up to 2^24 - 1 blocks of 128 rows a call. */
 int zf_quantize_blocks(const void *d_x, int32_t dtype, int64_t rows, int32_t cols, int64_t row_stride_elems, int32_t block_rows,
                        uint8_t *d_q, float *d_scale, int32_t device, void *hip_stream);
 

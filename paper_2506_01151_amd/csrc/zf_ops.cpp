@@ -60,6 +60,7 @@ int zf_quantize_blocks(const void *d_x, int32_t dtype, int64_t rows, int32_t col
         if (rows < 0 || rows > INT32_MAX || cols < 1 || cols > (1 << 24)) return refuse("rows must be 0..2^31-1, cols 1..2^24");
         if (row_stride_elems < cols) return refuse("the row stride is smaller than cols");
         if (block_rows != 1 && block_rows != SCALE_BLOCK) return refuse("block_rows must be 1 or 128");
+        if (block_rows == SCALE_BLOCK && (rows + SCALE_BLOCK - 1) / SCALE_BLOCK * (((int64_t)cols + SCALE_BLOCK - 1) / SCALE_BLOCK) > BLOCKS_MAX) return refuse("more blocks than a call takes: split the rows");
         if (rows == 0) return ZF_OK;
         if (!d_x || !d_q || !d_scale) return refuse("null argument");
         if (!element_aligned(d_x, dtype) || (uintptr_t)d_q % 16) return refuse("x must be aligned to an element, q to 16 bytes");
