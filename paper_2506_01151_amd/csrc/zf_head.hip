@@ -220,33 +220,31 @@ __device__ __forceinline__ uint32_t lds_at(const void *p) { return (uint32_t)(ui
 //
 // A workgroup takes ranges of TOKENS tokens, each of one scale, and up to 16 MT rows of the batch.  Under a mask it lists the tokens that some of its rows allows, of up to
 // RANGES ranges at a time.
-//   Long lists, a range at a time: a wavefront takes a quarter of it.  Blocks of columns of the weight's rows and the activations come straight into LDS, STAGES - STEP blocks ahead, in
+//   Long lists, a range at a time: a wavefront takes a quarter of it.  Blocks of columns of the weight's rows and the activations come straight into LDS, STAGES - 1 blocks ahead, in
 // lines: a fragment's own addresses (sixteen rows, 16 bytes of each) are taken a lane at a time, at a quarter of the rate.  Every wavefront issues the same number of loads for a
-// block, so that a count says which have arrived; one barrier a block, or (PAIRS) for two, whose lines of
-// one row are asked for one after the other.  Piece c of row r lies at place c ^ (r % 8), so that eight rows' pieces of one
+// block, so that a count says which have arrived; one barrier a block.  Piece c of row r lies at place c ^ (r % 8), so that eight rows' pieces of one
 // column lie in different banks (the loads write LDS in lanes' order: it is their addresses in memory that are exchanged).  Results gather in LDS, so that the logits
 // go out in whole rows of the range, -inf where nothing was computed.
-//   The weight's way from memory bounds it: 16 rows x 128,256 x 4,096 bf16 96 us (5.5 TB/s), 64 rows 114 (4.6); one row x 32,000 x 4,096 25 (5.3).  With 64 rows fp32 logits' operands, brought to bf16 in every wavefront, take two fifths of the time beside it: 64 x 152,064 x 2,048 fp32 80 us, bf16 73.  Under
+//   The weight's way from memory bounds it: 16 rows x 128,256 x 4,096 bf16 103 us (5.1 TB/s), x 8,192 187 (5.6), 64 rows x 4,096 114 to 118 (4.5); one row x 32,000 x 4,096 29 (4.4).  With 64 rows fp32 logits' operands, brought to bf16 in every wavefront, take two fifths of the time beside it: 64 x 152,064 x 2,048 fp32 80 us, bf16 73.  Under
 // masks workgroups take two or three ranges each, and the last ones run alone: 87 and 80.
 //   Up to 32 tokens of all ranges, or of one (TOKENS = 16 has no others), sixteen at a time: the wavefronts take every fourth block of columns each, the weight straight to registers,
 // activations through LDS (TOKENS = 16: straight to registers), and join their sums in a fixed order.  Everything is -inf first.  (16 x 128,256 x 4,096 with 200 tokens a
 // row: 13.6 us; when every range was a workgroup's own 22.)
-template <int MT, int TOKENS, bool PAIRS, bool MASK>
+template <int MT, int TOKENS, bool MASK>
 struct RowsLds {
     static constexpr int ROWS = MT * 16, PITCH = TOKENS + 4, RANGES = MASK && TOKENS > 16 ? 4 : 1, SHORT = 32;
     static constexpr int X_AT = TOKENS * SCALE_BLOCK, S_AT = X_AT + ROWS * SCALE_BLOCK, STAGE = S_AT + 64 * 4;   // weight, activations, their scales
-    static constexpr int STAGES = TOKENS == 64 ? (PAIRS ? 6 : 7) : MT == 1 ? 4 : 3, STEP = PAIRS ? 2 : 1;
+    static constexpr int STAGES = TOKENS == 64 ? 7 : MT == 1 ? 4 : 3;
     static constexpr int OWN = TOKENS > 16 ? TOKENS / 4 : 16, W_LOADS = OWN / 8, G = OWN / 16, LOADS = W_LOADS + (MT + 1) / 2 + 1;                       // of a wavefront for a stage
     static constexpr int SPAN = MT == 1 ? 4096 : 1024;      // columns of the activations that the short form has in LDS
     static constexpr int LOOP = TOKENS > 16 ? STAGES * STAGE : 0, TILE = TOKENS > 16 ? ROWS * PITCH * 4 : 0, JOIN = 3 * ROWS * 16 * 4;  // the loop, then the logits; the short form's sums
     static constexpr int BYTES = LOOP > TILE ? (LOOP > JOIN ? LOOP : JOIN) : (TILE > JOIN ? TILE : JOIN);
-    static_assert(STAGES % STEP == 0, "pairs");
     static_assert(!MASK || TOKENS == 16 || ROWS * SPAN <= STAGES * STAGE, "the short form's activations lie in the stages' memory");
 };
 
-template <int MT, int TOKENS, bool PAIRS, bool MASK, typename ElemT>
+template <int MT, int TOKENS, bool MASK, typename ElemT>
 __global__ __launch_bounds__(256, 2) void head_rows_kernel(HeadArgs a, int32_t n_ranges) {
-    typedef RowsLds<MT, TOKENS, PAIRS, MASK> Lds;
+    typedef RowsLds<MT, TOKENS, MASK> Lds;
     constexpr int ROWS = Lds::ROWS, PITCH = Lds::PITCH, WORDS = (TOKENS + 31) / 32, STAGES = Lds::STAGES, RANGES = Lds::RANGES, EPV = 16 / sizeof(ElemT);
     extern __shared__ __align__(16) uint8_t mem[];
     __shared__ uint32_t words[MASK ? RANGES : 1][MASK ? ROWS : 1][WORDS], need[RANGES][WORDS];
@@ -377,7 +375,7 @@ __global__ __launch_bounds__(256, 2) void head_rows_kernel(HeadArgs a, int32_t n
     // The listed tokens of one range, `count` from `at` on, 32 a wavefront.
     auto long_form = [&](int32_t v0, int at, int count) {
         constexpr int XN = (MT + 1) / 2;                                     // groups of eight of the activations' rows that a wavefront brings
-        constexpr int WL = Lds::W_LOADS, G = Lds::G, OWN = Lds::OWN, STEP = Lds::STEP;
+        constexpr int WL = Lds::W_LOADS, G = Lds::G, OWN = Lds::OWN;
         const uint8_t *from[WL + XN];
         const int place = (lane % 8 ^ lane / 8) * 16, first = wave * OWN;
 #pragma unroll
@@ -391,26 +389,16 @@ __global__ __launch_bounds__(256, 2) void head_rows_kernel(HeadArgs a, int32_t n
         const auto *const ws = (const __attribute__((address_space(4))) float *)(a.ws + (size_t)(v0 / SCALE_BLOCK) * n_k);   // read by the scalar unit
         // Workgroups begin at blocks of columns of their own: rows lie at multiples of a power of two, and who reads the same columns of many rows asks
         // few of the memory's channels (16 x 128,256 x 4,096: 113 us when all begin at the first, 103 so).
-        const int32_t turn = (int32_t)(blockIdx.x * 5u % (uint32_t)((n_k + STEP - 1) / STEP)) * STEP;
+        const int32_t turn = (int32_t)(blockIdx.x * 5u % (uint32_t)n_k);
         auto turned = [&](int32_t k) { return k + turn < n_k ? k + turn : k + turn - n_k; };
         auto fetch = [&](int32_t k) {                                        // behind the last block: that one once more, for the count
-            uint32_t to[STEP];
-            int32_t kk[STEP];
+            const uint32_t to = lds_at(mem) + k % STAGES * Lds::STAGE;
+            const int32_t kk = turned(k < n_k ? k : n_k - 1);
 #pragma unroll
-            for (int u = 0; u < STEP; u++) {
-                to[u] = lds_at(mem) + (k + u) % STAGES * Lds::STAGE;
-                kk[u] = turned(k + u < n_k ? k + u : n_k - 1);
-            }
+            for (int i = 0; i < WL; i++) to_lds(from[i] + (size_t)kk * SCALE_BLOCK, to + (first + i * 8) * SCALE_BLOCK);
 #pragma unroll
-            for (int i = 0; i < WL; i++)
-#pragma unroll
-                for (int u = 0; u < STEP; u++) to_lds(from[i] + (size_t)kk[u] * SCALE_BLOCK, to[u] + (first + i * 8) * SCALE_BLOCK);
-#pragma unroll
-            for (int i = 0; i < XN; i++)
-#pragma unroll
-                for (int u = 0; u < STEP; u++) to_lds(from[WL + i] + (size_t)kk[u] * SCALE_BLOCK, to[u] + Lds::X_AT + (wave * XN + i) % (2 * MT) * 8 * SCALE_BLOCK);
-#pragma unroll
-            for (int u = 0; u < STEP; u++) to_lds(xs + kk[u], to[u] + Lds::S_AT);
+            for (int i = 0; i < XN; i++) to_lds(from[WL + i] + (size_t)kk * SCALE_BLOCK, to + Lds::X_AT + (wave * XN + i) % (2 * MT) * 8 * SCALE_BLOCK);
+            to_lds(xs + kk, to + Lds::S_AT);
         };
         // The compiler has loads of the short form in mind, whose registers it uses again in the loop, and would wait there for all loads in flight: it is
         // told here that none is (64 x 152,064 x 2,048 under masks, bf16: 95 us -> 80).
@@ -421,43 +409,38 @@ __global__ __launch_bounds__(256, 2) void head_rows_kernel(HeadArgs a, int32_t n
 #pragma unroll
             for (int t = 0; t < MT; t++) acc[g][t] = f32x4{0, 0, 0, 0};
 #pragma unroll
-        for (int k = 0; k < STAGES / STEP - 1; k++) fetch(k * STEP);
-        for (int32_t k2 = 0; k2 < n_k; k2 += STEP) {
-            arrived<(STAGES / STEP - 2) * STEP * Lds::LOADS>();
+        for (int k = 0; k < STAGES - 1; k++) fetch(k);
+        for (int32_t k = 0; k < n_k; k++) {
+            arrived<(STAGES - 2) * Lds::LOADS>();
             __syncthreads();
-            fetch(k2 + STAGES - STEP);
+            fetch(k + STAGES - 1);
+            const uint8_t *const stage = mem + k % STAGES * Lds::STAGE;
+            const float s_w = ws[turned(k)];
+            Operand<ElemT> w[G];
 #pragma unroll
-            for (int u = 0; u < STEP; u++) {
-                const int32_t k = k2 + u;
-                if (k >= n_k) break;
-                const uint8_t *const stage = mem + k % STAGES * Lds::STAGE;
-                const float s_w = ws[turned(k)];
-                Operand<ElemT> w[G];
+            for (int g = 0; g < G; g++) {
+                const uint8_t *const p = stage + (first + g * 16 + lane % 16) * SCALE_BLOCK;
+                w[g].take(piece_at(p + c0), piece_at(p + c1));
+            }
+            constexpr int PAIR = MT > 1 ? 2 : 1;                             // sixteens of rows at a time
 #pragma unroll
-                for (int g = 0; g < G; g++) {
-                    const uint8_t *const p = stage + (first + g * 16 + lane % 16) * SCALE_BLOCK;
-                    w[g].take(piece_at(p + c0), piece_at(p + c1));
+            for (int t0 = 0; t0 < MT; t0 += PAIR) {
+                Operand<ElemT> v[PAIR];
+                float s[PAIR];
+                f32x4 part[G][PAIR];
+#pragma unroll
+                for (int t = 0; t < PAIR; t++) {
+                    const int r = (t0 + t) * 16 + lane % 16;
+                    v[t].take(piece_at(stage + Lds::X_AT + r * SCALE_BLOCK + c0), piece_at(stage + Lds::X_AT + r * SCALE_BLOCK + c1));
+                    s[t] = reinterpret_cast<const float *>(stage + Lds::S_AT)[r] * s_w;
                 }
-                constexpr int PAIR = MT > 1 ? 2 : 1;                             // sixteens of rows at a time
+                multiply(w, v, part);
 #pragma unroll
-                for (int t0 = 0; t0 < MT; t0 += PAIR) {
-                    Operand<ElemT> v[PAIR];
-                    float s[PAIR];
-                    f32x4 part[G][PAIR];
+                for (int t = 0; t < PAIR; t++)
 #pragma unroll
-                    for (int t = 0; t < PAIR; t++) {
-                        const int r = (t0 + t) * 16 + lane % 16;
-                        v[t].take(piece_at(stage + Lds::X_AT + r * SCALE_BLOCK + c0), piece_at(stage + Lds::X_AT + r * SCALE_BLOCK + c1));
-                        s[t] = reinterpret_cast<const float *>(stage + Lds::S_AT)[r] * s_w;
-                    }
-                    multiply(w, v, part);
+                    for (int g = 0; g < G; g++)
 #pragma unroll
-                    for (int t = 0; t < PAIR; t++)
-#pragma unroll
-                        for (int g = 0; g < G; g++)
-#pragma unroll
-                            for (int e = 0; e < 4; e++) acc[g][t0 + t][e] = fmaf(s[t], part[g][t][e], acc[g][t0 + t][e]);
-                }
+                        for (int e = 0; e < 4; e++) acc[g][t0 + t][e] = fmaf(s[t], part[g][t][e], acc[g][t0 + t][e]);
             }
         }
         arrived<0>();
@@ -722,39 +705,35 @@ hipError_t head_tile_of(const HeadArgs &a, int tokens, hipStream_t s) {
     return tokens == 256 ? head_tile<MJ, 4, MASK, ElemT>(a, s) : tokens == 192 ? head_tile<MJ, 3, MASK, ElemT>(a, s) : head_tile<MJ, 2, MASK, ElemT>(a, s);
 }
 
-template <int MT, int TOKENS, bool PAIRS, bool MASK, typename ElemT>
+template <int MT, int TOKENS, bool MASK, typename ElemT>
 hipError_t head_rows(const HeadArgs &a, hipStream_t s) {
-    typedef RowsLds<MT, TOKENS, PAIRS, MASK> Lds;
+    typedef RowsLds<MT, TOKENS, MASK> Lds;
     static std::atomic<uint64_t> allowed{0};
-    const hipError_t e = allow_lds((const void *)head_rows_kernel<MT, TOKENS, PAIRS, MASK, ElemT>, Lds::BYTES, allowed);
+    const hipError_t e = allow_lds((const void *)head_rows_kernel<MT, TOKENS, MASK, ElemT>, Lds::BYTES, allowed);
     if (e != hipSuccess) return e;
     // Without a mask a workgroup a range.  With one as many as the compute units hold, so that those with little to do in a range have several.
     const int32_t n = (a.V + TOKENS - 1) / TOKENS;
     const dim3 grid(Lds::RANGES > 1 ? std::min(n, 2 * COMPUTE_UNITS) : n, (a.M + MT * 16 - 1) / (MT * 16));
-    hipLaunchKernelGGL((head_rows_kernel<MT, TOKENS, PAIRS, MASK, ElemT>), grid, dim3(256), Lds::BYTES, s, a, n);
+    hipLaunchKernelGGL((head_rows_kernel<MT, TOKENS, MASK, ElemT>), grid, dim3(256), Lds::BYTES, s, a, n);
     return hipSuccess;
 }
 // Ranges of 16 tokens where those of 128 would leave three compute units of four idle (one row x 2,048 x 1,024: 4.2 us, 6.0 in ranges of 128; 64 rows x 8,192 x 1,024: 10.1 and 9.2).
 // Ranges of 64 where each finds a compute unit of its own (bf16, x 4,096: 8 rows x 9,000 12.4 us, in ranges of 128 16.0; 8 x 16,384 15.1 and 18.5; 64 x 10,000 19.2 and 25.0; 64 x 16,000 under
-// masks 24.4 and 32.7), not where some find one and others share (8 x 20,000 x 4,096: 21.3 and 19.5).
-// Pairs of blocks for long rows (memory likes the two lines of a row together): in ranges of 64 where two fill each compute unit (8 x 32,000 x 4,096 25.1 us, in ranges of 128, block by
-// block, 28.4; 30 x 32,000 27.3 and 29.0), in ranges of 128 beyond that and with so few rows that two workgroups of four blocks each fit a compute unit (16 x 50,257 x 4,096 43.3 and 45.7; 16 x
-// 128,256 96.6 and 100.0); not below, where there is too little on its way (8 x 20,000 x 4,096 23.6 and 19.6), nor for short rows (8 x 32,000 x 1,024 9.5 and 9.1; 16 x 70,000 x 1,024 20.9 and 19.8).
+// masks 24.4 and 32.7; of short rows some lose a little, 8 x 16,384 x 512 5.2 and 4.9, others win, 64 rows 6.8 and 7.4), not where some find one and others share (8 x 20,000: x 4,096 22.8 and
+// 19.7, x 1,024 8.3 and 6.6).
 template <int MT, bool MASK, typename ElemT>
 hipError_t head_few(const HeadArgs &a, hipStream_t s) {
     const int32_t n = (a.V + 63) / 64;                                       // ranges of 64
-    if (n < 128) return head_rows<MT, 16, false, MASK, ElemT>(a, s);
-    if (n <= COMPUTE_UNITS) return head_rows<MT, 64, false, MASK, ElemT>(a, s);
-    if constexpr (!MASK && MT <= 2) { if (a.K >= 4096 && n > 2 * COMPUTE_UNITS * 7 / 8 && n <= 2 * COMPUTE_UNITS) return head_rows<MT, 64, true, MASK, ElemT>(a, s); }
-    if constexpr (!MASK && MT == 1) { if (a.K >= 4096 && n > 2 * COMPUTE_UNITS) return head_rows<MT, 128, true, MASK, ElemT>(a, s); }
-    return head_rows<MT, 128, false, MASK, ElemT>(a, s);
+    if (n < 128) return head_rows<MT, 16, MASK, ElemT>(a, s);
+    if (n <= COMPUTE_UNITS) return head_rows<MT, 64, MASK, ElemT>(a, s);
+    return head_rows<MT, 128, MASK, ElemT>(a, s);
 }
 template <bool MASK, typename ElemT>
 hipError_t head(const HeadArgs &a, hipStream_t s) {
     if (a.M <= 16) return head_few<1, MASK, ElemT>(a, s);
     if (a.M <= 32) return head_few<2, MASK, ElemT>(a, s);
     if (a.M <= 64) return head_few<4, MASK, ElemT>(a, s);
-    if ((a.w_stride | a.x_stride) >= (1 << 24)) return head_rows<4, 128, false, MASK, ElemT>(a, s);   // a tile's rows would not lie within 32 bits
+    if ((a.w_stride | a.x_stride) >= (1 << 24)) return head_rows<4, 128, MASK, ElemT>(a, s);   // a tile's rows would not lie within 32 bits
     // Tiles of 128, 192 or 256 rows (operands in bf16 take twice the registers: 128) and as many tokens, whichever are done first: tiles that a compute unit has, a tile's work and 64 more
     // in each direction for what it costs whatever its size; smaller ones have to promise a twentieth (1,030 x 32,000 x 4,096 fp32 283 us, with 192 tokens 289).  With 256 tokens alone and
     // so: 70 x 32,000 x 1,024 bf16 16.9 and 13.4 us, fp32 20.5 and 15.7; 130 x 32,000 x 4,096 bf16 58.3 and 47.0; 256 rows 65.0 and 57.5; 100 x 8,192 x 2,048 18.3 and 14.7; 300 x 32,000 x 4,096
