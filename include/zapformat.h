@@ -262,8 +262,8 @@ int zf_quantize_blocks(const void *d_x, int32_t dtype, int64_t rows, int32_t col
 
 /* logits of a head whose weight is held in 8 bits:
  *   out[b][v] = sum over blocks k of x_scale[b][k] w_scale[v / 128][k] (sum over the block of x[b][..] w[v][..])   (x and w in e4m3)
- * and -inf where the mask does not allow token v in row b; rows of the weight that no row of the batch allows need not be read
- * (a grammar in the middle of its punctuation allows a few tokens of a vocabulary).  x: [batch][x_row_stride], w: [V][w_row_stride]
+ * and -inf where the mask does not allow token v in row b; rows of the weight that no row of a batch of up to 64 allows need not be read
+ * (a grammar in the middle of its punctuation allows a few tokens of a vocabulary; a larger batch reads them all).  x: [batch][x_row_stride], w: [V][w_row_stride]
  * bytes, K of them valid; K and both strides are multiples of 128 and 16, both pointers of 16.  x_scale: [batch][K/128], w_scale:
  * [ceil(V/128)][K/128].  out: device, [batch][out_row_stride_elems].
  * The sum over the blocks is held in 32 bits.  So is a block's own for fp32 logits; for bf16 ones it comes from an 8-bit matrix instruction, which cuts each of eight neighbouring

@@ -530,7 +530,8 @@ __global__ __launch_bounds__(256, 2) void head_rows_kernel(HeadArgs a, int32_t n
 //   2,048 x 128,256 x 4,096 bf16: 1,040 to 1,080 us, 2.0 PFLOP/s.  The matrix units are busy for 51 % of it, the other vector instructions (the scales, mostly) would be for 30 %
 // by themselves, LDS for 25 %; a third of the wavefronts' time is waits for blocks and at barriers (the chip runs at 1.9 GHz meanwhile, of 2.4).  fp32 logits, 2,048 x 32,000 x 4,096: 488 us, 1.1 PFLOP/s, half
 // of the bf16 instructions' rate and the operands' conversion beside them.
-//   Under a mask a tile is computed whole: of more than 64 rows some most often allow each of its ranges of tokens.
+//   Under a mask a tile is computed whole.  That is right where the rows together allow most ranges (half of the tokens each, 128,256 x 4,096 bf16: 65 rows 143 us, in calls of 64 rows 174; 130 rows 157
+// and 314), and far from it where they allow few: 50 tokens a row 65 rows 150 us, in calls of 64 rows 37, 130 rows 165 and 66, 256 rows 187 and 128.
 //   Rows behind the last one are the last one again; their results are not stored.
 template <int MJ, int MI, typename ElemT>
 struct TileLds {

@@ -229,7 +229,9 @@ __device__ __forceinline__ int rank_of(Key mine, const Key *list, int n, int lan
 }
 
 // A segment of a row, or (n_seg = 1) the whole of it, to the end.
-//   Large inputs are bound by memory: 4,096 x 128,256 bf16 with entropy 181 us (5.8 TB/s; now and then 160 or 207), 1,030 x 40,037 bf16 at odd elements 15.6 (5.3).  Small ones by
+//   Large inputs are bound by memory: 4,096 x 128,256 bf16 with entropy 179 us in a row of such calls (5.9 TB/s), 161 to 223 one by one under a trace, 202 at the median; 1,030 x 40,037 bf16 at odd
+// elements 15.6 (5.3).  Alternatives are not hidden behind the memory's time: with 20 of them the former takes 314, the latter with the joining launch 34 (with 5 31, with 64 48, without 19), 2,048 x 32,000 bf16 under masks 78 (without
+// 35).  Small inputs are bound by
 // what follows in turn: 64 x 128,256 bf16 6.0 us without alternatives, of which 2.7 are its bytes; with 20 of them 10.5, with 64 12.3; one row of 32,000 fp32 4.5 without, with 5 7.0, with 64 8.2
 // (of the 2.5 a fifth is the lines, a half the lists and the waits for the slowest wavefront's, the rest ranks and stores); 64 x 32,000 bf16 5.1, with 20 9.0.
 template <int THREADS, int PIECES, bool ONCE, bool ENT, bool TOP, typename ElemT>
@@ -481,6 +483,8 @@ __global__ __launch_bounds__(ROWS_JOINED * 64) void logprobs_join_kernel(Logprob
 }
 
 // The gradient: every thread reads a piece before it writes it, so the two may be the same memory.  4,096 x 128,256 bf16 345 us (6.1 TB/s), 300 x 32,000 fp32 15.5 (5.0).
+// Every thread compares its elements with every token listed for the segment: 256 x 32,000 fp32 19 to 23 us a backward pass with one token a row, 23 with 64 (45 if they are the same one), 44 with 256, 127 with 1,024 (572); bf16 33 with 64 (67),
+// 299 with 1,024 (972).
 template <int PIECES, bool ONCE, typename ElemT>
 __global__ __launch_bounds__(THREADS) void logprobs_grad_kernel(GradArgs A) {
     constexpr int EPV = 16 / sizeof(ElemT);

@@ -113,7 +113,7 @@ class _NoDerivative(torch.autograd.Function):
 def head_logits(q, q_scale, weight, weight_scale, mask=None, *, dtype=torch.bfloat16, out=None):
     """Logits [batch, V] of activations q [batch, K] against a head's weight [V, K], both e4m3 with K a multiple of 128, scales [batch, K / 128] and
     [ceil(V / 128), K / 128] (quantize_blocks makes all four).  Under a mask the logits of tokens that it does not allow are -inf, and
-    rows of the weight that none of a batch of up to 64 allows are not read.  fp32 logits are sums in 32 bits; bf16 ones come from 8-bit matrix instructions, which are off by about 1.3e-5 of the norm of a logit's
+    rows of the weight that none of a batch of up to 64 allows are not read (a larger batch reads all: where its rows allow few tokens, calls of 64 rows each are quicker).  fp32 logits are sums in 32 bits; bf16 ones come from 8-bit matrix instructions, which are off by about 1.3e-5 of the norm of a logit's
     products (less than 7 x 2^-13 of the sum of their sizes) before they are rounded.  dtype: fp32 or bf16; out: rows of the result without gaps.  There is no derivative: where an operand requires grad the result does,
     and a backward pass that reaches it raises; out= is refused then, and an out that requires grad itself, as torch's own calls do."""
     if out is None:
