@@ -122,3 +122,26 @@ def test_head_logits_operands_far_apart(M, V, K, kind, far):
         # (bf16 logits: less than 7 x 2^-13 of the sum of the products' sizes, which the 32-bit bound holds (2 * 128 + 2 + K / 128) U of)
         cut = bound if dtype == torch.float32 else bound * (1 + 7 * 2.0 ** -13 / ((2 * 128 + 2 + K // 128) * U))
         check_head(zf.head_logits(q_on, qs.cuda(), w_on, ws.cuda(), mask, dtype=dtype), want, cut, bits)
+
+
+# ---- tiles of 128, 192 and 256 rows and tokens, those that a rule of sizes chooses, in one round of the compute units and in several ----
+@gpu
+@pytest.mark.parametrize("masked", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,V,K", [(65, 191, 384), (65, 32953, 128), (65, 65887, 256), (65, 49420, 384), (260, 32953, 128), (130, 16486, 640), (130, 32953, 256), (130, 65887, 384), (130, 49420, 128), (260, 49420, 256),
+                                   (385, 12494, 384), (385, 16486, 512), (385, 36945, 384), (580, 16486, 640), (385, 49420, 128)])
+def test_head_logits_tiles_of_every_shape(M, V, K, dtype, masked):
+    q, qs, wq, ws = (t.cuda() for t in head_case(M, V, K, M + V + K))
+    x = q.double() * qs.double().repeat_interleave(128, dim=1)
+    w = wq.double() * ws.double().repeat_interleave(128, dim=0)[:V].repeat_interleave(128, dim=1)
+    want, sizes = x @ w.t(), x.abs() @ w.abs().t()
+    # a block's sum in 32 bits, or as the 8-bit instructions make it; two products of scales and the sum over the blocks
+    cut = ((2 * 128 + 2 + K // 128) * U + (7 * 2.0 ** -13 if dtype == "bf16" else 0.0)) * sizes
+    bits = torch.rand((M, V), generator=torch.Generator().manual_seed(K)) < 0.5 if masked else None
+    y = zf.head_logits(q, qs, wq, ws, packed(bits, padding=True).cuda() if masked else None, dtype=DTYPES[dtype])
+    allowed = bits.cuda() if masked else torch.ones((M, V), dtype=torch.bool, device="cuda")
+    assert (y[~allowed] == -math.inf).all()
+    err, want, sizes, cut = ((y.double() - want).abs()[allowed], want[allowed], sizes[allowed], cut[allowed])
+    assert (err <= cut + half_step(y.dtype) * (want.abs() + cut)).all()
+    if dtype == "bf16":                                    # nearly all of them far within it, as a misplaced scale or block would not be
+        assert (err > half_step(y.dtype) * want.abs() + 2.0 ** -13 * sizes).double().mean() < 1e-4
