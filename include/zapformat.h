@@ -305,6 +305,80 @@ int zf_token_logprobs(const zf_logprobs_args *a, void *d_workspace, int64_t work
 int zf_token_logprobs_backward(const zf_logprobs_args *a, const float *g_logprobs, const float *g_entropy, const float *g_top,
                                void *d_grad, int64_t grad_row_stride_elems, int32_t device, void *hip_stream);
 
+/* ---- losses that a learner takes on logits under masks, with the gradient of the logits ----
+ * With z = logits / temperature over the tokens of a row that its mask allows and whose logit is not -inf, p = softmax(z), lp = ln p.  What is forbidden, by
+ * the mask or by -inf, has no gradient and is not looked at; a NaN or +inf among a row's allowed logits, and a token's id beyond V, make what is computed of the row NaN.
+ *   loss    = sum of weight[i] x losses[i], as one number; losses [rows] (preferences: [pairs]) are without the weights.  Where a weight is 1 / n, loss is a mean.
+ * The gradient is that of loss for the logits, times *d_g, rounded to the logits' type once.  Distillation and policy make it beside the losses, in the same pass over the
+ * logits (d_grad of the first call: the gradient for *d_g = 1; null: none); their backward calls then have nothing to do where *d_g is 1 (`held`: d_grad
+ * is what the first call wrote, and nothing else was written there since), and make it again elsewhere.  d_grad: device, [rows][grad_row_stride_elems], not the logits. */
+typedef struct {
+    const void *logits;        /* device, [rows][row_stride_elems], V valid elements per row */
+    int32_t dtype;
+    int32_t V;                 /* 1 .. 2^24 */
+    int64_t rows, row_stride_elems;
+    const uint32_t *mask;      /* device, [rows][ceil(V/32)], or null */
+    const float *weight;       /* device, [rows] (preferences: [pairs]), or null: one each */
+    double temperature;        /* 2^-126 at least, at most the largest number of 32 bits */
+    float *loss;               /* device, [1] */
+    float *losses;             /* device, [rows] (preferences: [pairs]) */
+} zf_loss_rows;
+
+/* Distillation from a teacher's listed tokens.  Of a row's n_listed entries those count whose id is not negative and whose token is allowed; q = softmax(values / temperature) over
+ * them, or with `rest` q = e^values (values: log probabilities at that temperature), and q_R = 1 - sum q (0 at least) for all other tokens together:
+ *   losses = sum of q_k (ln q_k - lp[id_k])  [+ q_R (ln q_R - ln p_R), p_R the sum of p over the tokens that are not listed; left out where there are none]
+ * A value of -inf is a share of zero.  A row of which no entry counts has loss 0 and no gradient, and is not read.  The same id twice: two entries. */
+typedef struct {
+    zf_loss_rows r;
+    const void *ids;           /* device, [rows][n_listed] */
+    const void *values;        /* device, [rows][n_listed] */
+    int32_t id_bytes;          /* 4 or 8: the ids' type */
+    int32_t values_dtype;      /* 0 or 1, as dtype */
+    int32_t n_listed;          /* 1 .. 1024 */
+    int32_t rest;
+} zf_distill_args;
+int zf_distill_loss(const zf_distill_args *a, void *d_grad, int64_t grad_row_stride_elems, int32_t device, void *hip_stream);
+int zf_distill_loss_backward(const zf_distill_args *a, const float *d_g, int32_t held, void *d_grad, int64_t grad_row_stride_elems, int32_t device, void *hip_stream);
+
+/* A policy's clipped loss.  With lp that of the row's token and ratio = e^(lp - old_logprobs):
+ *   losses = - min(ratio A, clamp(ratio, 1 - clip_low, 1 + clip_high) A) + kl_weight (e^(ref - lp) - (ref - lp) - 1) - entropy_weight H,   A the row's advantage, H = - sum p ln p
+ * A negative token is padding: loss, log probability and entropy 0, no gradient, the row is not read.  A token that is not allowed: log probability -inf, loss 0, no gradient. */
+typedef struct {
+    zf_loss_rows r;
+    const void *tokens;        /* device, [rows] */
+    const float *old_logprobs, *advantages;        /* device, [rows] */
+    const float *ref_logprobs; /* device, [rows], or null: without the term */
+    int32_t token_bytes;       /* 4 or 8 */
+    int32_t reserved;
+    double clip_low, clip_high, kl_weight, entropy_weight;
+    float *logprobs;           /* device, [rows] */
+    float *entropy;            /* device, [rows], or null: without the term */
+} zf_policy_args;
+int zf_policy_loss(const zf_policy_args *a, void *d_grad, int64_t grad_row_stride_elems, int32_t device, void *hip_stream);
+int zf_policy_loss_backward(const zf_policy_args *a, const float *d_g, int32_t held, void *d_grad, int64_t grad_row_stride_elems, int32_t device, void *hip_stream);
+
+/* Paired sequences.  Sequence s has the rows offsets[s] .. offsets[s + 1] - 1; of pair i sequence 2 i is the preferred one, 2 i + 1 the other.  D_s = sum of lp - ref_logprobs over the
+ * sequence's rows whose token is not negative (with `average` their mean; 0 where there are none), chosen = beta D_2i, rejected = beta D_2i+1, h = chosen - rejected:
+ *   losses = - (1 - label_smoothing) ln sigma(h) - label_smoothing ln sigma(-h)
+ * Rows of no sequence and of negative tokens have no gradient.  A token that is not allowed: log probability -inf, no gradient.  A pair whose offsets descend or leave 0 .. rows: NaN.
+ * logprobs, stats, slopes are what the gradient is made from (written by the first call). */
+typedef struct {
+    zf_loss_rows r;
+    const void *tokens;        /* device, [rows] */
+    const void *offsets;       /* device, [2 pairs + 1] */
+    const float *ref_logprobs; /* device, [rows], or null: zeros */
+    int32_t token_bytes, offset_bytes;             /* 4 or 8 */
+    int64_t pairs;
+    double beta, label_smoothing;
+    int32_t average, reserved;
+    float *chosen, *rejected;  /* device, [pairs] */
+    float *logprobs;           /* device, [rows] */
+    float *stats;              /* device, [rows][2] */
+    float *slopes;             /* device, [2 pairs] */
+} zf_preference_args;
+int zf_preference_loss(const zf_preference_args *a, int32_t device, void *hip_stream);
+int zf_preference_loss_backward(const zf_preference_args *a, const float *d_g, void *d_grad, int64_t grad_row_stride_elems, int32_t device, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -5,14 +5,18 @@ from .binding import (Engine, State, StateBatch, Twin, ZfError, load_library, co
 
 
 _OPERATORS = ("quantize_blocks", "head_logits", "token_logprobs", "TokenLogprobs")
+_LOSSES = ("distill_loss", "policy_loss", "preference_loss", "DistillLoss", "PolicyLoss", "PreferenceLoss")
 
 
 def __getattr__(name):                         # they need torch, which the rest of the binding loads with the first tensor
     if name in _OPERATORS:
         from . import operators
         return getattr(operators, name)
+    if name in _LOSSES:
+        from . import losses
+        return getattr(losses, name)
     raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
 
 
 def __dir__():
-    return sorted([*globals(), *_OPERATORS])
+    return sorted([*globals(), *_OPERATORS, *_LOSSES])

@@ -66,11 +66,31 @@ class LogprobsArgs(ctypes.Structure):
                 ("temperature", ctypes.c_float), ("logprobs", c_vp), ("entropy", c_vp), ("top_ids", c_vp), ("top_logprobs", c_vp), ("stats", c_vp)]
 
 
+class LossRows(ctypes.Structure):
+    _fields_ = [("logits", c_vp), ("dtype", c_i32), ("V", c_i32), ("rows", c_i64), ("row_stride", c_i64), ("mask", c_vp), ("weight", c_vp), ("temperature", ctypes.c_double), ("loss", c_vp), ("losses", c_vp)]
+
+
+class DistillArgs(ctypes.Structure):
+    _fields_ = [("r", LossRows), ("ids", c_vp), ("values", c_vp), ("id_bytes", c_i32), ("values_dtype", c_i32), ("n_listed", c_i32), ("rest", c_i32)]
+
+
+class PolicyArgs(ctypes.Structure):
+    _fields_ = [("r", LossRows), ("tokens", c_vp), ("old_logprobs", c_vp), ("advantages", c_vp), ("ref_logprobs", c_vp), ("token_bytes", c_i32), ("reserved", c_i32),
+                ("clip_low", ctypes.c_double), ("clip_high", ctypes.c_double), ("kl_weight", ctypes.c_double), ("entropy_weight", ctypes.c_double), ("logprobs", c_vp), ("entropy", c_vp)]
+
+
+class PreferenceArgs(ctypes.Structure):
+    _fields_ = [("r", LossRows), ("tokens", c_vp), ("offsets", c_vp), ("ref_logprobs", c_vp), ("token_bytes", c_i32), ("offset_bytes", c_i32), ("pairs", c_i64),
+                ("beta", ctypes.c_double), ("label_smoothing", ctypes.c_double), ("average", c_i32), ("reserved", c_i32),
+                ("chosen", c_vp), ("rejected", c_vp), ("logprobs", c_vp), ("stats", c_vp), ("slopes", c_vp)]
+
+
 EXPORTS = ["zf_strerror", "zf_last_error", "zf_compile", "zf_engine_destroy", "zf_engine_get_info",
            "zf_state_new", "zf_state_clone", "zf_state_reset", "zf_state_destroy", "zf_advance",
            "zf_advance_bytes", "zf_advance_batch", "zf_is_accepting", "zf_state_stats", "zf_state_chart", "zf_position_info",
            "zf_compute_mask", "zf_compute_mask_noalloc", "zf_compute_mask_async", "zf_compute_mask_apply_async", "zf_mask_wait", "zf_last_mask_report", "zf_engine_clear_state_cache", "zf_engine_set_profiling", "zf_apply_mask",
-           "zf_quantize_blocks", "zf_head_logits", "zf_token_logprobs_workspace", "zf_token_logprobs", "zf_token_logprobs_backward"]
+           "zf_quantize_blocks", "zf_head_logits", "zf_token_logprobs_workspace", "zf_token_logprobs", "zf_token_logprobs_backward",
+           "zf_distill_loss", "zf_distill_loss_backward", "zf_policy_loss", "zf_policy_loss_backward", "zf_preference_loss", "zf_preference_loss_backward"]
 # test-only diagnostics (include/zapformat_debug.h)
 DEBUG_EXPORTS = ["zf_debug_host_mask", "zf_debug_host_mask_stats", "zf_debug_host_mask_cached", "zf_debug_host_mask_automaton",
                  "zf_debug_look_polls", "zf_debug_fail_look_ups", "zf_debug_twin_new", "zf_debug_twin_destroy", "zf_debug_twin_advance", "zf_debug_twin_mask"]
@@ -125,6 +145,11 @@ def load_library():
     L.zf_token_logprobs_workspace.restype = c_i64
     L.zf_token_logprobs.argtypes = [c_vp, c_vp, c_i64, c_i32, c_vp]
     L.zf_token_logprobs_backward.argtypes = [c_vp, c_vp, c_vp, c_vp, c_vp, c_i64, c_i32, c_vp]
+    for n in ("zf_distill_loss", "zf_policy_loss"):
+        getattr(L, n).argtypes = [c_vp, c_vp, c_i64, c_i32, c_vp]
+        getattr(L, n + "_backward").argtypes = [c_vp, c_vp, c_i32, c_vp, c_i64, c_i32, c_vp]
+    L.zf_preference_loss.argtypes = [c_vp, c_i32, c_vp]
+    L.zf_preference_loss_backward.argtypes = [c_vp, c_vp, c_vp, c_i64, c_i32, c_vp]
     L.zf_debug_host_mask.argtypes = [c_vp, c_vp, c_vp]
     L.zf_debug_host_mask_stats.argtypes = [c_vp, c_vp, c_vp, c_vp]
     L.zf_debug_host_mask_cached.argtypes = [c_vp, c_vp, c_vp, c_vp]
