@@ -15,6 +15,8 @@ SOURCES = ["zf_regex.cpp", "zf_compile.cpp", "zf_earley.cpp", "zf_automaton.cpp"
 HEADERS = ["zf_device.h", "zf_internal.h", "zf_launch.h", "zf_kernel_common.h", "zf_aut_step.h", "zf_host_automaton.h", "zf_ops.h", "zf_ops_check.h", "zf_logit_rows.h"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function"]
+# zf_losses.hip: a row's end, in 64 bits, has dozens of constants, which the compiler would keep in registers beside a whole row's logits (and spill: 100 to 250 bytes a thread)
+OWN_FLAGS = {"zf_losses.hip": ["-mllvm", "-disable-machine-licm"]}
 # hipcc's host pass warns once per translation unit that it does not know the packed-fp32
 # feature (it only applies to the device pass); those lines are dropped, everything else is shown
 NOISE = "'-packed-fp32-ops' is not a recognized feature"
@@ -65,7 +67,7 @@ def build(force: bool = True, extra_flags=(), sanitize: bool = False) -> str:
     for s in SOURCES:
         src, obj = os.path.join(CSRC, s), os.path.join(OBJ, s + ".o")
         if force or extra_flags or not os.path.exists(obj) or os.path.getmtime(obj) < max(os.path.getmtime(src), newest_dep):
-            jobs.append(["hipcc", "-x", "hip", "-c", src, "-o", obj] + FLAGS + list(extra_flags))
+            jobs.append(["hipcc", "-x", "hip", "-c", src, "-o", obj] + FLAGS + OWN_FLAGS.get(s, []) + list(extra_flags))
     todo = jobs + _extension_jobs(force)
     with ThreadPoolExecutor(max_workers=min(8, max(1, len(todo)))) as pool:
         results = list(pool.map(_run, todo))

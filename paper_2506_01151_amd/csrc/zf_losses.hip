@@ -40,7 +40,6 @@ struct Args {
 struct Part { float m, S, T, pad; };
 struct Ends {                                  // what the gradient of a row is made from
     float m, base, slope, at_token;            // d = 2^((x - m) c) (base + slope y); the given token's own
-    int32_t nothing;                           // a gradient of zeros
 };
 
 __device__ __forceinline__ double wave_sum(double x) {
@@ -64,67 +63,79 @@ __device__ __forceinline__ Part join_wave(Part a, float c) {
     return Part{m, wave_sum(f * a.S), wave_sum(f * fmaf(a.S, d, a.T)), 0.0f};
 }
 
-// 16 bytes of a row from element v on as numbers: -inf where `bits` has none, where nothing is read either.
+// A row is whole pieces of 16 bytes, and its last V % EPV elements, which the first threads take one each.
 template <int EPV, typename ElemT>
-__device__ __forceinline__ void load_piece(const ElemT *row, int64_t v, int32_t V, uint32_t bits, float (&x)[EPV]) {
-    constexpr uint32_t FULL = (1u << EPV) - 1u;
-    union { u32x4 v; ElemT e[EPV]; } o;
-    o.v = u32x4{0, 0, 0, 0};
-    if (V - v >= EPV) {
-        if (bits) o.v = *reinterpret_cast<const typename Piece<ElemT>::type *>(row + v);
-    } else {
+__device__ __forceinline__ void numbers(const u32x4 &r, float (&x)[EPV]) {
 #pragma unroll
-        for (int k = 0; k < EPV; k++) if (v + k < V) o.e[k] = row[v + k];
-    }
+    for (int k = 0; k < EPV; k++) x[k] = __uint_as_float(sizeof(ElemT) == 4 ? r[k % 4] : k & 1 ? r[k / 2] & 0xFFFF0000u : r[k / 2] << 16);
+}
+// -inf in the places of a piece that `bits` has none of
+template <int EPV, typename ElemT>
+__device__ __forceinline__ void forbid(u32x4 &r, uint32_t bits) {
+    constexpr uint32_t NONE = sizeof(ElemT) == 4 ? 0xFF800000u : 0xFF80FF80u;
 #pragma unroll
-    for (int k = 0; k < EPV; k++) x[k] = __uint_as_float(sizeof(ElemT) == 4 ? o.v[k % 4] : k & 1 ? o.v[k / 2] & 0xFFFF0000u : o.v[k / 2] << 16);
-    if (bits != FULL) {
-#pragma unroll
-        for (int k = 0; k < EPV; k++) x[k] = (bits >> k) & 1u ? x[k] : -INFINITY;
+    for (int k = 0; k < 4; k++) {
+        uint32_t yes;
+        if (sizeof(ElemT) == 4) yes = (uint32_t)__builtin_amdgcn_sbfe((int)bits, k, 1);
+        else {
+            const uint32_t low = (uint32_t)__builtin_amdgcn_sbfe((int)bits, 2 * k, 1), high = (uint32_t)__builtin_amdgcn_sbfe((int)bits, 2 * k + 1, 1);
+            yes = (low & 0xFFFFu) | (high & 0xFFFF0000u);
+        }
+        r[k] = (r[k] & yes) | (NONE & ~yes);
     }
 }
-template <int EPV>
-__device__ __forceinline__ uint32_t bits_of(const uint32_t *mask_row, int64_t v, int32_t V) {
-    constexpr uint32_t FULL = (1u << EPV) - 1u;
-    const uint32_t inside = V - v >= EPV ? FULL : (1u << (int)(V - v)) - 1u;
-    return mask_row ? (mask_row[v >> 5] >> (v & 31)) & inside : inside;
-}
 template <int EPV, typename ElemT>
-__device__ __forceinline__ void store_piece(ElemT *grad, int64_t v, int32_t V, const float (&d)[EPV]) {
-    union { u32x4 v; ElemT e[EPV]; bf16x2 b[4]; } o;
+__device__ __forceinline__ void store_numbers(void *to, const float (&d)[EPV]) {
+    union { u32x4 v; bf16x2 b[4]; } o;
 #pragma unroll
     for (int k = 0; k < EPV; k += 2) {
         if (sizeof(ElemT) == 4) { o.v[k % 4] = __float_as_uint(d[k]); o.v[k % 4 + 1] = __float_as_uint(d[k + 1]); }
         else o.b[k / 2 % 4] = bf16x2{(__bf16)d[k], (__bf16)d[k + 1]};
     }
-    if (V - v >= EPV) *reinterpret_cast<typename Piece<ElemT>::type *>(grad + v) = o.v;
-    else
-#pragma unroll
-        for (int k = 0; k < EPV; k++) if (v + k < V) grad[v + k] = o.e[k];
+    *reinterpret_cast<typename Piece<ElemT>::type *>(to) = o.v;
 }
 template <typename ElemT>
 __device__ __forceinline__ void store_element(ElemT *to, float x) {
     if (sizeof(ElemT) == 4) *(float *)to = x;
     else *(__bf16 *)to = (__bf16)x;
 }
+// A piece from memory, of whose places `bits` are wanted: nothing is read where there are none.
+template <int EPV, typename ElemT>
+__device__ __forceinline__ void load_numbers(const ElemT *at, uint32_t bits, float (&x)[EPV]) {
+    constexpr uint32_t NONE = sizeof(ElemT) == 4 ? 0xFF800000u : 0xFF80FF80u;
+    u32x4 r{NONE, NONE, NONE, NONE};
+    if (bits) r = *reinterpret_cast<const typename Piece<ElemT>::type *>(at);
+    if (bits != (1u << EPV) - 1u) forbid<EPV, ElemT>(r, bits);
+    numbers<EPV, ElemT>(r, x);
+}
+template <int EPV>
+__device__ __forceinline__ uint32_t bits_of(const uint32_t *mask_row, int64_t v) {
+    constexpr uint32_t FULL = (1u << EPV) - 1u;
+    return mask_row ? (mask_row[v >> 5] >> (v & 31)) & FULL : FULL;
+}
 
+// What is known of a row beside its logits, asked for ahead of its turn.
+struct Head {
+    int64_t t;                                 // the given token
+    float x, weight, old_logprob, advantage, ref;          // its logit, -inf where it is not allowed
+};
 // What a policy's loss makes of a row, by every lane of a wavefront alike.  Returns the row's loss.
-__device__ __forceinline__ double policy_row(const Args &A, const Part &sum, int64_t row, int64_t t, float x, float wg, Ends *ends, float *logprob, float *entropy) {
+__device__ __forceinline__ double policy_row(const Args &A, const Part &sum, const Head &h, float wg, Ends *ends, float *logprob, float *entropy) {
     const double lnS = log((double)sum.S);
-    const bool nan = t >= A.r.V || sum.S != sum.S;
-    const bool counts = nan || x != -INFINITY;
+    const bool nan = h.t >= A.r.V || sum.S != sum.S;
+    const bool counts = nan || h.x != -INFINITY;
     *entropy = nan ? NAN : sum.S == 0.0f ? 0.0f : (float)(lnS - (double)LN_2 * sum.T / sum.S);
-    *ends = Ends{0.0f, 0.0f, 0.0f, 0.0f, 1};
+    *ends = Ends{sum.m, 0.0f, 0.0f, 0.0f};
     *logprob = -INFINITY;
     if (!counts) return 0.0;
-    const double lp = nan ? (double)NAN : ((double)x - sum.m) / A.r.temperature - lnS;
+    const double lp = nan ? (double)NAN : ((double)h.x - sum.m) / A.r.temperature - lnS;
     *logprob = lp < -FLT_MAX ? -FLT_MAX : (float)lp;
-    const double a = A.advantages[row], ratio = exp(lp - A.old_logprobs[row]);
+    const double a = h.advantage, ratio = exp(lp - h.old_logprob);
     const double kept = ratio < A.lowest ? A.lowest : ratio > A.highest ? A.highest : ratio;
     const bool clipped = kept * a < ratio * a;
     double loss = -(clipped ? kept * a : ratio * a), f = clipped ? 0.0 : -ratio * a;
     if (A.ref) {
-        const double d = A.ref[row] - lp, up = expm1(d);
+        const double d = h.ref - lp, up = expm1(d);
         loss += A.kl_weight * (up - d);
         f -= A.kl_weight * up;
     }
@@ -132,28 +143,268 @@ __device__ __forceinline__ double policy_row(const Args &A, const Part &sum, int
     loss -= b * H;
     // p (-f + b (ln p + H)), ln p = ln 2 y - ln S; for the token itself f more
     const double scale = (double)wg / A.r.temperature, toS = scale / sum.S;
-    ends->m = sum.m;
     ends->base = (float)(toS * (b * (H - lnS) - f));
     ends->slope = (float)(toS * b * LN_2);
     ends->at_token = (float)(scale * (f + exp(lp) * (b * (lp + H) - f)));
-    ends->nothing = 0;
     return loss;
 }
 
-// A row a workgroup, read twice where its gradient is wanted: for the sums, and for the gradient.
+// ---- a teacher's listed tokens ----
+// Each wavefront sums 64 entries around its own largest logit x_most and value v_most (with `rest` 0); the sums join as those of a row do.
+struct Teacher {
+    double total, mixed, S;                    // of e = e^((v - v_most) / T):  sum e,  sum e ((v - v_most) / T - (x - x_most) / T);  sum 2^((x - x_most) c) over different tokens
+    double v_most;
+    float x_most;
+    int32_t some;
+};
+struct EntriesEnd {
+    double v_most, scale;                      // q = e^((v - v_most) / T) times what is in `scale` but for the sign
+    float x_most, to_listed;                   // a listed token's gradient: its 2^((x - x_most) c) times this, and the entries' own
+    uint32_t flags;                            // 1: an entry counts, 2: an id is beyond V, 4: a token is listed twice
+    uint32_t pad;
+};
+struct Entries {                               // in LDS, room for the call's n_listed
+    Teacher *part;                             // [n / 64]
+    EntriesEnd *end;
+    int32_t *id;                               // [n]; -1: does not count
+    float *x, *v;
+    __device__ __forceinline__ Entries(char *at, int K) {
+        part = (Teacher *)at;
+        end = (EntriesEnd *)(part + (K + 63) / 64);
+        id = (int32_t *)(end + 1);
+        x = (float *)(id + K);
+        v = x + K;
+    }
+};
+__host__ __device__ __forceinline__ int entries_bytes(int K) { return ((K + 63) / 64 * (int)sizeof(Teacher) + (int)sizeof(EntriesEnd) + 12 * K + 15) / 16 * 16; }
+
+// An entry as memory has it, asked for ahead of its turn.
+struct Entry {
+    int32_t id;                                // -1: none, V: beyond the vocabulary
+    float v, x;                                // x: the token's logit, whether it is allowed or not
+    uint32_t word;                             // of the mask
+};
+__device__ __forceinline__ void ask_id(const Args &A, int64_t row, int k, Entry &e) {
+    const int64_t at = row * A.K + k;
+    const int64_t id = id_at(A, at);
+    e.id = id < 0 ? -1 : id < A.r.V ? (int32_t)id : A.r.V;
+    e.v = A.values_dtype == 0 ? ((const float *)A.values)[at] : of_bits(((const uint16_t *)A.values)[at]);
+}
+template <typename ElemT>
+__device__ __forceinline__ void ask_logit(const Args &A, const ElemT *logits, const uint32_t *mask, Entry &e) {
+    e.x = -INFINITY;
+    e.word = ~0u;
+    if (e.id < 0 || e.id >= A.r.V) return;
+    e.x = of_bits(logits[e.id]);
+    if (mask) e.word = mask[e.id >> 5];
+}
+// Whether it counts
+__device__ __forceinline__ bool list_entry(const Args &A, const Entry &e, int k, const Entries &E) {
+    const bool inside = e.id >= 0 && e.id < A.r.V && ((e.word >> (e.id & 31)) & 1u), counts = inside && e.x != -INFINITY;
+    E.id[k] = counts ? (int32_t)e.id : -1;
+    E.x[k] = inside ? e.x : -INFINITY;
+    E.v[k] = e.v;
+    if (counts || e.id >= A.r.V) atomicOr(&E.end->flags, e.id >= A.r.V ? 2u : 1u);
+    return counts;
+}
+__device__ __forceinline__ bool first_of(const Entries &E, int k) {      // of the entries of one token
+    if (E.end->flags & 4u) for (int i = 0; i < k; i++) if (E.id[i] == E.id[k]) return false;
+    return true;
+}
+// Entries 64 wave .. 64 wave + 63, by one wavefront; every entry has been read.
+__device__ __forceinline__ void sum_entries(const Args &A, int wave, int lane, const Entries &E) {
+    const int k = wave * 64 + lane;
+    const bool counts = k < A.K && E.id[k] >= 0;
+    const float x = counts ? E.x[k] : -INFINITY, x_most = zf::wave_max(x);
+    const double v = counts ? (double)E.v[k] : -INFINITY, T = A.r.temperature;
+    const double v_most = A.rest ? 0.0 : (double)zf::wave_max((float)v);
+    double ln = 0.0, e = 0.0, S = 0.0;
+    if (v != -INFINITY) {
+        ln = A.rest ? v : (v - v_most) / T;
+        e = exp(ln);
+    }
+    const double mixed = e == 0.0 ? 0.0 : e * (ln - ((double)x - x_most) / T);
+    if (counts && first_of(E, k)) S = two_to((x - x_most) * A.c);
+    const Teacher t{wave_sum(e), wave_sum(mixed), wave_sum(S), v_most, x_most, __any(counts)};
+    if (lane == 0) E.part[wave] = t;
+}
+// A row's end, from the sums over what is not listed; by every lane of one wavefront alike.  Returns the row's loss.
+__device__ __forceinline__ double distill_row(const Args &A, const Part &sum, float wg, const Entries &E, Ends *ends) {
+    const double T = A.r.temperature;
+    Teacher t{0.0, 0.0, 0.0, -INFINITY, -INFINITY, 0};
+    for (int w = 0; w < (A.K + 63) / 64; w++) {
+        const Teacher u = E.part[w];
+        if (!u.some) continue;
+        if (!t.some) { t = u; continue; }
+        const double v = A.rest ? 0.0 : fmax(t.v_most, u.v_most);
+        const float x = fmaxf(t.x_most, u.x_most);
+        const double vt = t.v_most == v ? 0.0 : (t.v_most - v) / T, vu = u.v_most == v ? 0.0 : (u.v_most - v) / T, ft = exp(vt), fu = exp(vu);
+        const double xt = ((double)t.x_most - x) / T, xu = ((double)u.x_most - x) / T;
+        t.mixed = (ft == 0.0 ? 0.0 : ft * (t.mixed + t.total * (vt - xt))) + (fu == 0.0 ? 0.0 : fu * (u.mixed + u.total * (vu - xu)));
+        t.total = ft * t.total + fu * u.total;
+        t.S = exp(xt) * t.S + exp(xu) * u.S;
+        t.v_most = v;
+        t.x_most = x;
+    }
+    const bool none = sum.S == 0.0f;                       // nothing that is not listed
+    const float x_most = none ? t.x_most : fmaxf(t.x_most, sum.m);
+    const double S_rest = sum.S, down = none ? 0.0 : ((double)sum.m - x_most) / T, listed_down = t.some ? ((double)t.x_most - x_most) / T : 0.0;
+    const double S = (none ? 0.0 : S_rest * exp(down)) + t.S * exp(listed_down), lnS = log(S);
+    const double share = A.rest ? 1.0 : t.total == 0.0 ? 0.0 : 1.0 / t.total;
+    double all = t.total * share;                          // sum of q
+    double loss = t.total == 0.0 ? 0.0 : (A.rest ? t.mixed : t.mixed * share - log(t.total)) + all * (lnS - listed_down);
+    double q_rest = A.rest ? 1.0 - all : 0.0;
+    if (q_rest < 0.0 || none) q_rest = 0.0;
+    const double ln_rest = none ? 0.0 : log(S_rest) + down - lnS;          // ln p_R, also where p_R is 0 in 64 bits
+    if (q_rest != 0.0) loss += q_rest * (log(q_rest) - ln_rest);
+    const bool nan = (E.end->flags & 2u) || S != S;
+    all += q_rest;
+    const double scale = (double)wg / T;
+    ends->m = sum.m;
+    ends->base = nan ? NAN : none ? 0.0f : (float)(scale * (all * exp(ln_rest) - q_rest) / S_rest);
+    ends->slope = 0.0f;
+    ends->at_token = 0.0f;
+    E.end->x_most = x_most;
+    E.end->v_most = A.rest ? 0.0 : t.v_most;
+    E.end->scale = scale * share;
+    E.end->to_listed = nan ? NAN : (float)(scale * all / S);
+    return nan ? NAN : loss;
+}
+// The gradient of listed tokens, over what the row's own pass wrote there.
+template <int TH, typename ElemT>
+__device__ __forceinline__ void store_entries(const Args &A, const Entries &E, ElemT *grad) {
+    for (int k = threadIdx.x; k < A.K; k += TH) {
+        const int32_t id = E.id[k];
+        if (id < 0) continue;
+        auto q = [&](int i) {
+            const double v = E.v[i];
+            return v == -INFINITY ? 0.0f : (float)(exp(A.rest ? v : (v - E.end->v_most) / A.r.temperature) * E.end->scale);
+        };
+        float f = q(k);
+        if (E.end->flags & 4u) {                                // the entries of the same token in order, by the first
+            if (!first_of(E, k)) continue;
+            for (int i = k + 1; i < A.K; i++) if (E.id[i] == id) f += q(i);
+        }
+        store_element(grad + id, fmaf(two_to((E.x[k] - E.end->x_most) * A.c), E.end->to_listed, -f));
+    }
+}
+
+// ---- a row's results ----
+template <int KIND>
+__device__ __forceinline__ void ask_head(const Args &A, int64_t row, Head &h) {
+    h.weight = A.r.weight && KIND != LOGPROB ? A.r.weight[row] : 1.0f;
+    if (KIND == POLICY) {
+        h.old_logprob = A.old_logprobs[row];
+        h.advantage = A.advantages[row];
+        h.ref = A.ref ? A.ref[row] : 0.0f;
+    }
+}
+template <typename ElemT>
+__device__ __forceinline__ void ask_token(const Args &A, const ElemT *logits, const uint32_t *mask, Head &h) {
+    h.x = -INFINITY;
+    if (h.t >= 0 && h.t < A.r.V) {
+        const float x = of_bits(logits[h.t]);
+        if (allowed(mask, h.t)) h.x = x;
+    }
+}
+template <int KIND, bool ENT>
+__device__ __forceinline__ void no_row(const Args &A, int64_t row) {       // by one thread: a row that is padding
+    if (!A.results) return;
+    if (KIND != LOGPROB) A.r.losses[row] = 0.0f;
+    if (KIND != DISTILL) A.logprobs[row] = 0.0f;
+    if (KIND == LOGPROB) A.stats[2 * row] = A.stats[2 * row + 1] = 0.0f;
+    if (ENT) A.entropy[row] = 0.0f;
+}
+// By one wavefront: what the sums over a row lead to.
+template <int KIND, bool ENT>
+__device__ __forceinline__ void finish_row(const Args &A, const Part &sum, int64_t row, const Head &h, float wg, int lane, const Entries &E, Ends &ends) {
+    Ends e{};
+    if (KIND == POLICY) {
+        float logprob, entropy;
+        const double loss = policy_row(A, sum, h, wg, &e, &logprob, &entropy);
+        if (lane != 0) return;
+        ends = e;
+        if (!A.results) return;
+        A.r.losses[row] = (float)loss;
+        A.logprobs[row] = logprob;
+        if (ENT) A.entropy[row] = entropy;
+    } else if (KIND == LOGPROB) {
+        const bool nan = h.t >= A.r.V || sum.S != sum.S;
+        const double lp = nan ? (double)NAN : h.x == -INFINITY ? -INFINITY : ((double)h.x - sum.m) / A.r.temperature - log((double)sum.S);
+        if (lane != 0) return;
+        A.logprobs[row] = lp < -FLT_MAX && h.x != -INFINITY ? -FLT_MAX : (float)lp;
+        A.stats[2 * row] = sum.m;
+        A.stats[2 * row + 1] = sum.S == 0.0f ? 0.0f : 1.0f / sum.S;
+    } else {
+        const double loss = distill_row(A, sum, wg, E, &e);
+        if (lane != 0) return;
+        ends = e;
+        if (A.results) A.r.losses[row] = (float)loss;
+    }
+}
+
+// ---- pieces of a row ----
+template <bool ENT, int EPV>
+__device__ __forceinline__ void add_piece(const float (&x)[EPV], float c, Part &sum) {
+    float most = sum.m;
+#pragma unroll
+    for (int k = 0; k < EPV; k++) most = fmaxf(most, x[k]);
+    if (most > sum.m) {
+        const float d = apart(sum.m, most, c), f = two_to(d);
+        if (ENT) sum.T = f * fmaf(sum.S, d, sum.T);
+        sum.S *= f;
+        sum.m = most;
+    }
+    float S = 0.0f, T = 0.0f;
+#pragma unroll
+    for (int k = 0; k < EPV; k++) {
+        const float y = (x[k] - sum.m) * c, e = two_to(y);
+        S += e;
+        if (ENT) T = fmaf(e, fmaxf(y, -1e4f), T);
+    }
+    sum.S += S;
+    if (ENT) sum.T += T;
+}
+template <bool ENT, int EPV>
+__device__ __forceinline__ void grad_of(const float (&x)[EPV], const Ends &ends, float c, float (&d)[EPV]) {
+#pragma unroll
+    for (int k = 0; k < EPV; k++) {
+        const float y = (x[k] - ends.m) * c, e = two_to(y);
+        d[k] = ENT ? e * fmaf(ends.slope, fmaxf(y, -1e4f), ends.base) : e * ends.base;
+    }
+}
+// Where factors are not finite, or near it: 0 times them is not 0, and what is forbidden is to have 0.
+__device__ __forceinline__ bool wild(const Ends &e) { return !(fabsf(e.base) + 2e4f * fabsf(e.slope) < INFINITY); }
+template <bool ENT, int EPV>
+__device__ __forceinline__ void grad_of_wild(const float (&x)[EPV], const Ends &ends, float c, float (&d)[EPV]) {
+#pragma unroll
+    for (int k = 0; k < EPV; k++) {
+        const float y = (x[k] - ends.m) * c, e = two_to(y);
+        d[k] = x[k] == -INFINITY ? 0.0f : ENT ? fmaf(e * fmaxf(y, -1e4f), ends.slope, e * ends.base) : e * ends.base;
+    }
+}
+template <int TH, int EPV, typename ElemT>
+__device__ __forceinline__ void store_zeros(ElemT *grad, int32_t V) {
+    const float zeros[EPV] = {};
+    for (int32_t j = threadIdx.x; j < V / EPV; j += TH) store_numbers<EPV, ElemT>(grad + (int64_t)j * EPV, zeros);
+    if ((int)threadIdx.x < V % EPV) store_element(grad + V - V % EPV + threadIdx.x, 0.0f);
+}
+
+template <int TH, int EPV>
+__device__ __forceinline__ int writer_of(int64_t v, int32_t V) { return v >= V - V % EPV ? (int)(v % EPV) : (int)(v / EPV % TH); }
+
+// A row a workgroup, from memory: read for the sums, and again where its gradient is wanted.  For rows that do not fit a compute unit's registers, and calls without a gradient.
 template <int TH, int KIND, bool ENT, typename ElemT>
 __global__ __launch_bounds__(TH) void loss_rows_kernel(const Args A) {
     constexpr int EPV = 16 / sizeof(ElemT), WAVES = TH / 64;
     constexpr bool LIST = KIND == DISTILL;
     __shared__ Part part[WAVES];
-    __shared__ Ends ends;
+    __shared__ Ends shared_ends;
     __shared__ uint32_t listed[LIST ? CHUNK / 32 : 1];
-    __shared__ int32_t entry_id[LIST ? TEACHER_MAX : 1];
-    __shared__ float entry_x[LIST ? TEACHER_MAX : 1], entry_f[LIST ? TEACHER_MAX : 1];
-    __shared__ uint32_t flags;                             // 1: an entry counts, 2: an id is beyond V, 4: an id is listed twice
-    __shared__ float to_listed;                            // a listed token's gradient: its 2^y times this, and the entries' own
+    extern __shared__ __align__(16) char entries[];
+    const Entries E(entries, A.K);
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64;
-    const int32_t V = A.r.V, n_pieces = (V + EPV - 1) / EPV;
+    const int32_t V = A.r.V, n_pieces = V / EPV;
     float g = 1.0f;
     if (A.g) {
         g = *A.g;
@@ -161,45 +412,34 @@ __global__ __launch_bounds__(TH) void loss_rows_kernel(const Args A) {
     }
     if (LIST) {
         for (int i = tid; i < CHUNK / 32; i += TH) listed[i] = 0;
-        if (tid == 0) flags = 0;
+        if (tid == 0) E.end->flags = 0;
         __syncthreads();
     }
     for (int64_t row = blockIdx.x; row < A.r.rows; row += gridDim.x) {
         const ElemT *const logits = (const ElemT *)A.r.logits + row * A.r.row_stride_elems;
         const uint32_t *const mask = A.r.mask ? A.r.mask + row * A.W : nullptr;
         ElemT *const grad = (ElemT *)A.grad + row * A.grad_stride;
-        const float w = A.r.weight && KIND != LOGPROB ? A.r.weight[row] : 1.0f, wg = w * g;
-        int64_t t = -1;
-        float x_t = -INFINITY;
-        bool looked = true;                                // the row is read
+        Head h{-1, -INFINITY, 1.0f, 0.0f, 0.0f, 0.0f};
+        ask_head<KIND>(A, row, h);
+        const float wg = h.weight * g;
+        bool looked;                                       // the row is read
         if (LIST) {
             for (int k = tid; k < A.K; k += TH) {
-                const int64_t id = id_at(A, row * A.K + k);
-                float x = -INFINITY;
-                if (id >= 0 && id < V && allowed(mask, id)) x = of_bits(logits[id]);
-                const bool counts = x != -INFINITY;
-                entry_id[k] = counts ? (int32_t)id : -1;
-                entry_x[k] = x;
-                if (counts || id >= V) atomicOr(&flags, id >= V ? 2u : 1u);
+                Entry e;
+                ask_id(A, row, k, e);
+                ask_logit(A, logits, mask, e);
+                list_entry(A, e, k, E);
             }
             __syncthreads();
-            looked = flags != 0;
+            looked = E.end->flags != 0;
         } else {
-            t = id_at(A, row);
-            looked = t >= 0;
-            if (looked && t < V && allowed(mask, t)) x_t = of_bits(logits[t]);
+            h.t = id_at(A, row);
+            looked = h.t >= 0;
+            ask_token(A, logits, mask, h);
         }
         if (!looked) {                                     // (alike in the whole workgroup)
-            if (tid == 0 && A.results) {
-                if (KIND != LOGPROB) A.r.losses[row] = 0.0f;
-                if (KIND != DISTILL) A.logprobs[row] = 0.0f;
-                if (KIND == LOGPROB) A.stats[2 * row] = A.stats[2 * row + 1] = 0.0f;
-                if (ENT) A.entropy[row] = 0.0f;
-            }
-            if (A.grad) {
-                const float zeros[EPV] = {};
-                for (int j = tid; j < n_pieces; j += TH) store_piece<EPV>(grad, (int64_t)j * EPV, V, zeros);
-            }
+            if (tid == 0) no_row<KIND, ENT>(A, row);
+            if (A.grad) store_zeros<TH, EPV>(grad, V);
             if (LIST) __syncthreads();                     // before the lists are written again
             continue;
         }
@@ -213,166 +453,272 @@ __global__ __launch_bounds__(TH) void loss_rows_kernel(const Args A) {
                     __syncthreads();
                 }
                 for (int k = tid; k < A.K; k += TH) {
-                    const int32_t id = entry_id[k];
+                    const int32_t id = E.id[k];
                     if (id < from || id >= to) continue;
                     const uint32_t bit = 1u << (id & 31), was = atomicOr(&listed[(id - from) >> 5], bit);
-                    if (was & bit) atomicOr(&flags, 4u);
+                    if (was & bit) atomicOr(&E.end->flags, 4u);
                 }
                 __syncthreads();
             }
-            for (int32_t j = from / EPV + tid; j < (to + EPV - 1) / EPV; j += TH) {
+            for (int32_t j = from / EPV + tid; j < to / EPV; j += TH) {
                 const int64_t v = (int64_t)j * EPV;
-                uint32_t bits = bits_of<EPV>(mask, v, V);
+                uint32_t bits = bits_of<EPV>(mask, v);
                 if (LIST) bits &= ~(listed[(v - from) >> 5] >> (v & 31));
-                float x[EPV], most = mine.m;
-                load_piece<EPV>(logits, v, V, bits, x);
-#pragma unroll
-                for (int k = 0; k < EPV; k++) most = fmaxf(most, x[k]);
-                if (most > mine.m) {
-                    const float d = apart(mine.m, most, A.c), f = two_to(d);
-                    if (ENT) mine.T = f * fmaf(mine.S, d, mine.T);
-                    mine.S *= f;
-                    mine.m = most;
-                }
-                float S = 0.0f, T = 0.0f;
-#pragma unroll
-                for (int k = 0; k < EPV; k++) {
-                    const float y = (x[k] - mine.m) * A.c, e = two_to(y);
-                    S += e;
-                    if (ENT) T = fmaf(e, fmaxf(y, -1e4f), T);
-                }
-                mine.S += S;
-                if (ENT) mine.T += T;
+                float x[EPV];
+                load_numbers<EPV>(logits + v, bits, x);
+                add_piece<ENT>(x, A.c, mine);
+            }
+            if (to == V && tid < V % EPV) {
+                const int32_t v = V - V % EPV + tid;
+                const bool mine_to_add = allowed(mask, v) && !(LIST && ((listed[(v - from) >> 5] >> (v & 31)) & 1u));
+                const float x[1] = {mine_to_add ? of_bits(logits[v]) : -INFINITY};
+                add_piece<ENT>(x, A.c, mine);
             }
             if (!LIST) break;
         }
         mine = join_wave(mine, A.c);
         if (lane == 0) part[wave] = mine;
+        if (LIST) for (int u = wave; u < (A.K + 63) / 64; u += WAVES) sum_entries(A, u, lane, E);
         __syncthreads();
-        if (wave == 0) {
-            const Part sum = join_wave(lane < WAVES ? part[lane] : Part{-FLT_MAX, 0.0f, 0.0f, 0.0f}, A.c);
-            if (KIND == POLICY) {
-                Ends e;
-                float logprob, entropy;
-                const double loss = policy_row(A, sum, row, t, x_t, wg, &e, &logprob, &entropy);
-                if (lane == 0) {
-                    ends = e;
-                    if (A.results) {
-                        A.r.losses[row] = (float)loss;
-                        A.logprobs[row] = logprob;
-                        if (ENT) A.entropy[row] = entropy;
-                    }
-                }
-            } else if (KIND == LOGPROB) {
-                const bool nan = t >= V || sum.S != sum.S;
-                const double lp = nan ? (double)NAN : x_t == -INFINITY ? -INFINITY : ((double)x_t - sum.m) / A.r.temperature - log((double)sum.S);
-                if (lane == 0) {
-                    A.logprobs[row] = lp < -FLT_MAX && x_t != -INFINITY ? -FLT_MAX : (float)lp;
-                    A.stats[2 * row] = sum.m;
-                    A.stats[2 * row + 1] = sum.S == 0.0f ? 0.0f : 1.0f / sum.S;
-                }
-            } else {
-                // the teacher's side
-                double most = -INFINITY, total = 0.0;
-                auto value = [&](int k) { const int64_t i = row * A.K + k; return (double)(A.values_dtype == 0 ? ((const float *)A.values)[i] : of_bits(((const uint16_t *)A.values)[i])); };
-                const double T = A.r.temperature;
-                float x_most = sum.m;
-                for (int k = lane; k < A.K; k += 64) {
-                    if (entry_id[k] < 0) continue;
-                    x_most = fmaxf(x_most, entry_x[k]);
-                    most = fmax(most, value(k));
-                }
-                x_most = zf::wave_max(x_most);
-                most = A.rest ? 0.0 : wave_max(most);
-                auto first = [&](int k) {                  // of the entries of one token
-                    if (flags & 4u) for (int i = 0; i < k; i++) if (entry_id[i] == entry_id[k]) return false;
-                    return true;
-                };
-                double S_listed = 0.0;
-                for (int k = lane; k < A.K; k += 64) {
-                    if (entry_id[k] < 0) continue;
-                    const double v = value(k);
-                    total += v == -INFINITY ? 0.0 : exp(A.rest ? v : (v - most) / T);
-                    if (first(k)) S_listed += two_to((entry_x[k] - x_most) * A.c);
-                }
-                total = wave_sum(total);
-                const double S_rest = sum.S, rest_down = ((double)sum.m - x_most) / T;       // ln of what brings S_rest to the same reference
-                const double S = wave_sum(S_listed) + (S_rest == 0.0 ? 0.0 : S_rest * exp(rest_down)), lnS = log(S);
-                const double inv = A.rest || total == 0.0 ? 1.0 : 1.0 / total, ln_total = A.rest || total == 0.0 ? 0.0 : log(total);
-                double loss = 0.0, all = 0.0;
-                const double scale = (double)wg / T;
-                for (int k = lane; k < A.K; k += 64) {
-                    if (entry_id[k] < 0) continue;
-                    const double v = value(k), ln_q = A.rest ? v : (v - most) / T - ln_total, q = v == -INFINITY ? 0.0 : exp(A.rest ? v : (v - most) / T) * inv;
-                    if (q != 0.0) loss += q * (ln_q - (((double)entry_x[k] - x_most) / T - lnS));
-                    all += q;
-                    entry_f[k] = (float)(-q * scale);
-                }
-                loss = wave_sum(loss);
-                all = wave_sum(all);
-                double q_rest = A.rest ? 1.0 - all : 0.0;
-                if (q_rest < 0.0 || S_rest == 0.0) q_rest = 0.0;
-                const double ln_rest = log(S_rest) + rest_down - lnS, p_rest = S_rest == 0.0 ? 0.0 : exp(ln_rest);
-                if (q_rest != 0.0) loss += q_rest * (log(q_rest) - ln_rest);
-                const bool nan = (flags & 2u) || S != S;
-                all += q_rest;
-                if (lane == 0) {
-                    ends.m = sum.m;
-                    ends.base = nan ? NAN : S_rest == 0.0 ? 0.0f : (float)(scale * (all * p_rest - q_rest) / S_rest);
-                    ends.slope = 0.0f;
-                    ends.nothing = 0;
-                    ends.at_token = x_most;
-                    to_listed = nan ? NAN : (float)(scale * all / S);
-                    if (A.results) A.r.losses[row] = nan ? NAN : (float)loss;
-                }
-            }
-        }
-        if (KIND == LOGPROB) {
-            __syncthreads();                               // before part is written again
-            continue;
-        }
+        if (wave == 0) finish_row<KIND, ENT>(A, join_wave(lane < WAVES ? part[lane] : Part{-FLT_MAX, 0.0f, 0.0f, 0.0f}, A.c), row, h, wg, lane, E, shared_ends);
         __syncthreads();
-        if (A.grad) {
-            const float m = ends.m, base = ends.base, slope = ends.slope;
-            const bool zero = ends.nothing, look = !(fabsf(base) + 2e4f * fabsf(slope) < INFINITY);   // 0 times what is not finite is not 0
+        if (KIND != LOGPROB && A.grad) {
+            const Ends ends = shared_ends;
+            const bool all = wild(ends);
             for (int32_t j = tid; j < n_pieces; j += TH) {
                 const int64_t v = (int64_t)j * EPV;
                 float x[EPV], d[EPV];
-                load_piece<EPV>(logits, v, V, zero ? 0u : bits_of<EPV>(mask, v, V), x);
-#pragma unroll
-                for (int k = 0; k < EPV; k++) {
-                    const float y = (x[k] - m) * A.c, e = two_to(y), near = fmaxf(y, -1e4f);
-                    d[k] = ENT ? (look ? fmaf(e * near, slope, e * base) : e * fmaf(slope, near, base)) : e * base;
-                    if (zero || (look && x[k] == -INFINITY)) d[k] = 0.0f;
-                }
-                store_piece<EPV>(grad, v, V, d);
+                load_numbers<EPV>(logits + v, bits_of<EPV>(mask, v), x);
+                if (all) grad_of_wild<ENT>(x, ends, A.c, d);
+                else grad_of<ENT>(x, ends, A.c, d);
+                store_numbers<EPV, ElemT>(grad + v, d);
+            }
+            if (tid < V % EPV) {
+                const int32_t v = V - V % EPV + tid;
+                const float x[1] = {allowed(mask, v) ? of_bits(logits[v]) : -INFINITY};
+                float d[1];
+                grad_of_wild<ENT>(x, ends, A.c, d);
+                store_element(grad + v, d[0]);
             }
             if (!LIST) {                                   // by the thread that has just written the token's piece
-                if (x_t != -INFINITY && tid == (int)(t / EPV % TH) && t < V) store_element(grad + t, ends.at_token);
+                if (h.x != -INFINITY && tid == writer_of<TH, EPV>(h.t, V)) store_element(grad + h.t, ends.at_token);
             } else {
                 __syncthreads();
-                const float x_most = ends.at_token;
-                for (int k = tid; k < A.K; k += TH) {
-                    const int32_t id = entry_id[k];
-                    if (id < 0) continue;
-                    float f = entry_f[k];
-                    if (flags & 4u) {                      // the entries of the same token in order, by the first
-                        bool first = true;
-                        for (int i = 0; i < k; i++) first &= entry_id[i] != id;
-                        if (!first) continue;
-                        for (int i = k + 1; i < A.K; i++) if (entry_id[i] == id) f += entry_f[i];
-                    }
-                    store_element(grad + id, fmaf(two_to((entry_x[k] - x_most) * A.c), to_listed, f));
-                }
+                store_entries<TH>(A, E, grad);
             }
         }
         if (LIST) {
             __syncthreads();
-            if (V <= CHUNK) for (int k = tid; k < A.K; k += TH) { if (entry_id[k] >= 0) listed[entry_id[k] >> 5] = 0; }
+            if (V <= CHUNK) for (int k = tid; k < A.K; k += TH) { if (E.id[k] >= 0) listed[E.id[k] >> 5] = 0; }
             else for (int i = tid; i < CHUNK / 32; i += TH) listed[i] = 0;
-            if (tid == 0) flags = 0;
+            if (tid == 0) E.end->flags = 0;
             __syncthreads();
         }
+    }
+}
+
+// A row a workgroup, held in registers between its sums and its gradient: NP pieces of 16 bytes a thread.  Workgroups stay.  As soon as the gradient of a piece is on
+// the way its registers take the next row's piece, which is added to that row's sums LAG pieces later: memory is asked for, written and waited for all along the
+// arithmetic of both.  A row's mask lies in LDS, without the tokens that a teacher listed: their sums and their gradient are taken from the list.
+template <int TH, int NP, int KIND, bool MASKED, bool ENT, typename ElemT>
+__global__ __launch_bounds__(TH, 4) void loss_resident_kernel(const Args A) {
+    constexpr int EPV = 16 / sizeof(ElemT), WAVES = TH / 64, WORDS = NP * TH * EPV / 32, OWN_WORDS = (WORDS + TH - 1) / TH, LAG = 4;
+    constexpr uint32_t FULL = (1u << EPV) - 1u, NONE = sizeof(ElemT) == 4 ? 0xFF800000u : 0xFF80FF80u;      // -inf
+    constexpr bool LIST = KIND == DISTILL;
+    static_assert(!LIST || MASKED, "listed tokens are taken out of the mask");
+    __shared__ Part part[WAVES];
+    __shared__ Ends shared_ends;
+    __shared__ uint32_t bits_lds[MASKED ? WORDS : 1];
+    extern __shared__ __align__(16) char entries[];
+    int tid = threadIdx.x;
+    const int wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64;
+    const int32_t V = A.r.V;
+    int32_t n_pieces = V / EPV;
+    float g = 1.0f;
+    if (A.g) {
+        g = *A.g;
+        if (A.held && g == 1.0f) return;
+    }
+    auto logits_of = [&](int64_t row) { return (const ElemT *)A.r.logits + row * A.r.row_stride_elems; };
+    auto mask_of = [&](int64_t row) { return A.r.mask ? A.r.mask + row * A.W : nullptr; };
+    u32x4 raw[NP];
+    uint32_t own_words[OWN_WORDS];
+    auto read_words = [&](int64_t row) {                   // a row's mask, without what lies behind V
+        const uint32_t *const m = mask_of(row);
+#pragma unroll
+        for (int i = 0; i < OWN_WORDS; i++) {
+            const int32_t at = tid + i * TH, left = V - at * 32;
+            own_words[i] = left <= 0 ? 0u : m ? m[at] : ~0u;
+            if (left > 0 && left < 32) own_words[i] &= (1u << left) - 1u;
+        }
+    };
+    auto store_words = [&]() {
+#pragma unroll
+        for (int i = 0; i < OWN_WORDS; i++) if (tid + i * TH < WORDS) bits_lds[tid + i * TH] = own_words[i];
+    };
+    auto bits_of_piece = [&](int i) -> uint32_t {
+        const int j = tid + i * TH;
+        const uint32_t byte = ((const uint8_t *)bits_lds)[EPV == 8 ? j : j / 2];
+        return EPV == 8 ? byte : (byte >> (j % 2 * 4)) & FULL;
+    };
+    const uint32_t at_tid = (uint32_t)tid * 16u;           // bytes; a piece's address is a row's and i's, alike in the workgroup, and this
+    auto piece_of = [&](const ElemT *of, int i) { return (const char *)of + i * (TH * 16) + at_tid; };
+    auto fetch = [&](const ElemT *from, int i) {           // piece i of the thread; -inf where there is nothing, or nothing that the mask allows
+        raw[i] = u32x4{NONE, NONE, NONE, NONE};
+        if (tid + i * TH < n_pieces && (!MASKED || bits_of_piece(i))) raw[i] = __builtin_nontemporal_load(reinterpret_cast<const typename Piece<ElemT>::type *>(piece_of(from, i)));
+    };
+    const bool last = tid < V % EPV;                       // the thread has one of the elements behind the whole pieces
+    const int32_t v_last = V - V % EPV + tid;
+    float x_last = -INFINITY;
+    Part mine;
+    uint32_t live, next_live = 0;                          // pieces with an allowed token
+    auto add = [&](int i) {
+        uint32_t bits = FULL;
+        if (MASKED) {
+            bits = bits_of_piece(i);
+            next_live |= (bits ? 1u : 0u) << i;
+            if (__any(bits != FULL)) forbid<EPV, ElemT>(raw[i], bits);
+        }
+        if (!MASKED || __any(bits != 0)) {
+            float x[EPV];
+            numbers<EPV, ElemT>(raw[i], x);
+            add_piece<ENT>(x, A.c, mine);
+        }
+        asm volatile("" : "+v"(raw[i]));                   // (the numbers are made from their 16 bits again: kept, they would be twice the registers)
+    };
+    auto fetch_last = [&](const ElemT *from) {
+        if (last) x_last = MASKED && !((bits_lds[v_last >> 5] >> (v_last & 31)) & 1u) ? -INFINITY : of_bits(from[v_last]);
+    };
+    auto add_last = [&]() {
+        if (!last) return;
+        const float x[1] = {x_last};
+        add_piece<ENT>(x, A.c, mine);
+    };
+    // A row's entries: ids and values are asked for two rows ahead, logits and masks one, up to TH of them; further ones when their row is listed.
+    Entry ahead{}, after{};
+    auto ask_entry = [&](int64_t row, Entry &e) { if (LIST && tid < A.K && row < A.r.rows) ask_id(A, row, tid, e); };
+    auto ask_entry_logit = [&](int64_t row, Entry &e) { if (LIST && tid < A.K && row < A.r.rows) ask_logit(A, logits_of(row), mask_of(row), e); };
+    auto list_row = [&](int64_t row, const Entries &E) {   // with the tokens' bits in LDS
+        for (int k = tid; k < A.K; k += TH) {
+            Entry e = ahead;
+            if (k >= TH) {
+                ask_id(A, row, k, e);
+                ask_logit(A, logits_of(row), mask_of(row), e);
+            }
+            if (list_entry(A, e, k, E) && !((atomicAnd(&bits_lds[e.id >> 5], ~(1u << (e.id & 31))) >> (e.id & 31)) & 1u)) atomicOr(&E.end->flags, 4u);
+        }
+    };
+    const int size = LIST ? entries_bytes(A.K) : 0;
+    int64_t row = blockIdx.x;
+    int turn = 0;
+    Head head{-1, -INFINITY, 1.0f, 0.0f, 0.0f, 0.0f}, next_head = head;
+    bool counts;
+    // The first row
+    ask_head<KIND>(A, row, head);
+    if (!LIST) {
+        head.t = id_at(A, row);
+        ask_token(A, logits_of(row), mask_of(row), head);
+        counts = head.t >= 0;
+    }
+    if (MASKED) {
+        read_words(row);
+        store_words();
+        if (LIST && tid < 2) Entries(entries + tid * size, A.K).end->flags = 0;
+        __syncthreads();
+        if (LIST) {
+            ask_entry(row, ahead);
+            ask_entry_logit(row, ahead);
+            list_row(row, Entries(entries, A.K));
+            ask_entry(row + gridDim.x, ahead);
+            ask_entry_logit(row + gridDim.x, ahead);
+            ask_entry(row + 2 * (int64_t)gridDim.x, after);
+            __syncthreads();
+            counts = Entries(entries, A.K).end->flags != 0;
+        }
+    }
+    mine = Part{-FLT_MAX, 0.0f, 0.0f, 0.0f};
+    if (counts) {
+#pragma unroll
+        for (int i = 0; i < NP; i++) if (i * TH < n_pieces) fetch(logits_of(row), i);
+#pragma unroll
+        for (int i = 0; i < NP; i++) if (i * TH < n_pieces) add(i);
+        fetch_last(logits_of(row));
+        add_last();
+    }
+    if (!LIST && row + gridDim.x < A.r.rows) next_head.t = id_at(A, row + gridDim.x);
+    for (;;) {
+        asm volatile("" : "+v"(tid), "+s"(n_pieces));      // (whether a thread has its i-th piece is found anew for each row: kept, that would be registers of every i)
+        const Entries E(entries + turn * size, A.K), next_E(entries + (turn ^ 1) * size, A.K);
+        const int64_t next = row + gridDim.x;
+        const bool more = next < A.r.rows;
+        ElemT *const grad = (ElemT *)A.grad + row * A.grad_stride;
+        if (LIST && counts) for (int u = wave; u < (A.K + 63) / 64; u += WAVES) sum_entries(A, u, lane, E);
+        if (MASKED && more) read_words(next);
+        if (more) {
+            ask_head<KIND>(A, next, next_head);
+            if (!LIST) ask_token(A, logits_of(next), mask_of(next), next_head);
+        }
+        live = next_live;
+        next_live = 0;
+        mine = join_wave(mine, A.c);
+        if (lane == 0) part[wave] = mine;
+        __syncthreads();
+        if (MASKED && more) store_words();
+        if (LIST) {
+            if (tid == 0) next_E.end->flags = 0;
+            __syncthreads();
+            if (more) list_row(next, next_E);
+        }
+        if (wave == 0) {
+            if (counts) finish_row<KIND, ENT>(A, join_wave(lane < WAVES ? part[lane] : Part{-FLT_MAX, 0.0f, 0.0f, 0.0f}, A.c), row, head, head.weight * g, lane, E, shared_ends);
+            else if (lane == 0) no_row<KIND, ENT>(A, row);
+        }
+        __syncthreads();
+        const Ends ends = shared_ends;
+        const bool next_counts = more && (LIST ? next_E.end->flags != 0 : next_head.t >= 0), all = wild(ends);
+        if (LIST) {
+            ahead = after;
+            ask_entry_logit(next + gridDim.x, ahead);
+            ask_entry(next + 2 * (int64_t)gridDim.x, after);
+        }
+        const int64_t next_t = !LIST && next + gridDim.x < A.r.rows ? id_at(A, next + gridDim.x) : -1;
+        const ElemT *const next_logits = logits_of(next);
+        mine = Part{-FLT_MAX, 0.0f, 0.0f, 0.0f};
+        const float x_of_row[1] = {x_last};
+        if (next_counts) fetch_last(next_logits);
+#pragma unroll
+        for (int i = 0; i < NP + LAG; i++) {
+            if (i < NP && i * TH < n_pieces) {
+                float d[EPV] = {};
+                if (counts && (!MASKED || __any((live >> i) & 1u))) {
+                    float x[EPV];
+                    numbers<EPV, ElemT>(raw[i], x);
+                    if (all) grad_of_wild<ENT>(x, ends, A.c, d);
+                    else grad_of<ENT>(x, ends, A.c, d);
+                }
+                if (tid + i * TH < n_pieces) store_numbers<EPV, ElemT>((char *)grad + i * (TH * 16) + at_tid, d);
+                if (next_counts) fetch(next_logits, i);
+            }
+            if (i >= LAG && (i - LAG) * TH < n_pieces && next_counts) add(i - LAG);
+        }
+        if (last) {
+            float d[1] = {0.0f};
+            if (counts) grad_of_wild<ENT>(x_of_row, ends, A.c, d);
+            store_element(grad + v_last, d[0]);
+        }
+        if (next_counts) add_last();
+        if (!LIST) {                                       // by the thread that has just written the token's piece
+            if (counts && head.x != -INFINITY && tid == writer_of<TH, EPV>(head.t, V)) store_element(grad + head.t, ends.at_token);
+        } else {
+            __syncthreads();
+            if (counts) store_entries<TH>(A, E, grad);
+        }
+        if (!more) return;
+        row = next;
+        turn ^= 1;
+        counts = next_counts;
+        head = next_head;
+        next_head.t = next_t;
     }
 }
 
@@ -444,7 +790,7 @@ template <int TH, typename ElemT>
 __global__ __launch_bounds__(TH) void preference_grad_kernel(const zf_preference_args p, const float *g, float c, int32_t W, void *grad_, int64_t grad_stride) {
     constexpr int EPV = 16 / sizeof(ElemT);
     const int tid = threadIdx.x;
-    const int32_t V = p.r.V, n_pieces = (V + EPV - 1) / EPV;
+    const int32_t V = p.r.V, n_pieces = V / EPV;
     for (int64_t row = blockIdx.x; row < p.r.rows; row += gridDim.x) {
         const ElemT *const logits = (const ElemT *)p.r.logits + row * p.r.row_stride_elems;
         ElemT *const grad = (ElemT *)grad_ + row * grad_stride;
@@ -459,36 +805,64 @@ __global__ __launch_bounds__(TH) void preference_grad_kernel(const zf_preference
         const float m = p.stats[2 * row], inv_S = p.stats[2 * row + 1], f = counts ? (float)((double)p.slopes[low] * *g / p.r.temperature) : 0.0f;
         const float base = -f * inv_S;
         const bool look = !(fabsf(base) < INFINITY);
+        const Ends ends{m, base, 0.0f, 0.0f};
         for (int32_t j = tid; j < n_pieces; j += TH) {
             const int64_t v = (int64_t)j * EPV;
-            float x[EPV], d[EPV];
-            load_piece<EPV>(logits, v, V, counts ? bits_of<EPV>(mask, v, V) : 0u, x);
+            float x[EPV], d[EPV] = {};
+            if (counts) {
+                load_numbers<EPV>(logits + v, bits_of<EPV>(mask, v), x);
+                if (look) grad_of_wild<false>(x, ends, c, d);
+                else grad_of<false>(x, ends, c, d);
+                if (t / EPV == j) {
 #pragma unroll
-            for (int k = 0; k < EPV; k++) {
-                d[k] = two_to((x[k] - m) * c) * base;
-                if (!counts || (look && x[k] == -INFINITY)) d[k] = 0.0f;
+                    for (int k = 0; k < EPV; k++) if (t % EPV == k) d[k] += f;
+                }
             }
-            if (counts && t / EPV == j) {
-#pragma unroll
-                for (int k = 0; k < EPV; k++) if (t % EPV == k) d[k] += f;
+            store_numbers<EPV, ElemT>(grad + v, d);
+        }
+        if (tid < V % EPV) {
+            const int32_t v = V - V % EPV + tid;
+            float d[1] = {0.0f};
+            if (counts) {
+                const float x[1] = {allowed(mask, v) ? of_bits(logits[v]) : -INFINITY};
+                grad_of_wild<false>(x, ends, c, d);
+                if (t == v) d[0] += f;
             }
-            store_piece<EPV>(grad, v, V, d);
+            store_element(grad + v, d[0]);
         }
     }
 }
 
+static const int COMPUTE_UNITS = 256;
 int grid_of(int64_t n) { return (int)std::min<int64_t>(n, 1 << 16); }
+// TH threads take a row, NP pieces each at most; `each`: workgroups that a compute unit's registers hold.  Without a gradient a row is read from memory by as many threads, in the same order.
+template <int TH, int NP, int KIND, bool ENT, typename ElemT>
+void rows_by(const Args &A, hipStream_t s) {
+    const int lds = KIND == DISTILL ? entries_bytes(A.K) : 0;
+    if constexpr (KIND != LOGPROB && NP > 0) {
+        if (A.grad) {
+            const dim3 grid((int)std::min<int64_t>(A.r.rows, 1024 / TH * COMPUTE_UNITS));
+            if (KIND == DISTILL || A.r.mask) hipLaunchKernelGGL((loss_resident_kernel<TH, NP, KIND, true, ENT, ElemT>), grid, dim3(TH), 2 * lds, s, A);
+            else if constexpr (KIND != DISTILL) hipLaunchKernelGGL((loss_resident_kernel<TH, NP, KIND, false, ENT, ElemT>), grid, dim3(TH), 0, s, A);
+            return;
+        }
+    }
+    hipLaunchKernelGGL((loss_rows_kernel<TH, KIND, ENT, ElemT>), dim3(grid_of(A.r.rows)), dim3(TH), lds, s, A);
+}
+template <int KIND, bool ENT, typename ElemT>
+void rows_of(const Args &A, hipStream_t s) {
+    const int32_t n = (A.r.V + (int)(16 / sizeof(ElemT)) - 1) / (int)(16 / sizeof(ElemT));    // pieces of a row
+    if (n <= 16 * 64) return rows_by<64, 16, KIND, ENT, ElemT>(A, s);
+    if (n <= 16 * 256) return rows_by<256, 16, KIND, ENT, ElemT>(A, s);
+    if (n <= 16 * 512) return rows_by<512, 16, KIND, ENT, ElemT>(A, s);
+    if (n <= 16 * 1024) return rows_by<1024, 16, KIND, ENT, ElemT>(A, s);
+    if (n <= 20 * 1024) return rows_by<1024, 20, KIND, ENT, ElemT>(A, s);
+    rows_by<1024, 0, KIND, ENT, ElemT>(A, s);
+}
 template <int KIND, bool ENT>
 void rows_of(const Args &A, hipStream_t s) {
-    const bool small = A.r.V * (A.r.dtype == 0 ? 4 : 2) <= 32768;
-    const dim3 grid(grid_of(A.r.rows));
-    if (A.r.dtype == 0) {
-        if (small) hipLaunchKernelGGL((loss_rows_kernel<256, KIND, ENT, uint32_t>), grid, dim3(256), 0, s, A);
-        else hipLaunchKernelGGL((loss_rows_kernel<1024, KIND, ENT, uint32_t>), grid, dim3(1024), 0, s, A);
-    } else {
-        if (small) hipLaunchKernelGGL((loss_rows_kernel<256, KIND, ENT, uint16_t>), grid, dim3(256), 0, s, A);
-        else hipLaunchKernelGGL((loss_rows_kernel<1024, KIND, ENT, uint16_t>), grid, dim3(1024), 0, s, A);
-    }
+    if (A.r.dtype == 0) rows_of<KIND, ENT, uint32_t>(A, s);
+    else rows_of<KIND, ENT, uint16_t>(A, s);
 }
 Args common(const zf_loss_rows &r, const LossGrad &g) {
     Args A{};
