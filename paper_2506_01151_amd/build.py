@@ -29,7 +29,7 @@ def _run(cmd):
 
 
 def _extension_jobs(force):
-    """The extension modules of the Python binding (host code): _native, and _native_torch and _native_ops, which are compiled against torch's headers."""
+    """The extension modules of the Python binding (host code): _native, and _native_torch, _native_ops and _native_losses, which are compiled against torch's headers."""
     import torch
     from torch.utils.cpp_extension import include_paths, library_paths
     abi = int(torch._C._GLIBCXX_USE_CXX11_ABI)
@@ -39,9 +39,10 @@ def _extension_jobs(force):
         torch_flags += ["-isystem", p]
     libs = [f for p in library_paths() if os.path.isdir(p) for f in ["-L" + p]] + ["-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python"]
     jobs = []
-    for src, name, flags, link in (("zf_py.cpp", "_native.so", [], []), ("zf_py_torch.cpp", "_native_torch.so", torch_flags, libs), ("zf_py_ops.cpp", "_native_ops.so", torch_flags, libs + ["-ltorch_hip"])):
+    for src, name, flags, link in (("zf_py.cpp", "_native.so", [], []), ("zf_py_torch.cpp", "_native_torch.so", torch_flags, libs), ("zf_py_ops.cpp", "_native_ops.so", torch_flags, libs + ["-ltorch_hip"]),
+                                  ("zf_py_losses.cpp", "_native_losses.so", torch_flags, libs + ["-ltorch_hip"])):
         path, out = os.path.join(CSRC, src), os.path.join(HERE, name)
-        newest = max(os.path.getmtime(p) for p in (path, os.path.join(CSRC, "zf_py.h"), os.path.join(HERE, "..", "include", "zapformat.h")))
+        newest = max(os.path.getmtime(p) for p in (path, os.path.join(CSRC, "zf_py.h"), os.path.join(CSRC, "zf_py_tensors.h"), os.path.join(HERE, "..", "include", "zapformat.h")))
         if force or not os.path.exists(out) or os.path.getmtime(out) < newest:
             jobs.append(common + flags + [path, "-o", out] + link)
     return jobs

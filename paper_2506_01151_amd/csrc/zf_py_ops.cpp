@@ -1,23 +1,9 @@
 // Extension module _native_ops: the calls at the two ends of a step's logits (operators.py), from Python to the library, with outputs and
 // workspace from torch's allocator.  In Python a call cost 13 us of checks and marshalling, and one with a gradient 70.
-//   As in _native, a call that is not the ordinary case -- other types, shapes that do not fit, tensors that cannot be looked at -- is not
-// taken (None is returned), and operators.py does, or refuses, what it defines.
 #define PY_SSIZE_T_CLEAN
-#include <torch/csrc/autograd/custom_function.h>
-#include <torch/csrc/autograd/functions/basic_ops.h>
-#include <torch/csrc/autograd/python_variable.h>
-#include <ATen/TracerMode.h>
-#include <ATen/hip/EmptyTensor.h>
-#include <c10/core/impl/TorchDispatchModeTLS.h>
-#include <c10/hip/HIPStream.h>
-#include <optional>
-#include <string>
-#include <vector>
-#include "../../include/zapformat.h"
+#include "zf_py_tensors.h"
 
 namespace {
-
-using at::Tensor;
 
 struct {                               // the library's calls (addresses given by binding.py)
     int (*quantize_blocks)(const void *, int32_t, int64_t, int32_t, int64_t, int32_t, uint8_t *, float *, int32_t, void *);
@@ -27,32 +13,8 @@ struct {                               // the library's calls (addresses given b
     int (*backward)(const zf_logprobs_args *, const float *, const float *, const float *, void *, int64_t, int32_t, void *);
     const char *(*last_error)(void);
 } L;
-PyObject *check_py = nullptr;          // binding._check: raises for a return code
-
-struct Failed { int rc; };             // a code of the library
 
 const int64_t BLOCK = 128;
-int logit_type(const Tensor &t) { return t.scalar_type() == at::kFloat ? 0 : t.scalar_type() == at::kBFloat16 ? 1 : -1; }
-bool has_tangent(const Tensor &t) { return t._fw_grad(0).defined(); }
-bool plain(const Tensor &t) { return t.layout() == at::kStrided && t.is_cuda() && !t.is_nested() && !t.unsafeGetTensorImpl()->has_symbolic_sizes_strides() && !t.is_neg() && !t.is_conj() && !has_tangent(t); }
-bool matrix(const Tensor &t) { return plain(t) && t.dim() == 2; }
-bool rows_without_gaps(const Tensor &t) { return t.size(1) <= 1 || t.stride(1) == 1; }
-int64_t row_stride(const Tensor &t) { return t.size(0) > 1 ? t.stride(0) : t.size(1); }
-void *stream_of(const Tensor &t) { return (void *)c10::hip::getCurrentHIPStream(t.get_device()).stream(); }
-// From torch's allocator, without the way through its dispatcher (a call of token_logprobs with four of them 8.0 us of the host, so 6.6).
-Tensor fresh(c10::IntArrayRef size, at::ScalarType type, const Tensor &like) { return at::detail::empty_cuda(size, type, like.device(), std::nullopt); }
-void must(int rc) { if (rc != ZF_OK) throw Failed{rc}; }
-
-// None for an object that is None, a tensor; false: neither, or not a plain one
-bool tensor_or_none(PyObject *o, std::optional<Tensor> *out) {
-    if (o == Py_None) { out->reset(); return true; }
-    if (!THPVariable_CheckExact(o)) return false;
-    *out = THPVariable_Unpack(o);
-    return true;
-}
-bool mask_fits(const std::optional<Tensor> &m, int64_t rows, int64_t V, const Tensor &with) {
-    return !m || (matrix(*m) && m->scalar_type() == at::kInt && m->is_contiguous() && m->size(0) == rows && m->size(1) == (V + 31) / 32 && m->device() == with.device());
-}
 
 // ---- the calls ----
 PyObject *quantize_blocks(PyObject *const *args, Py_ssize_t n) {       // (x, block_rows)
@@ -117,15 +79,6 @@ Results forward(const Tensor &logits, const std::optional<Tensor> &tokens, const
     return r;
 }
 
-// A saved tensor, or an incoming gradient, for a kernel to read: what hooks on saved tensors give back may lie anywhere, in any order.
-Tensor kept(const Tensor &t, const char *what, const Tensor &with, at::ScalarType type, c10::IntArrayRef size, bool rows_apart = false) {
-    TORCH_CHECK(t.layout() == at::kStrided && t.is_cuda() && !t.is_nested() && t.device() == with.device() && t.scalar_type() == type && t.sizes() == size, "token_logprobs: saved ", what,
-                " came back with another device, type or shape: ", t.toString(), " ", t.sizes(), " on ", t.device(), " instead of ", size, " on ", with.device());
-    TORCH_CHECK(!has_tangent(t), "token_logprobs: its gradient has no forward-mode derivative");
-    const bool as_it_is = rows_apart ? t.dim() == 2 && t.stride(1) == 1 && row_stride(t) >= t.size(1) : t.is_contiguous();
-    return as_it_is && plain(t) ? t : t.detach().resolve_neg().contiguous();
-}
-
 struct TokenLogprobs : public torch::autograd::Function<TokenLogprobs> {
     static torch::autograd::variable_list forward(torch::autograd::AutogradContext *ctx, const Tensor &logits, const std::optional<Tensor> &tokens, const std::optional<Tensor> &mask,
                                                   double temperature, bool entropy, int64_t top) {
@@ -141,10 +94,10 @@ struct TokenLogprobs : public torch::autograd::Function<TokenLogprobs> {
     }
     static torch::autograd::variable_list backward(torch::autograd::AutogradContext *ctx, torch::autograd::variable_list grads) {
         const auto saved = ctx->get_saved_variables();
-        const Tensor logits = kept(saved[0], "logits", saved[0], saved[0].scalar_type(), saved[0].sizes(), true);
+        const Tensor logits = kept("token_logprobs", saved[0], "logits", saved[0], saved[0].scalar_type(), saved[0].sizes(), true);
         TORCH_CHECK(logits.dim() == 2 && logit_type(logits) >= 0, "token_logprobs: saved logits came back as others");
         const int64_t rows = logits.size(0), V = logits.size(1);
-        auto some = [&](int i, const char *what, at::ScalarType type, c10::IntArrayRef size) { return saved[i].defined() ? std::optional<Tensor>(kept(saved[i], what, logits, type, size)) : std::nullopt; };
+        auto some = [&](int i, const char *what, at::ScalarType type, c10::IntArrayRef size) { return saved[i].defined() ? std::optional<Tensor>(kept("token_logprobs", saved[i], what, logits, type, size)) : std::nullopt; };
         auto width = [&](int i) { return saved[i].defined() && saved[i].dim() == 2 ? saved[i].size(1) : 0; };
         const int64_t of_rows[] = {rows, width(3)}, of_top[] = {rows, width(5)};
         const c10::IntArrayRef given(of_rows, saved[3].defined() && saved[3].dim() == 2 ? 2 : 1);
@@ -154,7 +107,7 @@ struct TokenLogprobs : public torch::autograd::Function<TokenLogprobs> {
         size_t at = 0;
         auto next = [&](const std::optional<Tensor> &of) {
             const Tensor g = of ? grads[at++] : Tensor();
-            return g.defined() ? kept(g.scalar_type() == at::kFloat ? g : g.detach().to(at::kFloat), "gradient", logits, at::kFloat, of->sizes()) : g;
+            return g.defined() ? kept("token_logprobs", g.scalar_type() == at::kFloat ? g : g.detach().to(at::kFloat), "gradient", logits, at::kFloat, of->sizes()) : g;
         };
         const Tensor g_lp = next(r.logprobs), g_H = next(r.entropy);
         (void)next(r.ids);
@@ -200,31 +153,6 @@ PyObject *token_logprobs(PyObject *const *args, Py_ssize_t n) {        // (logit
         PyTuple_SET_ITEM(t, i, o);
     }
     return t;
-}
-
-// Somebody watches what torch is asked for on this thread: a tracer, which operators.py refuses, or a dispatch mode that wants to see the allocations.
-bool watched() {
-    return at::tracer::impl::is_dispatch_enabled() || c10::impl::tls_is_dispatch_key_included(at::DispatchKey::PreDispatch) || c10::impl::TorchDispatchModeTLS::any_modes_set();
-}
-
-// Python calls C: no C++ exception goes that way.
-typedef PyObject *(*Call)(PyObject *const *, Py_ssize_t);
-template <Call F>
-PyObject *guarded(PyObject *, PyObject *const *args, Py_ssize_t n) {
-    try {
-        if (watched()) Py_RETURN_NONE;
-        PyObject *r = F(args, n);
-        if (r || PyErr_Occurred()) return r;
-    } catch (const Failed &e) {
-        PyObject *code = PyLong_FromLong(e.rc);
-        if (!code) return nullptr;
-        PyObject *r = PyObject_CallOneArg(check_py, code);      // raises
-        Py_DECREF(code);
-        Py_XDECREF(r);
-        if (!PyErr_Occurred()) PyErr_SetString(PyExc_RuntimeError, "an error code that raises nothing");
-        return nullptr;
-    } catch (...) {}                   // a tensor that torch does not let be looked at, no memory: operators.py meets the same and raises what torch raises
-    Py_RETURN_NONE;
 }
 
 PyObject *bind(PyObject *, PyObject *args) {                    // ({name: address}, _check)

@@ -18,8 +18,13 @@ from typing import NamedTuple, Optional
 
 import torch
 
+from . import _native_losses
 from .binding import DistillArgs, PolicyArgs, PreferenceArgs, _check
 from .operators import _DTYPES, _kept, _lib, _mask_ptr, _matrix, _need, _not_traced, _plain, _row_stride, _stream
+
+_native_losses.bind({n: ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in (
+    "zf_distill_loss", "zf_distill_loss_backward", "zf_policy_loss", "zf_policy_loss_backward", "zf_preference_loss", "zf_preference_loss_backward", "zf_last_error")}, _check)
+# The ordinary call is _native_losses' (csrc/zf_py_losses.cpp); what it does not take it answers with None, and the code here, its definition, does or refuses it.
 
 _IDS = (torch.int32, torch.int64)
 _F32 = (torch.float32,)
@@ -231,6 +236,9 @@ def distill_loss(logits, teacher_ids, teacher_values, mask=None, *, temperature=
     The teacher's shares are softmax(teacher_values / temperature) over them: logits, or log probabilities, of the teacher.  With rest=True they are e^teacher_values -- log probabilities, at that
     temperature, as token_logprobs reports them -- and what is missing from 1 is the share of all other tokens together, which the student's probability of these is held to
     (where there are none, or the listed shares are 1 or more, nothing is).  A row of which no token counts: loss 0, no gradient."""
+    got = _native_losses.distill_loss(logits, teacher_ids, teacher_values, mask, temperature, bool(rest), weight)
+    if got is not None:
+        return DistillLoss(*got)
     temperature = _checked(logits, mask, temperature)
     _need(isinstance(teacher_ids, torch.Tensor) and teacher_ids.dim() == 2 and 1 <= teacher_ids.shape[1] <= 1024, "teacher_ids: [rows, 1..1024] is wanted")
     shape = (logits.shape[0], teacher_ids.shape[1])
@@ -249,6 +257,10 @@ def policy_loss(logits, tokens, old_logprobs, advantages, mask=None, *, ref_logp
 
     tokens: int32 or int64 [rows]; old_logprobs, advantages, ref_logprobs, weight: fp32 [rows].  A negative token is padding: loss, log probability and entropy 0, no gradient.  A token
     that is not allowed: log probability -inf, loss 0, no gradient.  An id beyond V: NaN."""
+    if type(clip) is tuple and len(clip) == 2:
+        got = _native_losses.policy_loss(logits, tokens, old_logprobs, advantages, mask, ref_logprobs, temperature, *clip, kl_weight, entropy_weight is not None, entropy_weight or 0.0, weight)
+        if got is not None:
+            return PolicyLoss(*got)
     temperature = _checked(logits, mask, temperature)
     shape, dev = (logits.shape[0],), logits.device
     _constant(tokens, "tokens", _IDS, shape, dev)
@@ -271,6 +283,9 @@ def preference_loss(logits, tokens, offsets, ref_logprobs=None, mask=None, *, be
     offsets: int32 or int64 [2 pairs + 1]: sequence s has the rows offsets[s] up to offsets[s + 1]; of each pair the preferred one comes first.  tokens: int32 or int64 [rows], ref_logprobs:
     fp32 [rows]; weight: fp32 [pairs].  Negative tokens (prompts) and rows of no sequence are passed over.  A token that is not allowed: log probability -inf, no gradient of its
     own.  Offsets that descend or leave the rows: NaN for their pair."""
+    got = _native_losses.preference_loss(logits, tokens, offsets, ref_logprobs, mask, beta, label_smoothing, bool(average), temperature, weight)
+    if got is not None:
+        return PreferenceLoss(*got)
     temperature = _checked(logits, mask, temperature)
     shape, dev = (logits.shape[0],), logits.device
     _constant(tokens, "tokens", _IDS, shape, dev)

@@ -17,6 +17,19 @@ U, INF, TINY = 2.0 ** -24, math.inf, 2.0 ** -126
 IDS = {4: torch.int32, 8: torch.int64}
 
 
+@pytest.fixture(params=["module", "definition"])
+def by(request, monkeypatch):
+    """The extension module's way, and losses.py's own, which takes what the module does not."""
+    if request.param == "definition":
+        from paper_2506_01151_amd import losses
+
+        class Nothing:
+            distill_loss = policy_loss = preference_loss = staticmethod(lambda *args: None)
+
+        monkeypatch.setattr(losses, "_native_losses", Nothing)
+    return request.param
+
+
 # ---- rows, and what is known of them in 64 bits -----------------------------------------------------
 class Rows:
     """logits [rows, V] of a type, a mask of a kind, and in 64 bits: lp, p (0 where nothing is allowed), what is allowed, slack [rows, 1]."""
@@ -438,7 +451,7 @@ def three(x, mask=None, needs=None, **more):
 
 @gpu
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-def test_what_is_forbidden_is_not_looked_at(dtype):
+def test_what_is_forbidden_is_not_looked_at(dtype, by):
     """NaN, infinities and the type's largest numbers in forbidden places change nothing, and their gradient is 0; -inf in allowed places is as forbidden."""
     g = torch.Generator().manual_seed(5)
     x = torch.randn((6, 3000), generator=g).to(DTYPES[dtype])
@@ -474,7 +487,7 @@ def test_what_is_not_a_number_makes_its_row_nan(bad):
 
 
 @gpu
-def test_ids_beyond_the_vocabulary():
+def test_ids_beyond_the_vocabulary(by):
     x = torch.randn((4, 100), generator=torch.Generator().manual_seed(7)).cuda().requires_grad_()
     t = torch.tensor([3, 100, 2 ** 40, 99], device="cuda")
     one = torch.ones((4,), device="cuda")
@@ -542,7 +555,7 @@ def same_twice(x, mask):
 
 @gpu
 @pytest.mark.parametrize("V", [900, 40037])
-def test_gradients_of_any_factor_and_twice(V):
+def test_gradients_of_any_factor_and_twice(V, by):
     """A factor other than one; a second backward pass, with another factor, leaves what the first gave; a gradient that was written is not given again."""
     r = Rows(5, V, "f32", "share", 1.0, 10)
     r.bits[:, 1:3] = True
@@ -590,6 +603,42 @@ def test_gradients_against_differences():
 
 
 @gpu
+def test_module_and_definition_agree(monkeypatch):
+    """The same bits, with and without a gradient, of every argument."""
+    from paper_2506_01151_amd import losses
+    r = Rows(9, 3001, "bf16", "share", 1.0, 18)
+    r.bits[:, 1:3] = True
+    x, m = r.on_gpu("odd")
+    x.requires_grad_()
+    t, zeros, ids, v, half = beside(x)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    a, b, w = (torch.rand(9, generator=g, device="cuda") for _ in range(3))
+    calls = [lambda: zf.distill_loss(x, ids.int(), v.bfloat16(), m, temperature=0.7, rest=True, weight=w), lambda: zf.distill_loss(x, ids, v, temperature=2),
+             lambda: zf.policy_loss(x, t, a - 8, b, m, ref_logprobs=w - 8, temperature=1.3, clip=(0.1, 0.4), kl_weight=0.3, entropy_weight=0.2, weight=w), lambda: zf.policy_loss(x, t.int(), a - 8, b, clip=[0, 1]),
+             lambda: zf.preference_loss(x, t, half.int(), a - 8, m, beta=0.3, label_smoothing=0.1, average=True, temperature=0.9, weight=w[:1]), lambda: zf.preference_loss(x, t, half)]
+
+    def results():
+        out = []
+        for call in calls:
+            got = call()
+            with torch.no_grad():
+                alone = call()
+            assert type(got) is type(alone) and [y is None for y in got] == [y is None for y in alone]
+            assert got.loss.requires_grad and not any(y.requires_grad for y in got[1:] if y is not None) and not alone.loss.requires_grad
+            out += [y.detach() for y in (*got, *alone) if y is not None] + list(torch.autograd.grad(got.loss, x, torch.tensor(0.7, device="cuda")))
+        return out
+
+    mine = results()
+
+    class Nothing:
+        distill_loss = policy_loss = preference_loss = staticmethod(lambda *args: None)
+
+    monkeypatch.setattr(losses, "_native_losses", Nothing)
+    theirs = results()
+    assert len(mine) == len(theirs) and all(torch.equal(p, q) and p.dtype == q.dtype and p.stride() == q.stride() for p, q in zip(mine, theirs))
+
+
+@gpu
 def test_results_are_the_same_every_time():
     r = Rows(300, 20000, "bf16", "share", 1.0, 12)
     r.bits[:, 1:3] = True
@@ -602,7 +651,7 @@ def test_results_are_the_same_every_time():
 
 
 @gpu
-def test_what_was_written_since_raises():
+def test_what_was_written_since_raises(by):
     r = Rows(6, 1000, "f32", "share", 1.0, 13)
     r.bits[:, 1:3] = True
     x, m = r.on_gpu()
@@ -620,7 +669,7 @@ def test_what_was_written_since_raises():
 
 
 @gpu
-def test_hooks_on_saved_tensors():
+def test_hooks_on_saved_tensors(by):
     """What they give back may lie elsewhere, in another layout: the gradient is the same; another shape is refused."""
     r = Rows(6, 1003, "bf16", "share", 1.0, 14)
     r.bits[:, 1:3] = True
@@ -641,7 +690,7 @@ def test_hooks_on_saved_tensors():
 
 
 @gpu
-def test_on_another_stream_and_differentiated_once():
+def test_on_another_stream_and_differentiated_once(by):
     r = Rows(6, 1000, "f32", "share", 1.0, 15)
     r.bits[:, 1:3] = True
     x, m = r.on_gpu()
@@ -660,7 +709,7 @@ def test_on_another_stream_and_differentiated_once():
 
 
 @gpu
-def test_captured_into_a_graph():
+def test_captured_into_a_graph(by):
     """Losses and gradients replayed with other logits and other factors, eager work between the replays."""
     r = Rows(40, 5000, "f32", "share", 1.0, 16)
     r.bits[:, 1:3] = True
@@ -692,7 +741,7 @@ def test_captured_into_a_graph():
 
 
 @gpu
-def test_a_backward_pass_alone_in_a_graph():
+def test_a_backward_pass_alone_in_a_graph(by):
     """Made eagerly, followed back in a capture: each replay gives the gradient by the factor of its time."""
     r = Rows(7, 3000, "f32", "none", 1.0, 17)
     x, _ = r.on_gpu()
@@ -761,7 +810,7 @@ def test_refusals_on_the_host():
 
 
 @gpu
-def test_refusals():
+def test_refusals(by):
     x = torch.zeros((4, 40), device="cuda", requires_grad=True)
     t, f = torch.zeros(4, dtype=torch.int64, device="cuda"), torch.zeros(4, device="cuda")
     ids, v, o = torch.zeros((4, 2), dtype=torch.int32, device="cuda"), torch.zeros((4, 2), device="cuda"), torch.tensor([0, 2, 4], device="cuda")
@@ -808,7 +857,7 @@ def test_refusals():
 
 # ---- together ---------------------------------------------------------------------------------------
 @gpu
-def test_a_learner_with_all_three():
+def test_a_learner_with_all_three(by):
     """Sequences decoded under a grammar; their policy's loss, distillation from a teacher that reports as a server does, and a preference between them, on one batch of logits."""
     from examples import decode_and_train as ex
     from workloads import configs
