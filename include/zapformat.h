@@ -361,7 +361,7 @@ int zf_policy_loss_backward(const zf_policy_args *a, const float *d_g, int32_t h
  * sequence's rows whose token is not negative (with `average` their mean; 0 where there are none), chosen = beta D_2i, rejected = beta D_2i+1, h = chosen - rejected:
  *   losses = - (1 - label_smoothing) ln sigma(h) - label_smoothing ln sigma(-h)
  * Rows of no sequence and of negative tokens have no gradient.  A token that is not allowed: log probability -inf, no gradient.  A pair whose offsets descend or leave 0 .. rows: NaN.
- * logprobs, stats, slopes are what the gradient is made from (written by the first call). */
+ * stats and slopes are what the gradient is made from (written by the first call). */
 typedef struct {
     zf_loss_rows r;
     const void *tokens;        /* device, [rows] */
@@ -372,8 +372,7 @@ typedef struct {
     double beta, label_smoothing;
     int32_t average, reserved;
     float *chosen, *rejected;  /* device, [pairs] */
-    float *logprobs;           /* device, [rows] */
-    float *stats;              /* device, [rows][2] */
+    float *stats;              /* device, [rows][4], aligned to 16 bytes */
     float *slopes;             /* device, [2 pairs] */
 } zf_preference_args;
 int zf_preference_loss(const zf_preference_args *a, int32_t device, void *hip_stream);

@@ -82,7 +82,7 @@ class PolicyArgs(ctypes.Structure):
 class PreferenceArgs(ctypes.Structure):
     _fields_ = [("r", LossRows), ("tokens", c_vp), ("offsets", c_vp), ("ref_logprobs", c_vp), ("token_bytes", c_i32), ("offset_bytes", c_i32), ("pairs", c_i64),
                 ("beta", ctypes.c_double), ("label_smoothing", ctypes.c_double), ("average", c_i32), ("reserved", c_i32),
-                ("chosen", c_vp), ("rejected", c_vp), ("logprobs", c_vp), ("stats", c_vp), ("slopes", c_vp)]
+                ("chosen", c_vp), ("rejected", c_vp), ("stats", c_vp), ("slopes", c_vp)]
 
 
 EXPORTS = ["zf_strerror", "zf_last_error", "zf_compile", "zf_engine_destroy", "zf_engine_get_info",

@@ -17,7 +17,7 @@
 namespace zf {
 namespace {
 
-enum Kind { POLICY, DISTILL, LOGPROB };       // LOGPROB: of the given tokens alone, and what a gradient needs (preferences)
+enum Kind { POLICY, DISTILL, LOGPROB };       // LOGPROB: of preferences' tokens alone, and what their gradient needs
 
 static const int CHUNK = 1 << 17;             // tokens whose bits LDS holds: which of them a row's teacher listed
 
@@ -32,9 +32,14 @@ struct Args {
     const float *g;                            // the loss's own gradient, or null: one
     int32_t held;                              // the gradient for g = 1 is in place
     int32_t results;                           // the losses are wanted
+    int32_t once;                              // logits and gradient are larger than the last-level cache: they pass it by
     const float *old_logprobs, *advantages, *ref;
     double lowest, highest, kl_weight, entropy_weight;
-    float *logprobs, *entropy, *stats;
+    float *logprobs, *entropy;
+    const void *offsets;                       // preferences: [sequences + 1]
+    int64_t sequences;
+    int32_t offset_bytes;
+    float4 *found;                             // [rows], of preferences
 };
 
 struct Part { float m, S, T, pad; };
@@ -84,29 +89,39 @@ __device__ __forceinline__ void forbid(u32x4 &r, uint32_t bits) {
         r[k] = (r[k] & yes) | (NONE & ~yes);
     }
 }
-template <int EPV, typename ElemT>
-__device__ __forceinline__ void store_numbers(void *to, const float (&d)[EPV]) {
-    union { u32x4 v; bf16x2 b[4]; } o;
-#pragma unroll
-    for (int k = 0; k < EPV; k += 2) {
-        if (sizeof(ElemT) == 4) { o.v[k % 4] = __float_as_uint(d[k]); o.v[k % 4 + 1] = __float_as_uint(d[k + 1]); }
-        else o.b[k / 2 % 4] = bf16x2{(__bf16)d[k], (__bf16)d[k + 1]};
-    }
-    *reinterpret_cast<typename Piece<ElemT>::type *>(to) = o.v;
+#define GLOBAL __attribute__((address_space(1)))
+// (Statements of nothing at either end of a branch: else the compiler makes the two accesses one, an ordinary one.)
+template <typename ElemT>
+__device__ __forceinline__ void store_raw(GLOBAL char *to, u32x4 v, bool once) {
+    GLOBAL typename Piece<ElemT>::type *const at = (GLOBAL typename Piece<ElemT>::type *)to;
+    if (once) {
+        asm volatile("");
+        __builtin_nontemporal_store(v, at);
+        asm volatile("");
+    } else *at = v;
 }
+template <typename ElemT>
+__device__ __forceinline__ void store_raw(ElemT *to, u32x4 v, bool once) { store_raw<ElemT>((GLOBAL char *)to, v, once); }
 template <typename ElemT>
 __device__ __forceinline__ void store_element(ElemT *to, float x) {
     if (sizeof(ElemT) == 4) *(float *)to = x;
     else *(__bf16 *)to = (__bf16)x;
 }
-// A piece from memory, of whose places `bits` are wanted: nothing is read where there are none.
-template <int EPV, typename ElemT>
-__device__ __forceinline__ void load_numbers(const ElemT *at, uint32_t bits, float (&x)[EPV]) {
+// U pieces from memory at a distance of TH, of whose places `bits` are wanted: all are asked for before the first is looked at, and nothing is where there are none.
+template <int TH, int U, int EPV, typename ElemT>
+__device__ __forceinline__ void load_pieces(const ElemT *at, const uint32_t (&bits)[U], bool once, u32x4 (&r)[U]) {
     constexpr uint32_t NONE = sizeof(ElemT) == 4 ? 0xFF800000u : 0xFF80FF80u;
-    u32x4 r{NONE, NONE, NONE, NONE};
-    if (bits) r = *reinterpret_cast<const typename Piece<ElemT>::type *>(at);
-    if (bits != (1u << EPV) - 1u) forbid<EPV, ElemT>(r, bits);
-    numbers<EPV, ElemT>(r, x);
+#pragma unroll
+    for (int u = 0; u < U; u++) r[u] = u32x4{NONE, NONE, NONE, NONE};
+    if (once) {
+        asm volatile("");
+#pragma unroll
+        for (int u = 0; u < U; u++) if (bits[u]) r[u] = __builtin_nontemporal_load(reinterpret_cast<const typename Piece<ElemT>::type *>(at + u * TH * EPV));
+        asm volatile("");
+    } else {
+#pragma unroll
+        for (int u = 0; u < U; u++) if (bits[u]) r[u] = *reinterpret_cast<const typename Piece<ElemT>::type *>(at + u * TH * EPV);
+    }
 }
 template <int EPV>
 __device__ __forceinline__ uint32_t bits_of(const uint32_t *mask_row, int64_t v) {
@@ -118,6 +133,7 @@ __device__ __forceinline__ uint32_t bits_of(const uint32_t *mask_row, int64_t v)
 struct Head {
     int64_t t;                                 // the given token
     float x, weight, old_logprob, advantage, ref;          // its logit, -inf where it is not allowed
+    int32_t sequence;                          // of preferences: the row's
 };
 // What a policy's loss makes of a row, by every lane of a wavefront alike.  Returns the row's loss.
 __device__ __forceinline__ double policy_row(const Args &A, const Part &sum, const Head &h, float wg, Ends *ends, float *logprob, float *entropy) {
@@ -289,6 +305,24 @@ __device__ __forceinline__ void store_entries(const Args &A, const Entries &E, E
     }
 }
 
+// ---- preferences' sequences ----
+__device__ __forceinline__ int64_t offset_at(const void *offsets, int32_t bytes, int64_t s) { return bytes == 8 ? ((const int64_t *)offsets)[s] : ((const int32_t *)offsets)[s]; }
+// The sequence that a row belongs to, by one wavefront: the last that begins at or before it, if it ends behind it; -1: none.  64 offsets are looked at at a time.
+__device__ __forceinline__ int32_t sequence_of(const Args &A, int64_t row, int lane) {
+    int64_t first = 0, n = A.sequences;
+    while (n > 0) {
+        const int64_t step = (n + 63) / 64;
+        const int64_t at = first + lane * step;
+        const int64_t before = __popcll(__ballot(at < first + n && offset_at(A.offsets, A.offset_bytes, at < A.sequences ? at : 0) <= row));
+        if (before == 0) return -1;
+        const int64_t end = first + n;
+        first += (before - 1) * step;
+        if (step == 1) break;
+        n = min(step, end - first);
+    }
+    return n > 0 && offset_at(A.offsets, A.offset_bytes, first) <= row && row < offset_at(A.offsets, A.offset_bytes, first + 1) ? (int32_t)first : -1;
+}
+
 // ---- a row's results ----
 template <int KIND>
 __device__ __forceinline__ void ask_head(const Args &A, int64_t row, Head &h) {
@@ -311,8 +345,8 @@ template <int KIND, bool ENT>
 __device__ __forceinline__ void no_row(const Args &A, int64_t row) {       // by one thread: a row that is padding
     if (!A.results) return;
     if (KIND != LOGPROB) A.r.losses[row] = 0.0f;
-    if (KIND != DISTILL) A.logprobs[row] = 0.0f;
-    if (KIND == LOGPROB) A.stats[2 * row] = A.stats[2 * row + 1] = 0.0f;
+    if (KIND == POLICY) A.logprobs[row] = 0.0f;
+    if (KIND == LOGPROB) A.found[row] = float4{0.0f, 0.0f, 0.0f, __int_as_float(-1)};
     if (ENT) A.entropy[row] = 0.0f;
 }
 // By one wavefront: what the sums over a row lead to.
@@ -331,10 +365,8 @@ __device__ __forceinline__ void finish_row(const Args &A, const Part &sum, int64
     } else if (KIND == LOGPROB) {
         const bool nan = h.t >= A.r.V || sum.S != sum.S;
         const double lp = nan ? (double)NAN : h.x == -INFINITY ? -INFINITY : ((double)h.x - sum.m) / A.r.temperature - log((double)sum.S);
-        if (lane != 0) return;
-        A.logprobs[row] = lp < -FLT_MAX && h.x != -INFINITY ? -FLT_MAX : (float)lp;
-        A.stats[2 * row] = sum.m;
-        A.stats[2 * row + 1] = sum.S == 0.0f ? 0.0f : 1.0f / sum.S;
+        const float logprob = lp < -FLT_MAX && h.x != -INFINITY ? -FLT_MAX : (float)lp;
+        if (lane == 0) A.found[row] = float4{sum.m, sum.S == 0.0f ? 0.0f : 1.0f / sum.S, logprob, __int_as_float(h.sequence)};
     } else {
         const double loss = distill_row(A, sum, wg, E, &e);
         if (lane != 0) return;
@@ -365,16 +397,42 @@ __device__ __forceinline__ void add_piece(const float (&x)[EPV], float c, Part &
     sum.S += S;
     if (ENT) sum.T += T;
 }
-template <bool ENT, int EPV>
-__device__ __forceinline__ void grad_of(const float (&x)[EPV], const Ends &ends, float c, float (&d)[EPV]) {
+// d = 2^y (base + slope y), y = (x - m) c.  For bf16 without the entropy's slope it is sign 2^(x c - K), K = m c - log2 |base|, in one multiply-add and the instruction that makes 2^: K is off by u |K|,
+// d by as much, which is below a thousandth of its rounding to bf16 for |K| up to 100 or so (rows further out than 4,096 are taken the other way, see wild()).
+struct Slope {
+    float m, base, slope, K;
+    uint32_t sign;                             // of two bf16 numbers
+    __device__ __forceinline__ Slope(const Ends &e, float c) : m(e.m), base(e.base), slope(e.slope), K(fmaf(e.m, c, -__builtin_amdgcn_logf(fabsf(e.base)))), sign(e.base < 0.0f ? 0x80008000u : 0u) {}
+};
+template <bool ENT, int EPV, typename ElemT>
+__device__ __forceinline__ u32x4 grad_of(const u32x4 &raw, const Slope &s, float c) {
+    float x[EPV];
+    numbers<EPV, ElemT>(raw, x);
+    union { u32x4 v; bf16x2 b[4]; } o;
 #pragma unroll
     for (int k = 0; k < EPV; k++) {
-        const float y = (x[k] - ends.m) * c, e = two_to(y);
-        d[k] = ENT ? e * fmaf(ends.slope, fmaxf(y, -1e4f), ends.base) : e * ends.base;
+        if (EPV == 8 && !ENT) {
+            x[k] = two_to(fmaf(x[k], c, -s.K));
+            continue;
+        }
+        const float y = (x[k] - s.m) * c, e = two_to(y);
+        x[k] = ENT ? e * fmaf(s.slope, fmaxf(y, -1e4f), s.base) : e * s.base;
     }
+#pragma unroll
+    for (int k = 0; k < EPV; k += 2) {
+        if (EPV == 4) { o.v[k % 4] = __float_as_uint(x[k]); o.v[k % 4 + 1] = __float_as_uint(x[k + 1]); }
+        else {
+            o.b[k / 2 % 4] = bf16x2{(__bf16)x[k], (__bf16)x[k + 1]};
+            if (!ENT) o.v[k / 2 % 4] |= s.sign;
+        }
+    }
+    return o.v;
 }
-// Where factors are not finite, or near it: 0 times them is not 0, and what is forbidden is to have 0.
-__device__ __forceinline__ bool wild(const Ends &e) { return !(fabsf(e.base) + 2e4f * fabsf(e.slope) < INFINITY); }
+// Where factors are not finite, or near it -- 0 times them is not 0, and what is forbidden is to have 0 --, and where K would lose too much.
+template <bool ENT, typename ElemT>
+__device__ __forceinline__ bool wild(const Ends &e, float c) {
+    return !(fabsf(e.base) + 2e4f * fabsf(e.slope) < INFINITY) || (sizeof(ElemT) == 2 && !ENT && !(fabsf(e.m * c) < 4096.0f));
+}
 template <bool ENT, int EPV>
 __device__ __forceinline__ void grad_of_wild(const float (&x)[EPV], const Ends &ends, float c, float (&d)[EPV]) {
 #pragma unroll
@@ -384,10 +442,24 @@ __device__ __forceinline__ void grad_of_wild(const float (&x)[EPV], const Ends &
     }
 }
 template <int TH, int EPV, typename ElemT>
-__device__ __forceinline__ void store_zeros(ElemT *grad, int32_t V) {
-    const float zeros[EPV] = {};
-    for (int32_t j = threadIdx.x; j < V / EPV; j += TH) store_numbers<EPV, ElemT>(grad + (int64_t)j * EPV, zeros);
+__device__ __forceinline__ void store_zeros(ElemT *grad, int32_t V, bool once) {
+    for (int32_t j = threadIdx.x; j < V / EPV; j += TH) store_raw<ElemT>(grad + (int64_t)j * EPV, u32x4{0, 0, 0, 0}, once);
     if ((int)threadIdx.x < V % EPV) store_element(grad + V - V % EPV + threadIdx.x, 0.0f);
+}
+
+// A row's gradient, from memory, where wild() says so.
+template <int TH, bool ENT, int EPV, typename ElemT>
+__device__ __forceinline__ void wild_row(const ElemT *logits, const uint32_t *mask, ElemT *grad, int32_t V, const Ends &ends, float c) {
+    for (int32_t j = threadIdx.x; j < V / EPV; j += TH) {
+        const uint32_t bits = bits_of<EPV>(mask, (int64_t)j * EPV);
+        for (int k = 0; k < EPV; k++) {
+            const int32_t v = j * EPV + k;
+            const float x[1] = {(bits >> k) & 1u ? of_bits(logits[v]) : -INFINITY};
+            float d[1];
+            grad_of_wild<ENT>(x, ends, c, d);
+            store_element(grad + v, d[0]);
+        }
+    }
 }
 
 template <int TH, int EPV>
@@ -396,7 +468,8 @@ __device__ __forceinline__ int writer_of(int64_t v, int32_t V) { return v >= V -
 // A row a workgroup, from memory: read for the sums, and again where its gradient is wanted.  For rows that do not fit a compute unit's registers, and calls without a gradient.
 template <int TH, int KIND, bool ENT, typename ElemT>
 __global__ __launch_bounds__(TH) void loss_rows_kernel(const Args A) {
-    constexpr int EPV = 16 / sizeof(ElemT), WAVES = TH / 64;
+    constexpr int EPV = 16 / sizeof(ElemT), WAVES = TH / 64, U = 4;
+    constexpr uint32_t FULL = (1u << EPV) - 1u;
     constexpr bool LIST = KIND == DISTILL;
     __shared__ Part part[WAVES];
     __shared__ Ends shared_ends;
@@ -419,7 +492,7 @@ __global__ __launch_bounds__(TH) void loss_rows_kernel(const Args A) {
         const ElemT *const logits = (const ElemT *)A.r.logits + row * A.r.row_stride_elems;
         const uint32_t *const mask = A.r.mask ? A.r.mask + row * A.W : nullptr;
         ElemT *const grad = (ElemT *)A.grad + row * A.grad_stride;
-        Head h{-1, -INFINITY, 1.0f, 0.0f, 0.0f, 0.0f};
+        Head h{-1, -INFINITY, 1.0f, 0.0f, 0.0f, 0.0f, -1};
         ask_head<KIND>(A, row, h);
         const float wg = h.weight * g;
         bool looked;                                       // the row is read
@@ -434,12 +507,13 @@ __global__ __launch_bounds__(TH) void loss_rows_kernel(const Args A) {
             looked = E.end->flags != 0;
         } else {
             h.t = id_at(A, row);
-            looked = h.t >= 0;
+            if (KIND == LOGPROB && h.t >= 0) h.sequence = sequence_of(A, row, lane);
+            looked = h.t >= 0 && (KIND != LOGPROB || h.sequence >= 0);
             ask_token(A, logits, mask, h);
         }
         if (!looked) {                                     // (alike in the whole workgroup)
             if (tid == 0) no_row<KIND, ENT>(A, row);
-            if (A.grad) store_zeros<TH, EPV>(grad, V);
+            if (A.grad) store_zeros<TH, EPV>(grad, V, A.once);
             if (LIST) __syncthreads();                     // before the lists are written again
             continue;
         }
@@ -460,13 +534,24 @@ __global__ __launch_bounds__(TH) void loss_rows_kernel(const Args A) {
                 }
                 __syncthreads();
             }
-            for (int32_t j = from / EPV + tid; j < to / EPV; j += TH) {
-                const int64_t v = (int64_t)j * EPV;
-                uint32_t bits = bits_of<EPV>(mask, v);
-                if (LIST) bits &= ~(listed[(v - from) >> 5] >> (v & 31));
-                float x[EPV];
-                load_numbers<EPV>(logits + v, bits, x);
-                add_piece<ENT>(x, A.c, mine);
+            for (int32_t j = from / EPV + tid; j < to / EPV; j += U * TH) {
+                uint32_t bits[U];
+                u32x4 raw[U];
+#pragma unroll
+                for (int u = 0; u < U; u++) {
+                    const int64_t v = (int64_t)(j + u * TH) * EPV;
+                    bits[u] = j + u * TH < to / EPV ? bits_of<EPV>(mask, v) : 0u;
+                    if (LIST && bits[u]) bits[u] &= ~(listed[(v - from) >> 5] >> (v & 31));
+                }
+                load_pieces<TH, U, EPV>(logits + (int64_t)j * EPV, bits, KIND == LOGPROB && A.once, raw);
+#pragma unroll
+                for (int u = 0; u < U; u++) {
+                    if (!__any(bits[u] != 0)) continue;
+                    if (__any(bits[u] != FULL)) forbid<EPV, ElemT>(raw[u], bits[u]);
+                    float x[EPV];
+                    numbers<EPV, ElemT>(raw[u], x);
+                    add_piece<ENT>(x, A.c, mine);
+                }
             }
             if (to == V && tid < V % EPV) {
                 const int32_t v = V - V % EPV + tid;
@@ -484,14 +569,24 @@ __global__ __launch_bounds__(TH) void loss_rows_kernel(const Args A) {
         __syncthreads();
         if (KIND != LOGPROB && A.grad) {
             const Ends ends = shared_ends;
-            const bool all = wild(ends);
-            for (int32_t j = tid; j < n_pieces; j += TH) {
-                const int64_t v = (int64_t)j * EPV;
-                float x[EPV], d[EPV];
-                load_numbers<EPV>(logits + v, bits_of<EPV>(mask, v), x);
-                if (all) grad_of_wild<ENT>(x, ends, A.c, d);
-                else grad_of<ENT>(x, ends, A.c, d);
-                store_numbers<EPV, ElemT>(grad + v, d);
+            const Slope slope(ends, A.c);
+            const bool all = wild<ENT, ElemT>(ends, A.c);
+            if (all) wild_row<TH, ENT, EPV>(logits, mask, grad, V, ends, A.c);
+            for (int32_t j = tid; j < n_pieces && !all; j += U * TH) {
+                uint32_t bits[U];
+                u32x4 raw[U];
+#pragma unroll
+                for (int u = 0; u < U; u++) bits[u] = j + u * TH < n_pieces ? bits_of<EPV>(mask, (int64_t)(j + u * TH) * EPV) : 0u;
+                load_pieces<TH, U, EPV>(logits + (int64_t)j * EPV, bits, A.once, raw);
+#pragma unroll
+                for (int u = 0; u < U; u++) {
+                    u32x4 d{0, 0, 0, 0};
+                    if (__any(bits[u] != 0)) {
+                        if (__any(bits[u] != FULL)) forbid<EPV, ElemT>(raw[u], bits[u]);
+                        d = grad_of<ENT, EPV, ElemT>(raw[u], slope, A.c);
+                    }
+                    if (j + u * TH < n_pieces) store_raw<ElemT>(grad + (int64_t)(j + u * TH) * EPV, d, A.once);
+                }
             }
             if (tid < V % EPV) {
                 const int32_t v = V - V % EPV + tid;
@@ -562,22 +657,30 @@ __global__ __launch_bounds__(TH, 4) void loss_resident_kernel(const Args A) {
         return EPV == 8 ? byte : (byte >> (j % 2 * 4)) & FULL;
     };
     const uint32_t at_tid = (uint32_t)tid * 16u;           // bytes; a piece's address is a row's and i's, alike in the workgroup, and this
-    auto piece_of = [&](const ElemT *of, int i) { return (const char *)of + i * (TH * 16) + at_tid; };
-    auto fetch = [&](const ElemT *from, int i) {           // piece i of the thread; -inf where there is nothing, or nothing that the mask allows
-        raw[i] = u32x4{NONE, NONE, NONE, NONE};
-        if (tid + i * TH < n_pieces && (!MASKED || bits_of_piece(i))) raw[i] = __builtin_nontemporal_load(reinterpret_cast<const typename Piece<ElemT>::type *>(piece_of(from, i)));
+    auto place_of = [&](const void *of, int i) {           // (stated apart for each: of all, the compiler makes 64-bit additions in every thread)
+        uint64_t at = (uint64_t)(uintptr_t)of + (uint64_t)(i * (TH * 16));
+        asm volatile("" : "+s"(at));
+        return (GLOBAL char *)at;
+    };
+    auto has = [&](int i) { return (i + 1) * TH <= n_pieces || tid + i * TH < n_pieces; };
+    auto fetch = [&](const ElemT *from, int i) {           // piece i of the thread; nothing is read that the mask allows nothing of
+        GLOBAL char *const at = place_of(from, i);
+        if (has(i) && (!MASKED || bits_of_piece(i))) raw[i] = __builtin_nontemporal_load((GLOBAL const typename Piece<ElemT>::type *)(at + at_tid));
     };
     const bool last = tid < V % EPV;                       // the thread has one of the elements behind the whole pieces
     const int32_t v_last = V - V % EPV + tid;
     float x_last = -INFINITY;
     Part mine;
     uint32_t live, next_live = 0;                          // pieces with an allowed token
-    auto add = [&](int i) {
+    auto add = [&](int i) {                                // what was not read, or is not allowed, becomes -inf
         uint32_t bits = FULL;
         if (MASKED) {
             bits = bits_of_piece(i);
+            if ((i + 1) * TH > n_pieces && tid + i * TH >= n_pieces) bits = 0;       // (behind the whole pieces there may be bits of single elements)
             next_live |= (bits ? 1u : 0u) << i;
             if (__any(bits != FULL)) forbid<EPV, ElemT>(raw[i], bits);
+        } else if ((i + 1) * TH > n_pieces) {
+            if (tid + i * TH >= n_pieces) raw[i] = u32x4{NONE, NONE, NONE, NONE};
         }
         if (!MASKED || __any(bits != 0)) {
             float x[EPV];
@@ -611,7 +714,7 @@ __global__ __launch_bounds__(TH, 4) void loss_resident_kernel(const Args A) {
     const int size = LIST ? entries_bytes(A.K) : 0;
     int64_t row = blockIdx.x;
     int turn = 0;
-    Head head{-1, -INFINITY, 1.0f, 0.0f, 0.0f, 0.0f}, next_head = head;
+    Head head{-1, -INFINITY, 1.0f, 0.0f, 0.0f, 0.0f, -1}, next_head = head;
     bool counts;
     // The first row
     ask_head<KIND>(A, row, head);
@@ -675,7 +778,8 @@ __global__ __launch_bounds__(TH, 4) void loss_resident_kernel(const Args A) {
         }
         __syncthreads();
         const Ends ends = shared_ends;
-        const bool next_counts = more && (LIST ? next_E.end->flags != 0 : next_head.t >= 0), all = wild(ends);
+        const bool next_counts = more && (LIST ? next_E.end->flags != 0 : next_head.t >= 0);
+        const Slope slope(ends, A.c);
         if (LIST) {
             ahead = after;
             ask_entry_logit(next + gridDim.x, ahead);
@@ -689,18 +793,15 @@ __global__ __launch_bounds__(TH, 4) void loss_resident_kernel(const Args A) {
 #pragma unroll
         for (int i = 0; i < NP + LAG; i++) {
             if (i < NP && i * TH < n_pieces) {
-                float d[EPV] = {};
-                if (counts && (!MASKED || __any((live >> i) & 1u))) {
-                    float x[EPV];
-                    numbers<EPV, ElemT>(raw[i], x);
-                    if (all) grad_of_wild<ENT>(x, ends, A.c, d);
-                    else grad_of<ENT>(x, ends, A.c, d);
-                }
-                if (tid + i * TH < n_pieces) store_numbers<EPV, ElemT>((char *)grad + i * (TH * 16) + at_tid, d);
+                GLOBAL char *const to = place_of(grad, i);
+                u32x4 d{0, 0, 0, 0};
+                if (counts && (!MASKED || __any((live >> i) & 1u))) d = grad_of<ENT, EPV, ElemT>(raw[i], slope, A.c);
+                if (has(i)) store_raw<ElemT>(to + at_tid, d, A.once);
                 if (next_counts) fetch(next_logits, i);
             }
             if (i >= LAG && (i - LAG) * TH < n_pieces && next_counts) add(i - LAG);
         }
+        if (counts && wild<ENT, ElemT>(ends, A.c)) wild_row<TH, ENT, EPV>(logits_of(row), mask_of(row), grad, V, ends, A.c);
         if (last) {
             float d[1] = {0.0f};
             if (counts) grad_of_wild<ENT>(x_of_row, ends, A.c, d);
@@ -741,31 +842,36 @@ __global__ __launch_bounds__(1024) void total_kernel(const float *losses, const 
 }
 
 // ---- preferences ----
-__device__ __forceinline__ int64_t offset_at(const zf_preference_args &p, int64_t s) { return p.offset_bytes == 8 ? ((const int64_t *)p.offsets)[s] : ((const int32_t *)p.offsets)[s]; }
-__device__ __forceinline__ int64_t token_at(const zf_preference_args &p, int64_t row) { return p.token_bytes == 8 ? ((const int64_t *)p.tokens)[row] : ((const int32_t *)p.tokens)[row]; }
+__device__ __forceinline__ int64_t offset_at(const zf_preference_args &p, int64_t s) { return offset_at(p.offsets, p.offset_bytes, s); }
 
-// A pair a workgroup: the rows' log ratios in 64 bits, in one order; the first half of the wavefronts takes the one sequence, the second the other.
-__global__ __launch_bounds__(256) void pairs_kernel(const zf_preference_args p) {
-    __shared__ double sums[4], counts[4];
-    const int half = threadIdx.x / 128, lane = threadIdx.x % 128;
-    for (int64_t pair = blockIdx.x; pair < p.pairs; pair += gridDim.x) {
-        const int64_t o0 = offset_at(p, 2 * pair), o1 = offset_at(p, 2 * pair + 1), o2 = offset_at(p, 2 * pair + 2);
-        const bool fits = 0 <= o0 && o0 <= o1 && o1 <= o2 && o2 <= p.r.rows;
-        const int64_t begin = half ? o1 : o0, end = fits ? (half ? o2 : o1) : begin;
-        double sum = 0.0, n = 0.0;
-        for (int64_t row = begin + lane; row < end; row += 128) {
-            if (token_at(p, row) < 0) continue;
-            sum += p.ref_logprobs ? (double)p.logprobs[row] - p.ref_logprobs[row] : (double)p.logprobs[row];
-            n += 1.0;
+// A sequence a wavefront: its rows' log ratios in 64 bits, in one order.  A workgroup has 8 pairs at a time; a call of a single workgroup sums the losses too.
+static const int PAIRS = 8;
+__global__ __launch_bounds__(PAIRS * 128) void pairs_kernel(const zf_preference_args p) {
+    __shared__ double sums[2 * PAIRS], counts[2 * PAIRS], of_wave[2 * PAIRS];
+    const int wave = threadIdx.x / 64, lane = threadIdx.x % 64;
+    const float4 *const found = (const float4 *)p.stats;
+    for (int64_t first = (int64_t)blockIdx.x * PAIRS; first < p.pairs; first += (int64_t)gridDim.x * PAIRS) {
+        const int64_t pair = first + wave / 2;
+        bool fits = false;
+        if (pair < p.pairs) {
+            const int64_t o0 = offset_at(p, 2 * pair), o1 = offset_at(p, 2 * pair + 1), o2 = offset_at(p, 2 * pair + 2);
+            fits = 0 <= o0 && o0 <= o1 && o1 <= o2 && o2 <= p.r.rows;
+            const int64_t begin = wave % 2 ? o1 : o0, end = fits ? (wave % 2 ? o2 : o1) : begin;
+            double sum = 0.0, n = 0.0;
+            for (int64_t row = begin + lane; row < end; row += 64) {
+                const float4 f = found[row];
+                if (__float_as_int(f.w) < 0) continue;     // padding
+                sum += p.ref_logprobs ? (double)f.z - p.ref_logprobs[row] : (double)f.z;
+                n += 1.0;
+            }
+            sum = wave_sum(sum);
+            n = wave_sum(n);
+            if (lane == 0) { sums[wave] = sum; counts[wave] = n; }
         }
-        sum = wave_sum(sum);
-        n = wave_sum(n);
-        if (threadIdx.x % 64 == 0) { sums[threadIdx.x / 64] = sum; counts[threadIdx.x / 64] = n; }
         __syncthreads();
-        if (threadIdx.x == 0) {
-            double chosen = sums[0] + sums[1], rejected = sums[2] + sums[3];
-            double n0 = 1.0, n1 = 1.0;
-            if (p.average) { n0 = fmax(counts[0] + counts[1], 1.0); n1 = fmax(counts[2] + counts[3], 1.0); }
+        if (pair < p.pairs && wave % 2 == 0 && lane == 0) {
+            double chosen = sums[wave], rejected = sums[wave + 1], n0 = 1.0, n1 = 1.0;
+            if (p.average) { n0 = fmax(counts[wave], 1.0); n1 = fmax(counts[wave + 1], 1.0); }
             chosen *= p.beta / n0;
             rejected *= p.beta / n1;
             const double h = chosen - rejected, s = p.label_smoothing;
@@ -783,57 +889,73 @@ __global__ __launch_bounds__(256) void pairs_kernel(const zf_preference_args p) 
         }
         __syncthreads();
     }
+    if (gridDim.x == 1) sum_losses(p.r.losses, p.r.weight, p.pairs, p.r.loss, of_wave);
 }
 
-// The gradient of preferences: a row's slope is its sequence's.
-template <int TH, typename ElemT>
-__global__ __launch_bounds__(TH) void preference_grad_kernel(const zf_preference_args p, const float *g, float c, int32_t W, void *grad_, int64_t grad_stride) {
+// The gradient of preferences: a row's slope is its sequence's.  A workgroup has a segment of a row, U pieces of 16 bytes a thread.
+template <int TH, int U, typename ElemT>
+__global__ __launch_bounds__(TH) void preference_grad_kernel(const zf_preference_args p, const float *g, float c, int32_t W, ElemT *grad_, int64_t grad_stride, int32_t segments, int32_t once) {
     constexpr int EPV = 16 / sizeof(ElemT);
+    constexpr uint32_t FULL = (1u << EPV) - 1u;
     const int tid = threadIdx.x;
-    const int32_t V = p.r.V, n_pieces = V / EPV;
-    for (int64_t row = blockIdx.x; row < p.r.rows; row += gridDim.x) {
-        const ElemT *const logits = (const ElemT *)p.r.logits + row * p.r.row_stride_elems;
-        ElemT *const grad = (ElemT *)grad_ + row * grad_stride;
-        const uint32_t *const mask = p.r.mask ? p.r.mask + row * W : nullptr;
-        int64_t low = 0, high = 2 * p.pairs;               // the last sequence that begins at or before the row
-        while (low < high) {
-            const int64_t mid = (low + high + 1) / 2;
-            if (offset_at(p, mid) <= row) low = mid; else high = mid - 1;
-        }
-        const int64_t t = token_at(p, row);
-        const bool counts = t >= 0 && low < 2 * p.pairs && offset_at(p, low) <= row && row < offset_at(p, low + 1) && p.logprobs[row] != -INFINITY;
-        const float m = p.stats[2 * row], inv_S = p.stats[2 * row + 1], f = counts ? (float)((double)p.slopes[low] * *g / p.r.temperature) : 0.0f;
-        const float base = -f * inv_S;
-        const bool look = !(fabsf(base) < INFINITY);
-        const Ends ends{m, base, 0.0f, 0.0f};
-        for (int32_t j = tid; j < n_pieces; j += TH) {
-            const int64_t v = (int64_t)j * EPV;
-            float x[EPV], d[EPV] = {};
-            if (counts) {
-                load_numbers<EPV>(logits + v, bits_of<EPV>(mask, v), x);
-                if (look) grad_of_wild<false>(x, ends, c, d);
-                else grad_of<false>(x, ends, c, d);
-                if (t / EPV == j) {
+    const int32_t V = p.r.V, n_pieces = V / EPV, segment = blockIdx.x % (uint32_t)segments, j = segment * (U * TH) + tid;
+    const int64_t row = blockIdx.x / (uint32_t)segments;
+    const ElemT *const logits = (const ElemT *)p.r.logits + row * p.r.row_stride_elems;
+    ElemT *const grad = grad_ + row * grad_stride;
+    const uint32_t *const mask = p.r.mask ? p.r.mask + row * W : nullptr;
+    const float4 found = ((const float4 *)p.stats)[row];
+    const int32_t sequence = __float_as_int(found.w);
+    const bool counts = sequence >= 0 && found.z != -INFINITY;
+    uint32_t bits[U];
+    u32x4 raw[U];
 #pragma unroll
-                    for (int k = 0; k < EPV; k++) if (t % EPV == k) d[k] += f;
+    for (int u = 0; u < U; u++) bits[u] = counts && j + u * TH < n_pieces ? bits_of<EPV>(mask, (int64_t)(j + u * TH) * EPV) : 0u;
+    load_pieces<TH, U, EPV>(logits + (int64_t)j * EPV, bits, once, raw);
+    const int64_t t = p.token_bytes == 8 ? ((const int64_t *)p.tokens)[row] : ((const int32_t *)p.tokens)[row];
+    const float f = counts ? (float)((double)p.slopes[sequence] * *g / p.r.temperature) : 0.0f, base = -f * found.y;
+    const Ends ends{found.x, base, 0.0f, 0.0f};
+    const Slope slope(ends, c);
+    const bool all = wild<false, ElemT>(ends, c);
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+        u32x4 d{0, 0, 0, 0};
+        if (__any(bits[u] != 0)) {
+            if (__any(bits[u] != FULL)) forbid<EPV, ElemT>(raw[u], bits[u]);
+            if (!all) d = grad_of<false, EPV, ElemT>(raw[u], slope, c);
+            else {
+                union { u32x4 v; bf16x2 b[4]; } o;
+                float x[EPV], e[EPV];
+                numbers<EPV, ElemT>(raw[u], x);
+                grad_of_wild<false>(x, ends, c, e);
+#pragma unroll
+                for (int k = 0; k < EPV; k += 2) {
+                    if (EPV == 4) { o.v[k % 4] = __float_as_uint(e[k]); o.v[k % 4 + 1] = __float_as_uint(e[k + 1]); }
+                    else o.b[k / 2 % 4] = bf16x2{(__bf16)e[k], (__bf16)e[k + 1]};
                 }
+                d = o.v;
             }
-            store_numbers<EPV, ElemT>(grad + v, d);
         }
-        if (tid < V % EPV) {
-            const int32_t v = V - V % EPV + tid;
-            float d[1] = {0.0f};
-            if (counts) {
-                const float x[1] = {allowed(mask, v) ? of_bits(logits[v]) : -INFINITY};
-                grad_of_wild<false>(x, ends, c, d);
-                if (t == v) d[0] += f;
-            }
-            store_element(grad + v, d[0]);
+        if (j + u * TH < n_pieces) store_raw<ElemT>(grad + (int64_t)(j + u * TH) * EPV, d, once);
+    }
+    if (counts && t < V - V % EPV && t / EPV % TH == tid && t / EPV >= segment * (U * TH) && t / EPV < (segment + 1) * (U * TH)) {   // the token's own element, by the thread that has just written its piece
+        const float x[1] = {of_bits(logits[t])};
+        float d[1];
+        grad_of_wild<false>(x, ends, c, d);
+        store_element(grad + t, d[0] + f);
+    }
+    if (segment == 0 && tid < V % EPV) {
+        const int32_t v = V - V % EPV + tid;
+        float d[1] = {0.0f};
+        if (counts) {
+            const float x[1] = {allowed(mask, v) ? of_bits(logits[v]) : -INFINITY};
+            grad_of_wild<false>(x, ends, c, d);
+            if (t == v) d[0] += f;
         }
+        store_element(grad + v, d[0]);
     }
 }
 
-static const int COMPUTE_UNITS = 256;
+static const int COMPUTE_UNITS = 256, GRAD_PIECES = 4;
 int grid_of(int64_t n) { return (int)std::min<int64_t>(n, 1 << 16); }
 // TH threads take a row, NP pieces each at most; `each`: workgroups that a compute unit's registers hold.  Without a gradient a row is read from memory by as many threads, in the same order.
 template <int TH, int NP, int KIND, bool ENT, typename ElemT>
@@ -852,6 +974,7 @@ void rows_by(const Args &A, hipStream_t s) {
 template <int KIND, bool ENT, typename ElemT>
 void rows_of(const Args &A, hipStream_t s) {
     const int32_t n = (A.r.V + (int)(16 / sizeof(ElemT)) - 1) / (int)(16 / sizeof(ElemT));    // pieces of a row
+    if (KIND == LOGPROB && A.r.rows >= 2048 && n > 16 * 64) return rows_by<256, 0, KIND, ENT, ElemT>(A, s);
     if (n <= 16 * 64) return rows_by<64, 16, KIND, ENT, ElemT>(A, s);
     if (n <= 16 * 256) return rows_by<256, 16, KIND, ENT, ElemT>(A, s);
     if (n <= 16 * 512) return rows_by<512, 16, KIND, ENT, ElemT>(A, s);
@@ -864,12 +987,19 @@ void rows_of(const Args &A, hipStream_t s) {
     if (A.r.dtype == 0) rows_of<KIND, ENT, uint32_t>(A, s);
     else rows_of<KIND, ENT, uint16_t>(A, s);
 }
+// Rows that the last-level cache (256 MB) cannot hold until somebody reads them again pass it by; not those at odd elements, whose lines are written in two parts.
+bool passes(const zf_loss_rows &r, const LossGrad &g) {
+    const int64_t size = r.dtype == 0 ? 4 : 2;
+    auto whole = [&](const void *p, int64_t stride) { return !p || ((uintptr_t)p % 16 == 0 && stride * size % 16 == 0); };
+    return r.rows * r.V * size > (256ll << 20) && whole(r.logits, r.row_stride_elems) && whole(g.grad, g.stride);
+}
 Args common(const zf_loss_rows &r, const LossGrad &g) {
     Args A{};
     A.r = r;
     A.W = (r.V + 31) / 32;
     A.c = (float)(1.4426950408889634 / r.temperature);
     A.grad = g.grad; A.grad_stride = g.stride; A.g = g.g; A.held = g.held; A.results = !g.g;
+    A.once = passes(r, g);
     return A;
 }
 void total(const zf_loss_rows &r, int64_t n, hipStream_t s) { hipLaunchKernelGGL(total_kernel, dim3(1), dim3(1024), 0, s, r.losses, r.weight, n, r.loss); }
@@ -896,19 +1026,27 @@ hipError_t launch_policy(const zf_policy_args &a, const LossGrad &g, hipStream_t
 
 hipError_t launch_preference(const zf_preference_args &a, hipStream_t s) {
     Args A = common(a.r, LossGrad{});
-    A.ids = a.tokens; A.id_bytes = a.token_bytes; A.logprobs = a.logprobs; A.stats = a.stats;
+    A.ids = a.tokens; A.id_bytes = a.token_bytes; A.found = (float4 *)a.stats;
+    A.offsets = a.offsets; A.offset_bytes = a.offset_bytes; A.sequences = 2 * a.pairs;
     if (a.r.rows) rows_of<LOGPROB, false>(A, s);
-    if (a.pairs) hipLaunchKernelGGL(pairs_kernel, dim3(grid_of(a.pairs)), dim3(256), 0, s, a);
-    total(a.r, a.pairs, s);
+    // One workgroup has the pairs of a few thousand rows in a few microseconds, and the sum with them
+    const int grid = a.pairs <= 4 * PAIRS && a.r.rows <= 32768 ? 1 : grid_of((a.pairs + PAIRS - 1) / PAIRS);
+    hipLaunchKernelGGL(pairs_kernel, dim3(std::max(grid, 1)), dim3(PAIRS * 128), 0, s, a);
+    if (grid > 1) total(a.r, a.pairs, s);
     return hipGetLastError();
 }
 
+int64_t preference_blocks(const zf_preference_args &a) {
+    const int32_t n = a.r.V / (a.r.dtype == 0 ? 4 : 8);
+    return a.r.rows * std::max(1, (n + GRAD_PIECES * 256 - 1) / (GRAD_PIECES * 256));
+}
 hipError_t launch_preference_backward(const zf_preference_args &a, const LossGrad &g, hipStream_t s) {
-    const int32_t W = (a.r.V + 31) / 32;
-    const float c = (float)(1.4426950408889634 / a.r.temperature);
     if (a.r.rows == 0) return hipSuccess;
-    if (a.r.dtype == 0) hipLaunchKernelGGL((preference_grad_kernel<1024, uint32_t>), dim3(grid_of(a.r.rows)), dim3(1024), 0, s, a, g.g, c, W, g.grad, g.stride);
-    else hipLaunchKernelGGL((preference_grad_kernel<1024, uint16_t>), dim3(grid_of(a.r.rows)), dim3(1024), 0, s, a, g.g, c, W, g.grad, g.stride);
+    const int64_t blocks = preference_blocks(a);
+    const int32_t W = (a.r.V + 31) / 32, segments = (int32_t)(blocks / a.r.rows);
+    const float c = (float)(1.4426950408889634 / a.r.temperature);
+    if (a.r.dtype == 0) hipLaunchKernelGGL((preference_grad_kernel<256, GRAD_PIECES, uint32_t>), dim3((uint32_t)blocks), dim3(256), 0, s, a, g.g, c, W, (uint32_t *)g.grad, g.stride, segments, passes(a.r, g));
+    else hipLaunchKernelGGL((preference_grad_kernel<256, GRAD_PIECES, uint16_t>), dim3((uint32_t)blocks), dim3(256), 0, s, a, g.g, c, W, (uint16_t *)g.grad, g.stride, segments, passes(a.r, g));
     return hipGetLastError();
 }
 

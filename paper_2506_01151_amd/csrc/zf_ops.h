@@ -44,6 +44,7 @@ hipError_t launch_logprobs(const zf_logprobs_args &a, void *workspace, hipStream
 hipError_t launch_logprobs_backward(const zf_logprobs_args &a, const LogprobsGrad &g, hipStream_t s);
 hipError_t launch_distill(const zf_distill_args &a, const LossGrad &g, hipStream_t s);
 hipError_t launch_policy(const zf_policy_args &a, const LossGrad &g, hipStream_t s);
+int64_t preference_blocks(const zf_preference_args &a);   // workgroups of its gradient
 hipError_t launch_preference(const zf_preference_args &a, hipStream_t s);
 hipError_t launch_preference_backward(const zf_preference_args &a, const LossGrad &g, hipStream_t s);
 

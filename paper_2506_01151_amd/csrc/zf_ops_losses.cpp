@@ -52,7 +52,9 @@ int check(const zf_preference_args *a) {
     if (a->pairs < 0 || a->pairs > INT32_MAX / 2) return refuse("pairs must be 0..2^30-1");
     if (!std::isfinite(a->beta)) return refuse("beta must be finite");
     if (!(a->label_smoothing >= 0.0 && a->label_smoothing <= 1.0)) return refuse("label_smoothing must be 0..1");
-    if (a->r.rows && (!a->tokens || !a->logprobs || !a->stats)) return refuse("null argument");
+    if (a->r.rows && (!a->tokens || !a->stats)) return refuse("null argument");
+    if ((uintptr_t)a->stats % 16) return refuse("stats must be aligned to 16 bytes");
+    if (preference_blocks(*a) > BLOCKS_MAX) return refuse("more logits than a call takes: split the rows");
     if (!a->offsets || (a->pairs && (!a->r.losses || !a->chosen || !a->rejected || !a->slopes))) return refuse("null argument");
     return ZF_OK;
 }

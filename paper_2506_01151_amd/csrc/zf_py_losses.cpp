@@ -54,7 +54,7 @@ zf_preference_args preference_args(const Inputs &in, const Numbers &n, const Res
     a.r = rows_of(in, n, r);
     a.tokens = in.ids.data_ptr(); a.token_bytes = id_bytes(in.ids); a.offsets = in.offsets.data_ptr(); a.offset_bytes = id_bytes(in.offsets); a.ref_logprobs = f32(in.ref);
     a.pairs = in.offsets.size(0) / 2; a.beta = n.beta; a.label_smoothing = n.label_smoothing; a.average = n.average;
-    a.chosen = f32(r.chosen); a.rejected = f32(r.rejected); a.logprobs = f32(r.logprobs); a.stats = f32(r.stats); a.slopes = f32(r.slopes);
+    a.chosen = f32(r.chosen); a.rejected = f32(r.rejected); a.stats = f32(r.stats); a.slopes = f32(r.slopes);
     return a;
 }
 Results results_of(int kind, const Inputs &in, const Numbers &n) {
@@ -62,9 +62,9 @@ Results results_of(int kind, const Inputs &in, const Numbers &n) {
     const int64_t rows = in.logits.size(0), items = kind == PREFERENCE ? in.offsets.size(0) / 2 : rows;
     Results r;
     r.loss = of({}); r.losses = of({items});
-    if (kind != DISTILL) r.logprobs = of({rows});
+    if (kind == POLICY) r.logprobs = of({rows});
     if (n.entropy) r.entropy = of({rows});
-    if (kind == PREFERENCE) { r.chosen = of({items}); r.rejected = of({items}); r.stats = of({rows, 2}); r.slopes = of({2 * items}); }
+    if (kind == PREFERENCE) { r.chosen = of({items}); r.rejected = of({items}); r.stats = of({rows, 4}); r.slopes = of({2 * items}); }
     return r;
 }
 int call(int kind, const Inputs &in, const Numbers &n, const Results &r, void *grad) {
@@ -98,7 +98,7 @@ struct Shapes : torch::CustomClassHolder {
 };
 
 struct LossOf : public torch::autograd::Function<LossOf> {
-    // saved: logits, mask, weight, ids, values, old_logprobs, advantages, ref, offsets, then of a preference logprobs, stats, slopes
+    // saved: logits, mask, weight, ids, values, old_logprobs, advantages, ref, offsets, then of a preference stats, slopes
     static torch::autograd::variable_list forward(torch::autograd::AutogradContext *ctx, const Tensor &logits, const Inputs &in, int64_t kind, const Numbers &n) {
         const Results r = results_of((int)kind, in, n);
         auto like = c10::make_intrusive<Shapes>();
@@ -109,12 +109,11 @@ struct LossOf : public torch::autograd::Function<LossOf> {
         like->offset_type = kind == PREFERENCE ? in.offsets.scalar_type() : at::kLong;
         if (kind != PREFERENCE && !capturing()) like->held = fresh(logits.sizes(), logits.scalar_type(), logits);
         must(call((int)kind, in, n, r, like->held.defined() ? like->held.data_ptr() : nullptr));
-        const bool more = kind == PREFERENCE;
-        ctx->save_for_backward({logits, in.mask, in.weight, in.ids, in.values, in.old_logprobs, in.advantages, in.ref, in.offsets, more ? r.logprobs : Tensor(), r.stats, r.slopes});
+        ctx->save_for_backward({logits, in.mask, in.weight, in.ids, in.values, in.old_logprobs, in.advantages, in.ref, in.offsets, r.stats, r.slopes});
         ctx->saved_data["shapes"] = c10::IValue::make_capsule(std::move(like));
         ctx->set_materialize_grads(false);
         torch::autograd::variable_list out, constant;
-        for (const Tensor *t : {&r.loss, &r.losses, kind == POLICY ? &r.logprobs : nullptr, &r.entropy, &r.chosen, &r.rejected}) if (t && t->defined()) out.push_back(*t);
+        for (const Tensor *t : {&r.loss, &r.losses, &r.logprobs, &r.entropy, &r.chosen, &r.rejected}) if (t && t->defined()) out.push_back(*t);
         constant.assign(out.begin() + 1, out.end());
         ctx->mark_non_differentiable(constant);
         return out;
@@ -139,13 +138,11 @@ struct LossOf : public torch::autograd::Function<LossOf> {
         in.advantages = some(6, "advantages", at::kFloat, {rows});
         in.ref = some(7, "ref_logprobs", at::kFloat, {rows});
         in.offsets = some(8, "offsets", like->offset_type, {like->offsets});
-        Results r = results_of(kind, in, like->n);
-        if (kind == PREFERENCE) {
-            r.logprobs = some(9, "logprobs", at::kFloat, {rows});
-            r.stats = some(10, "stats", at::kFloat, {rows, 2});
-            r.slopes = some(11, "slopes", at::kFloat, {2 * items});
-        }
         const Tensor g = kept(name, grads[0].scalar_type() == at::kFloat ? grads[0] : grads[0].detach().to(at::kFloat), "gradient", in.logits, at::kFloat, {});
+        Results r;                                           // none is written: the addresses only say that they are there
+        r.loss = r.losses = r.logprobs = r.chosen = r.rejected = g;
+        if (like->n.entropy) r.entropy = g;
+        if (kind == PREFERENCE) { r.stats = some(9, "stats", at::kFloat, {rows, 4}); r.slopes = some(10, "slopes", at::kFloat, {2 * items}); }
         // The gradient for a factor of one is handed out once: whoever has it may write it.  What a capture records may run again under another factor.
         Tensor grad;
         bool held = false;
@@ -186,7 +183,7 @@ PyObject *run(Kind kind, const Inputs &in, const Numbers &n, int n_out) {
     else {
         const Results r = results_of(kind, in, n);
         must(call(kind, in, n, r, nullptr));
-        for (const Tensor *t : {&r.loss, &r.losses, kind == POLICY ? &r.logprobs : nullptr, &r.entropy, &r.chosen, &r.rejected}) if (t && t->defined()) out.push_back(*t);
+        for (const Tensor *t : {&r.loss, &r.losses, &r.logprobs, &r.entropy, &r.chosen, &r.rejected}) if (t && t->defined()) out.push_back(*t);
     }
     PyObject *t = PyTuple_New(n_out);
     if (!t) return nullptr;

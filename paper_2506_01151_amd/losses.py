@@ -140,7 +140,7 @@ class _Policy(_Loss):
 
 class _Preference(_Loss):
     at_once = False
-    saved = ("logprobs", "stats", "slopes")        # what the gradient is made from
+    saved = ("stats", "slopes")                    # what the gradient is made from
 
     @staticmethod
     def call(a, grad, stride, device, stream):
@@ -152,21 +152,21 @@ class _Preference(_Loss):
 
     def outputs(self):
         n, P = self.t["logits"].shape[0], self.o["pairs"]
-        return self.fresh(loss=(), losses=(P,), chosen=(P,), rejected=(P,), logprobs=(n,), stats=(n, 2), slopes=(2 * P,))
+        return self.fresh(loss=(), losses=(P,), chosen=(P,), rejected=(P,), stats=(n, 4), slopes=(2 * P,))
 
     def args(self, out):
         a, t, o = PreferenceArgs(), self.t, self.o
         self.rows(a.r, out)
         a.tokens, a.token_bytes, a.offsets, a.offset_bytes, a.ref_logprobs = t["tokens"].data_ptr(), t["tokens"].element_size(), t["offsets"].data_ptr(), t["offsets"].element_size(), _ptr(t["ref"])
         a.pairs, a.beta, a.label_smoothing, a.average = o["pairs"], o["beta"], o["label_smoothing"], o["average"]
-        for n in ("chosen", "rejected", "logprobs", "stats", "slopes"):
+        for n in ("chosen", "rejected", "stats", "slopes"):
             setattr(a, n, out[n].data_ptr())
         return a
 
     def shapes(self, rows):
         P = self.o["pairs"]
         return {"tokens": (_IDS, (rows,)), "offsets": (_IDS, (2 * P + 1,)), "ref": (_F32, (rows,)), "weight": (_F32, (P,)),
-                "logprobs": (_F32, (rows,)), "stats": (_F32, (rows, 2)), "slopes": (_F32, (2 * P,))}
+                "stats": (_F32, (rows, 4)), "slopes": (_F32, (2 * P,))}
 
 
 def _returned(out):
@@ -298,4 +298,4 @@ def preference_loss(logits, tokens, offsets, ref_logprobs=None, mask=None, *, be
         _constant(weight, "weight", _F32, (pairs,), dev)
     o = {"temperature": temperature, "pairs": pairs, "beta": _number(beta, "beta", -1e300, 1e300), "label_smoothing": _number(label_smoothing, "label_smoothing", 0.0, 1.0), "average": bool(average)}
     t = {"logits": logits, "tokens": tokens, "offsets": offsets, "ref": ref_logprobs, "mask": mask, "weight": weight}
-    return PreferenceLoss(*_run(_Preference, t, o)[:4])
+    return PreferenceLoss(*_run(_Preference, t, o))

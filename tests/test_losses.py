@@ -780,7 +780,7 @@ def test_refusals_on_the_host():
     L, at = zf.load_library(), 4096
     rows = dict(logits=at, dtype=0, V=10, rows=3, row_stride=10, temperature=1.0, loss=at, losses=at)
     mine = {DistillArgs: dict(ids=at, values=at, id_bytes=4, values_dtype=0, n_listed=2), PolicyArgs: dict(tokens=at, old_logprobs=at, advantages=at, token_bytes=8, clip_low=0.2, clip_high=0.2, logprobs=at),
-            PreferenceArgs: dict(tokens=at, offsets=at, token_bytes=4, offset_bytes=8, pairs=1, beta=0.1, label_smoothing=0.0, chosen=at, rejected=at, logprobs=at, stats=at, slopes=at)}
+            PreferenceArgs: dict(tokens=at, offsets=at, token_bytes=4, offset_bytes=8, pairs=1, beta=0.1, label_smoothing=0.0, chosen=at, rejected=at, stats=at, slopes=at)}
     calls = {DistillArgs: (L.zf_distill_loss, L.zf_distill_loss_backward), PolicyArgs: (L.zf_policy_loss, L.zf_policy_loss_backward), PreferenceArgs: (L.zf_preference_loss, L.zf_preference_loss_backward)}
 
     def code(kind, changed, back=False, grad=at + 64, stride=10, g=at):
@@ -800,7 +800,7 @@ def test_refusals_on_the_host():
         own = {DistillArgs: [dict(n_listed=0), dict(n_listed=1025), dict(id_bytes=2), dict(values_dtype=3), dict(ids=None), dict(values=None)],
                PolicyArgs: [dict(token_bytes=1), dict(clip_low=-0.1), dict(clip_high=math.nan), dict(tokens=None), dict(old_logprobs=None), dict(advantages=None), dict(logprobs=None)],
                PreferenceArgs: [dict(token_bytes=0), dict(offset_bytes=3), dict(pairs=-1), dict(pairs=1 << 30), dict(beta=INF), dict(label_smoothing=1.1), dict(label_smoothing=math.nan), dict(tokens=None), dict(offsets=None),
-                                dict(chosen=None), dict(rejected=None), dict(stats=None), dict(slopes=None), dict(logprobs=None)]}[kind]
+                                dict(chosen=None), dict(rejected=None), dict(stats=None), dict(stats=at + 8), dict(slopes=None), dict(rows=1 << 20, V=1 << 24, row_stride=1 << 24)]}[kind]
         for changed in common + own:
             assert code(kind, changed) == zf.ZF_ERR_INVALID_ARG, (kind, changed)
             assert code(kind, changed, back=True) == zf.ZF_ERR_INVALID_ARG, (kind, changed)
