@@ -17,8 +17,11 @@
 namespace zf {
 namespace {
 
+__host__ __device__ constexpr int own_words_of(int pieces, int epv) { return (pieces * epv + 31) / 32; }      // words of a row's mask that a thread brings
+__host__ __device__ constexpr int early_of(int pieces) { return pieces <= 16 ? 3 : 0; }                       // (more pieces leave no registers)
 enum Kind { POLICY, DISTILL, LOGPROB };       // LOGPROB: of preferences' tokens alone, and what their gradient needs
 
+static const int THREADS_MAX = 1024;
 static const int CHUNK = 1 << 17;             // tokens whose bits LDS holds: which of them a row's teacher listed
 
 struct Args {
@@ -57,6 +60,16 @@ __device__ __forceinline__ double wave_max(double x) {
     for (int d = 1; d < 64; d *= 2) x = fmax(x, __shfl_xor(x, d));
     return x;
 }
+// What is alike in the whole workgroup and not written by the kernel comes through the scalar unit, whose loads are waited for apart from a row's pieces: a vector load behind them would make everything that is
+// asked for and written before it be waited for.
+#define CONSTANT __attribute__((address_space(4)))
+template <typename T> __device__ __forceinline__ T alike(const T *p) { return *(const CONSTANT T *)(uintptr_t)p; }
+__device__ __forceinline__ float logit_alike(const uint32_t *p) { return of_bits(alike(p)); }
+__device__ __forceinline__ float logit_alike(const uint16_t *p) {        // (of the four bytes that hold it)
+    const uintptr_t at = (uintptr_t)p;
+    return of_bits((uint16_t)(alike((const uint32_t *)(at & ~(uintptr_t)3)) >> (at & 2 ? 16 : 0)));
+}
+__device__ __forceinline__ int64_t token_at(const Args &A, int64_t row) { return A.id_bytes == 8 ? alike((const int64_t *)A.ids + row) : alike((const int32_t *)A.ids + row); }
 __device__ __forceinline__ int64_t id_at(const Args &A, int64_t i) { return A.id_bytes == 8 ? ((const int64_t *)A.ids)[i] : ((const int32_t *)A.ids)[i]; }
 __device__ __forceinline__ bool allowed(const uint32_t *mask_row, int64_t v) { return !mask_row || ((mask_row[v >> 5] >> (v & 31)) & 1u); }
 
@@ -108,8 +121,8 @@ __device__ __forceinline__ void store_element(ElemT *to, float x) {
     else *(__bf16 *)to = (__bf16)x;
 }
 // U pieces from memory at a distance of TH, of whose places `bits` are wanted: all are asked for before the first is looked at, and nothing is where there are none.
-template <int TH, int U, int EPV, typename ElemT>
-__device__ __forceinline__ void load_pieces(const ElemT *at, const uint32_t (&bits)[U], bool once, u32x4 (&r)[U]) {
+template <int U, int EPV, typename ElemT>
+__device__ __forceinline__ void load_pieces(const int TH, const ElemT *at, const uint32_t (&bits)[U], bool once, u32x4 (&r)[U]) {
     constexpr uint32_t NONE = sizeof(ElemT) == 4 ? 0xFF800000u : 0xFF80FF80u;
 #pragma unroll
     for (int u = 0; u < U; u++) r[u] = u32x4{NONE, NONE, NONE, NONE};
@@ -287,8 +300,8 @@ __device__ __forceinline__ double distill_row(const Args &A, const Part &sum, fl
     return nan ? NAN : loss;
 }
 // The gradient of listed tokens, over what the row's own pass wrote there.
-template <int TH, typename ElemT>
-__device__ __forceinline__ void store_entries(const Args &A, const Entries &E, ElemT *grad) {
+template <typename ElemT>
+__device__ __forceinline__ void store_entries(const int TH, const Args &A, const Entries &E, ElemT *grad) {
     for (int k = threadIdx.x; k < A.K; k += TH) {
         const int32_t id = E.id[k];
         if (id < 0) continue;
@@ -326,20 +339,17 @@ __device__ __forceinline__ int32_t sequence_of(const Args &A, int64_t row, int l
 // ---- a row's results ----
 template <int KIND>
 __device__ __forceinline__ void ask_head(const Args &A, int64_t row, Head &h) {
-    h.weight = A.r.weight && KIND != LOGPROB ? A.r.weight[row] : 1.0f;
+    h.weight = A.r.weight && KIND != LOGPROB ? alike(A.r.weight + row) : 1.0f;
     if (KIND == POLICY) {
-        h.old_logprob = A.old_logprobs[row];
-        h.advantage = A.advantages[row];
-        h.ref = A.ref ? A.ref[row] : 0.0f;
+        h.old_logprob = alike(A.old_logprobs + row);
+        h.advantage = alike(A.advantages + row);
+        h.ref = A.ref ? alike(A.ref + row) : 0.0f;
     }
 }
 template <typename ElemT>
 __device__ __forceinline__ void ask_token(const Args &A, const ElemT *logits, const uint32_t *mask, Head &h) {
     h.x = -INFINITY;
-    if (h.t >= 0 && h.t < A.r.V) {
-        const float x = of_bits(logits[h.t]);
-        if (allowed(mask, h.t)) h.x = x;
-    }
+    if (h.t >= 0 && h.t < A.r.V && (!mask || ((alike(mask + (h.t >> 5)) >> (h.t & 31)) & 1u))) h.x = logit_alike(logits + h.t);
 }
 template <int KIND, bool ENT>
 __device__ __forceinline__ void no_row(const Args &A, int64_t row) {       // by one thread: a row that is padding
@@ -441,15 +451,15 @@ __device__ __forceinline__ void grad_of_wild(const float (&x)[EPV], const Ends &
         d[k] = x[k] == -INFINITY ? 0.0f : ENT ? fmaf(e * fmaxf(y, -1e4f), ends.slope, e * ends.base) : e * ends.base;
     }
 }
-template <int TH, int EPV, typename ElemT>
-__device__ __forceinline__ void store_zeros(ElemT *grad, int32_t V, bool once) {
+template <int EPV, typename ElemT>
+__device__ __forceinline__ void store_zeros(const int TH, ElemT *grad, int32_t V, bool once) {
     for (int32_t j = threadIdx.x; j < V / EPV; j += TH) store_raw<ElemT>(grad + (int64_t)j * EPV, u32x4{0, 0, 0, 0}, once);
     if ((int)threadIdx.x < V % EPV) store_element(grad + V - V % EPV + threadIdx.x, 0.0f);
 }
 
 // A row's gradient, from memory, where wild() says so.
-template <int TH, bool ENT, int EPV, typename ElemT>
-__device__ __forceinline__ void wild_row(const ElemT *logits, const uint32_t *mask, ElemT *grad, int32_t V, const Ends &ends, float c) {
+template <bool ENT, int EPV, typename ElemT>
+__device__ __forceinline__ void wild_row(const int TH, const ElemT *logits, const uint32_t *mask, ElemT *grad, int32_t V, const Ends &ends, float c) {
     for (int32_t j = threadIdx.x; j < V / EPV; j += TH) {
         const uint32_t bits = bits_of<EPV>(mask, (int64_t)j * EPV);
         for (int k = 0; k < EPV; k++) {
@@ -462,16 +472,17 @@ __device__ __forceinline__ void wild_row(const ElemT *logits, const uint32_t *ma
     }
 }
 
-template <int TH, int EPV>
-__device__ __forceinline__ int writer_of(int64_t v, int32_t V) { return v >= V - V % EPV ? (int)(v % EPV) : (int)(v / EPV % TH); }
+template <int EPV>
+__device__ __forceinline__ int writer_of(const int TH, int64_t v, int32_t V) { return v >= V - V % EPV ? (int)(v % EPV) : (int)(v / EPV % TH); }
 
 // A row a workgroup, from memory: read for the sums, and again where its gradient is wanted.  For rows that do not fit a compute unit's registers, and calls without a gradient.
-template <int TH, int KIND, bool ENT, typename ElemT>
-__global__ __launch_bounds__(TH) void loss_rows_kernel(const Args A) {
-    constexpr int EPV = 16 / sizeof(ElemT), WAVES = TH / 64, U = 4;
+template <int KIND, bool ENT, typename ElemT>
+__global__ __launch_bounds__(THREADS_MAX) void loss_rows_kernel(const Args A) {
+    constexpr int EPV = 16 / sizeof(ElemT), U = 4;
+    const int TH = blockDim.x, WAVES = TH / 64;
     constexpr uint32_t FULL = (1u << EPV) - 1u;
     constexpr bool LIST = KIND == DISTILL;
-    __shared__ Part part[WAVES];
+    __shared__ Part part[THREADS_MAX / 64];
     __shared__ Ends shared_ends;
     __shared__ uint32_t listed[LIST ? CHUNK / 32 : 1];
     extern __shared__ __align__(16) char entries[];
@@ -506,14 +517,14 @@ __global__ __launch_bounds__(TH) void loss_rows_kernel(const Args A) {
             __syncthreads();
             looked = E.end->flags != 0;
         } else {
-            h.t = id_at(A, row);
+            h.t = token_at(A, row);
             if (KIND == LOGPROB && h.t >= 0) h.sequence = sequence_of(A, row, lane);
             looked = h.t >= 0 && (KIND != LOGPROB || h.sequence >= 0);
             ask_token(A, logits, mask, h);
         }
         if (!looked) {                                     // (alike in the whole workgroup)
             if (tid == 0) no_row<KIND, ENT>(A, row);
-            if (A.grad) store_zeros<TH, EPV>(grad, V, A.once);
+            if (A.grad) store_zeros<EPV>(TH, grad, V, A.once);
             if (LIST) __syncthreads();                     // before the lists are written again
             continue;
         }
@@ -543,7 +554,7 @@ __global__ __launch_bounds__(TH) void loss_rows_kernel(const Args A) {
                     bits[u] = j + u * TH < to / EPV ? bits_of<EPV>(mask, v) : 0u;
                     if (LIST && bits[u]) bits[u] &= ~(listed[(v - from) >> 5] >> (v & 31));
                 }
-                load_pieces<TH, U, EPV>(logits + (int64_t)j * EPV, bits, KIND == LOGPROB && A.once, raw);
+                load_pieces<U, EPV>(TH, logits + (int64_t)j * EPV, bits, KIND == LOGPROB && A.once, raw);
 #pragma unroll
                 for (int u = 0; u < U; u++) {
                     if (!__any(bits[u] != 0)) continue;
@@ -571,13 +582,13 @@ __global__ __launch_bounds__(TH) void loss_rows_kernel(const Args A) {
             const Ends ends = shared_ends;
             const Slope slope(ends, A.c);
             const bool all = wild<ENT, ElemT>(ends, A.c);
-            if (all) wild_row<TH, ENT, EPV>(logits, mask, grad, V, ends, A.c);
+            if (all) wild_row<ENT, EPV>(TH, logits, mask, grad, V, ends, A.c);
             for (int32_t j = tid; j < n_pieces && !all; j += U * TH) {
                 uint32_t bits[U];
                 u32x4 raw[U];
 #pragma unroll
                 for (int u = 0; u < U; u++) bits[u] = j + u * TH < n_pieces ? bits_of<EPV>(mask, (int64_t)(j + u * TH) * EPV) : 0u;
-                load_pieces<TH, U, EPV>(logits + (int64_t)j * EPV, bits, A.once, raw);
+                load_pieces<U, EPV>(TH, logits + (int64_t)j * EPV, bits, A.once, raw);
 #pragma unroll
                 for (int u = 0; u < U; u++) {
                     u32x4 d{0, 0, 0, 0};
@@ -596,10 +607,10 @@ __global__ __launch_bounds__(TH) void loss_rows_kernel(const Args A) {
                 store_element(grad + v, d[0]);
             }
             if (!LIST) {                                   // by the thread that has just written the token's piece
-                if (h.x != -INFINITY && tid == writer_of<TH, EPV>(h.t, V)) store_element(grad + h.t, ends.at_token);
+                if (h.x != -INFINITY && tid == writer_of<EPV>(TH, h.t, V)) store_element(grad + h.t, ends.at_token);
             } else {
                 __syncthreads();
-                store_entries<TH>(A, E, grad);
+                store_entries(TH, A, E, grad);
             }
         }
         if (LIST) {
@@ -615,16 +626,17 @@ __global__ __launch_bounds__(TH) void loss_rows_kernel(const Args A) {
 // A row a workgroup, held in registers between its sums and its gradient: NP pieces of 16 bytes a thread.  Workgroups stay.  As soon as the gradient of a piece is on
 // the way its registers take the next row's piece, which is added to that row's sums LAG pieces later: memory is asked for, written and waited for all along the
 // arithmetic of both.  A row's mask lies in LDS, without the tokens that a teacher listed: their sums and their gradient are taken from the list.
-template <int TH, int NP, int KIND, bool MASKED, bool ENT, typename ElemT>
-__global__ __launch_bounds__(TH, 4) void loss_resident_kernel(const Args A) {
-    constexpr int EPV = 16 / sizeof(ElemT), WAVES = TH / 64, WORDS = NP * TH * EPV / 32, OWN_WORDS = (WORDS + TH - 1) / TH, LAG = 4;
-    constexpr uint32_t FULL = (1u << EPV) - 1u, NONE = sizeof(ElemT) == 4 ? 0xFF800000u : 0xFF80FF80u;      // -inf
+template <int NP, int KIND, bool MASKED, bool ENT, typename ElemT>
+__global__ __launch_bounds__(THREADS_MAX, 4) void loss_resident_kernel(const Args A) {
+    constexpr int EPV = 16 / sizeof(ElemT), OWN_WORDS = own_words_of(NP, EPV), LAG = 4, EARLY = early_of(NP), SPARE = 3;
+    const int TH = blockDim.x, WAVES = TH / 64;
+    constexpr uint32_t FULL = (1u << EPV) - 1u;
     constexpr bool LIST = KIND == DISTILL;
     static_assert(!LIST || MASKED, "listed tokens are taken out of the mask");
-    __shared__ Part part[WAVES];
+    __shared__ Part part[THREADS_MAX / 64];
     __shared__ Ends shared_ends;
-    __shared__ uint32_t bits_lds[MASKED ? WORDS : 1];
-    extern __shared__ __align__(16) char entries[];
+    extern __shared__ __align__(16) char entries[];         // two rows' entries, a row's mask
+    uint32_t *const bits_lds = (uint32_t *)(entries + (LIST ? 2 * entries_bytes(A.K) : 0));
     int tid = threadIdx.x;
     const int wave = __builtin_amdgcn_readfirstlane(tid / 64), lane = tid % 64;
     const int32_t V = A.r.V;
@@ -649,52 +661,55 @@ __global__ __launch_bounds__(TH, 4) void loss_resident_kernel(const Args A) {
     };
     auto store_words = [&]() {
 #pragma unroll
-        for (int i = 0; i < OWN_WORDS; i++) if (tid + i * TH < WORDS) bits_lds[tid + i * TH] = own_words[i];
+        for (int i = 0; i < OWN_WORDS; i++) bits_lds[tid + i * TH] = own_words[i];
     };
-    auto bits_of_piece = [&](int i) -> uint32_t {
-        const int j = tid + i * TH;
-        const uint32_t byte = ((const uint8_t *)bits_lds)[EPV == 8 ? j : j / 2];
-        return EPV == 8 ? byte : (byte >> (j % 2 * 4)) & FULL;
+    // Every access to memory in the loop over pieces is made by all lanes and whatever the row: the wait for a piece can then leave those that were asked for after it on their way (a
+    // piece that may or may not have been asked for would have to be waited for as the last one).  Pieces beyond the row's last are that one once more, written with the same bytes;
+    // what is not wanted is asked for from one place.
+    uint32_t top;                                          // bytes from a row's start to its last piece
+    auto place_of = [&](int i) { return min(((uint32_t)tid + (uint32_t)(i * TH)) * 16u, top); };
+    auto bits_at = [&](uint32_t place) -> uint32_t {
+        const uint32_t byte = ((const uint8_t *)bits_lds)[place / (EPV == 8 ? 16u : 32u)];
+        return EPV == 8 ? byte : (byte >> ((place / 16u & 1u) * 4u)) & FULL;
     };
-    const uint32_t at_tid = (uint32_t)tid * 16u;           // bytes; a piece's address is a row's and i's, alike in the workgroup, and this
-    auto place_of = [&](const void *of, int i) {           // (stated apart for each: of all, the compiler makes 64-bit additions in every thread)
-        uint64_t at = (uint64_t)(uintptr_t)of + (uint64_t)(i * (TH * 16));
-        asm volatile("" : "+s"(at));
-        return (GLOBAL char *)at;
+    auto load = [&](const ElemT *from, uint32_t place) { return __builtin_nontemporal_load((GLOBAL const typename Piece<ElemT>::type *)((GLOBAL const char *)(uintptr_t)from + place)); };
+    auto fetch = [&](const ElemT *from, int i, bool wanted) {            // piece i of the thread; none is read of which the mask allows nothing
+        uint32_t place = place_of(i);
+        if (MASKED) place = bits_at(place) ? place : 0u;
+        raw[i] = load(from, wanted ? place : 0u);
     };
-    auto has = [&](int i) { return (i + 1) * TH <= n_pieces || tid + i * TH < n_pieces; };
-    auto fetch = [&](const ElemT *from, int i) {           // piece i of the thread; nothing is read that the mask allows nothing of
-        GLOBAL char *const at = place_of(from, i);
-        if (has(i) && (!MASKED || bits_of_piece(i))) raw[i] = __builtin_nontemporal_load((GLOBAL const typename Piece<ElemT>::type *)(at + at_tid));
-    };
+    // The last EARLY pieces of the row after the next are asked for before the next row's sums come to an end: while a row's end is worked out, memory has them to bring,
+    // and the sums do not wait for what was asked for last.  (Nobody knows yet which of them the mask allows, or whether the row counts.)
+    u32x4 early[EARLY ? EARLY : 1];
     const bool last = tid < V % EPV;                       // the thread has one of the elements behind the whole pieces
     const int32_t v_last = V - V % EPV + tid;
-    float x_last = -INFINITY;
+    ElemT raw_last = 0;                                    // (not looked at before its turn)
+    bool last_allowed = false;
     Part mine;
     uint32_t live, next_live = 0;                          // pieces with an allowed token
-    auto add = [&](int i) {                                // what was not read, or is not allowed, becomes -inf
+    auto add = [&](int i) {                                // what is not allowed becomes -inf
         uint32_t bits = FULL;
         if (MASKED) {
-            bits = bits_of_piece(i);
-            if ((i + 1) * TH > n_pieces && tid + i * TH >= n_pieces) bits = 0;       // (behind the whole pieces there may be bits of single elements)
+            bits = bits_at(place_of(i));
             next_live |= (bits ? 1u : 0u) << i;
             if (__any(bits != FULL)) forbid<EPV, ElemT>(raw[i], bits);
-        } else if ((i + 1) * TH > n_pieces) {
-            if (tid + i * TH >= n_pieces) raw[i] = u32x4{NONE, NONE, NONE, NONE};
         }
         if (!MASKED || __any(bits != 0)) {
             float x[EPV];
             numbers<EPV, ElemT>(raw[i], x);
+            const Part before = mine;
             add_piece<ENT>(x, A.c, mine);
+            if ((i + 1) * TH > n_pieces && tid + i * TH >= n_pieces) mine = before;      // the last piece once more
         }
         asm volatile("" : "+v"(raw[i]));                   // (the numbers are made from their 16 bits again: kept, they would be twice the registers)
     };
     auto fetch_last = [&](const ElemT *from) {
-        if (last) x_last = MASKED && !((bits_lds[v_last >> 5] >> (v_last & 31)) & 1u) ? -INFINITY : of_bits(from[v_last]);
+        raw_last = from[last ? v_last : 0];
+        last_allowed = !MASKED || (last && ((bits_lds[v_last >> 5] >> (v_last & 31)) & 1u));
     };
     auto add_last = [&]() {
         if (!last) return;
-        const float x[1] = {x_last};
+        const float x[1] = {last_allowed ? of_bits(raw_last) : -INFINITY};
         add_piece<ENT>(x, A.c, mine);
     };
     // A row's entries: ids and values are asked for two rows ahead, logits and masks one, up to TH of them; further ones when their row is listed.
@@ -719,7 +734,7 @@ __global__ __launch_bounds__(TH, 4) void loss_resident_kernel(const Args A) {
     // The first row
     ask_head<KIND>(A, row, head);
     if (!LIST) {
-        head.t = id_at(A, row);
+        head.t = token_at(A, row);
         ask_token(A, logits_of(row), mask_of(row), head);
         counts = head.t >= 0;
     }
@@ -740,23 +755,28 @@ __global__ __launch_bounds__(TH, 4) void loss_resident_kernel(const Args A) {
         }
     }
     mine = Part{-FLT_MAX, 0.0f, 0.0f, 0.0f};
+    top = (uint32_t)(n_pieces - 1) * 16u;
     if (counts) {
 #pragma unroll
-        for (int i = 0; i < NP; i++) if (i * TH < n_pieces) fetch(logits_of(row), i);
+        for (int i = 0; i < NP; i++) fetch(logits_of(row), i, true);
 #pragma unroll
-        for (int i = 0; i < NP; i++) if (i * TH < n_pieces) add(i);
+        for (int i = 0; i < NP; i++) if (i < NP - SPARE || i * TH < n_pieces) add(i);
         fetch_last(logits_of(row));
         add_last();
     }
-    if (!LIST && row + gridDim.x < A.r.rows) next_head.t = id_at(A, row + gridDim.x);
+    if (!LIST && row + gridDim.x < A.r.rows) next_head.t = token_at(A, row + gridDim.x);
+    if (MASKED && row + gridDim.x < A.r.rows) read_words(row + gridDim.x);
+    if (row + gridDim.x < A.r.rows)
+#pragma unroll
+        for (int i = NP - EARLY; i < NP; i++) early[i - (NP - EARLY)] = load(logits_of(row + gridDim.x), place_of(i));
     for (;;) {
+        n_pieces = __builtin_amdgcn_readfirstlane(n_pieces);
         asm volatile("" : "+v"(tid), "+s"(n_pieces));      // (whether a thread has its i-th piece is found anew for each row: kept, that would be registers of every i)
         const Entries E(entries + turn * size, A.K), next_E(entries + (turn ^ 1) * size, A.K);
         const int64_t next = row + gridDim.x;
         const bool more = next < A.r.rows;
         ElemT *const grad = (ElemT *)A.grad + row * A.grad_stride;
         if (LIST && counts) for (int u = wave; u < (A.K + 63) / 64; u += WAVES) sum_entries(A, u, lane, E);
-        if (MASKED && more) read_words(next);
         if (more) {
             ask_head<KIND>(A, next, next_head);
             if (!LIST) ask_token(A, logits_of(next), mask_of(next), next_head);
@@ -785,23 +805,31 @@ __global__ __launch_bounds__(TH, 4) void loss_resident_kernel(const Args A) {
             ask_entry_logit(next + gridDim.x, ahead);
             ask_entry(next + 2 * (int64_t)gridDim.x, after);
         }
-        const int64_t next_t = !LIST && next + gridDim.x < A.r.rows ? id_at(A, next + gridDim.x) : -1;
-        const ElemT *const next_logits = logits_of(next);
+        const int64_t next_t = !LIST && next + gridDim.x < A.r.rows ? token_at(A, next + gridDim.x) : -1;
+        const bool third = next + gridDim.x < A.r.rows;    // there is a row after the next
+        const ElemT *const next_logits = logits_of(next_counts ? next : row), *const third_logits = logits_of(third ? next + gridDim.x : row);
         mine = Part{-FLT_MAX, 0.0f, 0.0f, 0.0f};
-        const float x_of_row[1] = {x_last};
-        if (next_counts) fetch_last(next_logits);
+        const float x_of_row[1] = {last && last_allowed ? of_bits(raw_last) : -INFINITY};
+        fetch_last(next_logits);
 #pragma unroll
         for (int i = 0; i < NP + LAG; i++) {
-            if (i < NP && i * TH < n_pieces) {
-                GLOBAL char *const to = place_of(grad, i);
+            if (MASKED && i == NP - EARLY - 2) read_words(third ? next + gridDim.x : row);     // (here, so that they are there when the loop is done)
+            if (i < NP && (i < NP - SPARE || i * TH < n_pieces)) {
                 u32x4 d{0, 0, 0, 0};
                 if (counts && (!MASKED || __any((live >> i) & 1u))) d = grad_of<ENT, EPV, ElemT>(raw[i], slope, A.c);
-                if (has(i)) store_raw<ElemT>(to + at_tid, d, A.once);
-                if (next_counts) fetch(next_logits, i);
+                store_raw<ElemT>((GLOBAL char *)(uintptr_t)grad + place_of(i), d, A.once);
+                if (i < NP - EARLY) fetch(next_logits, i, next_counts);
+                else {
+                    raw[i] = early[i - (NP - EARLY)];
+                    early[i - (NP - EARLY)] = load(third_logits, third ? place_of(i) : 0u);
+                }
             }
-            if (i >= LAG && (i - LAG) * TH < n_pieces && next_counts) add(i - LAG);
+            if (i >= LAG && next_counts && (i - LAG < NP - SPARE || (i - LAG) * TH < n_pieces)) add(i - LAG);
         }
-        if (counts && wild<ENT, ElemT>(ends, A.c)) wild_row<TH, ENT, EPV>(logits_of(row), mask_of(row), grad, V, ends, A.c);
+        if (counts && wild<ENT, ElemT>(ends, A.c)) {
+            __syncthreads();                               // the last piece may have been written by several
+            wild_row<ENT, EPV>(TH, logits_of(row), mask_of(row), grad, V, ends, A.c);
+        }
         if (last) {
             float d[1] = {0.0f};
             if (counts) grad_of_wild<ENT>(x_of_row, ends, A.c, d);
@@ -809,10 +837,12 @@ __global__ __launch_bounds__(TH, 4) void loss_resident_kernel(const Args A) {
         }
         if (next_counts) add_last();
         if (!LIST) {                                       // by the thread that has just written the token's piece
-            if (counts && head.x != -INFINITY && tid == writer_of<TH, EPV>(head.t, V)) store_element(grad + head.t, ends.at_token);
+            const int passes = max(NP - SPARE, (n_pieces + TH - 1) / TH);
+            const bool wrote = tid == writer_of<EPV>(TH, head.t, V) || (head.t / EPV == n_pieces - 1 && tid + (passes - 1) * TH >= n_pieces);      // (the last piece: each that did)
+            if (counts && head.x != -INFINITY && wrote) store_element(grad + head.t, ends.at_token);
         } else {
             __syncthreads();
-            if (counts) store_entries<TH>(A, E, grad);
+            if (counts) store_entries(TH, A, E, grad);
         }
         if (!more) return;
         row = next;
@@ -910,7 +940,7 @@ __global__ __launch_bounds__(TH) void preference_grad_kernel(const zf_preference
     u32x4 raw[U];
 #pragma unroll
     for (int u = 0; u < U; u++) bits[u] = counts && j + u * TH < n_pieces ? bits_of<EPV>(mask, (int64_t)(j + u * TH) * EPV) : 0u;
-    load_pieces<TH, U, EPV>(logits + (int64_t)j * EPV, bits, once, raw);
+    load_pieces<U, EPV>(TH, logits + (int64_t)j * EPV, bits, once, raw);
     const int64_t t = p.token_bytes == 8 ? ((const int64_t *)p.tokens)[row] : ((const int32_t *)p.tokens)[row];
     const float f = counts ? (float)((double)p.slopes[sequence] * *g / p.r.temperature) : 0.0f, base = -f * found.y;
     const Ends ends{found.x, base, 0.0f, 0.0f};
@@ -957,30 +987,33 @@ __global__ __launch_bounds__(TH) void preference_grad_kernel(const zf_preference
 
 static const int COMPUTE_UNITS = 256, GRAD_PIECES = 4;
 int grid_of(int64_t n) { return (int)std::min<int64_t>(n, 1 << 16); }
-// TH threads take a row, NP pieces each at most; `each`: workgroups that a compute unit's registers hold.  Without a gradient a row is read from memory by as many threads, in the same order.
-template <int TH, int NP, int KIND, bool ENT, typename ElemT>
-void rows_by(const Args &A, hipStream_t s) {
+// `threads` take a row, NP pieces each at most; as many workgroups as the compute units' registers hold (128 of a thread).  Without a gradient a row is read from memory by as many
+// threads, in the same order, to the same bits.
+template <int NP, int KIND, bool ENT, typename ElemT>
+void rows_by(const Args &A, int threads, hipStream_t s) {
     const int lds = KIND == DISTILL ? entries_bytes(A.K) : 0;
     if constexpr (KIND != LOGPROB && NP > 0) {
-        if (A.grad) {
-            const dim3 grid((int)std::min<int64_t>(A.r.rows, 1024 / TH * COMPUTE_UNITS));
-            if (KIND == DISTILL || A.r.mask) hipLaunchKernelGGL((loss_resident_kernel<TH, NP, KIND, true, ENT, ElemT>), grid, dim3(TH), 2 * lds, s, A);
-            else if constexpr (KIND != DISTILL) hipLaunchKernelGGL((loss_resident_kernel<TH, NP, KIND, false, ENT, ElemT>), grid, dim3(TH), 0, s, A);
+        if (A.grad && A.r.V >= 16 / (int)sizeof(ElemT)) {
+            const dim3 grid((int)std::min<int64_t>(A.r.rows, THREADS_MAX / threads * COMPUTE_UNITS));
+            const int words = own_words_of(NP, 16 / (int)sizeof(ElemT)) * threads * 4;
+            if (KIND == DISTILL || A.r.mask) hipLaunchKernelGGL((loss_resident_kernel<NP, KIND, true, ENT, ElemT>), grid, dim3(threads), 2 * lds + words, s, A);
+            else if constexpr (KIND != DISTILL) hipLaunchKernelGGL((loss_resident_kernel<NP, KIND, false, ENT, ElemT>), grid, dim3(threads), 0, s, A);
             return;
         }
     }
-    hipLaunchKernelGGL((loss_rows_kernel<TH, KIND, ENT, ElemT>), dim3(grid_of(A.r.rows)), dim3(TH), lds, s, A);
+    hipLaunchKernelGGL((loss_rows_kernel<KIND, ENT, ElemT>), dim3(grid_of(A.r.rows)), dim3(threads), lds, s, A);
 }
 template <int KIND, bool ENT, typename ElemT>
 void rows_of(const Args &A, hipStream_t s) {
     const int32_t n = (A.r.V + (int)(16 / sizeof(ElemT)) - 1) / (int)(16 / sizeof(ElemT));    // pieces of a row
-    if (KIND == LOGPROB && A.r.rows >= 2048 && n > 16 * 64) return rows_by<256, 0, KIND, ENT, ElemT>(A, s);
-    if (n <= 16 * 64) return rows_by<64, 16, KIND, ENT, ElemT>(A, s);
-    if (n <= 16 * 256) return rows_by<256, 16, KIND, ENT, ElemT>(A, s);
-    if (n <= 16 * 512) return rows_by<512, 16, KIND, ENT, ElemT>(A, s);
-    if (n <= 16 * 1024) return rows_by<1024, 16, KIND, ENT, ElemT>(A, s);
-    if (n <= 20 * 1024) return rows_by<1024, 20, KIND, ENT, ElemT>(A, s);
-    rows_by<1024, 0, KIND, ENT, ElemT>(A, s);
+    if (KIND == LOGPROB && A.r.rows >= 2048 && n > 16 * 64) return rows_by<0, KIND, ENT, ElemT>(A, 256, s);
+    // A thread has all its pieces but the last three at least, or does some again: 16 of them where that fits, else 8.  A workgroup of its own on a compute unit takes a row in the shorter
+    // time with twice the threads.
+    const int by_16 = (n + 16 * 64 - 1) / (16 * 64) * 64, by_8 = (n + 8 * 64 - 1) / (8 * 64) * 64;
+    if (by_8 <= THREADS_MAX && (A.r.rows <= COMPUTE_UNITS || n <= 13 * by_16)) return rows_by<8, KIND, ENT, ElemT>(A, by_8, s);
+    if (n <= 16 * THREADS_MAX) return rows_by<16, KIND, ENT, ElemT>(A, by_16, s);
+    if (n <= 20 * THREADS_MAX) return rows_by<20, KIND, ENT, ElemT>(A, THREADS_MAX, s);
+    rows_by<0, KIND, ENT, ElemT>(A, THREADS_MAX, s);
 }
 template <int KIND, bool ENT>
 void rows_of(const Args &A, hipStream_t s) {
