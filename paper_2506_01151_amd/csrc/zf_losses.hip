@@ -174,7 +174,7 @@ __device__ __forceinline__ double policy_row(const Args &A, const Part &sum, con
     const double scale = (double)wg / A.r.temperature, toS = scale / sum.S;
     ends->base = (float)(toS * (b * (H - lnS) - f));
     ends->slope = (float)(toS * b * LN_2);
-    ends->at_token = (float)(scale * (f + exp(lp) * (b * (lp + H) - f)));
+    ends->at_token = (float)(scale * (f + (double)two_to((h.x - sum.m) * A.c) / sum.S * (b * (lp + H) - f)));
     return loss;
 }
 
@@ -185,9 +185,9 @@ struct Teacher {
     double v_most;
     float x_most;
     int32_t some;
+    double to_shares;                          // the call's factor and what makes e the entry's share of the whole
 };
 struct EntriesEnd {
-    double v_most, scale;                      // q = e^((v - v_most) / T) times what is in `scale` but for the sign
     float x_most, to_listed;                   // a listed token's gradient: its 2^((x - x_most) c) times this, and the entries' own
     uint32_t flags;                            // 1: an entry counts, 2: an id is beyond V, 4: a token is listed twice
     uint32_t pad;
@@ -196,7 +196,7 @@ struct Entries {                               // in LDS, room for the call's n_
     Teacher *part;                             // [n / 64]
     EntriesEnd *end;
     int32_t *id;                               // [n]; -1: does not count
-    float *x, *v;
+    float *x, *v;                              // v: the teacher's value, then e
     __device__ __forceinline__ Entries(char *at, int K) {
         part = (Teacher *)at;
         end = (EntriesEnd *)(part + (K + 63) / 64);
@@ -252,15 +252,16 @@ __device__ __forceinline__ void sum_entries(const Args &A, int wave, int lane, c
         ln = A.rest ? v : (v - v_most) / T;
         e = exp(ln);
     }
+    if (k < A.K) E.v[k] = (float)e;
     const double mixed = e == 0.0 ? 0.0 : e * (ln - ((double)x - x_most) / T);
     if (counts && first_of(E, k)) S = two_to((x - x_most) * A.c);
-    const Teacher t{wave_sum(e), wave_sum(mixed), wave_sum(S), v_most, x_most, __any(counts)};
+    const Teacher t{wave_sum(e), wave_sum(mixed), wave_sum(S), v_most, x_most, __any(counts), 0.0};
     if (lane == 0) E.part[wave] = t;
 }
 // A row's end, from the sums over what is not listed; by every lane of one wavefront alike.  Returns the row's loss.
 __device__ __forceinline__ double distill_row(const Args &A, const Part &sum, float wg, const Entries &E, Ends *ends) {
     const double T = A.r.temperature;
-    Teacher t{0.0, 0.0, 0.0, -INFINITY, -INFINITY, 0};
+    Teacher t{0.0, 0.0, 0.0, -INFINITY, -INFINITY, 0, 0.0};
     for (int w = 0; w < (A.K + 63) / 64; w++) {
         const Teacher u = E.part[w];
         if (!u.some) continue;
@@ -277,26 +278,25 @@ __device__ __forceinline__ double distill_row(const Args &A, const Part &sum, fl
     }
     const bool none = sum.S == 0.0f;                       // nothing that is not listed
     const float x_most = none ? t.x_most : fmaxf(t.x_most, sum.m);
+    auto power = [](double ln) { return ln == 0.0 ? 1.0 : exp(ln); };
     const double S_rest = sum.S, down = none ? 0.0 : ((double)sum.m - x_most) / T, listed_down = t.some ? ((double)t.x_most - x_most) / T : 0.0;
-    const double S = (none ? 0.0 : S_rest * exp(down)) + t.S * exp(listed_down), lnS = log(S);
+    const double rest_to_S = power(down), S = S_rest * rest_to_S + t.S * power(listed_down), lnS = log(S);
     const double share = A.rest ? 1.0 : t.total == 0.0 ? 0.0 : 1.0 / t.total;
     double all = t.total * share;                          // sum of q
     double loss = t.total == 0.0 ? 0.0 : (A.rest ? t.mixed : t.mixed * share - log(t.total)) + all * (lnS - listed_down);
     double q_rest = A.rest ? 1.0 - all : 0.0;
     if (q_rest < 0.0 || none) q_rest = 0.0;
-    const double ln_rest = none ? 0.0 : log(S_rest) + down - lnS;          // ln p_R, also where p_R is 0 in 64 bits
-    if (q_rest != 0.0) loss += q_rest * (log(q_rest) - ln_rest);
+    if (q_rest != 0.0) loss += q_rest * (log(q_rest) - (log(S_rest) + down - lnS));        // (ln p_R, also where p_R is 0 in 64 bits)
     const bool nan = (E.end->flags & 2u) || S != S;
     all += q_rest;
     const double scale = (double)wg / T;
     ends->m = sum.m;
-    ends->base = nan ? NAN : none ? 0.0f : (float)(scale * (all * exp(ln_rest) - q_rest) / S_rest);
+    ends->base = nan ? NAN : none ? 0.0f : (float)(scale * (all * rest_to_S / S - q_rest / S_rest));
     ends->slope = 0.0f;
     ends->at_token = 0.0f;
     E.end->x_most = x_most;
-    E.end->v_most = A.rest ? 0.0 : t.v_most;
-    E.end->scale = scale * share;
     E.end->to_listed = nan ? NAN : (float)(scale * all / S);
+    for (int w = 0; w < (A.K + 63) / 64; w++) E.part[w].to_shares = scale * share * (A.rest || !E.part[w].some ? 1.0 : power((E.part[w].v_most - t.v_most) / T));
     return nan ? NAN : loss;
 }
 // The gradient of listed tokens, over what the row's own pass wrote there.
@@ -305,10 +305,7 @@ __device__ __forceinline__ void store_entries(const int TH, const Args &A, const
     for (int k = threadIdx.x; k < A.K; k += TH) {
         const int32_t id = E.id[k];
         if (id < 0) continue;
-        auto q = [&](int i) {
-            const double v = E.v[i];
-            return v == -INFINITY ? 0.0f : (float)(exp(A.rest ? v : (v - E.end->v_most) / A.r.temperature) * E.end->scale);
-        };
+        auto q = [&](int i) { return (float)(E.v[i] * E.part[i / 64].to_shares); };
         float f = q(k);
         if (E.end->flags & 4u) {                                // the entries of the same token in order, by the first
             if (!first_of(E, k)) continue;
@@ -626,7 +623,7 @@ __global__ __launch_bounds__(THREADS_MAX) void loss_rows_kernel(const Args A) {
 // A row a workgroup, held in registers between its sums and its gradient: NP pieces of 16 bytes a thread.  Workgroups stay.  As soon as the gradient of a piece is on
 // the way its registers take the next row's piece, which is added to that row's sums LAG pieces later: memory is asked for, written and waited for all along the
 // arithmetic of both.  A row's mask lies in LDS, without the tokens that a teacher listed: their sums and their gradient are taken from the list.
-template <int NP, int KIND, bool MASKED, bool ENT, typename ElemT>
+template <int NP, int KIND, bool MASKED, bool ENT, bool ALIGNED, typename ElemT>
 __global__ __launch_bounds__(THREADS_MAX, 4) void loss_resident_kernel(const Args A) {
     constexpr int EPV = 16 / sizeof(ElemT), OWN_WORDS = own_words_of(NP, EPV), LAG = 4, EARLY = early_of(NP), SPARE = 3;
     const int TH = blockDim.x, WAVES = TH / 64;
@@ -672,7 +669,11 @@ __global__ __launch_bounds__(THREADS_MAX, 4) void loss_resident_kernel(const Arg
         const uint32_t byte = ((const uint8_t *)bits_lds)[place / (EPV == 8 ? 16u : 32u)];
         return EPV == 8 ? byte : (byte >> ((place / 16u & 1u) * 4u)) & FULL;
     };
-    auto load = [&](const ElemT *from, uint32_t place) { return __builtin_nontemporal_load((GLOBAL const typename Piece<ElemT>::type *)((GLOBAL const char *)(uintptr_t)from + place)); };
+    // (Rows that begin at multiples of 16 bytes pass the cache by, whatever their number: 32,768 x 2,048 fp32 111 us, else 135; others share lines with their neighbours: 1,030 x 40,037 bf16 50 and 58.)
+    auto load = [&](const ElemT *from, uint32_t place) {
+        const GLOBAL typename Piece<ElemT>::type *const at = (const GLOBAL typename Piece<ElemT>::type *)((const GLOBAL char *)(uintptr_t)from + place);
+        return ALIGNED ? __builtin_nontemporal_load(at) : *at;
+    };
     auto fetch = [&](const ElemT *from, int i, bool wanted) {            // piece i of the thread; none is read of which the mask allows nothing
         uint32_t place = place_of(i);
         if (MASKED) place = bits_at(place) ? place : 0u;
@@ -754,6 +755,9 @@ __global__ __launch_bounds__(THREADS_MAX, 4) void loss_resident_kernel(const Arg
             counts = Entries(entries, A.K).end->flags != 0;
         }
     }
+    // (The last wavefronts' work, beside the pieces: the first one's comes at the row's end.)
+    auto sum_listed = [&](const Entries &E) { for (int u = WAVES - 1 - wave; u < (A.K + 63) / 64; u += WAVES) sum_entries(A, u, lane, E); };
+    if (LIST && counts) sum_listed(Entries(entries, A.K));
     mine = Part{-FLT_MAX, 0.0f, 0.0f, 0.0f};
     top = (uint32_t)(n_pieces - 1) * 16u;
     if (counts) {
@@ -776,7 +780,6 @@ __global__ __launch_bounds__(THREADS_MAX, 4) void loss_resident_kernel(const Arg
         const int64_t next = row + gridDim.x;
         const bool more = next < A.r.rows;
         ElemT *const grad = (ElemT *)A.grad + row * A.grad_stride;
-        if (LIST && counts) for (int u = wave; u < (A.K + 63) / 64; u += WAVES) sum_entries(A, u, lane, E);
         if (more) {
             ask_head<KIND>(A, next, next_head);
             if (!LIST) ask_token(A, logits_of(next), mask_of(next), next_head);
@@ -801,6 +804,7 @@ __global__ __launch_bounds__(THREADS_MAX, 4) void loss_resident_kernel(const Arg
         const bool next_counts = more && (LIST ? next_E.end->flags != 0 : next_head.t >= 0);
         const Slope slope(ends, A.c);
         if (LIST) {
+            if (next_counts) sum_listed(next_E);
             ahead = after;
             ask_entry_logit(next + gridDim.x, ahead);
             ask_entry(next + 2 * (int64_t)gridDim.x, after);
@@ -985,6 +989,11 @@ __global__ __launch_bounds__(TH) void preference_grad_kernel(const zf_preference
     }
 }
 
+// Rows that the last-level cache (256 MB) cannot hold until somebody reads them again pass it by; not those at odd elements, whose lines are written in two parts.
+bool whole(const zf_loss_rows &r, const void *p, int64_t stride) { return !p || ((uintptr_t)p % 16 == 0 && stride * (r.dtype == 0 ? 4 : 2) % 16 == 0); }
+bool passes(const zf_loss_rows &r, const LossGrad &g) {
+    return r.rows * r.V * (r.dtype == 0 ? 4 : 2) > (256ll << 20) && whole(r, r.logits, r.row_stride_elems) && whole(r, g.grad, g.stride);
+}
 static const int COMPUTE_UNITS = 256, GRAD_PIECES = 4;
 int grid_of(int64_t n) { return (int)std::min<int64_t>(n, 1 << 16); }
 // `threads` take a row, NP pieces each at most; as many workgroups as the compute units' registers hold (128 of a thread).  Without a gradient a row is read from memory by as many
@@ -995,9 +1004,11 @@ void rows_by(const Args &A, int threads, hipStream_t s) {
     if constexpr (KIND != LOGPROB && NP > 0) {
         if (A.grad && A.r.V >= 16 / (int)sizeof(ElemT)) {
             const dim3 grid((int)std::min<int64_t>(A.r.rows, THREADS_MAX / threads * COMPUTE_UNITS));
+            const bool aligned = whole(A.r, A.r.logits, A.r.row_stride_elems);
             const int words = own_words_of(NP, 16 / (int)sizeof(ElemT)) * threads * 4;
-            if (KIND == DISTILL || A.r.mask) hipLaunchKernelGGL((loss_resident_kernel<NP, KIND, true, ENT, ElemT>), grid, dim3(threads), 2 * lds + words, s, A);
-            else if constexpr (KIND != DISTILL) hipLaunchKernelGGL((loss_resident_kernel<NP, KIND, false, ENT, ElemT>), grid, dim3(threads), 0, s, A);
+            auto launch = [&](auto *kernel, int bytes) { hipLaunchKernelGGL(kernel, grid, dim3(threads), bytes, s, A); };
+            if (KIND == DISTILL || A.r.mask) launch(aligned ? loss_resident_kernel<NP, KIND, true, ENT, true, ElemT> : loss_resident_kernel<NP, KIND, true, ENT, false, ElemT>, 2 * lds + words);
+            else if constexpr (KIND != DISTILL) launch(aligned ? loss_resident_kernel<NP, KIND, false, ENT, true, ElemT> : loss_resident_kernel<NP, KIND, false, ENT, false, ElemT>, 0);
             return;
         }
     }
@@ -1019,12 +1030,6 @@ template <int KIND, bool ENT>
 void rows_of(const Args &A, hipStream_t s) {
     if (A.r.dtype == 0) rows_of<KIND, ENT, uint32_t>(A, s);
     else rows_of<KIND, ENT, uint16_t>(A, s);
-}
-// Rows that the last-level cache (256 MB) cannot hold until somebody reads them again pass it by; not those at odd elements, whose lines are written in two parts.
-bool passes(const zf_loss_rows &r, const LossGrad &g) {
-    const int64_t size = r.dtype == 0 ? 4 : 2;
-    auto whole = [&](const void *p, int64_t stride) { return !p || ((uintptr_t)p % 16 == 0 && stride * size % 16 == 0); };
-    return r.rows * r.V * size > (256ll << 20) && whole(r.logits, r.row_stride_elems) && whole(g.grad, g.stride);
 }
 Args common(const zf_loss_rows &r, const LossGrad &g) {
     Args A{};
