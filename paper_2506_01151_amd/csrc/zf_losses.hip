@@ -937,7 +937,8 @@ __global__ __launch_bounds__(TH) void preference_grad_kernel(const zf_preference
     const ElemT *const logits = (const ElemT *)p.r.logits + row * p.r.row_stride_elems;
     ElemT *const grad = grad_ + row * grad_stride;
     const uint32_t *const mask = p.r.mask ? p.r.mask + row * W : nullptr;
-    const float4 found = ((const float4 *)p.stats)[row];
+    typedef float f32x4 __attribute__((ext_vector_type(4)));
+    const f32x4 found = alike((const f32x4 *)p.stats + row);
     const int32_t sequence = __float_as_int(found.w);
     const bool counts = sequence >= 0 && found.z != -INFINITY;
     uint32_t bits[U];
@@ -945,8 +946,8 @@ __global__ __launch_bounds__(TH) void preference_grad_kernel(const zf_preference
 #pragma unroll
     for (int u = 0; u < U; u++) bits[u] = counts && j + u * TH < n_pieces ? bits_of<EPV>(mask, (int64_t)(j + u * TH) * EPV) : 0u;
     load_pieces<U, EPV>(TH, logits + (int64_t)j * EPV, bits, once, raw);
-    const int64_t t = p.token_bytes == 8 ? ((const int64_t *)p.tokens)[row] : ((const int32_t *)p.tokens)[row];
-    const float f = counts ? (float)((double)p.slopes[sequence] * *g / p.r.temperature) : 0.0f, base = -f * found.y;
+    const int64_t t = p.token_bytes == 8 ? alike((const int64_t *)p.tokens + row) : alike((const int32_t *)p.tokens + row);
+    const float f = counts ? (float)((double)alike(p.slopes + sequence) * alike(g) / p.r.temperature) : 0.0f, base = -f * found.y;
     const Ends ends{found.x, base, 0.0f, 0.0f};
     const Slope slope(ends, c);
     const bool all = wild<false, ElemT>(ends, c);

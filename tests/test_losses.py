@@ -328,6 +328,64 @@ def test_policy_sides_of_the_clipping():
         assert (slope - torch.where(free, -(ratios * adv), 0.0)).abs().max() < 1e-5
 
 
+# ---- masks that leave few tokens of large calls, which another kernel takes (up to 2,048 of a row, from 32 MB of logits on) ----
+def few_rows(dtype, seed, rows, V):
+    r = Rows(rows, V, dtype, "few", 0.8, seed)
+    for i, n in enumerate((0, 1, 2, 64, 300, 2047, 2048, 2049, 2050, V)):
+        where = torch.randperm(V, generator=r.g)[:n]
+        r.bits[i] = False
+        r.bits[i, where] = True
+    r.bits[10] = False
+    r.bits[10, V - 2048:] = True                   # at the row's end
+    r.bits[11] = False
+    r.bits[11, :2048] = True
+    r.bits[11, V - 1] = True                       # one too many, which comes last
+    r.bits[12, :40] = True
+    r.x[12, :40] = -INF                            # allowed and -inf
+    r.update()
+    return r
+
+
+@gpu
+@pytest.mark.parametrize("dtype,rows,V", [("f32", 280, 30011), ("bf16", 300, 60001), ("bf16", 131, 131072), ("f32", 64, 152064), ("bf16", 150, 152065), ("f32", 33, 262144), ("f32", 33, 262176)])
+@pytest.mark.parametrize("e", [None, 0.05])
+def test_policy_of_few_tokens(dtype, rows, V, e):
+    r = few_rows(dtype, rows + V, rows, V)
+    t = r.tokens(8)
+    lp, counts = r.at(t)
+    old = torch.where(counts, lp, 0.0).float() + 0.1
+    adv = torch.randn((rows,), generator=r.g)
+    losses, bound, lp, H, H_off, grad, off = policy_want(r, t, old, adv, None, (0.2, 0.2), 0.0, e, None)
+    x, m = r.on_gpu("odd" if V % 2 else "packed")
+    x.requires_grad_()
+    got = zf.policy_loss(x, t.cuda(), old.cuda(), adv.cuda(), m, temperature=0.8, entropy_weight=e)
+    close(got.logprobs, lp, torch.where(lp > -INF, r.slack[:, 0], 0.0), "log probabilities")
+    close(got.losses, losses, bound, "losses")
+    if e is not None:
+        close(got.entropy, H, H_off, "entropy")
+    g, = torch.autograd.grad(got.loss, x, retain_graph=True)
+    close(g, grad, off, "gradient", x.dtype)
+    g, = torch.autograd.grad(got.loss, x, torch.tensor(-2.0, device="cuda"))
+    close(g, -2 * grad, 2 * off, "gradient", x.dtype)
+    assert all(torch.equal(p, q) for p, q in zip(zf.policy_loss(x.detach(), t.cuda(), old.cuda(), adv.cuda(), m, temperature=0.8, entropy_weight=e), got) if p is not None)
+
+
+@gpu
+@pytest.mark.parametrize("dtype,rows,V,K", [("f32", 280, 30011, 3), ("bf16", 131, 131072, 70), ("f32", 64, 152064, 1024)])
+@pytest.mark.parametrize("rest", [False, True])
+def test_distill_of_few_tokens(dtype, rows, V, K, rest):
+    r = few_rows(dtype, rows + V, rows, V)
+    listed, v = teacher(r, K, 4, "f32", rest, 5, twice=rows % 3 == 1)
+    weight = torch.rand((rows,), generator=r.g)
+    losses, bound, grad, off = distill_want(r, listed, v, rest, weight, dtype)
+    x, m = r.on_gpu()
+    x.requires_grad_()
+    got = zf.distill_loss(x, listed.cuda(), v.cuda(), m, temperature=0.8, rest=rest, weight=weight.cuda())
+    close(got.losses, losses, bound, "losses")
+    g, = torch.autograd.grad(got.loss, x)
+    close(g, grad, off, "gradient", x.dtype)
+
+
 # ---- preferences ------------------------------------------------------------------------------------
 def preference_want(r, t, offsets, ref, beta, s, average, weight):
     lp, counts = r.at(t)
