@@ -334,6 +334,11 @@ __device__ __forceinline__ int32_t sequence_of(const Args &A, int64_t row, int l
 }
 
 // ---- a row's results ----
+// The call's sum, where there is no other row; of more, total_kernel makes it.
+__device__ __forceinline__ void store_loss(const Args &A, int64_t row, float loss, float weight) {
+    A.r.losses[row] = loss;
+    if (A.r.rows == 1) *A.r.loss = (float)((double)weight * loss);
+}
 template <int KIND>
 __device__ __forceinline__ void ask_head(const Args &A, int64_t row, Head &h) {
     h.weight = A.r.weight && KIND != LOGPROB ? alike(A.r.weight + row) : 1.0f;
@@ -351,7 +356,7 @@ __device__ __forceinline__ void ask_token(const Args &A, const ElemT *logits, co
 template <int KIND, bool ENT>
 __device__ __forceinline__ void no_row(const Args &A, int64_t row) {       // by one thread: a row that is padding
     if (!A.results) return;
-    if (KIND != LOGPROB) A.r.losses[row] = 0.0f;
+    if (KIND != LOGPROB) store_loss(A, row, 0.0f, 0.0f);
     if (KIND == POLICY) A.logprobs[row] = 0.0f;
     if (KIND == LOGPROB) A.found[row] = float4{0.0f, 0.0f, 0.0f, __int_as_float(-1)};
     if (ENT) A.entropy[row] = 0.0f;
@@ -366,7 +371,7 @@ __device__ __forceinline__ void finish_row(const Args &A, const Part &sum, int64
         if (lane != 0) return;
         ends = e;
         if (!A.results) return;
-        A.r.losses[row] = (float)loss;
+        store_loss(A, row, (float)loss, h.weight);
         A.logprobs[row] = logprob;
         if (ENT) A.entropy[row] = entropy;
     } else if (KIND == LOGPROB) {
@@ -378,7 +383,7 @@ __device__ __forceinline__ void finish_row(const Args &A, const Part &sum, int64
         const double loss = distill_row(A, sum, wg, E, &e);
         if (lane != 0) return;
         ends = e;
-        if (A.results) A.r.losses[row] = (float)loss;
+        if (A.results) store_loss(A, row, (float)loss, h.weight);
     }
 }
 
@@ -1049,7 +1054,7 @@ hipError_t launch_distill(const zf_distill_args &a, const LossGrad &g, hipStream
     Args A = common(a.r, g);
     A.K = a.n_listed; A.ids = a.ids; A.id_bytes = a.id_bytes; A.values = a.values; A.values_dtype = a.values_dtype; A.rest = a.rest;
     if (a.r.rows) rows_of<DISTILL, false>(A, s);
-    if (A.results) total(a.r, a.r.rows, s);
+    if (A.results && a.r.rows != 1) total(a.r, a.r.rows, s);
     return hipGetLastError();
 }
 
@@ -1059,7 +1064,7 @@ hipError_t launch_policy(const zf_policy_args &a, const LossGrad &g, hipStream_t
     A.lowest = 1.0 - a.clip_low; A.highest = 1.0 + a.clip_high; A.kl_weight = a.kl_weight; A.entropy_weight = a.entropy_weight;
     A.logprobs = a.logprobs; A.entropy = a.entropy;
     if (a.r.rows) { if (a.entropy) rows_of<POLICY, true>(A, s); else rows_of<POLICY, false>(A, s); }
-    if (A.results) total(a.r, a.r.rows, s);
+    if (A.results && a.r.rows != 1) total(a.r, a.r.rows, s);
     return hipGetLastError();
 }
 

@@ -594,6 +594,16 @@ def test_no_rows():
 
 
 @gpu
+def test_one_row_with_a_weight():
+    """The sum of a single row's call is made by the row itself."""
+    for t in (3, -1):
+        x = torch.randn((1, 50), generator=torch.Generator().manual_seed(2)).cuda()
+        w, one = torch.tensor([0.37], device="cuda"), torch.ones((1,), device="cuda")
+        for got in (zf.policy_loss(x, torch.tensor([t], device="cuda"), one, one, entropy_weight=0.3, weight=w), zf.distill_loss(x, torch.tensor([[t, 4]], device="cuda") if t > 0 else torch.tensor([[-1, -1]], device="cuda"), torch.zeros((1, 2), device="cuda"), weight=w)):
+            assert float(got.loss) == float(torch.tensor(float(w.double()[0] * got.losses.double()[0]), dtype=torch.float64).float()) and (t > 0) == (float(got.loss) != 0)
+
+
+@gpu
 def test_rows_far_apart():
     """Rows 2^30 elements apart: the third begins beyond what 31 bits count."""
     r = Rows(3, 5000, "bf16", "share", 1.0, 9)
