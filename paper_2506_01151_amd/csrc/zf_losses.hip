@@ -443,7 +443,7 @@ __device__ __forceinline__ u32x4 grad_of(const u32x4 &raw, const Slope &s, float
 // Where factors are not finite, or near it -- 0 times them is not 0, and what is forbidden is to have 0 --, and where K would lose too much.
 template <bool ENT, typename ElemT>
 __device__ __forceinline__ bool wild(const Ends &e, float c) {
-    return !(fabsf(e.base) + 2e4f * fabsf(e.slope) < INFINITY) || (sizeof(ElemT) == 2 && !ENT && !(fabsf(e.m * c) < 4096.0f));
+    return !(fabsf(e.base) + 2e4f * fabsf(e.slope) < INFINITY) || (sizeof(ElemT) == 2 && !ENT && e.base != 0.0f && !(fabsf(e.m * c) < 4096.0f));      // (of 0 K is infinite, and all d are 0)
 }
 template <bool ENT, int EPV>
 __device__ __forceinline__ void grad_of_wild(const float (&x)[EPV], const Ends &ends, float c, float (&d)[EPV]) {
@@ -459,18 +459,28 @@ __device__ __forceinline__ void store_zeros(const int TH, ElemT *grad, int32_t V
     if ((int)threadIdx.x < V % EPV) store_element(grad + V - V % EPV + threadIdx.x, 0.0f);
 }
 
+template <bool ENT, int EPV, typename ElemT>
+__device__ __forceinline__ u32x4 wild_grad_of(const u32x4 &raw, const Ends &ends, float c) {
+    float x[EPV], d[EPV];
+    numbers<EPV, ElemT>(raw, x);
+    grad_of_wild<ENT>(x, ends, c, d);
+    union { u32x4 v; bf16x2 b[4]; } o;
+#pragma unroll
+    for (int k = 0; k < EPV; k += 2) {
+        if (EPV == 4) { o.v[k % 4] = __float_as_uint(d[k]); o.v[k % 4 + 1] = __float_as_uint(d[k + 1]); }
+        else o.b[k / 2 % 4] = bf16x2{(__bf16)d[k], (__bf16)d[k + 1]};
+    }
+    return o.v;
+}
 // A row's gradient, from memory, where wild() says so.
 template <bool ENT, int EPV, typename ElemT>
 __device__ __forceinline__ void wild_row(const int TH, const ElemT *logits, const uint32_t *mask, ElemT *grad, int32_t V, const Ends &ends, float c) {
     for (int32_t j = threadIdx.x; j < V / EPV; j += TH) {
-        const uint32_t bits = bits_of<EPV>(mask, (int64_t)j * EPV);
-        for (int k = 0; k < EPV; k++) {
-            const int32_t v = j * EPV + k;
-            const float x[1] = {(bits >> k) & 1u ? of_bits(logits[v]) : -INFINITY};
-            float d[1];
-            grad_of_wild<ENT>(x, ends, c, d);
-            store_element(grad + v, d[0]);
-        }
+        const uint32_t bits[1] = {bits_of<EPV>(mask, (int64_t)j * EPV)};
+        u32x4 raw[1];
+        load_pieces<1, EPV>(TH, logits + (int64_t)j * EPV, bits, false, raw);
+        forbid<EPV, ElemT>(raw[0], bits[0]);
+        store_raw<ElemT>(grad + (int64_t)j * EPV, wild_grad_of<ENT, EPV, ElemT>(raw[0], ends, c), false);
     }
 }
 
@@ -962,18 +972,7 @@ __global__ __launch_bounds__(TH) void preference_grad_kernel(const zf_preference
         if (__any(bits[u] != 0)) {
             if (__any(bits[u] != FULL)) forbid<EPV, ElemT>(raw[u], bits[u]);
             if (!all) d = grad_of<false, EPV, ElemT>(raw[u], slope, c);
-            else {
-                union { u32x4 v; bf16x2 b[4]; } o;
-                float x[EPV], e[EPV];
-                numbers<EPV, ElemT>(raw[u], x);
-                grad_of_wild<false>(x, ends, c, e);
-#pragma unroll
-                for (int k = 0; k < EPV; k += 2) {
-                    if (EPV == 4) { o.v[k % 4] = __float_as_uint(e[k]); o.v[k % 4 + 1] = __float_as_uint(e[k + 1]); }
-                    else o.b[k / 2 % 4] = bf16x2{(__bf16)e[k], (__bf16)e[k + 1]};
-                }
-                d = o.v;
-            }
+            else d = wild_grad_of<false, EPV, ElemT>(raw[u], ends, c);
         }
         if (j + u * TH < n_pieces) store_raw<ElemT>(grad + (int64_t)(j + u * TH) * EPV, d, once);
     }

@@ -85,7 +85,10 @@ int call_back(int kind, const Inputs &in, const Numbers &n, const Results &r, co
     const auto a = preference_args(in, n, r);
     return L.preference_back(&a, g, grad, V, device, s);
 }
-bool capturing() { return c10::hip::currentStreamCaptureStatusMayInitCtx() != c10::hip::CaptureStatus::None; }
+bool capturing(const Tensor &with) {
+    hipStreamCaptureStatus status = hipStreamCaptureStatusNone;
+    return hipStreamIsCapturing((hipStream_t)stream_of(with), &status) != hipSuccess || status != hipStreamCaptureStatusNone;
+}
 
 // What a backward pass is given beside what was saved: shapes as they were.
 struct Shapes : torch::CustomClassHolder {
@@ -107,7 +110,7 @@ struct LossOf : public torch::autograd::Function<LossOf> {
         like->offsets = kind == PREFERENCE ? in.offsets.size(0) : 0;
         like->value_type = kind == DISTILL ? in.values.scalar_type() : at::kFloat;
         like->offset_type = kind == PREFERENCE ? in.offsets.scalar_type() : at::kLong;
-        if (kind != PREFERENCE && !capturing()) like->held = fresh(logits.sizes(), logits.scalar_type(), logits);
+        if (kind != PREFERENCE && !capturing(logits)) like->held = fresh(logits.sizes(), logits.scalar_type(), logits);
         must(call((int)kind, in, n, r, like->held.defined() ? like->held.data_ptr() : nullptr));
         ctx->save_for_backward({logits, in.mask, in.weight, in.ids, in.values, in.old_logprobs, in.advantages, in.ref, in.offsets, r.stats, r.slopes});
         ctx->saved_data["shapes"] = c10::IValue::make_capsule(std::move(like));
@@ -146,7 +149,7 @@ struct LossOf : public torch::autograd::Function<LossOf> {
         // The gradient for a factor of one is handed out once: whoever has it may write it.  What a capture records may run again under another factor.
         Tensor grad;
         bool held = false;
-        if (!capturing()) { grad = std::move(like->held); like->held.reset(); held = grad.defined(); }
+        if (!capturing(in.logits)) { grad = std::move(like->held); like->held.reset(); held = grad.defined(); }
         if (!held) grad = fresh(like->logits, like->dtype, in.logits);
         const int rc = call_back(kind, in, like->n, r, g.data_ptr<float>(), held, grad.data_ptr());
         TORCH_CHECK(rc == ZF_OK, "zapformat error ", rc, ": ", L.last_error());

@@ -8,7 +8,6 @@
 #include <ATen/TracerMode.h>
 #include <ATen/hip/EmptyTensor.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
-#include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPStream.h>
 #include <optional>
 #include <string>

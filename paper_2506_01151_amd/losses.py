@@ -65,8 +65,17 @@ def _ptr(t):
     return t.data_ptr() if t is not None else None
 
 
-def _capturing():
-    return torch.cuda.is_current_stream_capturing()
+def _capturing(device):
+    with torch.cuda.device(device):
+        return torch.cuda.is_current_stream_capturing()
+
+
+def _pop(held):
+    """What is in the list, taken out, or None: two backward passes at once get it once."""
+    try:
+        return held.pop()
+    except IndexError:
+        return None
 
 
 class _Loss:
@@ -177,7 +186,7 @@ class _LossOf(torch.autograd.Function):
     @staticmethod
     def forward(ctx, kind, o, names, *tensors):
         it = kind(dict(zip(names, tensors)), o)
-        held = it.grad() if kind.at_once and not _capturing() else None
+        held = it.grad() if kind.at_once and not _capturing(it.t["logits"].device) else None
         out = it.forward(held)
         ctx.save_for_backward(*tensors, *(out[n] for n in kind.saved))
         x = it.t["logits"]
@@ -206,7 +215,7 @@ class _LossOf(torch.autograd.Function):
                 t[n] = _kept(t[n], n, dtypes, shape, device)
         g = _kept(g.to(torch.float32), "gradient", _F32, (), device)
         # The gradient for g = 1 is handed out once: whoever has it may write it.  What a capture records may run again under another g.
-        held = ctx.held.pop() if ctx.held and not _capturing() else None
+        held = None if _capturing(device) else _pop(ctx.held)
         grad = held if held is not None else it.grad()
         out = it.outputs()
         out.update((n, t[n]) for n in ctx.kind.saved)

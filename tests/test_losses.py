@@ -583,6 +583,77 @@ def test_lowest_values_and_far_temperatures(dtype):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("T,by,offset", [(0.02, 3.0, 400.0), (1.0, 3000.0, -9000.0), (50.0, 1.0, 0.0)])
+def test_logits_far_from_zero(dtype, T, by, offset):
+    """Logits over temperature in the thousands, of either sign, where a gradient of bf16 takes another way: all three losses."""
+    r = Rows(9, 3001, dtype, "share", T, 20, sigma=by)
+    r.x = (r.x.float() + offset).to(r.x.dtype)
+    r.bits[:, 5:7] = True
+    r.update()
+    t = torch.where(r.at(torch.full((9,), 5))[1], r.x[:, :].float().masked_fill(~r.allowed, -INF).argmax(dim=1), -1)
+    lp, counts = r.at(t)
+    x, m = r.on_gpu()
+    x.requires_grad_()
+    old, adv = lp.float() + 0.05, torch.randn((9,), generator=r.g)
+    losses, bound, lp, H, H_off, grad, off = policy_want(r, t, old, adv, None, (0.2, 0.2), 0.0, None, None)
+    got = zf.policy_loss(x, t.cuda(), old.cuda(), adv.cuda(), m, temperature=T)
+    close(got.losses, losses, bound, "losses")
+    close(torch.autograd.grad(got.loss, x)[0], grad, off, "gradient", x.dtype)
+    listed, v = teacher(r, 4, 8, "f32", False, 3)
+    v = (v * (1.0 / by)).float()
+    losses, bound, grad, off = distill_want(r, listed, v, False, torch.ones(9), dtype)
+    got = zf.distill_loss(x, listed.cuda(), v.cuda(), m, temperature=T)
+    close(got.losses, losses, bound, "losses")
+    close(torch.autograd.grad(got.loss, x)[0], grad, off, "gradient", x.dtype)
+    offsets = torch.tensor([0, 3, 9])
+    losses, bound, chosen, rejected, D_off, grad, off = preference_want(r, t, offsets, old, 0.1, 0.0, False, None)
+    got = zf.preference_loss(x, t.cuda(), offsets.cuda(), old.cuda(), m, temperature=T)
+    close(got.losses, losses, bound, "losses")
+    close(torch.autograd.grad(got.loss, x)[0], grad, off, "gradient", x.dtype)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("rest", [False, True])
+@pytest.mark.parametrize("rows,V", [(5, 900), (300, 5000), (3, 170000)])
+def test_distill_all_that_is_allowed_is_listed(rows, V, rest, dtype):
+    r = Rows(rows, V, dtype, "few", 1.0, 21)
+    listed, v = teacher(r, 64, 4, "f32", rest, 22)
+    losses, bound, grad, off = distill_want(r, listed, v, rest, torch.ones(rows), dtype)
+    x, m = r.on_gpu()
+    x.requires_grad_()
+    got = zf.distill_loss(x, listed.cuda(), v.cuda(), m, rest=rest)
+    close(got.losses, losses, bound, "losses")
+    close(torch.autograd.grad(got.loss, x)[0], grad, off, "gradient", x.dtype)
+
+
+@gpu
+def test_two_backward_passes_at_once(by):
+    """Of one graph, by two threads: both gradients are whole, and neither is the other's memory."""
+    import threading
+    r = Rows(64, 9000, "f32", "none", 1.0, 23)
+    x, _ = r.on_gpu()
+    x.requires_grad_()
+    for i in range(3):
+        want, = torch.autograd.grad(three(x)[i].loss, x)
+        for _ in range(5):
+            got, out = three(x)[i], [None, None]
+            torch.cuda.synchronize()
+
+            def run(k):
+                out[k], = torch.autograd.grad(got.loss, x, retain_graph=True)
+
+            threads = [threading.Thread(target=run, args=(k,)) for k in range(2)]
+            for th in threads:
+                th.start()
+            for th in threads:
+                th.join()
+            torch.cuda.synchronize()
+            assert torch.equal(out[0], want) and torch.equal(out[1], want) and out[0].data_ptr() != out[1].data_ptr()
+
+
+@gpu
 def test_no_rows():
     x = torch.empty((0, 40), device="cuda", requires_grad=True)
     e = torch.empty((0,), device="cuda")
