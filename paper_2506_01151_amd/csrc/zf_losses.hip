@@ -489,7 +489,7 @@ __device__ __forceinline__ int writer_of(const int TH, int64_t v, int32_t V) { r
 
 // A row a workgroup, from memory: read for the sums, and again where its gradient is wanted.  For rows that do not fit a compute unit's registers, and calls without a gradient.
 template <int KIND, bool ENT, typename ElemT>
-__global__ __launch_bounds__(THREADS_MAX) void loss_rows_kernel(const Args A) {
+__global__ __launch_bounds__(THREADS_MAX, 8) void loss_rows_kernel(const Args A) {
     constexpr int EPV = 16 / sizeof(ElemT), U = 4;
     const int TH = blockDim.x, WAVES = TH / 64;
     constexpr uint32_t FULL = (1u << EPV) - 1u;
@@ -540,6 +540,10 @@ __global__ __launch_bounds__(THREADS_MAX) void loss_rows_kernel(const Args A) {
             if (LIST) __syncthreads();                     // before the lists are written again
             continue;
         }
+        auto ask_words = [&](int32_t j, uint32_t (&words)[U]) {              // the mask's words that pieces j, j + TH .. lie in, a batch ahead of them
+#pragma unroll
+            for (int u = 0; u < U; u++) words[u] = mask ? mask[min(((int64_t)j + u * TH) * EPV, (int64_t)V - 1) >> 5] : ~0u;
+        };
         Part mine{-FLT_MAX, 0.0f, 0.0f, 0.0f};
         for (int32_t from = 0; from < V; from += CHUNK) {  // (one turn, unless bits of listed tokens are wanted of more than CHUNK of them)
             const int32_t to = LIST ? min(V, from + CHUNK) : V;
@@ -557,16 +561,19 @@ __global__ __launch_bounds__(THREADS_MAX) void loss_rows_kernel(const Args A) {
                 }
                 __syncthreads();
             }
+            uint32_t words[U];
+            ask_words(from / EPV + tid, words);
             for (int32_t j = from / EPV + tid; j < to / EPV; j += U * TH) {
                 uint32_t bits[U];
                 u32x4 raw[U];
 #pragma unroll
                 for (int u = 0; u < U; u++) {
                     const int64_t v = (int64_t)(j + u * TH) * EPV;
-                    bits[u] = j + u * TH < to / EPV ? bits_of<EPV>(mask, v) : 0u;
+                    bits[u] = j + u * TH < to / EPV ? (words[u] >> (v & 31)) & FULL : 0u;
                     if (LIST && bits[u]) bits[u] &= ~(listed[(v - from) >> 5] >> (v & 31));
                 }
                 load_pieces<U, EPV>(TH, logits + (int64_t)j * EPV, bits, KIND == LOGPROB && A.once, raw);
+                ask_words(j + U * TH, words);
 #pragma unroll
                 for (int u = 0; u < U; u++) {
                     if (!__any(bits[u] != 0)) continue;
@@ -595,12 +602,15 @@ __global__ __launch_bounds__(THREADS_MAX) void loss_rows_kernel(const Args A) {
             const Slope slope(ends, A.c);
             const bool all = wild<ENT, ElemT>(ends, A.c);
             if (all) wild_row<ENT, EPV>(TH, logits, mask, grad, V, ends, A.c);
+            uint32_t words[U];
+            ask_words(tid, words);
             for (int32_t j = tid; j < n_pieces && !all; j += U * TH) {
                 uint32_t bits[U];
                 u32x4 raw[U];
 #pragma unroll
-                for (int u = 0; u < U; u++) bits[u] = j + u * TH < n_pieces ? bits_of<EPV>(mask, (int64_t)(j + u * TH) * EPV) : 0u;
+                for (int u = 0; u < U; u++) bits[u] = j + u * TH < n_pieces ? (words[u] >> ((j + u * TH) * EPV & 31)) & FULL : 0u;
                 load_pieces<U, EPV>(TH, logits + (int64_t)j * EPV, bits, A.once, raw);
+                ask_words(j + U * TH, words);
 #pragma unroll
                 for (int u = 0; u < U; u++) {
                     u32x4 d{0, 0, 0, 0};
@@ -1017,7 +1027,9 @@ void rows_by(const Args &A, int threads, hipStream_t s) {
             return;
         }
     }
-    hipLaunchKernelGGL((loss_rows_kernel<KIND, ENT, ElemT>), dim3(grid_of(A.r.rows)), dim3(threads), lds, s, A);
+    // Rows that are read twice should still be in the last-level cache the second time: without masks one a compute unit (608 KB each, 256 MB of cache).
+    const int64_t most = A.grad && !A.r.mask ? COMPUTE_UNITS : 1 << 16;
+    hipLaunchKernelGGL((loss_rows_kernel<KIND, ENT, ElemT>), dim3((int)std::min(A.r.rows, most)), dim3(threads), lds, s, A);
 }
 template <int KIND, bool ENT, typename ElemT>
 void rows_of(const Args &A, hipStream_t s) {
