@@ -360,7 +360,8 @@ int zf_policy_loss_backward(const zf_policy_args *a, const float *d_g, int32_t h
 /* Paired sequences.  Sequence s has the rows offsets[s] .. offsets[s + 1] - 1; of pair i sequence 2 i is the preferred one, 2 i + 1 the other.  D_s = sum of lp - ref_logprobs over the
  * sequence's rows whose token is not negative (with `average` their mean; 0 where there are none), chosen = beta D_2i, rejected = beta D_2i+1, h = chosen - rejected:
  *   losses = - (1 - label_smoothing) ln sigma(h) - label_smoothing ln sigma(-h)
- * Rows of no sequence and of negative tokens have no gradient.  A token that is not allowed: log probability -inf, no gradient.  A pair whose offsets descend or leave 0 .. rows: NaN.
+ * Rows of no sequence and of negative tokens have no gradient.  A token that is not allowed: log probability -inf, no gradient.  A pair whose offsets descend or
+ * leave 0 .. rows, or of whose rows another sequence has one too: NaN.
  * stats and slopes are what the gradient is made from (written by the first call). */
 typedef struct {
     zf_loss_rows r;

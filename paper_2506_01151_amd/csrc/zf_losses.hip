@@ -146,8 +146,9 @@ __device__ __forceinline__ uint32_t bits_of(const uint32_t *mask_row, int64_t v)
 struct Head {
     int64_t t;                                 // the given token
     float x, weight, old_logprob, advantage, ref;          // its logit, -inf where it is not allowed
-    int32_t sequence;                          // of preferences: the row's
+    int32_t sequence;                          // of preferences: the row's; PADDING, or NOWHERE: it has a token and no sequence
 };
+static const int32_t PADDING = -1, NOWHERE = -2;
 // What a policy's loss makes of a row, by every lane of a wavefront alike.  Returns the row's loss.
 __device__ __forceinline__ double policy_row(const Args &A, const Part &sum, const Head &h, float wg, Ends *ends, float *logprob, float *entropy) {
     const double lnS = log((double)sum.S);
@@ -354,11 +355,11 @@ __device__ __forceinline__ void ask_token(const Args &A, const ElemT *logits, co
     if (h.t >= 0 && h.t < A.r.V && (!mask || ((alike(mask + (h.t >> 5)) >> (h.t & 31)) & 1u))) h.x = logit_alike(logits + h.t);
 }
 template <int KIND, bool ENT>
-__device__ __forceinline__ void no_row(const Args &A, int64_t row) {       // by one thread: a row that is padding
+__device__ __forceinline__ void no_row(const Args &A, int64_t row, bool padding = true) {       // by one thread: a row that does not count
     if (!A.results) return;
     if (KIND != LOGPROB) store_loss(A, row, 0.0f, 0.0f);
     if (KIND == POLICY) A.logprobs[row] = 0.0f;
-    if (KIND == LOGPROB) A.found[row] = float4{0.0f, 0.0f, 0.0f, __int_as_float(-1)};
+    if (KIND == LOGPROB) A.found[row] = float4{0.0f, 0.0f, 0.0f, __int_as_float(padding ? PADDING : NOWHERE)};
     if (ENT) A.entropy[row] = 0.0f;
 }
 // By one wavefront: what the sums over a row lead to.
@@ -535,7 +536,7 @@ __global__ __launch_bounds__(THREADS_MAX, 8) void loss_rows_kernel(const Args A)
             ask_token(A, logits, mask, h);
         }
         if (!looked) {                                     // (alike in the whole workgroup)
-            if (tid == 0) no_row<KIND, ENT>(A, row);
+            if (tid == 0) no_row<KIND, ENT>(A, row, h.t < 0);
             if (A.grad) store_zeros<EPV>(TH, grad, V, A.once);
             if (LIST) __syncthreads();                     // before the lists are written again
             continue;
@@ -917,18 +918,22 @@ __global__ __launch_bounds__(PAIRS * 128) void pairs_kernel(const zf_preference_
             fits = 0 <= o0 && o0 <= o1 && o1 <= o2 && o2 <= p.r.rows;
             const int64_t begin = wave % 2 ? o1 : o0, end = fits ? (wave % 2 ? o2 : o1) : begin;
             double sum = 0.0, n = 0.0;
+            bool shared = false;                           // the offsets say that a row is in this sequence, and the row was found in another or in none: they descend elsewhere
             for (int64_t row = begin + lane; row < end; row += 64) {
                 const float4 f = found[row];
-                if (__float_as_int(f.w) < 0) continue;     // padding
+                if (__float_as_int(f.w) == PADDING) continue;
+                shared |= __float_as_int(f.w) != 2 * pair + wave % 2;
                 sum += p.ref_logprobs ? (double)f.z - p.ref_logprobs[row] : (double)f.z;
                 n += 1.0;
             }
             sum = wave_sum(sum);
             n = wave_sum(n);
+            if (__any(shared)) n = -1.0;
             if (lane == 0) { sums[wave] = sum; counts[wave] = n; }
         }
         __syncthreads();
         if (pair < p.pairs && wave % 2 == 0 && lane == 0) {
+            fits = fits && counts[wave] >= 0.0 && counts[wave + 1] >= 0.0;
             double chosen = sums[wave], rejected = sums[wave + 1], n0 = 1.0, n1 = 1.0;
             if (p.average) { n0 = fmax(counts[wave], 1.0); n1 = fmax(counts[wave + 1], 1.0); }
             chosen *= p.beta / n0;
@@ -1018,7 +1023,8 @@ void rows_by(const Args &A, int threads, hipStream_t s) {
     const int lds = KIND == DISTILL ? entries_bytes(A.K) : 0;
     if constexpr (KIND != LOGPROB && NP > 0) {
         if (A.grad && A.r.V >= 16 / (int)sizeof(ElemT)) {
-            const dim3 grid((int)std::min<int64_t>(A.r.rows, THREADS_MAX / threads * COMPUTE_UNITS));
+            const int64_t most = THREADS_MAX / threads * COMPUTE_UNITS, turns = (A.r.rows + most - 1) / most;
+            const dim3 grid((int)((A.r.rows + turns - 1) / turns));
             const bool aligned = whole(A.r, A.r.logits, A.r.row_stride_elems);
             const int words = own_words_of(NP, 16 / (int)sizeof(ElemT)) * threads * 4;
             auto launch = [&](auto *kernel, int bytes) { hipLaunchKernelGGL(kernel, grid, dim3(threads), bytes, s, A); };

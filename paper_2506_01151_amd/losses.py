@@ -291,7 +291,7 @@ def preference_loss(logits, tokens, offsets, ref_logprobs=None, mask=None, *, be
 
     offsets: int32 or int64 [2 pairs + 1]: sequence s has the rows offsets[s] up to offsets[s + 1]; of each pair the preferred one comes first.  tokens: int32 or int64 [rows], ref_logprobs:
     fp32 [rows]; weight: fp32 [pairs].  Negative tokens (prompts) and rows of no sequence are passed over.  A token that is not allowed: log probability -inf, no gradient of its
-    own.  Offsets that descend or leave the rows: NaN for their pair."""
+    own.  Offsets that descend or leave the rows, or give a row to two sequences: NaN for their pair."""
     got = _native_losses.preference_loss(logits, tokens, offsets, ref_logprobs, mask, beta, label_smoothing, bool(average), temperature, weight)
     if got is not None:
         return PreferenceLoss(*got)

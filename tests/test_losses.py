@@ -481,15 +481,31 @@ def test_preference_of_tokens_that_are_not_allowed():
 
 
 @gpu
-@pytest.mark.parametrize("offsets", [[0, 5, 3, 6, 8], [0, 2, 4, 6, 9], [-1, 2, 4, 6, 8], [0, 2 ** 40, 4, 6, 8]])
-def test_preference_offsets_that_do_not_fit(offsets):
+@pytest.mark.parametrize("offsets,bad", [([0, 5, 3, 6, 8], [True, True]), ([0, 2, 4, 6, 9], [False, True]), ([-1, 2, 4, 6, 8], [True, False]), ([0, 2 ** 40, 4, 6, 8], [True, True])])
+def test_preference_offsets_that_do_not_fit(offsets, bad):
     x = torch.randn((8, 30), generator=torch.Generator().manual_seed(4)).cuda().requires_grad_()
     t = torch.arange(8, device="cuda")
     got = zf.preference_loss(x, t, torch.tensor(offsets, device="cuda"))
-    bad = [not (0 <= a <= b <= c <= 8) for a, b, c in zip(offsets[0::2], offsets[1::2], offsets[2::2])]
     assert torch.isnan(got.losses).tolist() == bad and torch.isnan(got.chosen).tolist() == bad
     g, = torch.autograd.grad(got.loss, x)
     assert g.shape == x.shape
+
+
+@gpu
+@pytest.mark.parametrize("offsets,may_be", [([0, 5, 3, 6, 8], [1]), ([4, 8, 2, 3, 6, 7, 8], [1, 2]), ([0, 4, 8, 0, 8], [0]), (list(range(0, 130)) + [5, 9, 130], list(range(0, 64)))])
+def test_preference_offsets_that_overlap(offsets, may_be):
+    """A pair is either right, as it is alone, or NaN: a row that the offsets give to two sequences is not left out without a word."""
+    n = max(offsets) + 1
+    x = torch.randn((n, 30), generator=torch.Generator().manual_seed(4)).cuda()
+    t = torch.arange(n, device="cuda") % 30
+    got = zf.preference_loss(x, t, torch.tensor(offsets, device="cuda"))
+    nan = torch.isnan(got.losses).tolist()
+    assert nan == torch.isnan(got.chosen).tolist() == torch.isnan(got.rejected).tolist()
+    for i, (a, b, c) in enumerate(zip(offsets[0::2], offsets[1::2], offsets[2::2])):
+        assert nan[i] or (i in may_be and a <= b <= c)
+        if not nan[i]:
+            alone = zf.preference_loss(x, t, torch.tensor([a, b, c], device="cuda"))
+            assert float(got.losses[i]) == float(alone.losses[0]) and float(got.chosen[i]) == float(alone.chosen[0])
 
 
 # ---- what rows can hold -----------------------------------------------------------------------------
