@@ -64,11 +64,6 @@ __device__ __forceinline__ double wave_max(double x) {
 // asked for and written before it be waited for.
 #define CONSTANT __attribute__((address_space(4)))
 template <typename T> __device__ __forceinline__ T alike(const T *p) { return *(const CONSTANT T *)(uintptr_t)p; }
-__device__ __forceinline__ float logit_alike(const uint32_t *p) { return of_bits(alike(p)); }
-__device__ __forceinline__ float logit_alike(const uint16_t *p) {        // (of the four bytes that hold it)
-    const uintptr_t at = (uintptr_t)p;
-    return of_bits((uint16_t)(alike((const uint32_t *)(at & ~(uintptr_t)3)) >> (at & 2 ? 16 : 0)));
-}
 __device__ __forceinline__ int64_t token_at(const Args &A, int64_t row) { return A.id_bytes == 8 ? alike((const int64_t *)A.ids + row) : alike((const int32_t *)A.ids + row); }
 __device__ __forceinline__ int64_t id_at(const Args &A, int64_t i) { return A.id_bytes == 8 ? ((const int64_t *)A.ids)[i] : ((const int32_t *)A.ids)[i]; }
 __device__ __forceinline__ bool allowed(const uint32_t *mask_row, int64_t v) { return !mask_row || ((mask_row[v >> 5] >> (v & 31)) & 1u); }
@@ -146,6 +141,7 @@ __device__ __forceinline__ uint32_t bits_of(const uint32_t *mask_row, int64_t v)
 struct Head {
     int64_t t;                                 // the given token
     float x, weight, old_logprob, advantage, ref;          // its logit, -inf where it is not allowed
+    uint32_t raw, word, shift;                 // the four bytes that hold the logit, and where; of the mask
     int32_t sequence;                          // of preferences: the row's; PADDING, or NOWHERE: it has a token and no sequence
 };
 static const int32_t PADDING = -1, NOWHERE = -2;
@@ -259,9 +255,14 @@ __device__ __forceinline__ void sum_entries(const Args &A, int wave, int lane, c
     const Teacher t{wave_sum(e), wave_sum(mixed), wave_sum(S), v_most, x_most, __any(counts), 0.0};
     if (lane == 0) E.part[wave] = t;
 }
+__device__ __forceinline__ double from_lane(double x, int lane) {
+    const uint64_t b = __double_as_longlong(x);
+    return __longlong_as_double((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, lane) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), lane) << 32);
+}
 // A row's end, from the sums over what is not listed; by every lane of one wavefront alike.  Returns the row's loss.
 __device__ __forceinline__ double distill_row(const Args &A, const Part &sum, float wg, const Entries &E, Ends *ends) {
     const double T = A.r.temperature;
+    const int lane = threadIdx.x % 64;
     Teacher t{0.0, 0.0, 0.0, -INFINITY, -INFINITY, 0, 0.0};
     for (int w = 0; w < (A.K + 63) / 64; w++) {
         const Teacher u = E.part[w];
@@ -281,22 +282,26 @@ __device__ __forceinline__ double distill_row(const Args &A, const Part &sum, fl
     const float x_most = none ? t.x_most : fmaxf(t.x_most, sum.m);
     auto power = [](double ln) { return ln == 0.0 ? 1.0 : exp(ln); };
     const double S_rest = sum.S, down = none ? 0.0 : ((double)sum.m - x_most) / T, listed_down = t.some ? ((double)t.x_most - x_most) / T : 0.0;
-    const double rest_to_S = power(down), S = S_rest * rest_to_S + t.S * power(listed_down), lnS = log(S);
-    const double share = A.rest ? 1.0 : t.total == 0.0 ? 0.0 : 1.0 / t.total;
+    const double rest_to_S = power(down), S = S_rest * rest_to_S + t.S * power(listed_down);
+    double q_rest = A.rest ? fmax(1.0 - t.total, 0.0) : 0.0;
+    if (t.total != t.total) q_rest = NAN;
+    if (none) q_rest = 0.0;
+    // The whole workgroup waits here: lanes 0 to 3 take a logarithm and a reciprocal each at once, of S, S_R, sum e and q_R.
+    const double of = lane == 0 ? S : lane == 1 ? S_rest : lane == 2 ? t.total : q_rest, ln = log(of), once = 1.0 / of;
+    const double lnS = from_lane(ln, 0), by_S = from_lane(once, 0), by_rest = from_lane(once, 1);
+    const double share = A.rest ? 1.0 : t.total == 0.0 ? 0.0 : from_lane(once, 2);
     double all = t.total * share;                          // sum of q
-    double loss = t.total == 0.0 ? 0.0 : (A.rest ? t.mixed : t.mixed * share - log(t.total)) + all * (lnS - listed_down);
-    double q_rest = A.rest ? 1.0 - all : 0.0;
-    if (q_rest < 0.0 || none) q_rest = 0.0;
-    if (q_rest != 0.0) loss += q_rest * (log(q_rest) - (log(S_rest) + down - lnS));        // (ln p_R, also where p_R is 0 in 64 bits)
+    double loss = t.total == 0.0 ? 0.0 : (A.rest ? t.mixed : t.mixed * share - from_lane(ln, 2)) + all * (lnS - listed_down);
+    if (q_rest != 0.0) loss += q_rest * (from_lane(ln, 3) - (from_lane(ln, 1) + down - lnS));        // (ln p_R, also where p_R is 0 in 64 bits)
     const bool nan = (E.end->flags & 2u) || S != S;
     all += q_rest;
     const double scale = (double)wg / T;
     ends->m = sum.m;
-    ends->base = nan ? NAN : none ? 0.0f : (float)(scale * (all * rest_to_S / S - q_rest / S_rest));
+    ends->base = nan ? NAN : none ? 0.0f : (float)(scale * (all * rest_to_S * by_S - q_rest * by_rest));
     ends->slope = 0.0f;
     ends->at_token = 0.0f;
     E.end->x_most = x_most;
-    E.end->to_listed = nan ? NAN : (float)(scale * all / S);
+    E.end->to_listed = nan ? NAN : (float)(scale * all * by_S);
     for (int w = 0; w < (A.K + 63) / 64; w++) E.part[w].to_shares = scale * share * (A.rest || !E.part[w].some ? 1.0 : power((E.part[w].v_most - t.v_most) / T));
     return nan ? NAN : loss;
 }
@@ -349,10 +354,19 @@ __device__ __forceinline__ void ask_head(const Args &A, int64_t row, Head &h) {
         h.ref = A.ref ? alike(A.ref + row) : 0.0f;
     }
 }
+// The token's logit and its word of the mask, whether they will be wanted or not: neither waits for the other.
 template <typename ElemT>
 __device__ __forceinline__ void ask_token(const Args &A, const ElemT *logits, const uint32_t *mask, Head &h) {
-    h.x = -INFINITY;
-    if (h.t >= 0 && h.t < A.r.V && (!mask || ((alike(mask + (h.t >> 5)) >> (h.t & 31)) & 1u))) h.x = logit_alike(logits + h.t);
+    const int64_t at = h.t < 0 ? 0 : h.t < A.r.V ? h.t : A.r.V - 1;
+    const uintptr_t place = (uintptr_t)(logits + at);
+    h.raw = alike((const uint32_t *)(place & ~(uintptr_t)3));
+    h.shift = sizeof(ElemT) == 4 ? 0 : place & 2 ? 0 : 16;
+    h.word = mask ? alike(mask + (at >> 5)) : ~0u;
+}
+template <typename ElemT>
+__device__ __forceinline__ void see_token(const Args &A, Head &h) {
+    const uint32_t bits = h.raw << h.shift;
+    h.x = h.t >= 0 && h.t < A.r.V && ((h.word >> (h.t & 31)) & 1u) ? of_bits(sizeof(ElemT) == 4 ? bits : bits & 0xFFFF0000u) : -INFINITY;
 }
 template <int KIND, bool ENT>
 __device__ __forceinline__ void no_row(const Args &A, int64_t row, bool padding = true) {       // by one thread: a row that does not count
@@ -516,7 +530,7 @@ __global__ __launch_bounds__(THREADS_MAX, 8) void loss_rows_kernel(const Args A)
         const ElemT *const logits = (const ElemT *)A.r.logits + row * A.r.row_stride_elems;
         const uint32_t *const mask = A.r.mask ? A.r.mask + row * A.W : nullptr;
         ElemT *const grad = (ElemT *)A.grad + row * A.grad_stride;
-        Head h{-1, -INFINITY, 1.0f, 0.0f, 0.0f, 0.0f, -1};
+        Head h{-1, -INFINITY, 1.0f, 0.0f, 0.0f, 0.0f, 0, 0, 0, PADDING};
         ask_head<KIND>(A, row, h);
         const float wg = h.weight * g;
         bool looked;                                       // the row is read
@@ -534,6 +548,7 @@ __global__ __launch_bounds__(THREADS_MAX, 8) void loss_rows_kernel(const Args A)
             if (KIND == LOGPROB && h.t >= 0) h.sequence = sequence_of(A, row, lane);
             looked = h.t >= 0 && (KIND != LOGPROB || h.sequence >= 0);
             ask_token(A, logits, mask, h);
+            see_token<ElemT>(A, h);
         }
         if (!looked) {                                     // (alike in the whole workgroup)
             if (tid == 0) no_row<KIND, ENT>(A, row, h.t < 0);
@@ -756,13 +771,14 @@ __global__ __launch_bounds__(THREADS_MAX, 4) void loss_resident_kernel(const Arg
     const int size = LIST ? entries_bytes(A.K) : 0;
     int64_t row = blockIdx.x;
     int turn = 0;
-    Head head{-1, -INFINITY, 1.0f, 0.0f, 0.0f, 0.0f, -1}, next_head = head;
+    Head head{-1, -INFINITY, 1.0f, 0.0f, 0.0f, 0.0f, 0, 0, 0, PADDING}, next_head = head;
     bool counts;
     // The first row
     ask_head<KIND>(A, row, head);
     if (!LIST) {
         head.t = token_at(A, row);
         ask_token(A, logits_of(row), mask_of(row), head);
+        see_token<ElemT>(A, head);
         counts = head.t >= 0;
     }
     if (MASKED) {
@@ -806,10 +822,6 @@ __global__ __launch_bounds__(THREADS_MAX, 4) void loss_resident_kernel(const Arg
         const int64_t next = row + gridDim.x;
         const bool more = next < A.r.rows;
         ElemT *const grad = (ElemT *)A.grad + row * A.grad_stride;
-        if (more) {
-            ask_head<KIND>(A, next, next_head);
-            if (!LIST) ask_token(A, logits_of(next), mask_of(next), next_head);
-        }
         live = next_live;
         next_live = 0;
         mine = join_wave(mine, A.c);
@@ -821,7 +833,8 @@ __global__ __launch_bounds__(THREADS_MAX, 4) void loss_resident_kernel(const Arg
             __syncthreads();
             if (more) list_row(next, next_E);
         }
-        if (wave == 0) {
+        // (A teacher's entries are listed by the first wavefronts at the same time: with what comes in the loop's middle 4,096 x 128,256 bf16 with 64 listed 479 -> 451 us.)
+        if (wave == (LIST ? WAVES - 1 : 0)) {
             if (counts) finish_row<KIND, ENT>(A, join_wave(lane < WAVES ? part[lane] : Part{-FLT_MAX, 0.0f, 0.0f, 0.0f}, A.c), row, head, head.weight * g, lane, E, shared_ends);
             else if (lane == 0) no_row<KIND, ENT>(A, row);
         }
@@ -835,7 +848,7 @@ __global__ __launch_bounds__(THREADS_MAX, 4) void loss_resident_kernel(const Arg
             ask_entry_logit(next + gridDim.x, ahead);
             ask_entry(next + 2 * (int64_t)gridDim.x, after);
         }
-        const int64_t next_t = !LIST && next + gridDim.x < A.r.rows ? token_at(A, next + gridDim.x) : -1;
+        int64_t next_t = -1;
         const bool third = next + gridDim.x < A.r.rows;    // there is a row after the next
         const ElemT *const next_logits = logits_of(next_counts ? next : row), *const third_logits = logits_of(third ? next + gridDim.x : row);
         mine = Part{-FLT_MAX, 0.0f, 0.0f, 0.0f};
@@ -843,6 +856,19 @@ __global__ __launch_bounds__(THREADS_MAX, 4) void loss_resident_kernel(const Arg
         fetch_last(next_logits);
 #pragma unroll
         for (int i = 0; i < NP + LAG; i++) {
+            // What is alike in the workgroup comes in the loop's middle, while there is much on its way: at a row's end everything would wait for it.  (Never read beyond the rows.)
+            if (i == NP / 2) {
+                ask_head<KIND>(A, more ? next : row, next_head);
+                if (!LIST) {
+                    ask_token(A, logits_of(more ? next : row), mask_of(more ? next : row), next_head);
+                    next_t = token_at(A, third ? next + gridDim.x : row);
+                }
+            }
+            if (i == NP - 2) {                             // (and is there before the loop ends)
+                if (!LIST) asm volatile("" : "+s"(next_head.raw), "+s"(next_head.word), "+s"(next_t));
+                if (KIND == POLICY) asm volatile("" : "+s"(next_head.old_logprob), "+s"(next_head.advantage), "+s"(next_head.ref));
+                asm volatile("" : "+s"(next_head.weight));
+            }
             if (MASKED && i == NP - EARLY - 2) read_words(third ? next + gridDim.x : row);     // (here, so that they are there when the loop is done)
             if (i < NP && (i < NP - SPARE || i * TH < n_pieces)) {
                 u32x4 d{0, 0, 0, 0};
@@ -879,6 +905,7 @@ __global__ __launch_bounds__(THREADS_MAX, 4) void loss_resident_kernel(const Arg
         turn ^= 1;
         counts = next_counts;
         head = next_head;
+        if (!LIST) see_token<ElemT>(A, head);
         next_head.t = next_t;
     }
 }
@@ -1023,8 +1050,10 @@ void rows_by(const Args &A, int threads, hipStream_t s) {
     const int lds = KIND == DISTILL ? entries_bytes(A.K) : 0;
     if constexpr (KIND != LOGPROB && NP > 0) {
         if (A.grad && A.r.V >= 16 / (int)sizeof(ElemT)) {
-            const int64_t most = THREADS_MAX / threads * COMPUTE_UNITS, turns = (A.r.rows + most - 1) / most;
-            const dim3 grid((int)((A.r.rows + turns - 1) / turns));
+            // Where a workgroup has a compute unit to itself all take the same number of rows, on fewer compute units: the others' share of the memory is worth more than their time
+            // (600 x 128,256 bf16 77.5 -> 73.3 us, 300 under masks 56.8 -> 54.1); of several on one some are done early either way (1,030 x 40,037 61 -> 63).
+            const int64_t most = THREADS_MAX / threads * COMPUTE_UNITS, turns = most == COMPUTE_UNITS ? (A.r.rows + most - 1) / most : 1;
+            const dim3 grid((int)std::min(most, (A.r.rows + turns - 1) / turns));
             const bool aligned = whole(A.r, A.r.logits, A.r.row_stride_elems);
             const int words = own_words_of(NP, 16 / (int)sizeof(ElemT)) * threads * 4;
             auto launch = [&](auto *kernel, int bytes) { hipLaunchKernelGGL(kernel, grid, dim3(threads), bytes, s, A); };
