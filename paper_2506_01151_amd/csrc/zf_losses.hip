@@ -664,9 +664,10 @@ __global__ __launch_bounds__(THREADS_MAX, 8) void loss_rows_kernel(const Args A)
 // A row a workgroup, held in registers between its sums and its gradient: NP pieces of 16 bytes a thread.  Workgroups stay.  As soon as the gradient of a piece is on
 // the way its registers take the next row's piece, which is added to that row's sums LAG pieces later: memory is asked for, written and waited for all along the
 // arithmetic of both.  A row's mask lies in LDS, without the tokens that a teacher listed: their sums and their gradient are taken from the list.
-template <int NP, int KIND, bool MASKED, bool ENT, bool ALIGNED, typename ElemT>
+// PASS: 1: rows begin at multiples of 16 bytes, 2: and the gradient passes the cache by (Args::once; a branch for it at each store would have the compiler wait for stores with the loads).
+template <int NP, int KIND, bool MASKED, bool ENT, int PASS, typename ElemT>
 __global__ __launch_bounds__(THREADS_MAX, 4) void loss_resident_kernel(const Args A) {
-    constexpr int EPV = 16 / sizeof(ElemT), OWN_WORDS = own_words_of(NP, EPV), LAG = 4, EARLY = early_of(NP), SPARE = 3;
+    constexpr int EPV = 16 / sizeof(ElemT), OWN_WORDS = own_words_of(NP, EPV), LAG = 4, EARLY = early_of(NP), SPARE = NP == 16 ? 0 : 3;
     const int TH = blockDim.x, WAVES = TH / 64;
     constexpr uint32_t FULL = (1u << EPV) - 1u;
     constexpr bool LIST = KIND == DISTILL;
@@ -701,6 +702,8 @@ __global__ __launch_bounds__(THREADS_MAX, 4) void loss_resident_kernel(const Arg
 #pragma unroll
         for (int i = 0; i < OWN_WORDS; i++) bits_lds[tid + i * TH] = own_words[i];
     };
+    // The last SPARE pieces may be none of the row's and are left out then; of 16, one or two at most can be so, and leaving none out lets the last waits be for single pieces too
+    // (4,096 x 128,256 bf16 with 64 listed tokens 448 -> 434 us; of 8 8,000 x 9,000 bf16 73 -> 80).
     // Every access to memory in the loop over pieces is made by all lanes and whatever the row: the wait for a piece can then leave those that were asked for after it on their way (a
     // piece that may or may not have been asked for would have to be waited for as the last one).  Pieces beyond the row's last are that one once more, written with the same bytes;
     // what is not wanted is asked for from one place.
@@ -713,7 +716,7 @@ __global__ __launch_bounds__(THREADS_MAX, 4) void loss_resident_kernel(const Arg
     // (Rows that begin at multiples of 16 bytes pass the cache by, whatever their number: 32,768 x 2,048 fp32 111 us, else 135; others share lines with their neighbours: 1,030 x 40,037 bf16 50 and 58.)
     auto load = [&](const ElemT *from, uint32_t place) {
         const GLOBAL typename Piece<ElemT>::type *const at = (const GLOBAL typename Piece<ElemT>::type *)((const GLOBAL char *)(uintptr_t)from + place);
-        return ALIGNED ? __builtin_nontemporal_load(at) : *at;
+        return PASS ? __builtin_nontemporal_load(at) : *at;
     };
     auto fetch = [&](const ElemT *from, int i, bool wanted) {            // piece i of the thread; none is read of which the mask allows nothing
         uint32_t place = place_of(i);
@@ -873,10 +876,16 @@ __global__ __launch_bounds__(THREADS_MAX, 4) void loss_resident_kernel(const Arg
             if (i < NP && (i < NP - SPARE || i * TH < n_pieces)) {
                 u32x4 d{0, 0, 0, 0};
                 if (counts && (!MASKED || __any((live >> i) & 1u))) d = grad_of<ENT, EPV, ElemT>(raw[i], slope, A.c);
-                store_raw<ElemT>((GLOBAL char *)(uintptr_t)grad + place_of(i), d, A.once);
+                store_raw<ElemT>((GLOBAL char *)(uintptr_t)grad + place_of(i), d, PASS == 2);
                 if (i < NP - EARLY) fetch(next_logits, i, next_counts);
                 else {
-                    raw[i] = early[i - (NP - EARLY)];
+                    // (Moves that the compiler does not see through: it would have the load bring its piece elsewhere, wait for it at once and move it here.)
+#pragma unroll
+                    for (int k = 0; k < 4; k++) {
+                        uint32_t x;
+                        asm volatile("v_mov_b32 %0, %1" : "=v"(x) : "v"(early[i - (NP - EARLY)][k]));
+                        raw[i][k] = x;
+                    }
                     early[i - (NP - EARLY)] = load(third_logits, third ? place_of(i) : 0u);
                 }
             }
@@ -1054,11 +1063,14 @@ void rows_by(const Args &A, int threads, hipStream_t s) {
             // (600 x 128,256 bf16 77.5 -> 73.3 us, 300 under masks 56.8 -> 54.1); of several on one some are done early either way (1,030 x 40,037 61 -> 63).
             const int64_t most = THREADS_MAX / threads * COMPUTE_UNITS, turns = most == COMPUTE_UNITS ? (A.r.rows + most - 1) / most : 1;
             const dim3 grid((int)std::min(most, (A.r.rows + turns - 1) / turns));
-            const bool aligned = whole(A.r, A.r.logits, A.r.row_stride_elems);
+            const int pass = A.once ? 2 : whole(A.r, A.r.logits, A.r.row_stride_elems);
             const int words = own_words_of(NP, 16 / (int)sizeof(ElemT)) * threads * 4;
             auto launch = [&](auto *kernel, int bytes) { hipLaunchKernelGGL(kernel, grid, dim3(threads), bytes, s, A); };
-            if (KIND == DISTILL || A.r.mask) launch(aligned ? loss_resident_kernel<NP, KIND, true, ENT, true, ElemT> : loss_resident_kernel<NP, KIND, true, ENT, false, ElemT>, 2 * lds + words);
-            else if constexpr (KIND != DISTILL) launch(aligned ? loss_resident_kernel<NP, KIND, false, ENT, true, ElemT> : loss_resident_kernel<NP, KIND, false, ENT, false, ElemT>, 0);
+            auto choose = [&](auto *k0, auto *k1, auto *k2, int bytes) { launch(pass == 0 ? k0 : pass == 1 ? k1 : k2, bytes); };
+#define KERNEL(MASKED, PASS) loss_resident_kernel<NP, KIND, MASKED, ENT, PASS, ElemT>
+            if (KIND == DISTILL || A.r.mask) choose(KERNEL(true, 0), KERNEL(true, 1), KERNEL(true, 2), 2 * lds + words);
+            else if constexpr (KIND != DISTILL) choose(KERNEL(false, 0), KERNEL(false, 1), KERNEL(false, 2), 0);
+#undef KERNEL
             return;
         }
     }
