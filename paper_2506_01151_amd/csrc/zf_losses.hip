@@ -50,15 +50,23 @@ struct Ends {                                  // what the gradient of a row is 
     float m, base, slope, at_token;            // d = 2^((x - m) c) (base + slope y); the given token's own
 };
 
-__device__ __forceinline__ double wave_sum(double x) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) x += __shfl_xor(x, d);
-    return x;
+// Over a wavefront, to all lanes, by moves between lanes as zf_logit_rows.h has them for 32 bits.
+__device__ __forceinline__ double from_lane(double x, int lane) {
+    const uint64_t b = __double_as_longlong(x);
+    return __longlong_as_double((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, lane) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), lane) << 32);
 }
-__device__ __forceinline__ double wave_max(double x) {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) x = fmax(x, __shfl_xor(x, d));
-    return x;
+template <int CTRL, int ROWS = 0xF> __device__ __forceinline__ double plus_moved(double x) {
+    const uint64_t b = __double_as_longlong(x);
+    return x + __longlong_as_double((uint64_t)moved<CTRL, ROWS>(0u, (uint32_t)b) | (uint64_t)moved<CTRL, ROWS>(0u, (uint32_t)(b >> 32)) << 32);
+}
+__device__ __forceinline__ double wave_sum(double x) {
+    x = plus_moved<0x111>(x);
+    x = plus_moved<0x112>(x);
+    x = plus_moved<0x114>(x);
+    x = plus_moved<0x118>(x);
+    x = plus_moved<0x142, 0xA>(x);
+    x = plus_moved<0x143, 0xC>(x);
+    return from_lane(x, 63);
 }
 // What is alike in the whole workgroup and not written by the kernel comes through the scalar unit, whose loads are waited for apart from a row's pieces: a vector load behind them would make everything that is
 // asked for and written before it be waited for.
@@ -241,9 +249,9 @@ __device__ __forceinline__ bool first_of(const Entries &E, int k) {      // of t
 __device__ __forceinline__ void sum_entries(const Args &A, int wave, int lane, const Entries &E) {
     const int k = wave * 64 + lane;
     const bool counts = k < A.K && E.id[k] >= 0;
-    const float x = counts ? E.x[k] : -INFINITY, x_most = zf::wave_max(x);
+    const float x = counts ? E.x[k] : -INFINITY, x_most = wave_max(x);
     const double v = counts ? (double)E.v[k] : -INFINITY, T = A.r.temperature;
-    const double v_most = A.rest ? 0.0 : (double)zf::wave_max((float)v);
+    const double v_most = A.rest ? 0.0 : (double)wave_max((float)v);
     double ln = 0.0, e = 0.0, S = 0.0;
     if (v != -INFINITY) {
         ln = A.rest ? v : (v - v_most) / T;
@@ -254,10 +262,6 @@ __device__ __forceinline__ void sum_entries(const Args &A, int wave, int lane, c
     if (counts && first_of(E, k)) S = two_to((x - x_most) * A.c);
     const Teacher t{wave_sum(e), wave_sum(mixed), wave_sum(S), v_most, x_most, __any(counts), 0.0};
     if (lane == 0) E.part[wave] = t;
-}
-__device__ __forceinline__ double from_lane(double x, int lane) {
-    const uint64_t b = __double_as_longlong(x);
-    return __longlong_as_double((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)b, lane) | (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(uint32_t)(b >> 32), lane) << 32);
 }
 // A row's end, from the sums over what is not listed; by every lane of one wavefront alike.  Returns the row's loss.
 __device__ __forceinline__ double distill_row(const Args &A, const Part &sum, float wg, const Entries &E, Ends *ends) {
@@ -921,8 +925,19 @@ __global__ __launch_bounds__(THREADS_MAX, 4) void loss_resident_kernel(const Arg
 
 // loss = sum of weight x losses, in 64 bits and one order.
 __device__ __forceinline__ void sum_losses(const float *losses, const float *weight, int64_t n, float *loss, double *of_wave) {
+    constexpr int U = 4;                                   // asked for together
     double sum = 0.0;
-    for (int64_t i = threadIdx.x; i < n; i += blockDim.x) sum += (weight ? (double)weight[i] : 1.0) * losses[i];
+    for (int64_t from = threadIdx.x; from < n; from += (int64_t)U * blockDim.x) {
+        float l[U], w[U];
+#pragma unroll
+        for (int u = 0; u < U; u++) {
+            const int64_t i = from + (int64_t)u * blockDim.x;
+            l[u] = losses[i < n ? i : 0];
+            w[u] = weight ? weight[i < n ? i : 0] : 1.0f;
+        }
+#pragma unroll
+        for (int u = 0; u < U; u++) if (from + (int64_t)u * blockDim.x < n) sum += (double)w[u] * l[u];
+    }
     sum = wave_sum(sum);
     if (threadIdx.x % 64 == 0) of_wave[threadIdx.x / 64] = sum;
     __syncthreads();
@@ -955,12 +970,25 @@ __global__ __launch_bounds__(PAIRS * 128) void pairs_kernel(const zf_preference_
             const int64_t begin = wave % 2 ? o1 : o0, end = fits ? (wave % 2 ? o2 : o1) : begin;
             double sum = 0.0, n = 0.0;
             bool shared = false;                           // the offsets say that a row is in this sequence, and the row was found in another or in none: they descend elsewhere
-            for (int64_t row = begin + lane; row < end; row += 64) {
-                const float4 f = found[row];
-                if (__float_as_int(f.w) == PADDING) continue;
-                shared |= __float_as_int(f.w) != 2 * pair + wave % 2;
-                sum += p.ref_logprobs ? (double)f.z - p.ref_logprobs[row] : (double)f.z;
-                n += 1.0;
+            constexpr int U = 4;                           // asked for together
+            for (int64_t from = begin + lane; from < end; from += U * 64) {
+                float lp[U], ref[U];
+                int32_t of[U];
+#pragma unroll
+                for (int u = 0; u < U; u++) {
+                    const int64_t row = from + u * 64 < end ? from + u * 64 : from;
+                    const float4 f = found[row];
+                    lp[u] = f.z;
+                    of[u] = __float_as_int(f.w);
+                    ref[u] = p.ref_logprobs ? p.ref_logprobs[row] : 0.0f;
+                }
+#pragma unroll
+                for (int u = 0; u < U; u++) {
+                    if (from + u * 64 >= end || of[u] == PADDING) continue;
+                    shared |= of[u] != 2 * pair + wave % 2;
+                    sum += (double)lp[u] - ref[u];
+                    n += 1.0;
+                }
             }
             sum = wave_sum(sum);
             n = wave_sum(n);
