@@ -10,7 +10,7 @@ weight x got.losses (weight: fp32, one each where it is None; 1 / n makes a mean
 every other tensor that goes in, is a constant (one that requires grad is refused).  distill_loss and policy_loss make the gradient beside the losses, in the
 same pass over the logits: where the loss's own gradient is 1, as that of got.loss.backward(), the backward pass has nothing left to do; elsewhere, when it runs a
 second time, and in a graph's capture it reads the logits again.  As in operators.py calls are enqueued on torch's current stream, wait for nothing and allocate through torch
-only; what does not fit raises ZfError; forward-mode derivatives, torch.func and tracers are refused; a tensor that was written before the backward pass makes it raise.
+only, so that they can be captured into a graph (a backward pass from leaves made for the capture, no eager graph of theirs alive); what does not fit raises ZfError; forward-mode derivatives, torch.func and tracers are refused; a tensor that was written before the backward pass makes it raise.
 """
 import ctypes
 import math
