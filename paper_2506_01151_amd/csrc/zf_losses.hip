@@ -1009,7 +1009,8 @@ __global__ __launch_bounds__(PAIRS * 128) void pairs_kernel(const zf_preference_
             const double h = chosen - rejected, s = p.label_smoothing;
             // -ln sigma(h) = max(-h, 0) + ln(1 + e^-|h|)
             const double tail = log1p(exp(-fabs(h)));
-            double loss = (1.0 - s) * (fmax(-h, 0.0) + tail), slope = -(1.0 - s) / (1.0 + exp(h));
+            double loss = 0.0, slope = 0.0;                // (a share of zero of an infinite term is none)
+            if (s != 1.0) { loss = (1.0 - s) * (fmax(-h, 0.0) + tail); slope = -(1.0 - s) / (1.0 + exp(h)); }
             if (s != 0.0) { loss += s * (fmax(h, 0.0) + tail); slope += s / (1.0 + exp(-h)); }
             const bool nan = !fits || h != h;
             p.r.losses[pair] = nan ? NAN : (float)loss;

@@ -481,6 +481,24 @@ def test_preference_of_tokens_that_are_not_allowed():
 
 
 @gpu
+@pytest.mark.parametrize("s,want", [(0.0, [INF, 0.0]), (1.0, [0.0, INF]), (0.5, [INF, INF])])
+def test_preference_shares_of_infinite_terms(s, want):
+    """Of pairs that are infinitely far apart: the term that has no share does not make the loss NaN."""
+    x = torch.zeros((4, 40), device="cuda").requires_grad_()
+    bits = torch.ones((4, 40), dtype=torch.bool)
+    bits[0, 9], bits[3, 9] = False, False
+    got = zf.preference_loss(x, torch.full((4,), 9, device="cuda"), torch.arange(5, device="cuda"), mask=packed(bits).cuda(), label_smoothing=s)
+    assert got.losses.tolist() == want and got.chosen[0] == -INF and got.rejected[1] == -INF
+    g, = torch.autograd.grad(got.loss, x)
+    # lp of row 1 counts -beta, of row 2 beta; d loss / d h is s - 1 for h = -inf, s for h = inf.  Three roundings of 0.1 at most: the slope's, p f's together, their sum's.
+    for row, f in ((1, 0.1 * (1 - s)), (2, 0.1 * s)):
+        at = torch.full((40,), -f / 40, dtype=torch.float64)
+        at[9] += f
+        assert (g[row].double().cpu() - at).abs().max() <= 0.3 * U
+    assert not g[0].any() and not g[3].any()
+
+
+@gpu
 @pytest.mark.parametrize("offsets,bad", [([0, 5, 3, 6, 8], [True, True]), ([0, 2, 4, 6, 9], [False, True]), ([-1, 2, 4, 6, 8], [True, False]), ([0, 2 ** 40, 4, 6, 8], [True, True])])
 def test_preference_offsets_that_do_not_fit(offsets, bad):
     x = torch.randn((8, 30), generator=torch.Generator().manual_seed(4)).cuda().requires_grad_()
