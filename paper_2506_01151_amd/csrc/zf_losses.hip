@@ -306,7 +306,8 @@ __device__ __forceinline__ double distill_row(const Args &A, const Part &sum, fl
     ends->at_token = 0.0f;
     E.end->x_most = x_most;
     E.end->to_listed = nan ? NAN : (float)(scale * all * by_S);
-    for (int w = 0; w < (A.K + 63) / 64; w++) E.part[w].to_shares = scale * share * (A.rest || !E.part[w].some ? 1.0 : power((E.part[w].v_most - t.v_most) / T));
+    // (Equal also where both are -inf: entries that count, and none with a share.  Their difference would be NaN.)
+    for (int w = 0; w < (A.K + 63) / 64; w++) E.part[w].to_shares = scale * share * (A.rest || !E.part[w].some || E.part[w].v_most == t.v_most ? 1.0 : exp((E.part[w].v_most - t.v_most) / T));
     return nan ? NAN : loss;
 }
 // The gradient of listed tokens, over what the row's own pass wrote there.

@@ -232,6 +232,46 @@ def test_distill_the_rest_that_underflows():
     close(torch.autograd.grad(got.loss, xg)[0], grad, off, "gradient")
 
 
+@gpu
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [3, 900, 40037, 170001])
+@pytest.mark.parametrize("K", [1, 3, 64, 65, 200])
+def test_distill_values_that_are_all_minus_infinity(K, V, dtype, by):
+    """Rows whose teacher gives nothing to any listed token that the student allows: loss 0 and no gradient at all, the forward call's or one made again; with `rest` all is the other tokens'.
+    Beside them rows of which a whole 64 entries, the first or the last, are so, and rows whose only finite value is of a forbidden token."""
+    n, T = 7, 0.7
+    r = Rows(n, V, dtype, "none", T, 31 + K)
+    r.bits = torch.rand((n, V), generator=r.g) < 0.6
+    r.bits[:, 0] = True
+    r.bits[3:5, V - 1] = False
+    r.bits[5, V - 1] = True
+    r.update()
+    ids = torch.randint(V - 1, (n, K), generator=r.g)
+    ids[:, 0] = 0
+    v = torch.full((n, K), -INF)
+    ids[3:6, K - 1] = V - 1                        # the only finite one: forbidden in rows 3 and 4, allowed in row 5
+    v[3:6, K - 1] = -0.25
+    v[6] = -1.0 - torch.rand((K,), generator=r.g)
+    v[6, :64 if K > 64 else 0] = -INF
+    ids[2, 1:] = -1                                # (one entry counts)
+    weight = torch.rand((n,), generator=r.g) + 0.5
+    x, m = r.on_gpu()
+    x.requires_grad_()
+    for rest in (False, True):
+        losses, bound, grad, off = distill_want(r, ids, v, rest, weight, dtype)
+        got = zf.distill_loss(x, ids.cuda(), v.cuda(), m, temperature=T, rest=rest, weight=weight.cuda())
+        close(got.losses, losses, bound, "losses")
+        first, = torch.autograd.grad(got.loss, x, retain_graph=True)
+        again, = torch.autograd.grad(got.loss * -2.0, x)
+        close(first, grad, off, "gradient", x.dtype)
+        close(again, -2 * grad, 2 * off, "gradient made again", x.dtype)
+        if not rest:
+            without = [0, 1, 2] + ([3, 4] if K > 1 else [])        # (of one entry, rows 3 and 4 have none that counts)
+            assert (got.losses[without] == 0).all() and (first[without] == 0).all() and (again[without] == 0).all()
+        with torch.no_grad():
+            assert torch.equal(zf.distill_loss(x, ids.cuda(), v.cuda(), m, temperature=T, rest=rest, weight=weight.cuda()).losses, got.losses)
+
+
 # ---- the policy's loss ------------------------------------------------------------------------------
 def policy_want(r, t, old, adv, ref, clip, kl, e, weight):
     lp, counts = r.at(t)
