@@ -435,6 +435,12 @@ struct Slope {
     float m, base, slope, K;
     uint32_t sign;                             // of two bf16 numbers
     __device__ __forceinline__ Slope(const Ends &e, float c) : m(e.m), base(e.base), slope(e.slope), K(fmaf(e.m, c, -__builtin_amdgcn_logf(fabsf(e.base)))), sign(e.base < 0.0f ? 0x80008000u : 0u) {}
+    // What grad_of() makes of -inf: nothing times a factor, a zero with the factor's sign
+    template <bool ENT, typename ElemT> __device__ __forceinline__ uint32_t zeros() const {
+        if (sizeof(ElemT) == 2 && !ENT) return sign;
+        const uint32_t of_factor = __float_as_uint(ENT ? fmaf(slope, -1e4f, base) : base) & 0x80000000u;
+        return sizeof(ElemT) == 4 ? of_factor : of_factor | of_factor >> 16;
+    }
 };
 template <bool ENT, int EPV, typename ElemT>
 __device__ __forceinline__ u32x4 grad_of(const u32x4 &raw, const Slope &s, float c) {
@@ -853,6 +859,8 @@ __global__ __launch_bounds__(THREADS_MAX, 4) void loss_resident_kernel(const Arg
         const Ends ends = shared_ends;
         const bool next_counts = more && (LIST ? next_E.end->flags != 0 : next_head.t >= 0);
         const Slope slope(ends, A.c);
+        // Pieces of which nothing is allowed get the zeros that a forbidden token has in others: the row's last piece is written by wavefronts that have such pieces alone and by one that may have more.
+        const uint32_t nothing = MASKED && counts ? slope.template zeros<ENT, ElemT>() : 0u;
         if (LIST) {
             if (next_counts) sum_listed(next_E);
             ahead = after;
@@ -882,7 +890,7 @@ __global__ __launch_bounds__(THREADS_MAX, 4) void loss_resident_kernel(const Arg
             }
             if (MASKED && i == NP - EARLY - 2) read_words(third ? next + gridDim.x : row);     // (here, so that they are there when the loop is done)
             if (i < NP && (i < NP - SPARE || i * TH < n_pieces)) {
-                u32x4 d{0, 0, 0, 0};
+                u32x4 d{nothing, nothing, nothing, nothing};
                 if (counts && (!MASKED || __any((live >> i) & 1u))) d = grad_of<ENT, EPV, ElemT>(raw[i], slope, A.c);
                 store_raw<ElemT>((GLOBAL char *)(uintptr_t)grad + place_of(i), d, PASS == 2);
                 if (i < NP - EARLY) fetch(next_logits, i, next_counts);

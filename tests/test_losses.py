@@ -761,6 +761,38 @@ def test_rows_far_apart():
         assert torch.equal(torch.autograd.grad(a.loss, x)[0].nan_to_num(), torch.autograd.grad(b.loss, near)[0].nan_to_num())
 
 
+@gpu
+@pytest.mark.parametrize("loss", ["policy", "entropy", "distill", "rest"])
+@pytest.mark.parametrize("dtype,rows,V", [("bf16", 64, 32000), ("f32", 48, 32000), ("f32", 300, 7700), ("bf16", 24, 123680), ("f32", 16, 78224)])
+def test_a_last_piece_that_several_wavefronts_write(dtype, rows, V, loss, by):
+    """A row's last 16 bytes are written by the wavefront that has them and, once more, by those that have no pieces left.  Where none of their tokens is allowed all write the same zero, of the sign that
+    other forbidden tokens of the row have: the bits are the same every time.  (Zeros are negative here: the factor of the tokens that were not drawn is.)"""
+    r = Rows(rows, V, dtype, "none", 1.0, rows + V)
+    r.bits = torch.ones((rows, V), dtype=torch.bool)
+    r.bits[:, V - 16:] = False                     # the last pieces, and one among others
+    r.bits[:, 4000:4008] = False
+    x, m = rows_of(r.x, "packed"), packed(r.bits, padding=True).cuda()
+    x.requires_grad_()
+    t, zeros = torch.full((rows,), 7, device="cuda"), torch.zeros((rows,), device="cuda")
+    weight = zeros - 1.0
+    ids, v = torch.tensor([[7, 4001]], device="cuda").expand(rows, 2).contiguous(), torch.tensor([[-3.0, -1.0]], device="cuda").expand(rows, 2).contiguous()
+
+    def gradient(factor):
+        if loss in ("policy", "entropy"):
+            got = zf.policy_loss(x, t, zeros - 9.0, zeros + 1.0, m, clip=(0.2, INF), entropy_weight=-0.01 if loss == "entropy" else None, weight=weight)
+        else:                                      # (of the rest the share that the teacher leaves is the smaller one: its tokens' factor has the sign of the others')
+            got = zf.distill_loss(x, ids, torch.cat([v[:, :1] + 2.9, v[:, 1:]], dim=1) if loss == "rest" else v, m, rest=loss == "rest", weight=weight)
+        return torch.autograd.grad(got.loss * factor, x)[0]
+
+    bits = lambda g: g.view(torch.int32 if dtype == "f32" else torch.int16)
+    for factor in (1.0, 2.0):
+        first = gradient(factor)
+        forbidden = first[~r.bits.cuda()]
+        assert (forbidden == 0).all() and torch.signbit(forbidden).all()
+        for _ in range(3):
+            assert torch.equal(bits(gradient(factor)), bits(first))
+
+
 # ---- autograd, streams, graphs ----------------------------------------------------------------------
 def same_twice(x, mask):
     return [lambda i=i: three(x, mask)[i] for i in range(4)]
