@@ -309,6 +309,7 @@ int zf_token_logprobs_backward(const zf_logprobs_args *a, const float *g_logprob
  * With z = logits / temperature over the tokens of a row that its mask allows and whose logit is not -inf, p = softmax(z), lp = ln p.  What is forbidden, by
  * the mask or by -inf, has no gradient and is not looked at; a NaN or +inf among a row's allowed logits, and a token's id beyond V, make what is computed of the row NaN.
  *   loss    = sum of weight[i] x losses[i], as one number; losses [rows] (preferences: [pairs]) are without the weights.  Where a weight is 1 / n, loss is a mean.
+ *             (A weight of 0 does not leave out a row whose loss is infinite or NaN, as their product is NaN; what the loss defines as passed over does.)
  * The gradient is that of loss for the logits, times *d_g, rounded to the logits' type once.  Distillation and policy make it beside the losses, in the same pass over the
  * logits (d_grad of the first call: the gradient for *d_g = 1; null: none); their backward calls then have nothing to do where *d_g is 1 (`held`: d_grad
  * is what the first call wrote, and nothing else was written there since), and make it again elsewhere.  d_grad: device, [rows][grad_row_stride_elems], not the logits. */
@@ -325,7 +326,8 @@ typedef struct {
 } zf_loss_rows;
 
 /* Distillation from a teacher's listed tokens.  Of a row's n_listed entries those count whose id is not negative and whose token is allowed; q = softmax(values / temperature) over
- * them, or with `rest` q = e^values (values: log probabilities at that temperature), and q_R = 1 - sum q (0 at least) for all other tokens together:
+ * them, or with `rest` q = e^values (values: log probabilities at that temperature), and q_R = 1 - sum q (0 at least) for all other tokens together (the teacher's report is to be one under the
+ * same mask: what it gives to tokens that this mask forbids is in q_R, and so goes to the allowed tokens that are not listed, where without `rest` the listed ones would share it):
  *   losses = sum of q_k (ln q_k - lp[id_k])  [+ q_R (ln q_R - ln p_R), p_R the sum of p over the tokens that are not listed; left out where there are none]
  * A value of -inf is a share of zero.  A row of which no entry counts has loss 0 and no gradient, and is not read.  The same id twice: two entries. */
 typedef struct {
@@ -361,7 +363,7 @@ int zf_policy_loss_backward(const zf_policy_args *a, const float *d_g, int32_t h
  * sequence's rows whose token is not negative (with `average` their mean; 0 where there are none), chosen = beta D_2i, rejected = beta D_2i+1, h = chosen - rejected:
  *   losses = - (1 - label_smoothing) ln sigma(h) - label_smoothing ln sigma(-h)
  * Rows of no sequence and of negative tokens have no gradient.  A token that is not allowed: log probability -inf, no gradient.  A pair whose offsets descend or
- * leave 0 .. rows, or of whose rows another sequence has one too: NaN.
+ * leave 0 .. rows, or of whose rows another sequence has one too: NaN.  So is the loss of a pair both of whose sequences have a token that is not allowed (-inf less -inf).
  * stats and slopes are what the gradient is made from (written by the first call). */
 typedef struct {
     zf_loss_rows r;

@@ -15,7 +15,8 @@ SOURCES = ["zf_regex.cpp", "zf_compile.cpp", "zf_earley.cpp", "zf_automaton.cpp"
 HEADERS = ["zf_device.h", "zf_internal.h", "zf_launch.h", "zf_kernel_common.h", "zf_aut_step.h", "zf_host_automaton.h", "zf_ops.h", "zf_ops_check.h", "zf_logit_rows.h"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-function"]
-# zf_losses.hip: a row's end, in 64 bits, has dozens of constants, which the compiler would keep in registers beside a whole row's logits (and spill: 100 to 250 bytes a thread)
+# zf_losses.hip: a row's end, in 64 bits, has dozens of constants, which the compiler would keep in registers beside a whole row's logits.  Of loss_resident_kernel's registers it then moves 52 to 300 bytes a thread to
+# memory, in every variant; so none with 8 pieces, with 16 but for a teacher's list (36 to 60), and with 20 without masks, 104 to 196 in the others of 20
 OWN_FLAGS = {"zf_losses.hip": ["-mllvm", "-disable-machine-licm"]}
 # hipcc's host pass warns once per translation unit that it does not know the packed-fp32
 # feature (it only applies to the device pass); those lines are dropped, everything else is shown

@@ -201,7 +201,7 @@ struct Entries {                               // in LDS, room for the call's n_
     Teacher *part;                             // [n / 64]
     EntriesEnd *end;
     int32_t *id;                               // [n]; -1: does not count
-    float *x, *v;                              // v: the teacher's value, then e
+    float *x, *v;                              // v: the teacher's value, then e (rounded by u: it makes the entry's gradient, which is 32 bits at most; sums are of what it was made from)
     __device__ __forceinline__ Entries(char *at, int K) {
         part = (Teacher *)at;
         end = (EntriesEnd *)(part + (K + 63) / 64);
@@ -677,7 +677,9 @@ __global__ __launch_bounds__(THREADS_MAX, 8) void loss_rows_kernel(const Args A)
 // A row a workgroup, held in registers between its sums and its gradient: NP pieces of 16 bytes a thread.  Workgroups stay.  As soon as the gradient of a piece is on
 // the way its registers take the next row's piece, which is added to that row's sums LAG pieces later: memory is asked for, written and waited for all along the
 // arithmetic of both.  Bound by memory: 4,096 x 128,256 bf16 under masks 402 to 417 us (2.1 GB, 5.1 TB/s; vector units busy for 60 %), 64 listed tokens and the rest 427 to 450; 8,192 x 32,000
-// fp32 395 (5.3 TB/s).  Reading rows twice instead took 519 and 696.  A row's mask lies in LDS, without the tokens that a teacher listed: their sums and their gradient are taken from the list.
+// fp32 375 to 390 (5.4 TB/s).  loss_rows_kernel, which reads a row again for its
+// gradient, in its place: distillation 438 -> 539, policy without masks 415 -> 468, under them 411 -> 416, 8,192 x 32,000 fp32 alike.  20 pieces leave too few registers for a row's state under a mask or with a
+// list: 104 to 196 bytes of it a thread lie in memory (16 pieces with a list: 36 to 60).  2,000 x 152,064 bf16: policy 252, under masks 262, distillation 299; 1,024 x 80,000 fp32: policy 140, distillation 176.  A row's mask lies in LDS, without the tokens that a teacher listed: their sums and their gradient are taken from the list.
 // PASS: 1: rows begin at multiples of 16 bytes, 2: and the gradient passes the cache by (Args::once; a branch for it at each store would have the compiler wait for stores with the loads).
 template <int NP, int KIND, bool MASKED, bool ENT, int PASS, typename ElemT>
 __global__ __launch_bounds__(THREADS_MAX, 4) void loss_resident_kernel(const Args A) {
@@ -1124,9 +1126,14 @@ void rows_by(const Args &A, int threads, hipStream_t s) {
 template <int KIND, bool ENT, typename ElemT>
 void rows_of(const Args &A, hipStream_t s) {
     const int32_t n = (A.r.V + (int)(16 / sizeof(ElemT)) - 1) / (int)(16 / sizeof(ElemT));    // pieces of a row
+    // Preferences' log probabilities of many long rows: 256 threads a row, several rows a compute unit, whose starts and ends lie beside others' middles.  The kernel with 1,024 threads (or as many as below)
+    // -> with 256: 4,096 x 100,001 bf16 under masks 152 -> 127 us, 20,000 x 17,000 fp32 203 -> 192, 4,096 x 128,256 bf16 with its gradient 139 -> 134; but without it, so that the cache has rows of the call
+    // before, 140 -> 152, and 2,048 x 152,064 fp32 172 -> 186, 2,048 x 32,000 45 -> 48.  Fewer or shorter rows: 1,024 x 152,064 fp32 105 -> 111 a call, 8,000 x 4,000 bf16 29.5 -> 34.
     if (KIND == LOGPROB && A.r.rows >= 2048 && n > 16 * 64) return rows_by<0, KIND, ENT, ElemT>(A, 256, s);
     // A thread has all its pieces but the last three at least, or does some again: 16 of them where that fits, else 8.  A workgroup of its own on a compute unit takes a row in the shorter
-    // time with twice the threads.
+    // time with twice the threads.  With 8 and with 16 pieces, policy steps: where 16 would have 3 or more again (n <= 13 by_16), 8,000 x 9,000 bf16 73 and 85 us, under masks 82 and 97, 6,000 x 12,000 73 and
+    // 79, 32,768 x 2,000 fp32 115 and 127; near the border alike or a little better with 16 (5,000 x 13,300 bf16 73 and 69, 20,000 x 3,400 fp32 129 and 132); beyond, 8,192 x 20,000 fp32 273 and 266,
+    // x 32,000 392 and 375, 2,400 x 32,000 bf16 79 and 70.
     const int by_16 = (n + 16 * 64 - 1) / (16 * 64) * 64, by_8 = (n + 8 * 64 - 1) / (8 * 64) * 64;
     if (by_8 <= THREADS_MAX && (A.r.rows <= COMPUTE_UNITS || n <= 13 * by_16)) return rows_by<8, KIND, ENT, ElemT>(A, by_8, s);
     if (n <= 16 * THREADS_MAX) return rows_by<16, KIND, ENT, ElemT>(A, by_16, s);
@@ -1142,7 +1149,7 @@ Args common(const zf_loss_rows &r, const LossGrad &g) {
     Args A{};
     A.r = r;
     A.W = (r.V + 31) / 32;
-    A.c = (float)(1.4426950408889634 / r.temperature);
+    A.c = (float)(1.4426950408889634 / r.temperature);      // (off by u: an element's exponent y by u |y|, as by its difference and its product each)
     A.grad = g.grad; A.grad_stride = g.stride; A.g = g.g; A.held = g.held; A.results = !g.g;
     A.once = passes(r, g);
     return A;

@@ -9,7 +9,8 @@ logits: fp32 or bf16 [rows, V], rows without gaps; masks are those of compute_ma
 weight x got.losses (weight: fp32, one each where it is None; 1 / n makes a mean) and has a gradient, once, for the logits; everything else that comes back, and
 every other tensor that goes in, is a constant (one that requires grad is refused).  distill_loss and policy_loss make the gradient beside the losses, in the
 same pass over the logits: where the loss's own gradient is 1, as that of got.loss.backward(), the backward pass has nothing left to do; elsewhere, when it runs a
-second time, and in a graph's capture it reads the logits again.  As in operators.py calls are enqueued on torch's current stream, wait for nothing and allocate through torch
+second time, and in a graph's capture it reads the logits again and makes the gradient anew: (0.5 * got.loss).backward() on 4,096 x 128,256 bf16 makes a step of policy_loss 817 us instead of 411, of distill_loss 867
+instead of 438.  A coefficient, or the share of a micro-batch, is better given in `weight`.  (A weight of 0 does not leave out a row whose loss is infinite or NaN; negative tokens and ids do.)  As in operators.py calls are enqueued on torch's current stream, wait for nothing and allocate through torch
 only, so that they can be captured into a graph (a backward pass from leaves made for the capture, no eager graph of theirs alive); what does not fit raises ZfError; forward-mode derivatives, torch.func and tracers are refused; a tensor that was written before the backward pass makes it raise.
 """
 import ctypes
@@ -244,7 +245,8 @@ def distill_loss(logits, teacher_ids, teacher_values, mask=None, *, temperature=
     teacher_ids: int32 or int64 [rows, n], n up to 1024, negative where there is none; teacher_values: fp32 or bf16 [rows, n].  Of the listed tokens those count that the student allows.
     The teacher's shares are softmax(teacher_values / temperature) over them: logits, or log probabilities, of the teacher.  With rest=True they are e^teacher_values -- log probabilities, at that
     temperature, as token_logprobs reports them -- and what is missing from 1 is the share of all other tokens together, which the student's probability of these is held to
-    (where there are none, or the listed shares are 1 or more, nothing is).  A row of which no token counts: loss 0, no gradient."""
+    (where there are none, or the listed shares are 1 or more, nothing is).  With rest=True the report is to be one under the same mask: what the teacher gave to tokens that `mask` forbids counts to what is
+    missing, and so teaches the allowed tokens that are not listed, where rest=False shares it among the listed ones.  A row of which no token counts: loss 0, no gradient."""
     got = _native_losses.distill_loss(logits, teacher_ids, teacher_values, mask, temperature, bool(rest), weight)
     if got is not None:
         return DistillLoss(*got)
@@ -291,7 +293,7 @@ def preference_loss(logits, tokens, offsets, ref_logprobs=None, mask=None, *, be
 
     offsets: int32 or int64 [2 pairs + 1]: sequence s has the rows offsets[s] up to offsets[s + 1]; of each pair the preferred one comes first.  tokens: int32 or int64 [rows], ref_logprobs:
     fp32 [rows]; weight: fp32 [pairs].  Negative tokens (prompts) and rows of no sequence are passed over.  A token that is not allowed: log probability -inf, no gradient of its
-    own.  Offsets that descend or leave the rows, or give a row to two sequences: NaN for their pair."""
+    own.  (In both sequences of a pair: a loss of NaN.)  Offsets that descend or leave the rows, or give a row to two sequences: NaN for their pair."""
     got = _native_losses.preference_loss(logits, tokens, offsets, ref_logprobs, mask, beta, label_smoothing, bool(average), temperature, weight)
     if got is not None:
         return PreferenceLoss(*got)

@@ -368,7 +368,7 @@ def test_policy_sides_of_the_clipping():
         assert (slope - torch.where(free, -(ratios * adv), 0.0)).abs().max() < 1e-5
 
 
-# ---- masks that leave few tokens of large calls, which another kernel takes (up to 2,048 of a row, from 32 MB of logits on) ----
+# ---- masks that leave few tokens, from none to all, of long rows: of up to 16 and 20 pieces a thread, and longer ones ----
 def few_rows(dtype, seed, rows, V):
     r = Rows(rows, V, dtype, "few", 0.8, seed)
     for i, n in enumerate((0, 1, 2, 64, 300, 2047, 2048, 2049, 2050, V)):
